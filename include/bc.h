@@ -374,6 +374,33 @@ int32_t bc_topk_kl_loss_bwd(int64_t T, int32_t V, int32_t k, const void *student
                             const int32_t *teacher_idx, const float *lse, float grad_scale,
                             void *dlogits, void *stream);
 
+/* From a layer's packed projections to the q, k and v the attention calls take: the RMS norm of every query and key head, the
+ * rotation by position, v copied, in one pass.  (Positions are the caller's, see Sec. 3.1 for the beacon's; keys enter the cache
+ * position-encoded.)  For a head x of d elements, h = rot / 2 and a_i = positions[row] * inv_freq[i]:
+ *   y = w * x / sqrt(mean(x^2) + eps), or y = x where the weight w (q_weight, k_weight: device [d]) is NULL;
+ *   out[i] = y[i] cos a_i - y[i+h] sin a_i,  out[i+h] = y[i+h] cos a_i + y[i] sin a_i  (i < h);  out[i] = y[i]  (i >= rot).
+ * shape: Hq, Hkv, d and kv_dtype, the type of qkv, the weights and q, k, v (B and scale are not read); Hq + 2 Hkv <= 65536.
+ * qkv: device [rows, Hq + 2 Hkv, d], rows qkv_row_stride elements apart (16 bytes' multiple); positions: device [rows] int32;
+ * inv_freq: device [rot / 2] fp32, rot a multiple of 8 from 0 to d.  q [rows, Hq, d], k and v [rows, Hkv, d]: dense; v NULL: not
+ * copied.  eps >= 0 and finite.  Arithmetic in fp32 (the angles' products in fp64), rounded once.  Rows of a decode step
+ * (rows = B) and of a prefill are the same call.  Pointers 16-byte aligned (positions, inv_freq: 4). */
+int32_t bc_qk_norm_rope(const bc_shape *shape, int64_t rows, const void *qkv, int64_t qkv_row_stride,
+                        const int32_t *positions, const float *inv_freq, int32_t rot, const void *q_weight,
+                        const void *k_weight, float eps, void *q, void *k, void *v, void *stream);
+
+/* Gradients of bc_qk_norm_rope.  dq [rows, Hq, d], dk, dv [rows, Hkv, d]: fp32, as bc_prefill_attn_bwd writes them; dqkv: of
+ * kv_dtype, rows dqkv_row_stride elements apart, every one of its (Hq + 2 Hkv) d columns written (dv NULL: those of v left as
+ * they were).  dqkv may be qkv itself (with the same stride).  dq_weight, dk_weight (nullable): device [d] fp32, the weights'
+ * gradients, sums over rows and heads in a fixed order (no atomics), for which the workspace is needed
+ * (bc_qk_norm_rope_bwd_workspace_bytes(), no initialisation; may be NULL where both are).  qkv is read where a weight is given.
+ * rows = 0 writes zeros to dq_weight and dk_weight. */
+size_t bc_qk_norm_rope_bwd_workspace_bytes(const bc_shape *shape);
+int32_t bc_qk_norm_rope_bwd(const bc_shape *shape, int64_t rows, const void *qkv, int64_t qkv_row_stride,
+                            const int32_t *positions, const float *inv_freq, int32_t rot, const void *q_weight,
+                            const void *k_weight, float eps, const float *dq, const float *dk, const float *dv,
+                            void *dqkv, int64_t dqkv_row_stride, float *dq_weight, float *dk_weight,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
 /* Copy nb[B], w[B] and err[1] to HOST arrays (any may be NULL) and wait for the stream. */
 int32_t bc_tables_to_host(const bc_shape *shape, const bc_cache *cache, int32_t *nb_host,
                           int32_t *w_host, int32_t *err_host, void *stream);

@@ -40,6 +40,7 @@ EXPORTS = [
     "bc_trajectory_tables", "bc_prefill_attn", "bc_prefill_workspace_bytes", "bc_prefill_attn_ws",
     "bc_prefill_bwd_workspace_bytes", "bc_prefill_attn_bwd", "bc_prefill_attn_host", "bc_prefill_attn_bwd_host",
     "bc_topk_kl_loss", "bc_topk_kl_loss_bwd", "bc_tables_to_host",
+    "bc_qk_norm_rope", "bc_qk_norm_rope_bwd_workspace_bytes", "bc_qk_norm_rope_bwd",
 ]
 DIAG_EXPORTS = ["bc_diag_stream_read"]
 
@@ -132,6 +133,12 @@ def load():
     lib.bc_topk_kl_loss.argtypes = [i64, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.bc_topk_kl_loss_bwd.restype = i32
     lib.bc_topk_kl_loss_bwd.argtypes = [i64, i32, i32, vp, i32, vp, vp, vp, C.c_float, vp, vp]
+    lib.bc_qk_norm_rope.restype = i32
+    lib.bc_qk_norm_rope.argtypes = [sp, i64, vp, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, vp, vp]
+    lib.bc_qk_norm_rope_bwd_workspace_bytes.restype = sz
+    lib.bc_qk_norm_rope_bwd_workspace_bytes.argtypes = [sp]
+    lib.bc_qk_norm_rope_bwd.restype = i32
+    lib.bc_qk_norm_rope_bwd.argtypes = [sp, i64, vp, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
     lib.bc_tables_to_host.restype = i32
     lib.bc_tables_to_host.argtypes = [sp, cp, vp, vp, vp, vp]
     call = at = None
@@ -301,6 +308,22 @@ def bc_topk_kl_loss_bwd(T, V, k, student_logits, logits_dtype, teacher_logits, t
                         grad_scale, dlogits, stream):
     return load().bc_topk_kl_loss_bwd(T, V, k, student_logits, logits_dtype, teacher_logits,
                                       teacher_idx, lse, grad_scale, dlogits, stream)
+
+
+def bc_qk_norm_rope(shape, rows, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight, k_weight, eps, q, k, v, stream):
+    return load().bc_qk_norm_rope(C.byref(shape), rows, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight,
+                                  k_weight, eps, q, k, v, stream)
+
+
+def bc_qk_norm_rope_bwd_workspace_bytes(shape):
+    return load().bc_qk_norm_rope_bwd_workspace_bytes(C.byref(shape))
+
+
+def bc_qk_norm_rope_bwd(shape, rows, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight, k_weight, eps, dq, dk, dv,
+                        dqkv, dqkv_row_stride, dq_weight, dk_weight, ws, ws_bytes, stream):
+    return load().bc_qk_norm_rope_bwd(C.byref(shape), rows, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight,
+                                      k_weight, eps, dq, dk, dv, dqkv, dqkv_row_stride, dq_weight, dk_weight, ws,
+                                      ws_bytes, stream)
 
 
 def bc_tables_to_host(shape, cache, nb_host, w_host, err_host, stream):
@@ -724,3 +747,61 @@ def topk_kl_loss_bwd(student_logits, teacher_logits, teacher_idx, lse, grad_scal
                                _ptr(dz), _stream_ptr()))
     _used_here(student_logits, teacher_logits, teacher_idx, lse)
     return dz
+
+
+def _is(t, name, dtype, shape, device):
+    """Whether a tensor is what a call takes: the library sees its address alone."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise BcError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, tuple(shape), device))
+
+
+def _rope_rows(qkv, positions, inv_freq, Hq, Hkv, d, q_weight, k_weight):
+    """Checks what both calls take; -> (shape, rows, row stride, rotated elements)."""
+    import torch
+    if qkv.dim() != 2 or qkv.shape[1] != (Hq + 2 * Hkv) * d or (qkv.numel() and qkv.stride(1) != 1):
+        raise BcError("qkv must be [rows, (Hq + 2 * Hkv) * d] with elements of a row back to back")
+    rows, dev = qkv.shape[0], qkv.device
+    if not qkv.is_cuda:
+        raise BcError("qkv must be a device tensor")
+    _is(positions, "positions", torch.int32, (rows,), dev)
+    _is(inv_freq, "inv_freq", torch.float32, (inv_freq.numel(),), dev)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _is(w, name, qkv.dtype, (d,), dev)
+    return bc_shape(1, Hq, Hkv, d, _logits_code(qkv), 1.0), rows, qkv.stride(0) if rows > 1 else qkv.shape[1], 2 * inv_freq.numel()
+
+
+@_on_its_device
+def qk_norm_rope(qkv, positions, inv_freq, Hq, Hkv, d, q_weight=None, k_weight=None, eps=1e-6):
+    """bc_qk_norm_rope on device tensors: qkv [R, (Hq + 2 Hkv) d] bf16/fp32 (rows may lie apart), positions [R] int32,
+    inv_freq [rot / 2] fp32, weights [d] of qkv's dtype or None (no norm).  Returns (q [R, Hq, d], k, v [R, Hkv, d]), which the
+    current stream works on."""
+    import torch
+    load()
+    shape, rows, stride, rot = _rope_rows(qkv, positions, inv_freq, Hq, Hkv, d, q_weight, k_weight)
+    q, k, v = (torch.empty(rows, h, d, dtype=qkv.dtype, device=qkv.device) for h in (Hq, Hkv, Hkv))
+    _check(bc_qk_norm_rope(shape, rows, _ptr(qkv), stride, _ptr(positions), _ptr(inv_freq), rot, _ptr(q_weight), _ptr(k_weight),
+                           float(eps), _ptr(q), _ptr(k), _ptr(v), _stream_ptr()))
+    _used_here(qkv, positions, inv_freq, q_weight, k_weight)
+    return q, k, v
+
+
+@_on_its_device
+def qk_norm_rope_bwd(qkv, dq, dk, dv, positions, inv_freq, Hq, Hkv, d, q_weight=None, k_weight=None, eps=1e-6):
+    """bc_qk_norm_rope_bwd on device tensors (see qk_norm_rope); dq, dk, dv: fp32, as prefill_attn_bwd returns them.  Returns
+    (dqkv [R, (Hq + 2 Hkv) d] in qkv's dtype, dq_weight, dk_weight [d] fp32 or None)."""
+    import torch
+    load()
+    shape, rows, stride, rot = _rope_rows(qkv, positions, inv_freq, Hq, Hkv, d, q_weight, k_weight)
+    dev = qkv.device
+    for name, g, h in (("dq", dq, Hq), ("dk", dk, Hkv), ("dv", dv, Hkv)):
+        _is(g, name, torch.float32, (rows, h, d), dev)
+    dqkv = torch.empty(rows, (Hq + 2 * Hkv) * d, dtype=qkv.dtype, device=dev)
+    dqw, dkw = (None if w is None else torch.empty(d, dtype=torch.float32, device=dev) for w in (q_weight, k_weight))
+    ws_bytes = int(bc_qk_norm_rope_bwd_workspace_bytes(shape)) if dqw is not None or dkw is not None else 0
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev) if ws_bytes else None
+    _check(bc_qk_norm_rope_bwd(shape, rows, _ptr(qkv), stride, _ptr(positions), _ptr(inv_freq), rot, _ptr(q_weight), _ptr(k_weight),
+                               float(eps), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dqkv), dqkv.shape[1], _ptr(dqw), _ptr(dkw), _ptr(ws),
+                               ws_bytes, _stream_ptr()))
+    _used_here(qkv, dq, dk, dv, positions, inv_freq, q_weight, k_weight)
+    return dqkv, dqw, dkw

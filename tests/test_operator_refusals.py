@@ -1,0 +1,57 @@
+"""What the calls around the attention refuse (host logic only: no GPU needed; addresses are made up and never dereferenced)."""
+import pytest
+import torch
+
+from paper_2510_13797_amd import bc
+
+PTR = 0x7F0000100000
+ODD = PTR + 4
+
+
+def shape(Hq=4, Hkv=2, d=64, dtype=bc.BC_BF16, B=1, scale=1.0):
+    return bc.bc_shape(B, Hq, Hkv, d, dtype, scale)
+
+
+def _rope(s=None, rows=3, qkv=PTR, stride=512, pos=PTR, freq=PTR, rot=64, qw=PTR, kw=PTR, eps=1e-6, q=PTR, k=PTR, v=PTR):
+    return bc.bc_qk_norm_rope(s or shape(), rows, qkv, stride, pos, freq, rot, qw, kw, eps, q, k, v, None)
+
+
+def _rope_bwd(s=None, rows=3, qkv=PTR, stride=512, pos=PTR, freq=PTR, rot=64, qw=PTR, kw=PTR, eps=1e-6, dq=PTR, dk=PTR, dv=PTR,
+              dqkv=PTR, dstride=512, dqw=PTR, dkw=PTR, ws=PTR, nbytes=1 << 30):
+    return bc.bc_qk_norm_rope_bwd(s or shape(), rows, qkv, stride, pos, freq, rot, qw, kw, eps, dq, dk, dv, dqkv, dstride, dqw, dkw,
+                                  ws, nbytes, None)
+
+
+@pytest.mark.parametrize("call", [_rope, _rope_bwd])
+def test_rope_refusals_of_both_directions(call):
+    bc.load()
+    for kw in (dict(Hq=5), dict(Hkv=0), dict(d=96), dict(d=256), dict(dtype=2), dict(Hq=18)):
+        assert call(s=shape(**kw)) == bc.BC_ERR_SHAPE, kw
+    for rot in (-8, 4, 12, 72):
+        assert call(rot=rot) == bc.BC_ERR_SHAPE, rot
+    assert call(rows=-1) == bc.BC_ERR_SHAPE and call(rows=1 << 31) == bc.BC_ERR_SHAPE
+    for eps in (-1e-6, float("nan"), float("inf")):
+        assert call(eps=eps) == bc.BC_ERR_ARG
+    for kw in (dict(pos=None), dict(freq=None), dict(stride=511), dict(stride=516), dict(stride=504), dict(stride=0), dict(stride=-512),
+               dict(qw=ODD), dict(kw=ODD), dict(qkv=None), dict(qkv=ODD), dict(stride=1 << 40)):
+        assert call(**kw) == bc.BC_ERR_ARG, kw
+
+
+def test_rope_refusals_of_one_direction():
+    for kw in (dict(q=None), dict(k=None), dict(q=ODD), dict(k=ODD), dict(v=ODD)):
+        assert _rope(**kw) == bc.BC_ERR_ARG, kw
+    for kw in (dict(dq=None), dict(dk=None), dict(dqkv=None), dict(dq=ODD), dict(dk=ODD), dict(dv=ODD), dict(dqkv=ODD), dict(dstride=510),
+               dict(dstride=516), dict(qw=None), dict(kw=None)):
+        assert _rope_bwd(**kw) == bc.BC_ERR_ARG, kw
+    need = bc.bc_qk_norm_rope_bwd_workspace_bytes(shape())
+    assert need > 0 and bc.bc_qk_norm_rope_bwd_workspace_bytes(shape(d=96)) == 0
+    for kw in (dict(ws=None), dict(ws=ODD), dict(nbytes=need - 1)):
+        assert _rope_bwd(**kw) == bc.BC_ERR_WORKSPACE, kw
+
+
+def test_rope_binding_refuses_what_the_library_cannot_see():
+    # tensors of the wrong type, length, place or order (here: on the host)
+    qkv, pos, freq = torch.zeros(3, 512, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32), torch.zeros(32)
+    for args in ((qkv[:, :500], pos, freq), (qkv[0], pos, freq), (qkv, pos, freq), (qkv.half(), pos, freq)):
+        with pytest.raises(bc.BcError):
+            bc.qk_norm_rope(*args, 4, 2, 64)
