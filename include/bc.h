@@ -269,6 +269,25 @@ int32_t bc_decode_step_budget(const bc_shape *shape, const bc_cache *cache, cons
                               const void *beacon_v, const int32_t *budget, uint8_t *live,
                               void *workspace, size_t workspace_bytes, void *stream);
 
+/* A chunk of new prompt rows for every sequence, appended and attended in one call: a long prompt in pieces, or the next turn's
+ * text over a cache that has decoded (Alg. 1, "encode the prompt", where entries are resident already).  With L = P + nb + w
+ * resident entries of sequence s and its n = row_offsets[s+1] - row_offsets[s] new rows,
+ *   out[i,h,:] = sum_j softmax_j(scale * q[i,h,:] . K_j[kvh,:]) V_j[kvh,:],  j over the L entries and new rows 0 .. i,
+ * the new rows go to entries L .. L + n - 1, and what is resident is prompt from then on: P = L + n, nb = w = 0 (beacons and a
+ * window begun before stay as they are and are not compressed further; a window can be closed first by bc_compress_evict with
+ * require_full_window = 0).  c stays.
+ * q: [rows, Hq, d], k, v: [rows, Hkv, d] (kv_dtype must be BC_BF16), the sequences' rows back to back; out: [rows, Hq, d] fp32.
+ * row_offsets: HOST [B + 1], not decreasing, read before the call returns.  Sequences that are not active or have no new rows are
+ * left alone, their rows of out with them.  A sequence whose rows do not fit its slab (L + n > cap) sets the capacity bit, one
+ * with a beacon at the tail (w == c + 1) the state bit; both are left alone.  k and v are finite: a product with an entry that
+ * is not may show in rows of its sequence that do not see it.  No atomics on results: they are reproducible.
+ * workspace: bc_prompt_workspace_bytes() of the longest chunk, the sum of all and max_cap, 16-byte aligned, no initialisation;
+ * calls that overlap in time need one each.  scale must be > 0 and finite. */
+size_t bc_prompt_workspace_bytes(const bc_shape *shape, int32_t max_new, int64_t total_new, int32_t max_cap);
+int32_t bc_prompt_step(const bc_shape *shape, const bc_cache *cache, const void *k, const void *v, const void *q,
+                       const int64_t *row_offsets, float *out, const uint8_t *active, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
 /* Change the compression ratio of active sequences in the middle of a generation (the paper
  * fixes c per generation and names dynamic ratios as future work, Sec. 6).  new_c: device [B]
  * int32.  Allowed when the current window fits the new ratio (w < new_c, or new_c <= 0, or a

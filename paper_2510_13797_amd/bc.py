@@ -40,6 +40,7 @@ EXPORTS = [
     "bc_trajectory_tables", "bc_prefill_attn", "bc_prefill_workspace_bytes", "bc_prefill_attn_ws",
     "bc_prefill_bwd_workspace_bytes", "bc_prefill_attn_bwd", "bc_prefill_attn_host", "bc_prefill_attn_bwd_host",
     "bc_topk_kl_loss", "bc_topk_kl_loss_bwd", "bc_tables_to_host",
+    "bc_prompt_workspace_bytes", "bc_prompt_step",
     "bc_qk_norm_rope", "bc_qk_norm_rope_bwd_workspace_bytes", "bc_qk_norm_rope_bwd",
 ]
 DIAG_EXPORTS = ["bc_diag_stream_read"]
@@ -133,6 +134,10 @@ def load():
     lib.bc_topk_kl_loss.argtypes = [i64, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.bc_topk_kl_loss_bwd.restype = i32
     lib.bc_topk_kl_loss_bwd.argtypes = [i64, i32, i32, vp, i32, vp, vp, vp, C.c_float, vp, vp]
+    lib.bc_prompt_workspace_bytes.restype = sz
+    lib.bc_prompt_workspace_bytes.argtypes = [sp, i32, i64, i32]
+    lib.bc_prompt_step.restype = i32
+    lib.bc_prompt_step.argtypes = [sp, cp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.bc_qk_norm_rope.restype = i32
     lib.bc_qk_norm_rope.argtypes = [sp, i64, vp, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, vp, vp]
     lib.bc_qk_norm_rope_bwd_workspace_bytes.restype = sz
@@ -310,6 +315,14 @@ def bc_topk_kl_loss_bwd(T, V, k, student_logits, logits_dtype, teacher_logits, t
                                       teacher_idx, lse, grad_scale, dlogits, stream)
 
 
+def bc_prompt_workspace_bytes(shape, max_new, total_new, max_cap):
+    return load().bc_prompt_workspace_bytes(C.byref(shape), max_new, total_new, max_cap)
+
+
+def bc_prompt_step(shape, cache, k, v, q, row_offsets, out, active, ws, ws_bytes, stream):
+    return load().bc_prompt_step(C.byref(shape), C.byref(cache), k, v, q, row_offsets, out, active, ws, ws_bytes, stream)
+
+
 def bc_qk_norm_rope(shape, rows, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight, k_weight, eps, q, k, v, stream):
     return load().bc_qk_norm_rope(C.byref(shape), rows, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight,
                                   k_weight, eps, q, k, v, stream)
@@ -408,6 +421,8 @@ def _on_its_device(call):
 
 class Runtime:
     """Owns slabs, tables and workspace of one batch of caches; calls the C ABI."""
+
+    _prompt_moved = False         # whether P on the device has left P_host behind
 
     def __init__(self, B, Hq, Hkv, d, dtype, scale, P, c, cap, device):
         import torch
@@ -578,6 +593,33 @@ class Runtime:
                                      self.ws_bytes, _stream_ptr()))
         return out
 
+    def prompt_step(self, k, v, q, row_offsets, active=None, out=None):
+        """bc_prompt_step: k, v [rows, Hkv, d], q [rows, Hq, d] bf16, the sequences' new rows back to back; row_offsets [B + 1]
+        (host).  Returns out [rows, Hq, d] fp32 (rows of sequences that take no part: as they were, in a new tensor unspecified)."""
+        torch = self.torch
+        k, v, q, a = self.dev(k), self.dev(v), self.dev(q), self.mask(active)
+        off = np.ascontiguousarray(row_offsets, dtype=np.int64)
+        if off.shape != (self.B + 1,):
+            raise BcError("row_offsets must have B + 1 entries")
+        n = np.diff(off)
+        rows, dev = q.shape[0], q.device
+        if n.min() < 0 or off[0] < 0 or off[-1] > rows:
+            raise BcError("row_offsets must not decrease and end within the %d rows" % rows)
+        for name, t, h in (("q", q, self.Hq), ("k", k, self.Hkv), ("v", v, self.Hkv)):
+            _is(t, name, self.elem_dtype, (rows, h, self.d), dev)
+        if a is not None:
+            _is(a, "active", torch.uint8, (self.B,), dev)
+        if out is None:
+            out = torch.empty(rows, self.Hq, self.d, dtype=torch.float32, device=dev)
+        else:
+            _is(out, "out", torch.float32, (rows, self.Hq, self.d), dev)
+        nbytes = int(bc_prompt_workspace_bytes(self.shape, int(n.max()), int(off[-1] - off[0]), self.max_cap))
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        _check(bc_prompt_step(self.shape, self.cache, _ptr(k), _ptr(v), _ptr(q), off.ctypes.data, _ptr(out), _ptr(a), _ptr(ws),
+                              nbytes, _stream_ptr()))
+        self._prompt_moved = True
+        return out
+
     def sort_by_length(self, active=None):
         """Refresh the dispatch order (longest resident sequence first) and attach it to the cache:
         large ragged batches then start their longest sequences first."""
@@ -612,6 +654,8 @@ class Runtime:
         if nb is None:
             nbs, ws, _ = self.tables()
             nb, w = int(nbs[s]), int(ws[s])
+        if self._prompt_moved:
+            self.P_host, self._prompt_moved = self.P.cpu().numpy().astype(np.int32), False
         L = int(self.P_host[s]) + nb + w
         cap = int(self.cap_host[s])
         E = self.Hkv * self.d

@@ -1,0 +1,600 @@
+// bc_prompt_step: a chunk of new prompt rows for every sequence of a cache - their attention over what is resident and over each
+// other, and their append (Sec. 2's attention; Alg. 1's "encode the prompt", in pieces or over a cache that has decoded).
+//
+//   out[i, h] = sum_j softmax_j(scale q[i, h] . K_j) V_j,  j over the L resident rows and new rows 0 .. i
+//
+// The query heads of a KV head see the same keys, so (row, head) pairs are the columns of the products: column i * g + h, with the
+// causal limit by i alone.  Tiles of 32 keys come from two places, first the slab's rows [0, L), then the new rows as the call got
+// them (the append need not be over), and go through LDS into 32x32x16 MFMA as in the prefill kernels: S^T = K.Q^T, O^T += V^T.P^T
+// with P in two bf16 parts (16 bits: what a decode step over the same rows gives), softmax online in registers.
+//
+// Two kernels share a wave's work on a tile:
+//   many columns: a workgroup's four waves have 32 columns each and share the tiles (3-stage ring, a barrier a tile);
+//   32 columns or fewer: all four waves have the same columns and every fourth tile each, in a ring of their own without barriers,
+//   and are merged through LDS.
+// Where that leaves compute units idle the keys are cut into parts, each of which leaves its sums in the workspace (plan_prompt()).
+// A second launch folds the parts in order, appends the rows to the slab and moves the tables: the first launch reads them.
+#include <vector>
+
+#include "bc_prefill_tiles.h"
+
+namespace bc {
+namespace {
+
+struct PromptParams {
+  const char* q;               // [total, Hq, d]
+  const char* k;               // [total, Hkv, d]
+  const char* v;
+  char* k_slab;
+  char* v_slab;
+  const int64_t* base;
+  const int32_t* cap;
+  int32_t* cacheP;
+  const int32_t* cachec;
+  int32_t* nb;
+  int32_t* w;
+  int32_t* err;
+  const uint8_t* active;
+  float* out;                  // [total, Hq, d]
+  int32_t* resident;           // [B] rows in front of the chunk, -1: the sequence takes no part
+  float2* ml;                  // [parts][npairs][columns] maximum (log2) and sum of a part
+  float* sums;                 // [parts][npairs][columns][d]
+  const int64_t* row_off;      // the chunks' rows, as trajectory() takes them
+  const int32_t* P;
+  const int32_t* c;
+  int32_t B, Hq, Hkv, g;
+  int32_t npairs, pstride, parts;
+  int32_t columns;             // most columns of a pair, padded to a workgroup's
+  int32_t table_blocks, copy_blocks;      // of the second launch
+  float qscale;
+  InlineTables tab;
+};
+
+#define BC_INLINE __attribute__((always_inline))
+
+constexpr float kRedo = 256.f;      // a lane's 16 weights may sum to this before the reference moves
+constexpr float kLazy = 2.0f;       // ... and then it moves where a column's maximum is this much (log2) above it
+constexpr int kColumns = 32 * kTileWaves;
+constexpr int kFewStages = 2;
+
+// What a sequence's tables say: rows in front of the chunk, or -1 and the error bit to set.
+struct Resident { int rows, bit; };
+__device__ __forceinline__ Resident resident_rows(const PromptParams& p, int s, int n) {
+  if (n <= 0 || (p.active && !p.active[s])) return {-1, 0};
+  const int c = p.cachec[s], w = p.w[s], L = p.cacheP[s] + p.nb[s] + w;
+  if (c > 0 && w > c) return {-1, BC_ERRBIT_STATE};            // a beacon at the tail that has not been compacted
+  if ((int64_t)L + n > p.cap[s]) return {-1, BC_ERRBIT_CAPACITY};
+  return {L, 0};
+}
+
+// The keys of a workgroup's columns as a list of tiles: the slab's full ones (F), the new rows' that all of the columns see
+// (F1: nothing is masked up to here), what is left of the slab, the new rows' others.  (Values that differ between slab and new rows are held
+// as one and what is added for the other: chosen between two members of the structure, the compiler kept all of it in memory.)
+struct PromptTiles {
+  const char* k0;              // slab: the pair's first row
+  const char* v0;
+  int64_t dk, dv;              // from there to the pair's first new row
+  uint32_t row, drow;          // bytes from row to row of the slab, and more from new row to new row
+  int L, dL, F, F1, rest;      // rows of the slab; new rows less that; rest: 1 where a part of a tile of the slab is left
+  struct At { bool fresh; int row0; };
+  __device__ __forceinline__ int dense() const { return F + F1; }
+  __device__ __forceinline__ At at(int t) const {
+    const int u = t - F - F1;
+    const bool left = u >= 0 && u < rest;                     // the slab's last tile
+    const bool fresh = t >= F && !left;
+    return {fresh, (t - (fresh ? F + (u >= rest ? rest : 0) : left ? F1 : 0)) * kTileRows};
+  }
+  struct Load { const char* k; const char* v; uint32_t step; int valid; };
+  __device__ __forceinline__ Load load(int t) const {
+    const At a = at(t);
+    const uint32_t step = row + (a.fresh ? drow : 0u);
+    const int64_t off = (int64_t)a.row0 * step;
+    return {k0 + (a.fresh ? dk : 0) + off, v0 + (a.fresh ? dv : 0) + off, step, L + (a.fresh ? dL : 0) - a.row0};
+  }
+  // bit x: new row i may see key x of tile t
+  __device__ __forceinline__ uint32_t visible(int t, int i) const {
+    const At a = at(t);
+    const int upto = (a.fresh ? i : L - 1) - a.row0;
+    return upto < 0 ? 0u : upto >= 31 ? ~0u : (2u << upto) - 1u;
+  }
+};
+
+// A wave's 32 columns: accumulators and the running softmax, whose reference m is lazy (it moves only where a lane's weights
+// pass kRedo; a column's first visible tile always goes that way, its weights against -1e30 being infinite).
+template <int D>
+struct Columns {
+  static constexpr int KS = D / 16, NJ = D / 32;
+  bf16x8_t qb[KS];
+  f32x16_t O[NJ];
+  float m, l;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) O[j] = f32x16_t{0.f};
+    m = kNegBig; l = 0.f;
+  }
+  // One tile (K, then V behind it).  `next` asks for further tiles, behind the scores' products.  The order is written out as in
+  // the prefill kernels: operands are asked for several instructions ahead.
+  template <bool MASKED, typename F>
+  __device__ __forceinline__ void tile(const char* tile, int koff, int voff, uint32_t see, float qscale, const F& next) {
+    float pe[16], psum;
+    auto weights = [&](const f32x16_t& s) BC_INLINE {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        pe[e] = fast_exp2(fmaf(s[e], qscale, -m));
+        if constexpr (MASKED) pe[e] = keep_if_visible(pe[e], see, e);
+      }
+      psum = (((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]))) +
+             (((pe[8] + pe[9]) + (pe[10] + pe[11])) + ((pe[12] + pe[13]) + (pe[14] + pe[15])));
+    };
+    bf16x8_t r[KS], c[2 * NJ];
+    auto col_of = [&](int n) BC_INLINE { return cols_operand<D>(tile + voff, n % NJ, n / NJ); };
+#pragma unroll
+    for (int i = 0; i < KS; ++i) r[i] = *reinterpret_cast<const bf16x8_t*>(tile + koff + rows_read_imm<D>(i));
+    step_fence();
+    {
+      f32x16_t s = f32x16_t{0.f};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r[i], qb[i], s, 0, 0, 0);
+        if (i >= KS - NJ) c[i - KS + NJ] = col_of(i - KS + NJ);
+        step_fence();
+      }
+      next();
+      weights(s);
+    }
+    if (__builtin_expect(__any(psum > kRedo), 0)) {
+      f32x16_t s = f32x16_t{0.f};
+      const char* ka = tile + opaque(koff);                  // (reads the operands again)
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_t*>(ka + rows_read_imm<D>(i)), qb[i], s, 0, 0, 0);
+      float tmax = kNegBig;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, !MASKED || visible_bit(see, e) ? s[e] : kNegBig);
+      const float cand = halves_max(tmax) * qscale;
+      const float to = cand > m + kLazy ? cand : m;
+      const float alpha = fast_exp2(m - to);
+      m = to;
+      l *= alpha;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) O[j] *= alpha;
+      weights(s);
+    }
+    l += psum;
+    Parts y;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) y.split(g, pe[2 * g], pe[2 * g + 1]);
+    step_fence();
+#pragma unroll
+    for (int k = 0; k < 4 * NJ; ++k) {
+      const int n = k / 2;
+      O[n % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[n], y.operand(k & 1, n / NJ), O[n % NJ], 0, 0, 0);
+      if (k % 2 == 0 && n + NJ < 2 * NJ) c[n + NJ] = col_of(n + NJ);
+#pragma unroll
+      for (int g = 4; g < 8; ++g)
+        if (k == (g - 4) * NJ / 2) y.split(g, pe[2 * g], pe[2 * g + 1]);
+      step_fence();
+    }
+  }
+};
+
+// A wave's 32 query columns from column `first` on (the last one repeated behind it) -> a tile of its own in LDS.
+template <int D>
+__device__ __forceinline__ void issue_columns(const PromptParams& p, int64_t off0, int kvh, int first, int columns, int lane,
+                                              uint32_t lds_addr) {
+  constexpr int ROWB = D * 2;
+  const int i0 = min(first, columns - 1) / p.g;
+  const char* at = p.q + ((off0 + i0) * p.Hq + kvh * p.g) * ROWB;
+#pragma unroll
+  for (int rg = 0; rg < kTileRows / 8; ++rg) {
+    const TileLane t = rows_tile_lane(lane, rg);
+    const int x = min(first + t.row, columns - 1), i = x / p.g;
+    const uint32_t o = (uint32_t)((i - i0) * p.Hq + x - i * p.g) * ROWB + t.in_row;
+#pragma unroll
+    for (int n = 0; n < D / 64; ++n) issue_block<false>(at + 128 * n, o, lds_addr + n * 4096 + rg * 1024);
+  }
+}
+
+// The workgroup's place and its sequence; false: nothing to do.
+struct PromptWork {
+  int part, pair, kvh, s, n, columns, first;
+  int64_t off0;
+  PromptTiles tiles;
+  int t0, t1;                  // tiles of this part
+  template <int D, int WIDE>
+  __device__ __forceinline__ bool start(const PromptParams& p) {
+    constexpr int ROWB = D * 2;
+    part = blockIdx.x / p.pstride;
+    pair = blockIdx.x - part * p.pstride;
+    if (pair >= p.npairs) return false;
+    kvh = pair % p.Hkv;
+    s = pair / p.Hkv;
+    const Trajectory chunk = trajectory(p, s);
+    off0 = chunk.off0;
+    n = chunk.rows;
+    const int block = gridDim.y - 1 - blockIdx.y;              // long ones first
+    const Resident r = resident_rows(p, s, n);
+    if (block == 0 && part == 0 && kvh == 0 && threadIdx.x == 0) {
+      p.resident[s] = r.rows;
+      if (r.bit) atomicOr(p.err, r.bit);
+    }
+    columns = n * p.g;
+    first = block * WIDE;
+    if (r.rows < 0 || first >= columns) return false;
+    const int cap = p.cap[s];
+    const int64_t slab = (p.base[s] * p.Hkv + (int64_t)kvh * cap) * ROWB, fresh = (off0 * p.Hkv + kvh) * ROWB;
+    tiles.L = r.rows; tiles.dL = n - r.rows;
+    tiles.F = r.rows / kTileRows;
+    tiles.rest = r.rows % kTileRows ? 1 : 0;
+    tiles.F1 = (first / p.g + 1) / kTileRows;
+    tiles.k0 = p.k_slab + slab; tiles.v0 = p.v_slab + slab;
+    tiles.row = ROWB; tiles.drow = (uint32_t)(p.Hkv - 1) * ROWB;
+    tiles.dk = p.k + fresh - tiles.k0; tiles.dv = p.v + fresh - tiles.v0;
+    const int last = (min(first + WIDE, columns) - 1) / p.g;                     // row of the last column
+    const int NT = tiles.F + tiles.rest + last / kTileRows + 1;
+    t0 = (int)((int64_t)NT * part / p.parts);
+    t1 = (int)((int64_t)NT * (part + 1) / p.parts);
+    return true;
+  }
+  // where a column's sums of this part go
+  __device__ __forceinline__ int64_t slot(const PromptParams& p, int column) const {
+    return ((int64_t)part * p.npairs + pair) * p.columns + column;
+  }
+};
+
+template <int D> constexpr int prompt_lds() { return kTileStages * 2 * kTileRows * D * 2; }
+
+// 128 columns: 32 a wave, tiles shared.
+template <int D>
+__global__ __launch_bounds__(kTileWaves * 64, 3) void prompt_attn_kernel(PromptParams p) {
+  constexpr int ROWB = D * 2, TILE = kTileRows * ROWB, NLD = TILE / 1024 / kTileWaves, OW = D / 2;
+  __shared__ __attribute__((aligned(1024))) char lds[prompt_lds<D>()];
+  static_assert(prompt_lds<D>() >= kTileWaves * 32 * OW * 4 && prompt_lds<D>() >= (2 + kTileWaves) * TILE, "LDS");
+  PromptWork wk;
+  if (!wk.start<D, kColumns>(p)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int first = wk.first + 32 * wave;
+  const int i = min(first + col, wk.columns - 1) / p.g;                                   // new row of this lane's column
+  const int i_last = (min(first + 32, wk.columns) - 1) / p.g;
+  // tiles this wave works on; the others it loads and passes with the workgroup
+  const int mine = first < wk.columns ? min(wk.t1, wk.tiles.F + wk.tiles.rest + i_last / kTileRows + 1) : 0;
+  const PromptTiles& tiles = wk.tiles;
+
+  const uint32_t lds0 = lds_address(lds) + wave * 1024;
+  const TileLane klane = rows_tile_lane(lane, wave), vlane = cols_tile_lane(lane, wave);
+  auto issue_tile = [&](int t, int stage) BC_INLINE {
+    const PromptTiles::Load ld = tiles.load(t);
+    const uint32_t ko = (uint32_t)(klane.row < ld.valid ? klane.row : 0) * ld.step + klane.in_row;
+    const uint32_t vo = (uint32_t)(vlane.row < ld.valid ? vlane.row : 0) * ld.step + vlane.in_row;
+#pragma unroll
+    for (int n = 0; n < NLD; ++n) {
+      issue_block<false>(ld.k + 128 * n, ko, lds0 + stage * (2 * TILE) + n * 4096);
+      issue_block<false>(ld.v + 128 * n, vo, lds0 + stage * (2 * TILE) + TILE + n * 4096);
+    }
+  };
+  Columns<D> x;
+  x.clear();
+  if (wk.t0 < wk.t1) {
+    issue_tile(wk.t0, 0);
+    issue_columns<D>(p, wk.off0, wk.kvh, first, wk.columns, lane, lds_address(lds) + (2 + wave) * TILE);
+    wait_vmcnt<0>();
+    read_wave_rows<D>(lds + (2 + wave) * TILE, lane, x.qb);
+    landed_operands(x.qb);
+    lds_barrier();
+    if (wk.t0 + 1 < wk.t1) issue_tile(wk.t0 + 1, 1);
+  }
+  const int koff = rows_read_offset(lane), voff = TILE + cols_read_offset(lane);
+  int stage = 0, t = wk.t0;
+  // tile t has landed and everyone has finished t - 1, whose stage t + 2 goes into
+  auto begin_pass = [&]() BC_INLINE {
+    if (t + 1 < wk.t1) wait_vmcnt<2 * NLD>();
+    else wait_vmcnt<0>();
+    lds_barrier();
+  };
+  auto next = [&]() BC_INLINE { if (t + 2 < wk.t1) issue_tile(t + 2, stage >= 1 ? stage - 1 : kTileStages - 1); };
+  auto end_pass = [&]() BC_INLINE { stage = stage + 1 == kTileStages ? 0 : stage + 1; };
+  for (const int dense = min(tiles.dense(), mine); t < dense; ++t) {
+    begin_pass();
+    x.template tile<false>(lds + stage * (2 * TILE), koff, voff, ~0u, p.qscale, next);
+    end_pass();
+  }
+  for (; t < mine; ++t) {
+    begin_pass();
+    x.template tile<true>(lds + stage * (2 * TILE), koff, voff, tiles.visible(t, i) >> (4 * half), p.qscale, next);
+    end_pass();
+  }
+  for (; t < wk.t1; ++t) {
+    begin_pass();
+    next();
+    end_pass();
+  }
+  lds_barrier();          // the stages are free: the results go through them
+  if (first >= wk.columns) return;
+  const float l = halves_sum(x.l);
+  float* my = reinterpret_cast<float*>(lds + wave * (32 * OW * 4));
+  const int left = wk.columns - first;
+  if (p.parts == 1) {
+    const float inv = 1.0f / l;
+    float* out = p.out + (wk.off0 * p.Hq + wk.kvh * p.g) * D;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass)
+      store_rows<D>(my, x.O, inv, pass, lane, out, D, [&](int t) {
+        const int c = first + t, r = c / p.g;
+        return t < left ? r * p.Hq + c - r * p.g : -1;
+      });
+  } else {
+    if (half == 0 && col < left) p.ml[wk.slot(p, first + col)] = make_float2(x.m, l);
+    if (wk.t0 >= wk.t1) return;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass)
+      store_rows<D>(my, x.O, 1.f, pass, lane, p.sums + wk.slot(p, first) * D, D, [&](int t) { return t < left ? t : -1; });
+  }
+}
+
+template <int D> constexpr int prompt_few_lds() { return kTileWaves * kFewStages * 2 * kTileRows * D * 2; }
+
+// 32 columns: the same for every wave, which has every fourth tile.
+template <int D>
+__global__ __launch_bounds__(kTileWaves * 64, 1) void prompt_few_kernel(PromptParams p) {
+  constexpr int ROWB = D * 2, TILE = kTileRows * ROWB, RG = kTileRows / 8, NLD = 2 * RG * (D / 64), MINE = kFewStages * 2 * TILE;
+  __shared__ __attribute__((aligned(1024))) char lds[prompt_few_lds<D>()];
+  __shared__ float2 wave_ml[kTileWaves][32];
+  PromptWork wk;
+  if (!wk.start<D, 32>(p)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int i = min(col, wk.columns - 1) / p.g;
+  const PromptTiles& tiles = wk.tiles;
+  char* own = lds + wave * MINE;
+  const uint32_t own_at = lds_address(lds) + wave * MINE;
+  auto issue_tile = [&](int t, int stage) BC_INLINE {
+    const PromptTiles::Load ld = tiles.load(t);
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const TileLane kl = rows_tile_lane(lane, rg), vl = cols_tile_lane(lane, rg);
+      const uint32_t ko = (uint32_t)(kl.row < ld.valid ? kl.row : 0) * ld.step + kl.in_row;
+      const uint32_t vo = (uint32_t)(vl.row < ld.valid ? vl.row : 0) * ld.step + vl.in_row;
+#pragma unroll
+      for (int n = 0; n < D / 64; ++n) {
+        issue_block<false>(ld.k + 128 * n, ko, own_at + stage * (2 * TILE) + n * 4096 + rg * 1024);
+        issue_block<false>(ld.v + 128 * n, vo, own_at + stage * (2 * TILE) + TILE + n * 4096 + rg * 1024);
+      }
+    }
+  };
+  Columns<D> x;
+  x.clear();
+  const int first = wk.t0 + wave;
+  if (first < wk.t1) {
+    issue_tile(first, 0);
+    issue_columns<D>(p, wk.off0, wk.kvh, 0, wk.columns, lane, own_at + 2 * TILE);
+    wait_vmcnt<0>();
+    read_wave_rows<D>(own + 2 * TILE, lane, x.qb);
+    landed_operands(x.qb);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (first + kTileWaves < wk.t1) issue_tile(first + kTileWaves, 1);
+  }
+  const int koff = rows_read_offset(lane), voff = TILE + cols_read_offset(lane);
+  int stage = 0;
+  for (int t = first; t < wk.t1; t += kTileWaves) {
+    if (t + kTileWaves < wk.t1) wait_vmcnt<NLD>();
+    else wait_vmcnt<0>();
+    const char* at = own + stage * (2 * TILE);
+    auto nothing = [] {};
+    if (t < tiles.dense())
+      x.template tile<false>(at, koff, voff, ~0u, p.qscale, nothing);
+    else
+      x.template tile<true>(at, koff, voff, tiles.visible(t, i) >> (4 * half), p.qscale, nothing);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // the stage has been read
+    if (t + 2 * kTileWaves < wk.t1) issue_tile(t + 2 * kTileWaves, stage);
+    stage ^= 1;
+  }
+  // merge: every wave's sums at the start of its own stages
+  constexpr int UNITS = D / 4;
+  const float l = halves_sum(x.l);
+  float* mine = reinterpret_cast<float*>(own);
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      *reinterpret_cast<f32x4_t*>(mine + col * D + (((8 * j + 2 * u + half) ^ (col & (UNITS - 1))) << 2)) =
+          f32x4_t{x.O[j][4 * u], x.O[j][4 * u + 1], x.O[j][4 * u + 2], x.O[j][4 * u + 3]};
+  if (half == 0) wave_ml[wave][col] = make_float2(x.m, l);
+  __syncthreads();
+  for (int at = threadIdx.x; at < 32 * UNITS; at += kTileWaves * 64) {
+    const int c = at / UNITS, unit = at % UNITS;
+    if (c >= wk.columns) break;
+    float M = kNegBig, sum = 0.f;
+#pragma unroll
+    for (int wv = 0; wv < kTileWaves; ++wv) M = fmaxf(M, wave_ml[wv][c].x);
+    f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int wv = 0; wv < kTileWaves; ++wv) {
+      const float f = fast_exp2(wave_ml[wv][c].x - M);
+      sum += wave_ml[wv][c].y * f;
+      o += *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(lds + wv * MINE) + c * D + ((unit ^ (c & (UNITS - 1))) << 2)) * f;
+    }
+    if (p.parts == 1) {
+      const int r = c / p.g;
+      float* to = p.out + ((wk.off0 + r) * p.Hq + wk.kvh * p.g + c - r * p.g) * D;
+      *reinterpret_cast<f32x4_t*>(to + 4 * unit) = o * (1.0f / sum);
+    } else {
+      const int64_t slot = wk.slot(p, c);
+      if (unit == 0) p.ml[slot] = make_float2(M, sum);
+      if (wk.t0 < wk.t1) *reinterpret_cast<f32x4_t*>(p.sums + slot * D + 4 * unit) = o;
+    }
+  }
+}
+
+// The second launch: tables, append, and the fold of the parts.  What the first one decided is in p.resident.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_finish_kernel(PromptParams p) {
+  constexpr int UNITS = D / 4, ROWB = D * 2, RU = ROWB / 16;
+  int block = blockIdx.x;
+  if (block < p.table_blocks) {
+    const int s = block * 256 + threadIdx.x;
+    if (s < p.B && p.resident[s] >= 0) {
+      const Trajectory chunk = trajectory(p, s);
+      p.cacheP[s] = p.resident[s] + chunk.rows;
+      p.nb[s] = 0;
+      p.w[s] = 0;
+    }
+    return;
+  }
+  block -= p.table_blocks;
+  if (block < p.copy_blocks * p.B) {
+    const int s = block / p.copy_blocks, slice = block - s * p.copy_blocks, L = p.resident[s];
+    if (L < 0) return;
+    const Trajectory chunk = trajectory(p, s);
+    const int cap = p.cap[s];
+    const int64_t slab = p.base[s] * p.Hkv, units = (int64_t)chunk.rows * p.Hkv * RU;
+    for (int64_t u = (int64_t)slice * 256 + threadIdx.x; u < units; u += (int64_t)p.copy_blocks * 256) {
+      const int64_t row = u / RU;                               // (new row, KV head)
+      const int i = (int)(row / p.Hkv), h = (int)(row - (int64_t)i * p.Hkv), at = (int)(u - row * RU);
+      const int64_t from = (chunk.off0 * p.Hkv + row) * ROWB + 16 * at, to = (slab + (int64_t)h * cap + L + i) * ROWB + 16 * at;
+      *reinterpret_cast<uint4*>(p.k_slab + to) = *reinterpret_cast<const uint4*>(p.k + from);
+      *reinterpret_cast<uint4*>(p.v_slab + to) = *reinterpret_cast<const uint4*>(p.v + from);
+    }
+    return;
+  }
+  block -= p.copy_blocks * p.B;
+  const int pair = block % p.npairs, s = pair / p.Hkv;
+  if (p.resident[s] < 0) return;
+  const Trajectory chunk = trajectory(p, s);
+  const int c = block / p.npairs * (256 / UNITS) + threadIdx.x / UNITS, unit = threadIdx.x % UNITS;
+  if (c >= chunk.rows * p.g) return;
+  const int64_t slot = (int64_t)pair * p.columns + c, step = (int64_t)p.npairs * p.columns;
+  float M = kNegBig;
+  for (int n = 0; n < p.parts; ++n) M = fmaxf(M, p.ml[slot + n * step].x);
+  float sum = 0.f;
+  f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < p.parts; ++n) {
+    const float2 ml = p.ml[slot + n * step];
+    if (ml.y > 0.f) {                                           // (a part without tiles has left no sums)
+      const float f = fast_exp2(ml.x - M);
+      sum += ml.y * f;
+      o += *reinterpret_cast<const f32x4_t*>(p.sums + (slot + n * step) * D + 4 * unit) * f;
+    }
+  }
+  const int r = c / p.g;
+  float* to = p.out + ((chunk.off0 + r) * p.Hq + pair % p.Hkv * p.g + c - r * p.g) * D;
+  *reinterpret_cast<f32x4_t*>(to + 4 * unit) = o * (1.0f / sum);
+}
+
+// How a call is cut.  Lengths of the caches are on the device; the capacity stands for them.
+struct PromptPlan {
+  bool few;
+  int blocks;                  // workgroups along a pair's columns
+  int parts;
+  int64_t columns;             // of a pair, padded
+  size_t bytes, ml_at, sums_at, tables_at;
+};
+PromptPlan plan_prompt(const bc_shape* sh, int64_t max_new, int64_t total, int32_t max_cap) {
+  const int64_t g = sh->Hq / sh->Hkv, npairs = (int64_t)sh->B * sh->Hkv;
+  PromptPlan pl;
+  pl.few = max_new * g <= 32;
+  const int64_t wide = pl.few ? 32 : kColumns;
+  pl.blocks = (int)((max_new * g + wide - 1) / wide);
+  if (pl.blocks < 1) pl.blocks = 1;
+  pl.columns = pl.blocks * wide;
+  // workgroups there will be about, and as many as run at once
+  const int64_t all = (total * g / wide + sh->B) * sh->Hkv, most = npairs * pl.blocks, work = all < most ? all : most;
+  const int64_t room = pl.few ? 256 : 768, tiles = (max_cap + kTileRows - 1) / kTileRows;
+  int64_t parts = work > 0 ? room / work : 1;
+  const int64_t enough = tiles / (pl.few ? 4 : 8);
+  if (parts > enough) parts = enough;
+  pl.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+  size_t at = ((size_t)sh->B * 4 + 15) & ~(size_t)15;
+  pl.tables_at = at;
+  if (sh->B > BC_INLINE_TRAJECTORIES) at += ((size_t)sh->B * 16 + 8 + 15) & ~(size_t)15;
+  pl.ml_at = at;
+  if (pl.parts > 1) at += (size_t)pl.parts * npairs * pl.columns * sizeof(float2);
+  pl.sums_at = at;
+  if (pl.parts > 1) at += (size_t)pl.parts * npairs * pl.columns * sh->d * sizeof(float);
+  pl.bytes = at;
+  return pl;
+}
+
+template <int D>
+void launch_prompt(const PromptParams& p, const PromptPlan& pl, hipStream_t s) {
+  const dim3 grid(p.pstride * p.parts, pl.blocks);
+  if (pl.few) prompt_few_kernel<D><<<grid, kTileWaves * 64, 0, s>>>(p);
+  else prompt_attn_kernel<D><<<grid, kTileWaves * 64, 0, s>>>(p);
+  const int per = 256 / (D / 4);
+  const int64_t fold = p.parts > 1 ? (int64_t)p.npairs * ((pl.columns + per - 1) / per) : 0;
+  prompt_finish_kernel<D><<<(unsigned)(p.table_blocks + (int64_t)p.copy_blocks * p.B + fold), 256, 0, s>>>(p);
+}
+
+}  // namespace
+}  // namespace bc
+
+using namespace bc;
+
+extern "C" size_t bc_prompt_workspace_bytes(const bc_shape* shape, int32_t max_new, int64_t total_new, int32_t max_cap) {
+  if (check_shape(shape) != BC_OK || max_new < 0 || total_new < 0 || max_cap < 1) return 0;
+  return plan_prompt(shape, max_new, total_new, max_cap).bytes;
+}
+
+extern "C" int32_t bc_prompt_step(const bc_shape* shape, const bc_cache* cache, const void* k, const void* v, const void* q,
+                                  const int64_t* row_offsets, float* out, const uint8_t* active, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  int32_t st = check_shape(shape);
+  if (st != BC_OK) return st;
+  if (shape->kv_dtype != BC_BF16) return BC_ERR_SHAPE;
+  st = check_cache(cache);
+  if (st != BC_OK) return st;
+  if (!row_offsets || !positive_finite(shape->scale)) return BC_ERR_ARG;
+  int64_t max_new = 0;
+  if (row_offsets[0] < 0) return BC_ERR_ARG;
+  for (int b = 0; b < shape->B; ++b) {
+    const int64_t n = row_offsets[b + 1] - row_offsets[b];
+    if (n < 0) return BC_ERR_ARG;
+    if (n > max_new) max_new = n;
+  }
+  const int64_t total = row_offsets[shape->B] - row_offsets[0];
+  if (total == 0) return BC_OK;
+  if (!k || !v || !q || !out || !aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(out)) return BC_ERR_ARG;
+  if (max_new * shape->Hq >= (1LL << 31) || (int64_t)shape->B * shape->Hkv > (1 << 24)) return BC_ERR_SHAPE;
+  const PromptPlan pl = plan_prompt(shape, max_new, total, cache->max_cap);
+  if (pl.blocks > 65535) return BC_ERR_SHAPE;
+  if (!workspace || !aligned16(workspace) || workspace_bytes < pl.bytes) return BC_ERR_WORKSPACE;
+  PromptParams p{};
+  if (shape->B <= BC_INLINE_TRAJECTORIES) {
+    const int32_t none[BC_INLINE_TRAJECTORIES] = {};
+    st = host_tables(p, row_offsets, none, none, shape->B, nullptr, stream);
+  } else {
+    std::vector<int64_t> words;                                // offsets, and in place of P and c zeros
+    try {
+      words.assign((size_t)2 * shape->B + 1, 0);
+    } catch (...) {
+      return BC_ERR_ARG;
+    }
+    for (int b = 0; b <= shape->B; ++b) words[b] = row_offsets[b];
+    const int32_t* none = reinterpret_cast<const int32_t*>(words.data() + shape->B + 1);
+    st = host_tables(p, words.data(), none, none + shape->B, shape->B, static_cast<char*>(workspace) + pl.tables_at, stream);
+  }
+  if (st != BC_OK) return st;
+  char* ws = static_cast<char*>(workspace);
+  p.q = static_cast<const char*>(q); p.k = static_cast<const char*>(k); p.v = static_cast<const char*>(v);
+  p.k_slab = static_cast<char*>(cache->k_slab); p.v_slab = static_cast<char*>(cache->v_slab);
+  p.base = cache->base; p.cap = cache->cap; p.cacheP = cache->P; p.cachec = cache->c;
+  p.nb = cache->nb; p.w = cache->w; p.err = cache->err;
+  p.active = active; p.out = out;
+  p.resident = reinterpret_cast<int32_t*>(ws);
+  p.ml = reinterpret_cast<float2*>(ws + pl.ml_at);
+  p.sums = reinterpret_cast<float*>(ws + pl.sums_at);
+  p.B = shape->B; p.Hq = shape->Hq; p.Hkv = shape->Hkv; p.g = shape->Hq / shape->Hkv;
+  p.npairs = shape->B * shape->Hkv;
+  p.pstride = pair_stride(p.npairs);
+  p.parts = pl.parts;
+  p.columns = (int32_t)pl.columns;
+  p.table_blocks = (shape->B + 255) / 256;
+  const int64_t units = max_new * shape->Hkv * (shape->d / 8);
+  const int64_t copies = (units + 1023) / 1024, share = 4096 / shape->B + 1;
+  p.copy_blocks = (int32_t)(copies < share ? copies : share);
+  p.qscale = shape->scale * kLog2e;
+  hipStream_t s = as_stream(stream);
+  if (shape->d == 128) launch_prompt<128>(p, pl, s);
+  else launch_prompt<64>(p, pl, s);
+  return launch_status();
+}

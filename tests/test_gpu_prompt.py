@@ -1,0 +1,217 @@
+"""GPU parity: bc_prompt_step against the fp64 oracle.
+
+Softmax weights enter the value product in two bf16 parts (relative error 2^-17), scores are fp32 sums of up to 128 products and go through a
+2^x of one step: relative error of a weight below 2e-5 in all, so outputs of N(0,1) values (below 5 in magnitude) are off by less
+than 1e-4.  Rows in the slab and tables are exact."""
+import numpy as np
+import pytest
+
+from oracle import attention as OA
+
+pytestmark = pytest.mark.gpu
+TOL = 1e-4
+
+
+@pytest.fixture(scope="module")
+def dev():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch.device("cuda:0")
+
+
+def _runtime(dev, Hq, Hkv, d, lens, cap, c=16, seed=0):
+    """Caches that hold lens = [(P, nb, w)] rows; rows beyond are NaN."""
+    import torch
+    from paper_2510_13797_amd import bc
+    P, nb, w = (np.array(x, np.int32) for x in zip(*lens))
+    rt = bc.Runtime(len(P), Hq, Hkv, d, "bf16", 1.0 / np.sqrt(d), P, np.full(len(P), c), cap, dev)
+    g = torch.Generator(device=dev).manual_seed(seed)
+    for s in range(len(P)):
+        L, E = int(P[s] + nb[s] + w[s]), Hkv * d
+        for slab in (rt.k_slab, rt.v_slab):
+            at = int(rt.base_host[s]) * E
+            slab[at:at + int(cap[s]) * E].view(Hkv, int(cap[s]), d)[:, :L] = torch.randn(Hkv, L, d, generator=g, device=dev).bfloat16()
+    rt.set_tables(nb, w)
+    return rt
+
+
+def _rows(dev, rt, rows, seed=1):
+    import torch
+    g = torch.Generator(device=dev).manual_seed(seed)
+    return tuple(torch.randn(rows, h, rt.d, generator=g, device=dev).bfloat16() for h in (rt.Hkv, rt.Hkv, rt.Hq))
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _check(dev, Hq, Hkv, d, lens, n, active=None, first=0, spare=3, cap=None, every=1):
+    import torch
+    B = len(lens)
+    n = np.asarray(n)
+    off = first + np.concatenate([[0], np.cumsum(n)])
+    L = np.array([sum(x) for x in lens])
+    cap = L + n + spare if cap is None else cap
+    rt = _runtime(dev, Hq, Hkv, d, lens, cap)
+    k, v, q = _rows(dev, rt, int(off[-1]))
+    before = [rt.resident(s) for s in range(B)]
+    out = torch.full((int(off[-1]), Hq, d), 7.0, device=dev)
+    assert rt.prompt_step(k, v, q, off, active=active, out=out) is out
+    nb, w, err = rt.tables()
+    assert err == 0
+    kn, vn, qn, got = _np(k), _np(v), _np(q), _np(out)
+    assert (got[:first] == 7).all()
+    Pn = rt.P.cpu().numpy()
+    for s in range(B):
+        K, V = before[s]
+        rows = slice(int(off[s]), int(off[s + 1]))
+        if n[s] == 0 or (active is not None and not active[s]):
+            assert (Pn[s], nb[s], w[s]) == tuple(lens[s]) and (got[rows] == 7).all()
+            continue
+        assert (Pn[s], nb[s], w[s]) == (L[s] + n[s], 0, 0)
+        K, V = np.concatenate([K, kn[rows]]), np.concatenate([V, vn[rows]])
+        Kd, Vd = rt.resident(s)
+        assert np.array_equal(Kd, K) and np.array_equal(Vd, V)
+        for i in range(0, int(n[s]), every):
+            ref = OA.decode_attention(qn[off[s] + i], K[:L[s] + i + 1], V[:L[s] + i + 1], rt.shape.scale)
+            worst = np.abs(got[off[s] + i] - ref).max()
+            assert worst <= TOL, (s, i, worst)
+
+
+HEADS = [(4, 1, 64), (12, 2, 128), (32, 8, 128), (7, 7, 64), (5, 1, 128), (16, 2, 64)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", HEADS)
+def test_few_rows(dev, Hq, Hkv, d):
+    # up to 32 columns a pair: no cached row, one, around a tile's 32, several
+    _check(dev, Hq, Hkv, d, [(0, 0, 0), (1, 0, 0), (20, 6, 5), (32, 0, 0), (33, 0, 0), (100, 40, 7)], [3, 1, 4, 2, 0, 4])
+    _check(dev, Hq, Hkv, d, [(0, 0, 0)], [1])
+    _check(dev, Hq, Hkv, d, [(1000, 100, 9)], [4])
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", HEADS)
+def test_many_rows(dev, Hq, Hkv, d):
+    _check(dev, Hq, Hkv, d, [(0, 0, 0), (31, 0, 0), (64, 0, 0), (50, 30, 16), (7, 1, 0)], [65, 33, 1, 130, 0], every=5)
+    _check(dev, Hq, Hkv, d, [(700, 20, 3)], [97], every=7)
+
+
+@pytest.mark.parametrize("n", [31, 32, 33, 63, 64, 65, 96, 127, 128, 129])
+@pytest.mark.parametrize("L", [0, 32, 45])
+def test_ends_of_tiles(dev, n, L):
+    _check(dev, 4, 1, 128, [(L, 0, 0)], [n], every=3)
+    _check(dev, 4, 4, 64, [(L, 0, 0)], [n], every=3)
+
+
+def test_more_sequences_than_travel_in_the_arguments(dev):
+    r = np.random.default_rng(3)
+    lens = [tuple(int(x) for x in (r.integers(0, 80), r.integers(0, 20), r.integers(0, 17))) for _ in range(40)]
+    n = r.integers(0, 40, 40)
+    n[[0, 39]] = 0, 5
+    _check(dev, 12, 2, 64, lens, n, active=(r.random(40) < 0.8).astype(np.uint8), every=3)
+    _check(dev, 12, 2, 128, lens, np.minimum(n, 5), every=2)
+
+
+def test_rows_in_front_and_idle_sequences(dev):
+    _check(dev, 8, 2, 128, [(40, 2, 1), (9, 0, 0), (60, 0, 3)], [20, 11, 30], active=np.array([1, 0, 1], np.uint8), first=5, every=2)
+
+
+def test_long_cache_in_parts(dev):
+    _check(dev, 4, 1, 128, [(9000, 0, 0)], [5])
+    _check(dev, 4, 1, 128, [(9000, 0, 0)], [70], every=23)
+    # capacity far beyond what is resident: parts without tiles
+    _check(dev, 4, 1, 64, [(3, 0, 0), (40, 0, 0)], [5, 6], cap=np.array([20000, 20000]))
+    _check(dev, 4, 1, 64, [(3, 0, 0), (40, 0, 0)], [50, 60], cap=np.array([20000, 20000]), every=7)
+
+
+def test_offsets_beyond_32_bits(dev):
+    # the second sequence starts 4.9 GB into its slab, and its heads lie 1.2 GB apart
+    cap = np.array([4800000, 4800000])
+    _check(dev, 8, 4, 128, [(3, 0, 0), (77, 0, 2)], [4, 70], cap=cap, every=9)
+    _check(dev, 8, 4, 128, [(3, 0, 0), (77, 0, 2)], [4, 7], cap=cap)
+
+
+def test_peaked_rows(dev):
+    # one key dominates, first or last: the reference of the running softmax has to move late
+    import torch
+    from paper_2510_13797_amd import bc
+    for n in (4, 60):
+        rt = _runtime(dev, 4, 1, 64, [(150, 0, 0)], np.array([300]))
+        k, v, q = _rows(dev, rt, n)
+        rt.k_slab.view(300, 64)[140] *= 16
+        k[n // 2] *= 24
+        K, V = rt.resident(0)
+        got = _np(rt.prompt_step(k, v, q, [0, n]))
+        K, V = np.concatenate([K, _np(k)]), np.concatenate([V, _np(v)])
+        for i in range(n):
+            ref = OA.decode_attention(_np(q)[i], K[:151 + i], V[:151 + i], rt.shape.scale)
+            # (scores of a hundred: fp32 sums of that size are off by 128 * 2^-24 * 100 in the exponent)
+            assert np.abs(got[i] - ref).max() <= 1e-3, i
+
+
+def test_sequences_that_cannot_take_their_rows_are_left_alone(dev):
+    import torch
+    from paper_2510_13797_amd import bc
+    for n in (3, 50):
+        lens, cap = [(10, 0, 0), (20, 1, 17), (12, 0, 2)], np.array([10 + n - 1, 200, 14 + n])
+        rt = _runtime(dev, 4, 1, 64, lens, cap)
+        k, v, q = _rows(dev, rt, 3 * n)
+        keep = [x.clone() for x in (rt.k_slab, rt.v_slab)]
+        out = torch.full((3 * n, 4, 64), 7.0, device=dev)
+        rt.prompt_step(k, v, q, [0, n, 2 * n, 3 * n], out=out)
+        nb, w, err = rt.tables()
+        assert err == bc.BC_ERRBIT_CAPACITY | bc.BC_ERRBIT_STATE
+        assert rt.P.tolist() == [10, 20, 14 + n] and list(nb) == [0, 1, 0] and list(w) == [0, 17, 0]
+        assert (out[:2 * n] == 7).all() and torch.isfinite(out[2 * n:]).all() and not (out[2 * n:] == 7).all()
+        own = int(rt.base_host[2]) * 64
+        for slab, old in zip((rt.k_slab, rt.v_slab), keep):
+            assert torch.equal(slab[:own].view(torch.int16), old[:own].view(torch.int16))
+
+
+def test_pieces_give_what_the_whole_prompt_gives(dev):
+    # a prompt in three chunks against the training-time attention without windows, then decode steps over either
+    import torch
+    from paper_2510_13797_amd import bc
+    n, Hq, Hkv, d = 213, 12, 2, 128
+    rt = _runtime(dev, Hq, Hkv, d, [(0, 0, 0)], np.array([400]), c=4)
+    k, v, q = _rows(dev, rt, n)
+    whole, _ = bc.prefill_attn(q, k, v, [0, n], [n], [0], Hq, Hkv, d, rt.shape.scale)
+    outs = []
+    for lo, hi in ((0, 100), (100, 103), (103, n)):
+        outs.append(rt.prompt_step(k[lo:hi], v[lo:hi], q[lo:hi], [0, hi - lo]))
+    assert (torch.cat(outs) - whole).abs().max().item() <= 2 * TOL
+    other = bc.Runtime(1, Hq, Hkv, d, "bf16", rt.shape.scale, [n], [4], [400], dev)
+    other.cache_init([k.float().cpu().numpy()], [v.float().cpu().numpy()])
+    for t in range(10):
+        x = [y[:1].contiguous() for y in _rows(dev, rt, 1, seed=50 + t)]
+        bk, bv, _ = _rows(dev, rt, 1, seed=80 + t)
+        assert torch.equal(rt.decode_step(*x, bk, bv).clone(), other.decode_step(*x, bk, bv).clone())
+    assert [list(y) for y in rt.tables()[:2]] == [list(y) for y in other.tables()[:2]] == [[2], [2]]
+
+
+def test_captured_and_replayed(dev):
+    import torch
+    lens = [(100, 3, 2), (5, 0, 0)]
+    for n in ((3, 2), (90, 40)):
+        rt = _runtime(dev, 12, 2, 128, lens, np.array([2000, 2000]))
+        start = torch.stack([rt.P, rt.nb, rt.w]).clone()
+        tables = start.clone()
+        rt.P, rt.nb, rt.w = tables[0], tables[1], tables[2]
+        rt.cache.P, rt.cache.nb, rt.cache.w = rt.P.data_ptr(), rt.nb.data_ptr(), rt.w.data_ptr()
+        k, v, q = _rows(dev, rt, sum(n))
+        off = [0, n[0], sum(n)]
+        want = rt.prompt_step(k, v, q, off).clone()
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=st):
+                torch.add(start, 0, out=tables)
+                out = rt.prompt_step(k, v, q, off)
+            for _ in range(3):
+                out.fill_(3.0)
+                graph.replay()
+                st.synchronize()
+                assert torch.equal(out, want) and tables[0].tolist() == [105 + n[0], 5 + n[1]]
+                rt.decode_attn(q[:2])                          # eager work between replays
+                st.synchronize()
+            assert rt.tables()[2] == 0

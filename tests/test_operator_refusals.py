@@ -1,4 +1,5 @@
 """What the calls around the attention refuse (host logic only: no GPU needed; addresses are made up and never dereferenced)."""
+import numpy as np
 import pytest
 import torch
 
@@ -55,3 +56,39 @@ def test_rope_binding_refuses_what_the_library_cannot_see():
     for args in ((qkv[:, :500], pos, freq), (qkv[0], pos, freq), (qkv, pos, freq), (qkv.half(), pos, freq)):
         with pytest.raises(bc.BcError):
             bc.qk_norm_rope(*args, 4, 2, 64)
+
+
+def _cache(**kw):
+    f = dict(k_slab=PTR, v_slab=PTR, base=PTR, cap=PTR, P=PTR, c=PTR, nb=PTR, w=PTR, err=PTR, max_cap=64, order=None, uniform_P=0,
+             uniform_cap=0, rows_per_workgroup=0, plan=0)
+    f.update(kw)
+    return bc.bc_cache(**f)
+
+
+def _prompt(s=None, c=None, k=PTR, v=PTR, q=PTR, off=(0, 3, 8), out=PTR, active=None, ws=PTR, nbytes=1 << 40):
+    host = None if off is None else np.asarray(off, np.int64)
+    return bc.bc_prompt_step(s or shape(B=2), c or _cache(), k, v, q, None if off is None else host.ctypes.data, out, active, ws, nbytes,
+                             None)
+
+
+def test_prompt_refusals():
+    bc.load()
+    for kw in (dict(Hq=5), dict(Hkv=0), dict(d=96), dict(dtype=bc.BC_F32), dict(Hq=18)):
+        assert _prompt(s=shape(B=2, **kw)) == bc.BC_ERR_SHAPE, kw
+    for field in ("k_slab", "v_slab", "base", "cap", "P", "c", "nb", "w", "err"):
+        assert _prompt(c=_cache(**{field: None})) == bc.BC_ERR_ARG, field
+    assert _prompt(c=_cache(max_cap=0)) == bc.BC_ERR_ARG
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert _prompt(s=shape(B=2, scale=scale)) == bc.BC_ERR_ARG
+    for kw in (dict(k=None), dict(v=None), dict(q=None), dict(out=None), dict(k=ODD), dict(v=ODD), dict(q=ODD), dict(out=ODD), dict(off=None),
+               dict(off=(0, 3, 2)), dict(off=(-1, 3, 8))):
+        assert _prompt(**kw) == bc.BC_ERR_ARG, kw
+    assert _prompt(off=(0, 1 << 30, 1 << 30)) == bc.BC_ERR_SHAPE
+    need = bc.bc_prompt_workspace_bytes(shape(B=2), 5, 8, 64)
+    assert need >= 8
+    for kw in (dict(ws=None), dict(ws=ODD), dict(nbytes=need - 1)):
+        assert _prompt(**kw) == bc.BC_ERR_WORKSPACE, kw
+    # nothing to do is no error
+    assert _prompt(off=(4, 4, 4), k=None, v=None, q=None, out=None, ws=None) == bc.BC_OK
+    assert bc.bc_prompt_workspace_bytes(shape(d=96), 5, 8, 64) == 0 and bc.bc_prompt_workspace_bytes(shape(), -1, 8, 64) == 0
+    assert bc.bc_prompt_workspace_bytes(shape(), 5, 8, 0) == 0
