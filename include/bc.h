@@ -420,6 +420,23 @@ int32_t bc_qk_norm_rope_bwd(const bc_shape *shape, int64_t rows, const void *qkv
                             void *dqkv, int64_t dqkv_row_stride, float *dq_weight, float *dk_weight,
                             void *workspace, size_t workspace_bytes, void *stream);
 
+/* The next token of every sequence from its logits (Alg. 1 samples x_i; Sec. 4 evaluates sampled generations), with random numbers
+ * that the caller gives.  Row b's tokens stand in order of falling logit, equal ones in order of their ids, and weigh
+ * exp((z - max z) / temperature[b]).  Kept are first parts of that order, all of these that are given at once, and always the first token:
+ *   top_k[b] > 0: the first top_k[b] tokens;
+ *   top_p[b] < 1: those in front of which there is less than top_p[b] times the weight of what top_k keeps;
+ *   min_p[b] > 0: those of at least min_p[b] times the first one's weight.
+ * tokens[b] is the first kept token up to and with which there is more than u[b] times the weight of all kept ones (u in [0, 1);
+ * 1 and more: the last that weighs anything).  temperature[b] = 0 takes the first token.  Weights are rounded to multiples of 2^-42
+ * of the largest one, sums of them are exact.  logprob (nullable): natural log of the token's share of the kept weight.
+ * logits: device, rows of V <= 2^20 elements, row_stride elements apart, at any element, logits_dtype BC_BF16 or BC_F32;
+ * -infinity is a token that is never drawn.  temperature, top_k (int32), top_p, min_p: device [B] fp32 or NULL (1, and no filter);
+ * u: device [B] fp32.  A row with a NaN or +infinity, no finite logit, a temperature that is negative or not finite or a u that is
+ * NaN gets token -1 and a logprob of NaN.  active: [B] bytes or NULL; rows of others are left as they were. */
+int32_t bc_sample_tokens(int32_t B, int32_t V, const void *logits, int32_t logits_dtype, int64_t row_stride,
+                         const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                         const float *u, const uint8_t *active, int32_t *tokens, float *logprob, void *stream);
+
 /* Copy nb[B], w[B] and err[1] to HOST arrays (any may be NULL) and wait for the stream. */
 int32_t bc_tables_to_host(const bc_shape *shape, const bc_cache *cache, int32_t *nb_host,
                           int32_t *w_host, int32_t *err_host, void *stream);

@@ -41,6 +41,7 @@ EXPORTS = [
     "bc_prefill_bwd_workspace_bytes", "bc_prefill_attn_bwd", "bc_prefill_attn_host", "bc_prefill_attn_bwd_host",
     "bc_topk_kl_loss", "bc_topk_kl_loss_bwd", "bc_tables_to_host",
     "bc_prompt_workspace_bytes", "bc_prompt_step",
+    "bc_sample_tokens",
     "bc_qk_norm_rope", "bc_qk_norm_rope_bwd_workspace_bytes", "bc_qk_norm_rope_bwd",
 ]
 DIAG_EXPORTS = ["bc_diag_stream_read"]
@@ -138,6 +139,8 @@ def load():
     lib.bc_prompt_workspace_bytes.argtypes = [sp, i32, i64, i32]
     lib.bc_prompt_step.restype = i32
     lib.bc_prompt_step.argtypes = [sp, cp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bc_sample_tokens.restype = i32
+    lib.bc_sample_tokens.argtypes = [i32, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.bc_qk_norm_rope.restype = i32
     lib.bc_qk_norm_rope.argtypes = [sp, i64, vp, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, vp, vp]
     lib.bc_qk_norm_rope_bwd_workspace_bytes.restype = sz
@@ -321,6 +324,11 @@ def bc_prompt_workspace_bytes(shape, max_new, total_new, max_cap):
 
 def bc_prompt_step(shape, cache, k, v, q, row_offsets, out, active, ws, ws_bytes, stream):
     return load().bc_prompt_step(C.byref(shape), C.byref(cache), k, v, q, row_offsets, out, active, ws, ws_bytes, stream)
+
+
+def bc_sample_tokens(B, V, logits, logits_dtype, row_stride, temperature, top_k, top_p, min_p, u, active, tokens, logprob, stream):
+    return load().bc_sample_tokens(B, V, logits, logits_dtype, row_stride, temperature, top_k, top_p, min_p, u, active, tokens,
+                                   logprob, stream)
 
 
 def bc_qk_norm_rope(shape, rows, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight, k_weight, eps, q, k, v, stream):
@@ -849,3 +857,26 @@ def qk_norm_rope_bwd(qkv, dq, dk, dv, positions, inv_freq, Hq, Hkv, d, q_weight=
                                ws_bytes, _stream_ptr()))
     _used_here(qkv, dq, dk, dv, positions, inv_freq, q_weight, k_weight)
     return dqkv, dqw, dkw
+
+
+@_on_its_device
+def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, active=None, tokens=None, want_logprob=False):
+    """bc_sample_tokens on device tensors: logits [B, V] bf16/fp32 (rows may lie apart), u, temperature, top_p, min_p [B] fp32,
+    top_k [B] int32, active [B] uint8; all but logits and u may be None.  Returns tokens [B] int32, and with want_logprob
+    (tokens, logprob [B] fp32), which the current stream works on; tokens=: where they go (rows that are not active stay)."""
+    import torch
+    load()
+    if logits.dim() != 2 or (logits.numel() and logits.stride(1) != 1) or not logits.is_cuda:
+        raise BcError("logits must be a device tensor [B, V] with elements of a row back to back")
+    (B, V), dev, f32 = logits.shape, logits.device, torch.float32
+    for name, t, dtype in (("u", u, f32), ("temperature", temperature, f32), ("top_k", top_k, torch.int32), ("top_p", top_p, f32),
+                           ("min_p", min_p, f32), ("active", active, torch.uint8), ("tokens", tokens, torch.int32)):
+        if t is not None or name == "u":
+            _is(t, name, dtype, (B,), dev)
+    if tokens is None:
+        tokens = torch.empty(B, dtype=torch.int32, device=dev)
+    logprob = torch.empty(B, dtype=f32, device=dev) if want_logprob else None
+    _check(bc_sample_tokens(B, V, _ptr(logits), _logits_code(logits), logits.stride(0) if B > 1 else V, _ptr(temperature), _ptr(top_k),
+                            _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(active), _ptr(tokens), _ptr(logprob), _stream_ptr()))
+    _used_here(logits, u, temperature, top_k, top_p, min_p, active)
+    return (tokens, logprob) if want_logprob else tokens

@@ -1,0 +1,174 @@
+"""GPU parity: bc_sample_tokens against the fp64 oracle.
+
+Tokens have to be equal.  The library rounds weights to 2^-42 of the largest: over V tokens sums are off by less than V * 2^-43 of it, 1.7e-8 at
+V = 151,936 if all roundings fell alike; a draw or a cut that lies nearer to a border than that may differ.  The inputs here are fixed and do not (the
+draw's distance is asserted).  The log of a share: 2^-24 of it for its rounding, and 1e-7."""
+import numpy as np
+import pytest
+
+from oracle import sample as OS
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return torch.device("cuda:0")
+
+
+def _check(dev, z, dtype, u, temperature=None, top_k=None, top_p=None, min_p=None, pad=0, shift=0):
+    """z [B, V] fp32; the others [B] or None."""
+    import torch
+    from paper_2510_13797_amd import bc
+    B, V = z.shape
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    room = torch.full((B * (V + pad) + shift,), float("nan"), dtype=tdt, device=dev)
+    zd = room[shift:].view(B, V + pad)[:, :V]
+    zd.copy_(torch.from_numpy(np.asarray(z, np.float32)))
+    ex = zd.double().cpu().numpy()
+    col = lambda x, dt=np.float32: None if x is None else torch.from_numpy(np.broadcast_to(np.asarray(x, dt), (B,)).copy()).to(dev)
+    args = dict(temperature=col(temperature), top_k=col(top_k, np.int32), top_p=col(top_p), min_p=col(min_p))
+    ud = col(u)
+    token, logprob = bc.sample_tokens(zd, ud, want_logprob=True, **args)
+    assert torch.equal(token, bc.sample_tokens(zd, ud, **args))
+    host = {k: None if v is None else v.double().cpu().numpy() for k, v in args.items()}
+    t, lp = token.cpu().numpy(), logprob.double().cpu().numpy()
+    for b in range(B):
+        kw = {k: v[b] for k, v in host.items() if v is not None}
+        want, wlp, margin = OS.sample(ex[b], float(ud[b]), **kw)
+        assert margin > 1e-9, (b, margin)
+        assert t[b] == want, (b, kw, t[b], want, ex[b][t[b]], ex[b][want])
+        assert abs(lp[b] - wlp) <= 2.0 ** -24 * abs(wlp) + 1e-7, (b, lp[b], wlp)
+
+
+def _peaked(r, B, V, few=40):
+    z = 2 * r.standard_normal((B, V))
+    for b in range(B):
+        at = r.integers(0, V, min(few, V))
+        z[b, at] += 5 + 9 * r.random(len(at))
+    return z
+
+
+FILTERS = [dict(), dict(temperature=0.7), dict(top_k=20), dict(top_k=1), dict(top_p=0.9), dict(min_p=0.05), dict(temperature=0.0),
+           dict(temperature=1.3, top_k=50, top_p=0.95, min_p=0.02), dict(top_k=700, top_p=0.99), dict(top_k=5000), dict(temperature=0.01),
+           dict(min_p=1e-12), dict(top_p=1e-6), dict(min_p=1.0), dict(top_p=0.999999, min_p=1e-3), dict(temperature=30.0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", FILTERS, ids=str)
+def test_filters_on_peaked_and_flat_rows(dev, dtype, kw):
+    r = np.random.default_rng(7)
+    for V in (2000, 50257):
+        z = np.concatenate([_peaked(r, 3, V), 2 * r.standard_normal((3, V)), 0.05 * r.standard_normal((2, V))])
+        _check(dev, z, dtype, r.random(8), **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 63, 64, 65, 1000, 1023, 1024, 1025, 8191, 8200])
+def test_small_vocabularies_and_rows_that_start_anywhere(dev, dtype, V):
+    r = np.random.default_rng(V)
+    for shift, pad in ((0, 0), (1, 0), (3, 5), (0, 1)):
+        z = r.standard_normal((5, V))
+        for kw in (dict(), dict(top_k=3), dict(top_p=0.7), dict(min_p=0.3, temperature=0.5), dict(top_k=V + 4, top_p=0.97)):
+            _check(dev, z, dtype, r.random(5), pad=pad, shift=shift, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_row_its_own_settings(dev, dtype):
+    r = np.random.default_rng(5)
+    B, V = 64, 151936
+    z = np.concatenate([_peaked(r, B // 2, V), 2 * r.standard_normal((B // 2, V))])
+    some = lambda x, off: np.where(r.random(B) < 0.6, x, off)
+    _check(dev, z, dtype, r.random(B), temperature=some(r.uniform(0.3, 1.5, B), 0.0), top_k=some(r.integers(1, 3000, B), 0),
+           top_p=some(r.uniform(0.3, 0.999, B), 1.0), min_p=some(r.uniform(0.001, 0.3, B), 0.0))
+
+
+def test_many_equal_logits(dev):
+    # ties decide: all equal, a few values only, thousands of equal ones at the cut and at the draw
+    r = np.random.default_rng(9)
+    for V in (900, 5000, 151936):
+        rows = [np.zeros(V), np.full(V, -3.5), r.integers(0, 3, V) * 0.5, r.integers(-1, 1, V) * 1e-3, np.where(np.arange(V) % 7 == 0, 2.0, -1.0),
+                np.where(np.arange(V) == V // 2, 9.0, 0.0), np.where(r.random(V) < 0.5, 0.0, -0.0)]
+        for kw in (dict(), dict(top_k=V // 3), dict(top_p=0.4), dict(min_p=0.9), dict(top_k=V // 2, top_p=0.6), dict(top_k=1), dict(temperature=0.0)):
+            for u in (0.0, 0.37337, 0.99987):
+                z = np.stack(rows)
+                # (a border of equal weights lies at every multiple of 1/n: u is kept clear of them by the assertion on the margin)
+                _check(dev, z, "f32", u if u else 1e-7, **kw)
+
+
+def test_ends_of_the_random_number(dev):
+    import torch
+    from paper_2510_13797_amd import bc
+    z = torch.tensor([[1.0, 3.0, 2.0, float("-inf")]] * 6, device=dev)
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, 7.0, -0.5, float("nan")], device=dev)
+    assert bc.sample_tokens(z, u).tolist() == [1, 0, 0, 0, 1, -1]
+
+
+def test_rows_without_an_answer_and_masked_tokens(dev):
+    import torch
+    from paper_2510_13797_amd import bc
+    inf, nan = float("inf"), float("nan")
+    for V in (5, 3000):
+        for dtype in (torch.float32, torch.bfloat16):
+            z = torch.zeros(8, V, device=dev, dtype=dtype)
+            z[0, 3], z[1, 4], z[2], z[3, 1:] = nan, inf, -inf, -inf
+            z[4] = torch.finfo(dtype).min                   # a mask of the type's lowest value: all alike
+            z[5, :4] = torch.finfo(dtype).min
+            z[6, 2] = -nan
+            t = torch.ones(8, device=dev)
+            t[7] = -1.0
+            token, lp = bc.sample_tokens(z, torch.full((8,), 0.5, device=dev), t, want_logprob=True)
+            got = token.tolist()
+            assert got[0] == got[1] == got[2] == got[6] == got[7] == -1 and got[3] == 0 and got[4] == V // 2 and 4 <= got[5] < V
+            assert torch.isnan(lp).tolist() == [x == -1 for x in got]
+            for bad in (nan, inf, -inf):
+                assert bc.sample_tokens(z[3:4], t[:1] * 0.5, torch.full((1,), bad, device=dev)).item() == -1
+            # filters that are not numbers do not filter
+            none = torch.full((1,), nan, device=dev)
+            assert bc.sample_tokens(z[4:5], t[:1] * 0.5, None, None, none, none).item() == V // 2
+
+
+def test_extreme_scales(dev):
+    r = np.random.default_rng(2)
+    z = r.standard_normal((4, 3000))
+    _check(dev, z * 1e30, "f32", r.random(4))
+    _check(dev, z * 1e-30, "f32", r.random(4))
+    _check(dev, z * 1e-30, "f32", r.random(4), temperature=1e-30)
+    _check(dev, z, "f32", r.random(4), temperature=1e-38)
+    _check(dev, z * 5e37, "f32", r.random(4), temperature=1e38)
+    _check(dev, z, "f32", r.random(4), temperature=1e30, top_p=0.5)
+
+
+def test_idle_rows_and_given_tensors(dev):
+    import torch
+    from paper_2510_13797_amd import bc
+    z = torch.randn(5, 400, device=dev)
+    tokens = torch.full((5,), 77, dtype=torch.int32, device=dev)
+    active = torch.tensor([1, 0, 1, 1, 0], dtype=torch.uint8, device=dev)
+    got = bc.sample_tokens(z, torch.rand(5, device=dev), torch.zeros(5, device=dev), active=active, tokens=tokens)
+    assert got is tokens
+    assert tokens.tolist() == [77 if i in (1, 4) else z[i].argmax().item() for i in range(5)]
+    assert bc.sample_tokens(z[:0], torch.rand(0, device=dev)).shape == (0,)
+
+
+def test_captured_and_replayed(dev):
+    import torch
+    from paper_2510_13797_amd import bc
+    g = torch.Generator(device=dev).manual_seed(3)
+    z = (2 * torch.randn(6, 30000, generator=g, device=dev)).bfloat16()
+    u = torch.rand(6, generator=g, device=dev)
+    p = torch.full((6,), 0.9, device=dev)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        want = bc.sample_tokens(z, u, top_p=p)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            got = bc.sample_tokens(z, u, top_p=p)
+        for i in range(3):
+            u.copy_(torch.rand(6, generator=g, device=dev))
+            graph.replay()
+            st.synchronize()
+            assert torch.equal(got, bc.sample_tokens(z, u, top_p=p)), i

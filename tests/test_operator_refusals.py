@@ -92,3 +92,20 @@ def test_prompt_refusals():
     assert _prompt(off=(4, 4, 4), k=None, v=None, q=None, out=None, ws=None) == bc.BC_OK
     assert bc.bc_prompt_workspace_bytes(shape(d=96), 5, 8, 64) == 0 and bc.bc_prompt_workspace_bytes(shape(), -1, 8, 64) == 0
     assert bc.bc_prompt_workspace_bytes(shape(), 5, 8, 0) == 0
+
+
+def _sample(B=2, V=100, z=PTR, dtype=bc.BC_BF16, stride=100, t=None, k=None, p=None, m=None, u=PTR, active=None, tokens=PTR, logprob=None):
+    return bc.bc_sample_tokens(B, V, z, dtype, stride, t, k, p, m, u, active, tokens, logprob, None)
+
+
+def test_sample_refusals():
+    bc.load()
+    for kw in (dict(B=-1), dict(V=0), dict(V=(1 << 20) + 1, stride=1 << 21), dict(dtype=2)):
+        assert _sample(**kw) == bc.BC_ERR_SHAPE, kw
+    for kw in (dict(z=None), dict(z=PTR + 1), dict(z=PTR + 2, dtype=bc.BC_F32), dict(u=None), dict(tokens=None), dict(stride=99), dict(stride=-100)):
+        assert _sample(**kw) == bc.BC_ERR_ARG, kw
+    assert _sample(B=0, z=None, u=None, tokens=None) == bc.BC_OK
+    z, u = torch.zeros(2, 100), torch.zeros(2)
+    for args in ((z, u), (z[0], u), (z.t(), u)):               # (on the host, wrong orders)
+        with pytest.raises(bc.BcError):
+            bc.sample_tokens(*args)
