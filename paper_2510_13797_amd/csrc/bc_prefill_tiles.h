@@ -314,8 +314,8 @@ __device__ __forceinline__ void step_fence() { __builtin_amdgcn_sched_barrier(0)
 
 // Half the columns (pass 0 or 1) of a wave's 32 x D results (accumulator layout: lane l holds
 // columns 32*j + 8*i + 4*(l/32) .. +3 of row l%32) -> LDS -> bursts of D/2 floats per row.
-// row(t): which row of `base` row t goes to, or -1.  Written once, not read again by the launch: streaming.
-template <int D, typename F>
+// row(t): which row of `base` row t goes to, or -1.  Written once, not read again by the launch: streaming (STREAM).
+template <int D, bool STREAM = true, typename F>
 __device__ __forceinline__ void store_rows(float* my, const f32x16_t (&acc)[D / 32], float mul, int pass, int lane,
                                            float* base, int row_stride, F row) {
   constexpr int OW = D / 2, UW = OW / 4, RPP = 64 / UW;      // columns and units of a pass, rows per instruction
@@ -341,7 +341,11 @@ __device__ __forceinline__ void store_rows(float* my, const f32x16_t (&acc)[D / 
   float* at = base + OW * pass + (lane & (UW - 1)) * 4;
 #pragma unroll
   for (int n = 0; n < 32 / RPP; ++n)
-    if (to[n] >= 0) __builtin_nontemporal_store(val[n], reinterpret_cast<f32x4_t*>(at + (int64_t)to[n] * row_stride));
+    if (to[n] >= 0) {
+      f32x4_t* dst = reinterpret_cast<f32x4_t*>(at + (int64_t)to[n] * row_stride);
+      if constexpr (STREAM) __builtin_nontemporal_store(val[n], dst);
+      else *dst = val[n];
+    }
 }
 
 // Whether byte offsets inside a trajectory's K or V rows may need more than 32 bits.

@@ -21,6 +21,13 @@
 namespace bc {
 namespace {
 
+// Where the chunks' rows are: in the kernel arguments for up to 128 sequences (a launch that stored them took 4.5 us).
+constexpr int kInlineChunks = 128;
+struct InlineOffsets {
+  int64_t first;
+  int32_t from[kInlineChunks + 1];        // less `first`
+};
+
 struct PromptParams {
   const char* q;               // [total, Hq, d]
   const char* k;               // [total, Hkv, d]
@@ -39,15 +46,13 @@ struct PromptParams {
   int32_t* resident;           // [B] rows in front of the chunk, -1: the sequence takes no part
   float2* ml;                  // [parts][npairs][columns] maximum (log2) and sum of a part
   float* sums;                 // [parts][npairs][columns][d]
-  const int64_t* row_off;      // the chunks' rows, as trajectory() takes them
-  const int32_t* P;
-  const int32_t* c;
+  const int64_t* row_off;      // [B + 1], null: `inl`
   int32_t B, Hq, Hkv, g;
-  int32_t npairs, pstride, parts;
+  int32_t npairs, pstride, turn, parts;      // as in the prefill kernels
   int32_t columns;             // most columns of a pair, padded to a workgroup's
   int32_t table_blocks, copy_blocks;      // of the second launch
   float qscale;
-  InlineTables tab;
+  InlineOffsets inl;
 };
 
 #define BC_INLINE __attribute__((always_inline))
@@ -56,6 +61,20 @@ constexpr float kRedo = 256.f;      // a lane's 16 weights may sum to this befor
 constexpr float kLazy = 2.0f;       // ... and then it moves where a column's maximum is this much (log2) above it
 constexpr int kColumns = 32 * kTileWaves;
 constexpr int kFewStages = 2;
+constexpr int kMostParts = 64;      // a lane each in the fold
+constexpr int kFoldGroups = 4;      // of threads that share a column's parts,
+constexpr int kFoldAtOnce = 8;      // each asking for eight together
+constexpr int kFoldLoads = 16;      // of a thread where there are up to eight parts
+
+struct Chunk { int64_t off0; int rows; };
+__device__ __forceinline__ Chunk chunk_of(const PromptParams& p, int s) {        // (p: the kernel's only argument)
+  if (p.row_off != nullptr) return {p.row_off[s], (int)(p.row_off[s + 1] - p.row_off[s])};
+  typedef __attribute__((address_space(4))) const char const_char_t;
+  typedef __attribute__((address_space(4))) const InlineOffsets const_offsets_t;
+  const_offsets_t* in = (const_offsets_t*)((const_char_t*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(PromptParams, inl));
+  const int at = in->from[s];
+  return {in->first + at, in->from[s + 1] - at};
+}
 
 // What a sequence's tables say: rows in front of the chunk, or -1 and the error bit to set.
 struct Resident { int rows, bit; };
@@ -205,11 +224,11 @@ struct PromptWork {
   __device__ __forceinline__ bool start(const PromptParams& p) {
     constexpr int ROWB = D * 2;
     part = blockIdx.x / p.pstride;
-    pair = blockIdx.x - part * p.pstride;
+    pair = pair_in_turn(blockIdx.x - part * p.pstride, p.pstride, p.turn, blockIdx.y * p.parts + part);
     if (pair >= p.npairs) return false;
     kvh = pair % p.Hkv;
     s = pair / p.Hkv;
-    const Trajectory chunk = trajectory(p, s);
+    const Chunk chunk = chunk_of(p, s);
     off0 = chunk.off0;
     n = chunk.rows;
     const int block = gridDim.y - 1 - blockIdx.y;              // long ones first
@@ -328,7 +347,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 3) void prompt_attn_kernel(PromptP
     if (wk.t0 >= wk.t1) return;
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass)
-      store_rows<D>(my, x.O, 1.f, pass, lane, p.sums + wk.slot(p, first) * D, D, [&](int t) { return t < left ? t : -1; });
+      store_rows<D, false>(my, x.O, 1.f, pass, lane, p.sums + wk.slot(p, first) * D, D, [&](int t) { return t < left ? t : -1; });
   }
 }
 
@@ -426,15 +445,128 @@ __global__ __launch_bounds__(kTileWaves * 64, 1) void prompt_few_kernel(PromptPa
   }
 }
 
-// The second launch: tables, append, and the fold of the parts.  What the first one decided is in p.resident.
+// Weights of a column's parts from their maxima and sums, a lane each.
+struct PartWeight { float f, inv; };
+template <int LANES>
+__device__ __forceinline__ PartWeight part_weight(float2 ml) {
+  float M = ml.x;
+#pragma unroll
+  for (int o = LANES / 2; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  const float f = ml.y > 0.f ? fast_exp2(ml.x - M) : 0.f;         // (0: the part had no tiles and left no sums)
+  float sum = ml.y * f;
+#pragma unroll
+  for (int o = LANES / 2; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  return {f, 1.0f / sum};
+}
+
+// Many parts of few columns: four groups of threads share a column's parts, eight loads of each together (one column's parts one after the other
+// by 32 threads: 7 rows over 16,000, 32 parts, 26 us; 4 so).
 template <int D>
+__device__ __forceinline__ void fold_many_parts(const PromptParams& p, int block) {
+  constexpr int UNITS = D / 4, COLS = 256 / UNITS / kFoldGroups;
+  const int pair = block % p.npairs, s = pair / p.Hkv;
+  if (p.resident[s] < 0) return;
+  const Chunk chunk = chunk_of(p, s);
+  const int columns = chunk.rows * p.g, first = block / p.npairs * COLS;
+  if (first >= columns) return;
+  __shared__ float weight[COLS][kMostParts];
+  __shared__ float inv[COLS];
+  __shared__ f32x4_t some[kFoldGroups][COLS * UNITS];
+  const int64_t slot0 = (int64_t)pair * p.columns + first, step = (int64_t)p.npairs * p.columns;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (wave < COLS) {
+    const int64_t slot = slot0 + min(wave, columns - 1 - first);
+    const PartWeight w = part_weight<64>(lane < p.parts ? p.ml[slot + lane * step] : make_float2(kNegBig, 0.f));
+    weight[wave][lane] = w.f;
+    if (lane == 0) inv[wave] = w.inv;
+  }
+  __syncthreads();
+  const int group = threadIdx.x / (COLS * UNITS), at = threadIdx.x % (COLS * UNITS), c = at / UNITS, unit = at % UNITS;
+  const float* sums = p.sums + (slot0 + min(c, columns - 1 - first)) * D + 4 * unit;
+  f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int n0 = group; n0 < p.parts; n0 += kFoldGroups * kFoldAtOnce) {
+    f32x4_t x[kFoldAtOnce];
+#pragma unroll
+    for (int e = 0; e < kFoldAtOnce; ++e) {
+      const int n = n0 + e * kFoldGroups;
+      if (n < p.parts) x[e] = *reinterpret_cast<const f32x4_t*>(sums + n * step * D);
+    }
+#pragma unroll
+    for (int e = 0; e < kFoldAtOnce; ++e) {
+      const int n = n0 + e * kFoldGroups;
+      const float f = n < p.parts ? weight[c][n] : 0.f;
+      if (f > 0.f) o += x[e] * f;
+    }
+  }
+  some[group][at] = o;
+  __syncthreads();
+  if (group != 0 || first + c >= columns) return;
+#pragma unroll
+  for (int n = 1; n < kFoldGroups; ++n) o += some[n][at];
+  const int col = first + c, r = col / p.g;
+  float* to = p.out + ((chunk.off0 + r) * p.Hq + pair % p.Hkv * p.g + col - r * p.g) * D;
+  *reinterpret_cast<f32x4_t*>(to + 4 * unit) = o * inv[c];
+}
+
+// Up to eight parts of many columns: D / 4 threads a column, each with kFoldLoads loads on their way (PARTS for each of several
+// columns; one column and two loads a thread: 4 x 2048 rows of 32 heads in two parts 252 us, 88 with eight loads), columns by their place in the
+// output.  Sequence s has the workgroups from fold_start(s) on, at least
+// as many as its columns take, so that there are next to none for rows that shorter chunks do not have.  (The sequence is found for the
+// workgroup, by scalar loads: by every thread for its own column, its chunk came from the kernel's arguments by vector loads.)
+template <int D, int PARTS> constexpr int fold_columns() { return 256 / (D / 4) * (kFoldLoads / PARTS); }
+template <int PER>
+__host__ __device__ __forceinline__ int64_t fold_start(int64_t rows, int s, int Hq) { return rows * Hq / PER + s; }
+template <int D, int PARTS>
+__device__ __forceinline__ void fold_few_parts(const PromptParams& p, int block) {
+  constexpr int UNITS = D / 4, PER = fold_columns<D, PARTS>(), COLS = kFoldLoads / PARTS, APART = 256 / UNITS;
+  const int64_t off = chunk_of(p, 0).off0;
+  int s = 0, end = p.B;
+  while (end - s > 1) {
+    const int mid = (s + end) >> 1;
+    if (fold_start<PER>(chunk_of(p, mid).off0 - off, mid, p.Hq) <= block) s = mid; else end = mid;
+  }
+  if (p.resident[s] < 0) return;
+  const Chunk chunk = chunk_of(p, s);
+  const int first = (int)(block - fold_start<PER>(chunk.off0 - off, s, p.Hq)) * PER + threadIdx.x / UNITS, unit = threadIdx.x % UNITS;
+  const int last = chunk.rows * p.Hq - 1;
+  const int64_t step = (int64_t)p.npairs * p.columns;
+  int64_t slot[COLS];
+  f32x4_t x[COLS][PARTS];
+  float2 ml[COLS];
+  const int lane = threadIdx.x & (PARTS - 1);
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) {
+    const int at = min(first + c * APART, last), i = at / p.Hq, head = at - i * p.Hq, kvh = head / p.g;
+    slot[c] = ((int64_t)s * p.Hkv + kvh) * p.columns + i * p.g + head - kvh * p.g;
+    ml[c] = lane < p.parts ? p.ml[slot[c] + lane * step] : make_float2(kNegBig, 0.f);
+#pragma unroll
+    for (int n = 0; n < PARTS; ++n)
+      if (n < p.parts) x[c][n] = *reinterpret_cast<const f32x4_t*>(p.sums + (slot[c] + n * step) * D + 4 * unit);
+  }
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) {
+    const PartWeight w = part_weight<PARTS>(ml[c]);
+    f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < PARTS; ++n) {
+      const float f = __shfl(w.f, (threadIdx.x & (64 - PARTS)) + n, 64);
+      if (n < p.parts && f > 0.f) o += x[c][n] * f;
+    }
+    const int at = first + c * APART;
+    if (at <= last) __builtin_nontemporal_store(o * w.inv, reinterpret_cast<f32x4_t*>(p.out + (chunk.off0 * p.Hq + at) * D + 4 * unit));
+  }
+}
+
+// The second launch: tables, append, and the fold of the parts.  What the first one decided is in p.resident.
+// PARTS: at most, 0: more.
+template <int D, int PARTS>
 __global__ __launch_bounds__(256) void prompt_finish_kernel(PromptParams p) {
-  constexpr int UNITS = D / 4, ROWB = D * 2, RU = ROWB / 16;
+  constexpr int ROWB = D * 2, RU = ROWB / 16;
   int block = blockIdx.x;
   if (block < p.table_blocks) {
     const int s = block * 256 + threadIdx.x;
     if (s < p.B && p.resident[s] >= 0) {
-      const Trajectory chunk = trajectory(p, s);
+      const Chunk chunk = chunk_of(p, s);
       p.cacheP[s] = p.resident[s] + chunk.rows;
       p.nb[s] = 0;
       p.w[s] = 0;
@@ -445,7 +577,7 @@ __global__ __launch_bounds__(256) void prompt_finish_kernel(PromptParams p) {
   if (block < p.copy_blocks * p.B) {
     const int s = block / p.copy_blocks, slice = block - s * p.copy_blocks, L = p.resident[s];
     if (L < 0) return;
-    const Trajectory chunk = trajectory(p, s);
+    const Chunk chunk = chunk_of(p, s);
     const int cap = p.cap[s];
     const int64_t slab = p.base[s] * p.Hkv, units = (int64_t)chunk.rows * p.Hkv * RU;
     for (int64_t u = (int64_t)slice * 256 + threadIdx.x; u < units; u += (int64_t)p.copy_blocks * 256) {
@@ -458,30 +590,19 @@ __global__ __launch_bounds__(256) void prompt_finish_kernel(PromptParams p) {
     return;
   }
   block -= p.copy_blocks * p.B;
-  const int pair = block % p.npairs, s = pair / p.Hkv;
-  if (p.resident[s] < 0) return;
-  const Trajectory chunk = trajectory(p, s);
-  const int c = block / p.npairs * (256 / UNITS) + threadIdx.x / UNITS, unit = threadIdx.x % UNITS;
-  if (c >= chunk.rows * p.g) return;
-  const int64_t slot = (int64_t)pair * p.columns + c, step = (int64_t)p.npairs * p.columns;
-  float M = kNegBig;
-  for (int n = 0; n < p.parts; ++n) M = fmaxf(M, p.ml[slot + n * step].x);
-  float sum = 0.f;
-  f32x4_t o = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int n = 0; n < p.parts; ++n) {
-    const float2 ml = p.ml[slot + n * step];
-    if (ml.y > 0.f) {                                           // (a part without tiles has left no sums)
-      const float f = fast_exp2(ml.x - M);
-      sum += ml.y * f;
-      o += *reinterpret_cast<const f32x4_t*>(p.sums + (slot + n * step) * D + 4 * unit) * f;
-    }
-  }
-  const int r = c / p.g;
-  float* to = p.out + ((chunk.off0 + r) * p.Hq + pair % p.Hkv * p.g + c - r * p.g) * D;
-  *reinterpret_cast<f32x4_t*>(to + 4 * unit) = o * (1.0f / sum);
+  if constexpr (PARTS == 0) fold_many_parts<D>(p, block);
+  else fold_few_parts<D, PARTS>(p, block);
 }
 
-// How a call is cut.  Lengths of the caches are on the device; the capacity stands for them.
+// How a call is cut.  Lengths of the caches are on the device; the capacity stands for them.  Many columns: as many workgroups as run at once (three
+// a compute unit), half as many again for several sequences, whose lengths differ, in parts of 16 tiles and more; 32 columns: one a
+// compute unit (its LDS), four tiles and more.  One, two, three, four, six, eight parts in us, with the rule's in brackets:
+//   512 rows over 7680, 32/8 heads      242 151 141 124 [120] 127
+//   700 over 3000, 12/2                 112  67  55  55 [46] 47
+//   8 x 64 over 2000, 32/8               74  52  52 [49] 51  61
+//   8 x 10-200 over 100-6000, 32/8      219 132 129 [123] 123 129
+//   64 x 5-120 over 0-3000, 12/2        145 [129] 124 125 141 159
+//   128 x 10-100 over 0-2000, 4/1        92  74 [67] 69  75  82
 struct PromptPlan {
   bool few;
   int blocks;                  // workgroups along a pair's columns
@@ -499,14 +620,14 @@ PromptPlan plan_prompt(const bc_shape* sh, int64_t max_new, int64_t total, int32
   pl.columns = pl.blocks * wide;
   // workgroups there will be about, and as many as run at once
   const int64_t all = (total * g / wide + sh->B) * sh->Hkv, most = npairs * pl.blocks, work = all < most ? all : most;
-  const int64_t room = pl.few ? 256 : 768, tiles = (max_cap + kTileRows - 1) / kTileRows;
+  const int64_t room = pl.few ? 256 : sh->B > 1 ? 1152 : 768, tiles = (max_cap + kTileRows - 1) / kTileRows;
   int64_t parts = work > 0 ? room / work : 1;
-  const int64_t enough = tiles / (pl.few ? 4 : 8);
+  const int64_t enough = tiles / (pl.few ? 4 : 16);
   if (parts > enough) parts = enough;
-  pl.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+  pl.parts = (int)(parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts);
   size_t at = ((size_t)sh->B * 4 + 15) & ~(size_t)15;
   pl.tables_at = at;
-  if (sh->B > BC_INLINE_TRAJECTORIES) at += ((size_t)sh->B * 16 + 8 + 15) & ~(size_t)15;
+  if (sh->B > kInlineChunks) at += ((size_t)sh->B * 16 + 8 + 15) & ~(size_t)15;
   pl.ml_at = at;
   if (pl.parts > 1) at += (size_t)pl.parts * npairs * pl.columns * sizeof(float2);
   pl.sums_at = at;
@@ -515,14 +636,23 @@ PromptPlan plan_prompt(const bc_shape* sh, int64_t max_new, int64_t total, int32
   return pl;
 }
 
+template <int D, int PARTS>
+void launch_finish(const PromptParams& p, const PromptPlan& pl, int64_t total, hipStream_t s) {
+  constexpr int PER = 256 / (D / 4) / kFoldGroups;
+  int64_t fold = 0;
+  if constexpr (PARTS == 0) fold = p.npairs * ((pl.columns + PER - 1) / PER);
+  else if (p.parts > 1) fold = fold_start<fold_columns<D, PARTS>()>(total, p.B, p.Hq);
+  prompt_finish_kernel<D, PARTS><<<(unsigned)(p.table_blocks + (int64_t)p.copy_blocks * p.B + fold), 256, 0, s>>>(p);
+}
 template <int D>
-void launch_prompt(const PromptParams& p, const PromptPlan& pl, hipStream_t s) {
+void launch_prompt(const PromptParams& p, const PromptPlan& pl, int64_t total, hipStream_t s) {
   const dim3 grid(p.pstride * p.parts, pl.blocks);
   if (pl.few) prompt_few_kernel<D><<<grid, kTileWaves * 64, 0, s>>>(p);
   else prompt_attn_kernel<D><<<grid, kTileWaves * 64, 0, s>>>(p);
-  const int per = 256 / (D / 4);
-  const int64_t fold = p.parts > 1 ? (int64_t)p.npairs * ((pl.columns + per - 1) / per) : 0;
-  prompt_finish_kernel<D><<<(unsigned)(p.table_blocks + (int64_t)p.copy_blocks * p.B + fold), 256, 0, s>>>(p);
+  if (p.parts <= 2) launch_finish<D, 2>(p, pl, total, s);
+  else if (p.parts <= 4) launch_finish<D, 4>(p, pl, total, s);
+  else if (p.parts <= 8) launch_finish<D, 8>(p, pl, total, s);
+  else launch_finish<D, 0>(p, pl, total, s);
 }
 
 }  // namespace
@@ -554,27 +684,28 @@ extern "C" int32_t bc_prompt_step(const bc_shape* shape, const bc_cache* cache, 
   const int64_t total = row_offsets[shape->B] - row_offsets[0];
   if (total == 0) return BC_OK;
   if (!k || !v || !q || !out || !aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(out)) return BC_ERR_ARG;
-  if (max_new * shape->Hq >= (1LL << 31) || (int64_t)shape->B * shape->Hkv > (1 << 24)) return BC_ERR_SHAPE;
+  if (max_new * shape->Hq >= (1LL << 31) || total >= (1LL << 31) || (int64_t)shape->B * shape->Hkv > (1 << 24)) return BC_ERR_SHAPE;
   const PromptPlan pl = plan_prompt(shape, max_new, total, cache->max_cap);
   if (pl.blocks > 65535) return BC_ERR_SHAPE;
   if (!workspace || !aligned16(workspace) || workspace_bytes < pl.bytes) return BC_ERR_WORKSPACE;
   PromptParams p{};
-  if (shape->B <= BC_INLINE_TRAJECTORIES) {
-    const int32_t none[BC_INLINE_TRAJECTORIES] = {};
-    st = host_tables(p, row_offsets, none, none, shape->B, nullptr, stream);
-  } else {
-    std::vector<int64_t> words;                                // offsets, and in place of P and c zeros
+  char* ws = static_cast<char*>(workspace);
+  if (shape->B <= kInlineChunks) {
+    p.inl.first = row_offsets[0];
+    for (int b = 0; b <= shape->B; ++b) p.inl.from[b] = (int32_t)(row_offsets[b] - row_offsets[0]);
+  } else {                                                     // (offsets, and in place of the other tables zeros)
+    std::vector<int64_t> words;
     try {
       words.assign((size_t)2 * shape->B + 1, 0);
     } catch (...) {
-      return BC_ERR_ARG;
+      return BC_ERR_WORKSPACE;
     }
     for (int b = 0; b <= shape->B; ++b) words[b] = row_offsets[b];
     const int32_t* none = reinterpret_cast<const int32_t*>(words.data() + shape->B + 1);
-    st = host_tables(p, words.data(), none, none + shape->B, shape->B, static_cast<char*>(workspace) + pl.tables_at, stream);
+    st = bc_trajectory_tables(words.data(), none, none + shape->B, shape->B, ws + pl.tables_at, stream);
+    if (st != BC_OK) return st;
+    p.row_off = reinterpret_cast<const int64_t*>(ws + pl.tables_at);
   }
-  if (st != BC_OK) return st;
-  char* ws = static_cast<char*>(workspace);
   p.q = static_cast<const char*>(q); p.k = static_cast<const char*>(k); p.v = static_cast<const char*>(v);
   p.k_slab = static_cast<char*>(cache->k_slab); p.v_slab = static_cast<char*>(cache->v_slab);
   p.base = cache->base; p.cap = cache->cap; p.cacheP = cache->P; p.cachec = cache->c;
@@ -585,7 +716,13 @@ extern "C" int32_t bc_prompt_step(const bc_shape* shape, const bc_cache* cache, 
   p.sums = reinterpret_cast<float*>(ws + pl.sums_at);
   p.B = shape->B; p.Hq = shape->Hq; p.Hkv = shape->Hkv; p.g = shape->Hq / shape->Hkv;
   p.npairs = shape->B * shape->Hkv;
-  p.pstride = pair_stride(p.npairs);
+  // All of a pair's workgroups on one XCD, as in the prefill kernels - but where the heads of a sequence do not take all XCDs alike, pairs of long and
+  // short sequences would weigh on some XCDs more than on others: there a pair moves on by one XCD from row to row of the grid.  (24 sequences of
+  // up to 300 rows over up to 3500, 12/2 heads: 102 us so, 123 on one XCD; 64 of up to 120 over 3000, 124 and 138; 32/8 heads, 8 sequences of up to 200
+  // over 6000, 131 and 123; 16 fresh ones of up to 1500, 248 and 220.)
+  const bool roam = shape->B > 1 && shape->Hkv % 8 != 0;
+  p.pstride = roam ? p.npairs | 1 : pair_stride(p.npairs);
+  p.turn = roam ? 0 : pair_turn(p.pstride);
   p.parts = pl.parts;
   p.columns = (int32_t)pl.columns;
   p.table_blocks = (shape->B + 255) / 256;
@@ -594,7 +731,7 @@ extern "C" int32_t bc_prompt_step(const bc_shape* shape, const bc_cache* cache, 
   p.copy_blocks = (int32_t)(copies < share ? copies : share);
   p.qscale = shape->scale * kLog2e;
   hipStream_t s = as_stream(stream);
-  if (shape->d == 128) launch_prompt<128>(p, pl, s);
-  else launch_prompt<64>(p, pl, s);
+  if (shape->d == 128) launch_prompt<128>(p, pl, total, s);
+  else launch_prompt<64>(p, pl, total, s);
   return launch_status();
 }

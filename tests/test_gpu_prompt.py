@@ -102,13 +102,24 @@ def test_ends_of_tiles(dev, n, L):
     _check(dev, 4, 4, 64, [(L, 0, 0)], [n], every=3)
 
 
-def test_more_sequences_than_travel_in_the_arguments(dev):
+@pytest.mark.parametrize("B", [40, 128, 129])
+def test_more_sequences_than_travel_in_the_arguments(dev, B):
     r = np.random.default_rng(3)
-    lens = [tuple(int(x) for x in (r.integers(0, 80), r.integers(0, 20), r.integers(0, 17))) for _ in range(40)]
-    n = r.integers(0, 40, 40)
-    n[[0, 39]] = 0, 5
-    _check(dev, 12, 2, 64, lens, n, active=(r.random(40) < 0.8).astype(np.uint8), every=3)
+    lens = [tuple(int(x) for x in (r.integers(0, 80), r.integers(0, 20), r.integers(0, 17))) for _ in range(B)]
+    n = r.integers(0, 40, B)
+    n[[0, B - 1]] = 0, 5
+    _check(dev, 12, 2, 64, lens, n, active=(r.random(B) < 0.8).astype(np.uint8), every=3)
     _check(dev, 12, 2, 128, lens, np.minimum(n, 5), every=2)
+
+
+def test_ragged_chunks_in_parts(dev):
+    # parts whose sums are folded by their place in the output, sequences without rows between others
+    r = np.random.default_rng(4)
+    lens = [(int(x), 0, 0) for x in r.integers(0, 1500, 7)]
+    for n in ([40, 0, 3, 130, 0, 17, 64], [0, 0, 33, 0, 0, 90, 0]):
+        for cap in (np.full(7, 1700), np.full(7, 9000)):
+            _check(dev, 12, 2, 128, lens, n, cap=cap, every=13)
+            _check(dev, 4, 4, 64, lens, n, cap=cap, every=13)
 
 
 def test_rows_in_front_and_idle_sequences(dev):
