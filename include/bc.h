@@ -427,7 +427,7 @@ int32_t bc_qk_norm_rope_bwd(const bc_shape *shape, int64_t rows, const void *qkv
  *   top_p[b] < 1: those in front of which there is less than top_p[b] times the weight of what top_k keeps;
  *   min_p[b] > 0: those of at least min_p[b] times the first one's weight.
  * tokens[b] is the first kept token up to and with which there is more than u[b] times the weight of all kept ones (u in [0, 1);
- * 1 and more: the last that weighs anything).  temperature[b] = 0 takes the first token.  Weights are rounded to multiples of 2^-42
+ * 1 and more: the last that weighs anything).  temperature[b] = 0 (or below 2^-126) takes the first token.  Weights are rounded to multiples of 2^-42
  * of the largest one, sums of them are exact.  logprob (nullable): natural log of the token's share of the kept weight.
  * logits: device, rows of V <= 2^20 elements, row_stride elements apart, at any element, logits_dtype BC_BF16 or BC_F32;
  * -infinity is a token that is never drawn.  temperature, top_k (int32), top_p, min_p: device [B] fp32 or NULL (1, and no filter);

@@ -10,11 +10,16 @@
 // A workgroup of 1024 threads has a row:
 //   A  the maximum; of the threads' own maxima the k-th largest (without top-k the 400th) gives a line above which all tokens
 //      that matter usually lie, and not many more than that;
-//   B  a second pass lists the tokens above the line (in LDS, 1024 at most) and sums all weights where they are asked for;
-//   C  the list is sorted and its sums formed: counts, masses and the draw are looked up.
-// Rows that this does not settle (nearly flat ones, where hundreds of tokens are kept, or many equal ones) go by
-//   D  a histogram of counts and masses over 2048 equal steps of (max - z) / temperature.  Where a count or mass falls, the
-//      step's tokens are listed and sorted as in C, after further histograms of it where there are too many.
+//   B  a second pass lists the tokens above the line (in LDS, 1024 at most).  Where the sum of all weights is asked for, it adds up those below
+//      the line in 32 bits, with a bound on how far off that is (tail_weight());
+//   C  the list is sorted and its sums formed: counts, masses and the draw are looked up, at both ends of the bound where there is one.
+// Rows that this does not settle (nearly flat ones, where hundreds of tokens are kept, many equal ones, a border inside the bound) go by
+//   D  sums of whole rows.  bf16 logits have few values: their counts are taken in LDS, and a value weighs its count times its weight.  fp32 logits go by a
+//      histogram of counts and masses over 2048 equal steps of (max - z) / temperature; where a count or mass falls, the step's
+//      tokens are listed and sorted as in C, after further histograms of it where there are too many.
+//
+// What bounds it is the vector work of a compute unit that has a row to itself, 148 logits a thread at V = 151,936: passes A and B look at 16
+// bytes at a time by packed 16-bit comparisons (bf16; 32-bit ones for fp32) and at single logits only where one is above the line.
 #include "bc_common.h"
 
 namespace bc {
@@ -27,6 +32,7 @@ constexpr int kSteps = 2048;               // of a histogram
 constexpr int kWeightBits = 42;            // the largest token weighs 2^42
 constexpr float kSpan = 43.5f;             // base-2 exponents a histogram covers: weights below 2^-43 round to nothing
 constexpr int kUsualLine = 400;            // thread maxima above the line without top-k: 0.5 tokens a thread, 512 in all
+constexpr int kValues = 4096;              // bf16 values counted: 16 binades of either sign
 
 struct SampleParams {
   const char* z;
@@ -43,23 +49,22 @@ struct SampleParams {
 };
 
 typedef unsigned long long u64;
+constexpr double kTailBound = 1.0 / (1 << 17);
 
 __device__ __forceinline__ float sample_value(uint32_t bits, float) { return __uint_as_float(bits); }
 __device__ __forceinline__ float sample_value(uint32_t bits, bf16_t) { return __uint_as_float(bits << 16); }
 
-// f(z, token) of every logit of a row, which may start at any element: those in front of the first 16-byte boundary and behind the last are
-// taken one by one, the others by 16 bytes, four loads of a thread at a time.
-template <typename T, typename F>
-__device__ __forceinline__ void each_logit(const char* row, int32_t V, const F& f) {
+// A row, which may start at any element: those in front of the first 16-byte boundary and behind the last are taken one by one (single(bits,
+// token)), the others by 16 bytes (unit(words, first token)), four loads of a thread at a time.
+template <typename T, typename FS, typename FU>
+__device__ __forceinline__ void each_unit(const char* row, int32_t V, const FS& single, const FU& unit_of) {
   constexpr int EPU = Elem<T>::per16, ES = Elem<T>::size, BATCH = 4;
   const int head = min(((16 - (int)(reinterpret_cast<uintptr_t>(row) & 15u)) & 15) / ES, V);
   const int units = (V - head) / EPU, tail = V - head - units * EPU, tid = threadIdx.x;
   if (tid < head + tail) {
     const int i = tid < head ? tid : V - tail + tid - head;
-    uint32_t bits;
-    if constexpr (ES == 4) bits = reinterpret_cast<const uint32_t*>(row)[i];
-    else bits = reinterpret_cast<const uint16_t*>(row)[i];
-    f(sample_value(bits, T{}), i);
+    if constexpr (ES == 4) single(reinterpret_cast<const uint32_t*>(row)[i], i);
+    else single((uint32_t)reinterpret_cast<const uint16_t*>(row)[i], i);
   }
   const uint4* at = reinterpret_cast<const uint4*>(row + head * ES);
   for (int base = 0; base < units; base += BATCH * kSampleThreads) {
@@ -72,27 +77,103 @@ __device__ __forceinline__ void each_logit(const char* row, int32_t V, const F& 
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
       const int unit = base + b * kSampleThreads + tid;
-      if (unit < units) {
-        float x[EPU];
-        unpack16(r[b], x, T{});
-#pragma unroll
-        for (int e = 0; e < EPU; ++e) f(x[e], head + unit * EPU + e);
-      }
+      if (unit < units) unit_of(r[b], head + unit * EPU);
     }
   }
 }
+// f(z, token) of every logit
+template <typename T, typename F>
+__device__ __forceinline__ void each_logit(const char* row, int32_t V, const F& f) {
+  each_unit<T>(row, V, [&](uint32_t bits, int token) { f(sample_value(bits, T{}), token); }, [&](const uint4& r, int token) {
+    float x[Elem<T>::per16];
+    unpack16(r, x, T{});
+#pragma unroll
+    for (int e = 0; e < Elem<T>::per16; ++e) f(x[e], token + e);
+  });
+}
+
+// Logits as signed integers: not negative ones rise with the value, negative ones fall.  The largest and smallest integer of some logits tell their
+// maximum, the largest unsigned one whether a NaN with a sign is among them.
+typedef __attribute__((ext_vector_type(2))) short pair16_t;
+typedef __attribute__((ext_vector_type(2))) unsigned short upair16_t;
+struct Ends16 {                // of bf16, packed
+  pair16_t most = {-32768, -32768}, least = {32767, 32767};
+  upair16_t umost = {0, 0};
+  __device__ __forceinline__ void add(uint32_t w) {
+    const pair16_t x = __builtin_bit_cast(pair16_t, w);
+    most = __builtin_elementwise_max(most, x);
+    least = __builtin_elementwise_min(least, x);
+    umost = __builtin_elementwise_max(umost, __builtin_bit_cast(upair16_t, w));
+  }
+  __device__ __forceinline__ void add(const uint4& r) { add(r.x); add(r.y); add(r.z); add(r.w); }
+  __device__ __forceinline__ void one(uint32_t bits) { add(bits * 0x10001u); }
+  __device__ __forceinline__ void finish(float& max, bool& bad) const {
+    const int hi = most.x > most.y ? most.x : most.y, lo = least.x < least.y ? least.x : least.y;
+    const uint32_t u = umost.x > umost.y ? umost.x : umost.y;
+    const bool any = hi >= lo;
+    max = any ? __uint_as_float((uint32_t)(hi >= 0 ? hi : lo & 0xffff) << 16) : -__builtin_inff();
+    bad = any && (hi >= 0x7f80 || u > 0xff80u);
+  }
+};
+struct Ends32 {
+  int32_t most = INT32_MIN, least = INT32_MAX;
+  uint32_t umost = 0;
+  __device__ __forceinline__ void one(uint32_t bits) {
+    most = max(most, (int32_t)bits);
+    least = min(least, (int32_t)bits);
+    umost = max(umost, bits);
+  }
+  __device__ __forceinline__ void add(const uint4& r) { one(r.x); one(r.y); one(r.z); one(r.w); }
+  __device__ __forceinline__ void finish(float& max, bool& bad) const {
+    const bool any = most >= least;
+    max = any ? __uint_as_float((uint32_t)(most >= 0 ? most : least)) : -__builtin_inff();
+    bad = any && (most >= 0x7f800000 || umost > 0xff800000u);
+  }
+};
+template <typename T> using Ends = std::conditional_t<std::is_same<T, float>::value, Ends32, Ends16>;
+
+// Whether one of the logits of 16 bytes may be at or above a line, given as its integer (rounded down): exact for fp32.
+struct Line {
+  float z;
+  int32_t i;
+  __device__ __forceinline__ Line(float z_, float) : z(z_), i((int32_t)__float_as_uint(z_)) {}
+  __device__ __forceinline__ Line(float z_, bf16_t) : z(z_) {
+    const uint32_t b = __float_as_uint(z_);
+    i = (int16_t)((b >> 16) + ((b & 0x80000000u) && (b & 0xffffu) ? 1 : 0));
+  }
+  template <typename N> __device__ __forceinline__ bool reached(N most, N least) const {
+    return i >= 0 ? most >= i : most >= 0 || least <= i;
+  }
+  __device__ __forceinline__ bool reached(const uint4& r, float) const {
+    const int32_t a = (int32_t)r.x, b = (int32_t)r.y, c = (int32_t)r.z, d = (int32_t)r.w;
+    const int32_t most = max(max(a, b), max(c, d));
+    return reached(most, i >= 0 ? most : min(min(a, b), min(c, d)));
+  }
+  __device__ __forceinline__ bool reached(const uint4& r, bf16_t) const {
+    const pair16_t a = __builtin_bit_cast(pair16_t, r.x), b = __builtin_bit_cast(pair16_t, r.y), c = __builtin_bit_cast(pair16_t, r.z),
+                   d = __builtin_bit_cast(pair16_t, r.w);
+    const pair16_t most = __builtin_elementwise_max(__builtin_elementwise_max(a, b), __builtin_elementwise_max(c, d));
+    const int32_t hi = most.x > most.y ? most.x : most.y;
+    if (i >= 0) return hi >= i;
+    const pair16_t least = __builtin_elementwise_min(__builtin_elementwise_min(a, b), __builtin_elementwise_min(c, d));
+    return reached(hi, (int32_t)(least.x < least.y ? least.x : least.y));
+  }
+};
 
 // What the threads share.
 struct SampleLds {
-  uint32_t count[kSteps];
-  u64 mass[kSteps];
+  union {
+    struct { u64 mass[kSteps]; uint32_t count[kSteps]; };
+    uint32_t value_count[kValues];
+  };
   u64 list[kListed];
   u64 wave64[kSampleWaves];
   uint32_t wave32[kSampleWaves];
   float wavef[kSampleWaves];
+  double waved[kSampleWaves];
   uint32_t n;
-  u64 found_mass, found_item, found_first, found_last;
-  uint32_t found_count;
+  u64 found_mass, found_item, found_first, found_last, found_weight;
+  uint32_t found_count, found_kind;
 };
 
 __device__ __forceinline__ u64 shuffle_up(u64 x, int by) {
@@ -137,6 +218,17 @@ __device__ __forceinline__ N block_sum(N x, N* waves) {
   for (int w = 0; w < kSampleWaves; ++w) all += waves[w];
   return all;
 }
+__device__ __forceinline__ double block_sum_double(double x, double* waves) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = x;
+  __syncthreads();
+  double all = 0.0;
+#pragma unroll
+  for (int w = 0; w < kSampleWaves; ++w) all += waves[w];
+  return all;
+}
 __device__ __forceinline__ float block_max(float x, float* waves) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
@@ -166,7 +258,10 @@ struct Scale {
   double rate;                 // log2(e) / temperature
   float steps;                 // steps of the histogram per unit of (max - z) / 2
   double temperature;
+  float rate_hi, rate_lo;      // twice the rate: for (max - z) / 2, which does not overflow
   __device__ __forceinline__ Scale(float m, double t) : max(m), rate(1.4426950408889634074 / t), temperature(t) {
+    rate_hi = (float)(2.0 * rate);
+    rate_lo = (float)(2.0 * rate - (double)rate_hi);
     steps = (float)fmin(rate * (2 * kSteps / kSpan), 1e30);       // (finite: max - z may be zero)
   }
   // step of a logit; kSteps and more: it weighs nothing (-inf too).  Rises with max - z whatever is rounded.
@@ -192,19 +287,27 @@ struct Scale {
     const double two = __longlong_as_double((long long)(1023 + (int)whole) << 52);
     return (u64)__double_as_longlong(__builtin_fma(y, two, 4503599627370496.0)) & 0xfffffffffffffull;
   }
+  // exp((z - max) / temperature) in 32 bits: the exponent's product with its rounding put back, so that what is left is the
+  // instruction's own (2^-23), that of max - z (kSpan * 2^-24 * ln 2 < 2^-19) and of sums of eight (3 * 2^-24): kTailBound covers them twice.
+  __device__ __forceinline__ float tail_weight(float z) const {
+    const float d = __builtin_fmaf(z, 0.5f, -0.5f * max), y = d * rate_hi, e = __builtin_fmaf(d, rate_hi, -y) + d * rate_lo, w = fast_exp2(y);
+    return y > -kSpan ? __builtin_fmaf(w, e * 0.69314718f, w) : 0.f;
+  }
   __device__ __forceinline__ bool above(float z, double log_min) const { return ((double)z - (double)max) / temperature >= log_min; }
 };
 
-// The listed items in order, one a thread; `n` of them.
+// The listed items in order, one a thread: bitonic, in registers inside a wave.
+template <bool WAVE>
 __device__ __forceinline__ u64 sort_list(SampleLds& s, int n) {
   const int tid = threadIdx.x;
   u64 x = tid < n ? s.list[tid] : ~0ull;
   int size = 64;
-  while (size < n) size <<= 1;
+  if constexpr (!WAVE)
+    while (size < n) size <<= 1;
   for (int k = 2; k <= size; k <<= 1)
     for (int j = k >> 1; j >= 1; j >>= 1) {
       u64 y;
-      if (j >= 64) {
+      if (!WAVE && j >= 64) {
         __syncthreads();
         s.list[tid] = x;
         __syncthreads();
@@ -218,28 +321,53 @@ __device__ __forceinline__ u64 sort_list(SampleLds& s, int n) {
   return x;
 }
 
-// A sorted list with its sums.
+// A sorted list with its sums.  WAVE: of 64 items at most, by the first wave alone, without barriers.
+template <bool WAVE>
 struct Sorted {
+  SampleLds& s;
   int n;
   u64 item, weight, upto;      // this thread's; upto: weights of the list up to and with it
   u64 all;
-  __device__ __forceinline__ Sorted(SampleLds& s, int count, const Scale& sc) : n(count) {
-    item = sort_list(s, n);
+  __device__ __forceinline__ Sorted(SampleLds& lds, int count, const Scale& sc) : s(lds), n(count) {
+    item = sort_list<WAVE>(s, n);
     weight = (int)threadIdx.x < n ? sc.weight(logit_of(item)) : 0;
-    upto = block_scan(weight, s.wave64);
-    all = 0;
+    if constexpr (WAVE) {
+      upto = wave_scan(weight);
+      all = from_lane(upto, 63);
+    } else {
+      upto = block_scan(weight, s.wave64);
+      all = 0;
 #pragma unroll
-    for (int w = 0; w < kSampleWaves; ++w) all += s.wave64[w];
+      for (int w = 0; w < kSampleWaves; ++w) all += s.wave64[w];
+    }
+  }
+  static __device__ __forceinline__ u64 from_lane(u64 x, int lane) {
+    const uint32_t lo = __shfl((uint32_t)x, lane, 64), hi = __shfl((uint32_t)(x >> 32), lane, 64);
+    return (u64)hi << 32 | lo;
+  }
+  __device__ __forceinline__ int how_many(bool mine) const {
+    if constexpr (WAVE) return __popcll(__ballot(mine));
+    else return __syncthreads_count(mine);
   }
   // how many items end at or before a mass
-  __device__ __forceinline__ int until(u64 mass) const { return __syncthreads_count((int)threadIdx.x < n && upto <= mass); }
+  __device__ __forceinline__ int until(u64 mass) const { return how_many((int)threadIdx.x < n && upto <= mass); }
   // the item at a place and the mass up to and with it, for every thread
-  __device__ __forceinline__ void at(SampleLds& s, int place, u64& the_item, u64& the_mass) const {
-    __syncthreads();
-    if ((int)threadIdx.x == place) { s.found_item = item; s.found_mass = upto; }
-    __syncthreads();
-    the_item = s.found_item;
-    the_mass = s.found_mass;
+  __device__ __forceinline__ void at(int place, u64& the_item, u64& the_mass) const {
+    if constexpr (WAVE) {
+      the_item = from_lane(item, place & 63);
+      the_mass = from_lane(upto, place & 63);
+    } else {
+      __syncthreads();
+      if ((int)threadIdx.x == place) { s.found_item = item; s.found_mass = upto; }
+      __syncthreads();
+      the_item = s.found_item;
+      the_mass = s.found_mass;
+    }
+  }
+  __device__ __forceinline__ u64 mass_at(int place) const {
+    u64 i, m;
+    at(place, i, m);
+    return m;
   }
 };
 
@@ -296,7 +424,8 @@ struct Found { u64 item, mass; };       // mass: up to and with it
 
 // Looks a target up in a row whose first histogram (sc.step()) is in `s`, as sum_steps() leaves it, and keeps it there.
 template <typename T>
-__device__ __noinline__ Found look_up(SampleLds& s, const char* row, int32_t V, const Scale& sc, const Totals& all, const Target& t) {
+__device__ __noinline__ Found look_up(SampleLds& s, const char* row, int32_t V, float max, double temperature, Totals all, Target t) {
+  const Scale sc(max, temperature);
   // the first histogram is put by: two counts and masses a thread
   Place at = step_of(s, t, all, 0, 0);
   const int i = 2 * threadIdx.x;
@@ -350,10 +479,10 @@ __device__ __noinline__ Found look_up(SampleLds& s, const char* row, int32_t V, 
     if (n < kListed) s.list[n] = x;
   });
   __syncthreads();
-  const Sorted list(s, (int)at.count, sc);
+  const Sorted<false> list(s, (int)at.count, sc);
   const int place = t.by_count ? (int)(t.count - at.before_count) - 1 : list.until(t.mass - at.before_mass);
   Found f;
-  list.at(s, place, f.item, f.mass);
+  list.at(place, f.item, f.mass);
   f.mass += at.before_mass;
   __syncthreads();
   s.count[i] = keep_c0; s.count[i + 1] = keep_c1;
@@ -375,6 +504,259 @@ __device__ __forceinline__ u64 cut_of(float p, u64 mass) {
   return (y < mass ? y : mass) - 1;
 }
 
+// What a row asks for.
+struct Wish {
+  bool by_k, by_p, by_m;
+  int k;
+  float top_p, u;
+  double log_min;
+};
+struct Drawn { u64 item, kept; bool settled; };
+
+// C: from the list of all tokens above a line.  complete: all that weigh anything.  tail: what the others weigh, in 32 bits.
+template <bool WAVE>
+__device__ __forceinline__ Drawn draw_from_list(SampleLds& s, int listed, const Scale& sc, const Wish& w, bool complete, double tail, int V) {
+  const Sorted<WAVE> list(s, listed, sc);
+  Drawn d{0, 0, false};
+  u64 other;
+  // the mass of all lies from lo to hi
+  u64 lo = list.all, hi = list.all;
+  if (!complete) {
+    lo += (u64)(tail * (1.0 - kTailBound));
+    hi += (u64)(tail * (1.0 + kTailBound)) + (u64)V;           // (and the weights' rounding to integers)
+    d.kept = list.all + (u64)tail;
+  } else {
+    d.kept = list.all;
+  }
+  bool known = true;           // what is kept, but for all of lo to hi
+  u64 least = 0;               // ... and if not, at least so much
+  if (w.by_k) {
+    if (w.k <= listed) { d.kept = list.mass_at(w.k - 1); lo = hi = d.kept; }
+    else if (!complete) { known = false; least = list.all; }
+  }
+  if (known && w.by_p) {
+    const int place = list.until(cut_of(w.top_p, lo));
+    const u64 upto = place < listed ? list.mass_at(place) : list.all;
+    if (place < listed && (lo == hi || place == list.until(cut_of(w.top_p, hi)))) d.kept = lo = hi = upto;
+    else { known = false; least = upto; }
+  }
+  if (w.by_m) {
+    const int above = list.how_many((int)threadIdx.x < listed && sc.above(logit_of(list.item), w.log_min));
+    const u64 m = above > 0 ? list.mass_at(above - 1) : 1ull << kWeightBits;       // (the largest is always kept)
+    const bool all_known = above < listed || complete;                              // (what lies behind the list is lower still)
+    if (all_known && (known ? lo != hi || m < lo : m <= least)) { d.kept = lo = hi = m; known = true; }
+    else if (!all_known) known = known && lo == hi && hi <= list.all;
+  }
+  if (known) {
+    const int place = list.until(part_of(w.u, lo));
+    if (place < listed && (lo == hi || place == list.until(part_of(w.u, hi)))) {
+      list.at(place, d.item, other);
+      d.settled = true;
+    }
+  }
+  return d;
+}
+
+// D for bf16 logits.  Values of 16 binades of either sign stand in falling order at 4096 places; those nearer to zero, which come between the signs, in
+// a list.  Not settled: too many of those, or of equal ones where the draw falls.
+struct ValueSums {
+  SampleLds& s;
+  uint32_t c[4];               // this thread's four places
+  u64 w[4];
+  uint32_t before_count, near_count, all_count;
+  u64 before_mass, near_mass, all_mass, half_mass;
+  uint32_t half_count;
+  // place, its first token's count and mass, and what each of its tokens weighs, for every thread; place kValues: the list near zero
+  struct At { uint32_t place, before_count; u64 before_mass, weight; };
+  __device__ __forceinline__ At find(const Target& t) {
+    __syncthreads();
+    uint32_t cc = before_count;
+    u64 m = before_mass;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool here = t.by_count ? cc < t.count && t.count <= cc + c[e] : m <= t.mass && t.mass < m + c[e] * w[e];
+      if (here) { s.found_kind = 4 * threadIdx.x + e; s.found_count = cc; s.found_mass = m; s.found_weight = w[e]; }
+      cc += c[e];
+      m += c[e] * w[e];
+    }
+    if (threadIdx.x == 0 && (t.by_count ? half_count < t.count && t.count <= half_count + near_count
+                                        : half_mass <= t.mass && t.mass < half_mass + near_mass)) {
+      s.found_kind = kValues; s.found_count = half_count; s.found_mass = half_mass; s.found_weight = 0;
+    }
+    __syncthreads();
+    return At{s.found_kind, s.found_count, s.found_mass, s.found_weight};
+  }
+};
+__device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, int32_t V, float max, double temperature, Wish w) {
+  const Scale sc(max, temperature);
+  const int tid = threadIdx.x;
+  Drawn d{0, 0, false};
+  // the lowest logit that weighs anything, and the binades: down from the larger magnitude of it and the largest
+  const float lowest = (float)fmax((double)max - (double)kSpan / sc.rate, -3.4028234663852886e38);
+  const uint32_t top = __float_as_uint(fmaxf(fabsf(max), fabsf(lowest))) >> 23, a0 = top > 15 ? (top - 15) << 7 : 1;        // (zeros are equal whatever their sign: never a place of their own)
+  __syncthreads();
+  for (int i = tid; i < kValues; i += kSampleThreads) s.value_count[i] = 0;
+  if (tid == 0) s.n = 0;
+  __syncthreads();
+  const auto add = [&](uint32_t h, int token) {      // (h: 16 bits)
+    const uint32_t v = (h & 0x7fffu) - a0;
+    if (v < kValues / 2) {
+      if (!(h & 0x8000u)) atomicAdd(&s.value_count[v ^ 0x7ffu], 1u);
+      else if (__uint_as_float(h << 16) >= lowest) atomicAdd(&s.value_count[v ^ 0x800u], 1u);
+    } else if ((int32_t)v < 0) {
+      const float z = __uint_as_float(h << 16);
+      if (z >= lowest) {
+        const uint32_t n = atomicAdd(&s.n, 1u);
+        if (n < kListed) s.list[n] = item_of(z, token);
+      }
+    }
+  };
+  each_unit<bf16_t>(row, V, add, [&](const uint4& r, int token) {
+    const uint32_t x[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      add(x[e] & 0xffffu, token + 2 * e);
+      add(x[e] >> 16, token + 2 * e + 1);
+    }
+  });
+  __syncthreads();
+  const int listed = (int)s.n;
+  if (listed > kListed) return d;
+  const Sorted<false> near(s, listed, sc);
+  const auto value_at = [&](int place) {
+    const uint32_t v = place < kValues / 2 ? (uint32_t)place ^ 0x7ffu : (uint32_t)place ^ 0x800u;
+    return __uint_as_float(((v + a0) | (place < kValues / 2 ? 0u : 0x8000u)) << 16);
+  };
+  ValueSums x{s};
+  uint32_t cc = 0;
+  u64 m = 0, above = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int place = 4 * tid + e;
+    x.c[e] = s.value_count[place];
+    x.w[e] = x.c[e] ? sc.weight(value_at(place)) : 0;
+    cc += x.c[e];
+    m += x.c[e] * x.w[e];
+    if (w.by_m && x.c[e] && sc.above(value_at(place), w.log_min)) above += x.c[e] * x.w[e];
+  }
+  x.near_count = (uint32_t)listed;
+  x.near_mass = near.all;
+  const uint32_t upto_count = block_scan(cc, s.wave32);
+  x.half_count = 0; x.all_count = x.near_count;
+#pragma unroll
+  for (int i = 0; i < kSampleWaves; ++i) {
+    if (i < kSampleWaves / 2) x.half_count += s.wave32[i];
+    x.all_count += s.wave32[i];
+  }
+  const u64 upto_mass = block_scan(m, s.wave64);
+  x.half_mass = 0; x.all_mass = x.near_mass;
+#pragma unroll
+  for (int i = 0; i < kSampleWaves; ++i) {
+    if (i < kSampleWaves / 2) x.half_mass += s.wave64[i];
+    x.all_mass += s.wave64[i];
+  }
+  const bool behind = tid >= kSampleThreads / 2;
+  x.before_count = upto_count - cc + (behind ? x.near_count : 0);
+  x.before_mass = upto_mass - m + (behind ? x.near_mass : 0);
+
+  // up to and with what a target finds
+  const auto mass_at = [&](const Target& t) {
+    const ValueSums::At at = x.find(t);
+    if (at.place == kValues) {
+      const int place = t.by_count ? (int)(t.count - at.before_count) - 1 : near.until(t.mass - at.before_mass);
+      return at.before_mass + near.mass_at(place);
+    }
+    return t.by_count ? at.before_mass + (u64)(t.count - at.before_count) * at.weight
+                      : at.before_mass + ((t.mass - at.before_mass) / at.weight + 1) * at.weight;
+  };
+  d.kept = x.all_mass;
+  if (w.by_k && (uint32_t)w.k < x.all_count) d.kept = mass_at(Target{true, (uint32_t)w.k, 0});
+  if (w.by_p) d.kept = mass_at(Target{false, 0, cut_of(w.top_p, d.kept)});
+  if (w.by_m) {
+    if (tid < listed && sc.above(logit_of(near.item), w.log_min)) above += near.weight;
+    u64 least = block_sum(above, s.wave64);
+    least = least < 1ull << kWeightBits ? 1ull << kWeightBits : least;
+    d.kept = least < d.kept ? least : d.kept;
+  }
+  const u64 mass = part_of(w.u, d.kept);
+  const ValueSums::At at = x.find(Target{false, 0, mass});
+  u64 other;
+  if (at.place == kValues) {
+    near.at(near.until(mass - at.before_mass), d.item, other);
+    d.settled = true;
+    return d;
+  }
+  // which of the equal ones: by id
+  const uint32_t count = s.value_count[at.place], h = __float_as_uint(value_at((int)at.place)) >> 16;
+  if (count > kListed) return d;
+  __syncthreads();
+  if (tid == 0) s.n = 0;
+  __syncthreads();
+  const auto note = [&](uint32_t bits, int token) {
+    if (bits == h) {
+      const uint32_t n = atomicAdd(&s.n, 1u);
+      if (n < kListed) s.list[n] = item_of(__uint_as_float(h << 16), token);
+    }
+  };
+  const uint32_t both = h * 0x10001u;
+  each_unit<bf16_t>(row, V, note, [&](const uint4& r, int token) {
+    const uint32_t x[4] = {r.x, r.y, r.z, r.w};
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t y = x[e] ^ both;                 // a half that is equal is zero
+      any = any || !(y & 0xffffu) || !(y >> 16);
+    }
+    if (any)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        note(x[e] & 0xffffu, token + 2 * e);
+        note(x[e] >> 16, token + 2 * e + 1);
+      }
+  });
+  __syncthreads();
+  const u64 items = sort_list<false>(s, (int)count);
+  __syncthreads();
+  if (tid == (int)((mass - at.before_mass) / at.weight)) s.found_item = items;
+  __syncthreads();
+  d.item = s.found_item;
+  d.settled = true;
+  return d;
+}
+
+// D for any logits.
+template <typename T>
+__device__ __noinline__ Drawn draw_from_steps(SampleLds& s, const char* row, int32_t V, float max, double temperature, Wish w) {
+  const Scale sc(max, temperature);
+  clear_steps(s, true);
+  each_logit<T>(row, V, [&](float z, int) {
+    const int step = sc.step(z);
+    if (step < kSteps) {
+      atomicAdd(&s.count[step], 1u);
+      atomicAdd(&s.mass[step], sc.weight(z));
+    }
+  });
+  const Totals total = sum_steps(s);
+  Drawn d{0, total.mass, true};
+  if (w.by_k && (uint32_t)w.k < total.count) d.kept = look_up<T>(s, row, V, max, temperature, total, Target{true, (uint32_t)w.k, 0}).mass;
+  if (w.by_p) d.kept = look_up<T>(s, row, V, max, temperature, total, Target{false, 0, cut_of(w.top_p, d.kept)}).mass;
+  if (w.by_m) {
+    // whole steps in front of the one the limit falls into, give or take one, and what of those three is above it
+    const double limit = -0.5 * w.log_min * sc.temperature * (double)sc.steps;
+    const int near = (int)fmin(fmax(limit, 0.0), (double)kSteps), from = near > 0 ? near - 1 : 0;
+    u64 m = 0;
+    each_logit<T>(row, V, [&](float z, int) {
+      const int step = sc.step(z);
+      if (step >= from && step <= near + 1 && step < kSteps && sc.above(z, w.log_min)) m += sc.weight(z);
+    });
+    m = block_sum(m, s.wave64) + (from < kSteps ? s.mass[from] : total.mass);
+    m = m < 1ull << kWeightBits ? 1ull << kWeightBits : m;
+    d.kept = m < d.kept ? m : d.kept;
+  }
+  d.item = look_up<T>(s, row, V, max, temperature, total, Target{false, 0, part_of(w.u, d.kept)}).item;
+  return d;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) {
   __shared__ SampleLds s;
@@ -382,18 +764,23 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
   if (p.active && !p.active[b]) return;
   const char* row = p.z + (int64_t)b * p.row_bytes;
   float t = p.temperature ? p.temperature[b] : 1.f;
-  int k = p.top_k ? p.top_k[b] : 0;
-  const float top_p = p.top_p ? p.top_p[b] : 1.f, min_p = p.min_p ? p.min_p[b] : 0.f, u = p.u[b];
-  if (t == 0.f) { t = 1.f; k = 1; }                    // the largest alone
+  Wish w;
+  w.k = p.top_k ? p.top_k[b] : 0;
+  w.top_p = p.top_p ? p.top_p[b] : 1.f;
+  const float min_p = p.min_p ? p.min_p[b] : 0.f;
+  w.u = p.u[b];
+  for (int i = threadIdx.x; i < kSteps; i += kSampleThreads) s.count[i] = 0;
+  if (threadIdx.x == 0) { s.n = 0; s.found_first = kSteps - 1; }
+  if (t >= 0.f && t < 1.17549435e-38f) { t = 1.f; w.k = 1; }      // the largest alone (2 log2(e) / t fits 32 bits otherwise)
 
   // A
-  float mine = -__builtin_inff();
-  bool bad = !(t > 0.f && t < __builtin_inff()) || u != u;
-  each_logit<T>(row, p.V, [&](float z, int) {
-    mine = fmaxf(mine, z);
-    bad = bad || !(z < __builtin_inff());
-  });
-  const float max = block_max(mine, s.wavef);
+  float mine;
+  bool bad;
+  Ends<T> ends;
+  each_unit<T>(row, p.V, [&](uint32_t bits, int) { ends.one(bits); }, [&](const uint4& r, int) { ends.add(r); });
+  ends.finish(mine, bad);
+  bad = bad || !(t > 0.f && t < __builtin_inff()) || w.u != w.u;
+  const float max = block_max(mine, s.wavef) + 0.f;      // (-0 is 0)
   if (__syncthreads_or(bad) || !(max > -__builtin_inff())) {
     if (threadIdx.x == 0) {
       p.token[b] = -1;
@@ -402,113 +789,85 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
     return;
   }
   const Scale sc(max, (double)t);
-  const bool by_k = k > 0 && k < p.V, by_p = top_p < 1.f, by_m = min_p > 0.f;
-  const double log_min = by_m ? log((double)min_p) : 0.0;
+  w.by_k = w.k > 0 && w.k < p.V;
+  w.by_p = w.top_p < 1.f;
+  w.by_m = min_p > 0.f;
+  w.log_min = w.by_m ? log((double)min_p) : 0.0;
 
   // the line: the step in which the wanted number of thread maxima is reached
-  const uint32_t wanted = by_k ? (uint32_t)k : (uint32_t)kUsualLine;
-  clear_steps(s, false);
+  const uint32_t wanted = w.by_k ? (uint32_t)w.k : (uint32_t)kUsualLine;
   {
     const int step = sc.step(mine);
     if (step < kSteps) atomicAdd(&s.count[step], 1u);
   }
   __syncthreads();
-  if (threadIdx.x == 0) s.found_first = kSteps - 1;
   const uint32_t c0 = s.count[2 * threadIdx.x], c1 = s.count[2 * threadIdx.x + 1], upto = block_scan(c0 + c1, s.wave32);
   if (upto >= wanted && upto - c0 - c1 < wanted) s.found_first = 2 * threadIdx.x + (upto - c1 >= wanted ? 0 : 1);
   __syncthreads();
-  const int line = (int)s.found_first;
+  const int step = (int)s.found_first;
+  const bool complete = step == kSteps - 1;              // all that weighs anything is above the line
+  // (its lower end, and what is rounded in it)
+  const float depth = 2.f * (float)(step + 1) / sc.steps;
+  const Line line(fmaxf(max - depth - 1e-6f * (fabsf(max) + depth), -3.4028235e38f), T{});
 
   // B
-  const bool sum_all = !by_k && (by_p || !by_m);
-  u64 sum = 0;
-  each_logit<T>(row, p.V, [&](float z, int token) {
-    const int step = sc.step(z);
-    if (step <= line) {
+  double tail = 0.0;
+  const auto note = [&](float z, int token) {
+    if (z >= line.z) {
       const uint32_t n = atomicAdd(&s.n, 1u);
       if (n < kListed) s.list[n] = item_of(z, token);
     }
-    if (sum_all && step < kSteps) sum += sc.weight(z);
-  });
-  u64 all = sum_all ? block_sum(sum, s.wave64) : 0;
-  __syncthreads();
-  const int listed = (int)s.n;
-  const bool complete = line == kSteps - 1;            // all that weighs anything is listed
-
-  // C
-  u64 item = 0, kept = 0;
-  bool settled = false;
-  if (listed <= kListed) {
-    const Sorted list(s, listed, sc);
-    u64 other;
-    if (complete) all = list.all;
-    bool known = true;
-    kept = all;
-    if (by_k) {
-      if (k <= listed) list.at(s, k - 1, other, kept);
-      else if (complete) kept = list.all;
-      else known = false;
-    }
-    if (known && by_p) {
-      const u64 cut = cut_of(top_p, kept);
-      if (cut < list.all) list.at(s, list.until(cut), other, kept);
-      else known = false;
-    }
-    if (by_m) {
-      const int above = __syncthreads_count((int)threadIdx.x < listed && sc.above(logit_of(list.item), log_min));
-      u64 m = 1ull << kWeightBits;                     // (the largest is always kept)
-      if (above > 0) list.at(s, above - 1, other, m);
-      const bool alone = !by_k && !by_p;
-      if (above < listed || complete) {
-        // (what lies behind the list is lower still, and a cut by top-p that is not settled lies behind it)
-        kept = !alone && known && kept < m ? kept : m;
-        known = true;
-      } else if (alone || !known || kept > list.all) {
-        known = false;
-      }
-    }
-    if (known) {
-      const u64 mass = part_of(u, kept);
-      if (mass < list.all) {
-        list.at(s, list.until(mass), item, other);
-        settled = true;
-      }
-    }
-  }
-
-  // D
-  if (!settled) {
-    clear_steps(s, true);
-    each_logit<T>(row, p.V, [&](float z, int) {
-      const int step = sc.step(z);
-      if (step < kSteps) {
-        atomicAdd(&s.count[step], 1u);
-        atomicAdd(&s.mass[step], sc.weight(z));
+  };
+  if (!w.by_k && (w.by_p || !w.by_m) && !complete) {
+    double part = 0.0;
+    each_unit<T>(row, p.V, [&](uint32_t bits, int token) {
+      const float z = sample_value(bits, T{});
+      note(z, token);
+      if (z < line.z) part += sc.tail_weight(z);
+    }, [&](const uint4& r, int token) {
+      float x[Elem<T>::per16], y[Elem<T>::per16];
+      unpack16(r, x, T{});
+#pragma unroll
+      for (int e = 0; e < Elem<T>::per16; ++e) y[e] = x[e] < line.z ? sc.tail_weight(x[e]) : 0.f;
+      if constexpr (Elem<T>::per16 == 8) part += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+      else part += (y[0] + y[1]) + (y[2] + y[3]);
+      if (line.reached(r, T{}))
+#pragma unroll
+        for (int e = 0; e < Elem<T>::per16; ++e) note(x[e], token + e);
+    });
+    tail = block_sum_double(part, s.waved) * (double)(1ull << kWeightBits);
+  } else {
+    each_unit<T>(row, p.V, [&](uint32_t bits, int token) { note(sample_value(bits, T{}), token); }, [&](const uint4& r, int token) {
+      if (line.reached(r, T{})) {
+        float x[Elem<T>::per16];
+        unpack16(r, x, T{});
+#pragma unroll
+        for (int e = 0; e < Elem<T>::per16; ++e) note(x[e], token + e);
       }
     });
-    const Totals total = sum_steps(s);
-    kept = total.mass;
-    if (by_k && (uint32_t)k < total.count) kept = look_up<T>(s, row, p.V, sc, total, Target{true, (uint32_t)k, 0}).mass;
-    if (by_p) kept = look_up<T>(s, row, p.V, sc, total, Target{false, 0, cut_of(top_p, kept)}).mass;
-    if (by_m) {
-      // whole steps in front of the one the limit falls into, give or take one, and what of those three is above it
-      const double limit = -0.5 * log_min * sc.temperature * (double)sc.steps;
-      const int near = (int)fmin(fmax(limit, 0.0), (double)kSteps), from = near > 0 ? near - 1 : 0;
-      u64 m = 0;
-      each_logit<T>(row, p.V, [&](float z, int) {
-        const int step = sc.step(z);
-        if (step >= from && step <= near + 1 && step < kSteps && sc.above(z, log_min)) m += sc.weight(z);
-      });
-      m = block_sum(m, s.wave64) + (from < kSteps ? s.mass[from] : total.mass);
-      m = m < 1ull << kWeightBits ? 1ull << kWeightBits : m;
-      kept = m < kept ? m : kept;
-    }
-    item = look_up<T>(s, row, p.V, sc, total, Target{false, 0, part_of(u, kept)}).item;
   }
+  __syncthreads();
+  const int listed = (int)s.n;
+
+  // C
+  Drawn d{0, 0, false};
+  if (listed <= 64) {
+    if (threadIdx.x < 64) {
+      d = draw_from_list<true>(s, listed, sc, w, complete, tail, p.V);
+      if (threadIdx.x == 0) { s.found_item = d.item; s.found_mass = d.kept; s.found_kind = d.settled; }
+    }
+    __syncthreads();
+    d = Drawn{s.found_item, s.found_mass, s.found_kind != 0};
+  } else if (listed <= kListed) {
+    d = draw_from_list<false>(s, listed, sc, w, complete, tail, p.V);
+  }
+  if constexpr (std::is_same<T, bf16_t>::value)
+    if (!d.settled) d = draw_from_values(s, row, p.V, max, (double)t, w);
+  if (!d.settled) d = draw_from_steps<T>(s, row, p.V, max, (double)t, w);
   if (threadIdx.x == 0) {
-    p.token[b] = (int32_t)(uint32_t)item;
+    p.token[b] = (int32_t)(uint32_t)d.item;
     if (p.logprob)
-      p.logprob[b] = (float)(((double)logit_of(item) - (double)max) / sc.temperature - log((double)kept * (1.0 / (1ull << kWeightBits))));
+      p.logprob[b] = (float)(((double)logit_of(d.item) - (double)max) / sc.temperature - log((double)d.kept * (1.0 / (1ull << kWeightBits))));
   }
 }
 
