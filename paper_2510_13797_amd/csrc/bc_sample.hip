@@ -8,7 +8,7 @@
 // included.  A token below 2^-43 of the largest weight weighs nothing.
 //
 // A workgroup of 1024 threads has a row:
-//   A  the maximum; of the threads' own maxima the k-th largest (without top-k the 400th) gives a line above which all tokens
+//   A  the maximum; of the threads' own maxima the k-th largest (without top-k the 200th) gives a line above which all tokens
 //      that matter usually lie, and not many more than that;
 //   B  a second pass lists the tokens above the line (in LDS, 1024 at most).  Where the sum of all weights is asked for, it adds up those below
 //      the line in 32 bits, with a bound on how far off that is (tail_weight());
@@ -27,12 +27,15 @@ namespace {
 
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / 64;
+constexpr int kAtOnce = 10;                // loads of a thread that are waited for together
 constexpr int kListed = 1024;              // tokens a sorted list holds
 constexpr int kSteps = 2048;               // of a histogram
 constexpr int kWeightBits = 42;            // the largest token weighs 2^42
 constexpr float kSpan = 43.5f;             // base-2 exponents a histogram covers: weights below 2^-43 round to nothing
-constexpr int kUsualLine = 400;            // thread maxima above the line without top-k: 0.5 tokens a thread, 512 in all
-constexpr int kValues = 4096;              // bf16 values counted: 16 binades of either sign
+constexpr int kUsualLine = 200;            // thread maxima above the line without top-k: some 220 tokens
+constexpr int kValues = 4096;              // bf16 values counted: 16 binades of either sign,
+constexpr int kCopies = 2;                 // odd and even lanes apart, so that fewer meet at a count
+constexpr int kNowhere = 64;               // counts for logits of no place, a lane's own each
 
 struct SampleParams {
   const char* z;
@@ -55,10 +58,11 @@ __device__ __forceinline__ float sample_value(uint32_t bits, float) { return __u
 __device__ __forceinline__ float sample_value(uint32_t bits, bf16_t) { return __uint_as_float(bits << 16); }
 
 // A row, which may start at any element: those in front of the first 16-byte boundary and behind the last are taken one by one (single(bits,
-// token)), the others by 16 bytes (unit(words, first token)), four loads of a thread at a time.
-template <typename T, typename FS, typename FU>
+// token)), the others by 16 bytes (unit(words, first token)), BATCH loads of a thread at a time: kAtOnce where there is little to do
+// with them; fewer where there is more, with the next ones on their way meanwhile (AHEAD).
+template <typename T, int BATCH, bool AHEAD, typename FS, typename FU>
 __device__ __forceinline__ void each_unit(const char* row, int32_t V, const FS& single, const FU& unit_of) {
-  constexpr int EPU = Elem<T>::per16, ES = Elem<T>::size, BATCH = 4;
+  constexpr int EPU = Elem<T>::per16, ES = Elem<T>::size;
   const int head = min(((16 - (int)(reinterpret_cast<uintptr_t>(row) & 15u)) & 15) / ES, V);
   const int units = (V - head) / EPU, tail = V - head - units * EPU, tid = threadIdx.x;
   if (tid < head + tail) {
@@ -66,25 +70,46 @@ __device__ __forceinline__ void each_unit(const char* row, int32_t V, const FS& 
     if constexpr (ES == 4) single(reinterpret_cast<const uint32_t*>(row)[i], i);
     else single((uint32_t)reinterpret_cast<const uint16_t*>(row)[i], i);
   }
-  const uint4* at = reinterpret_cast<const uint4*>(row + head * ES);
-  for (int base = 0; base < units; base += BATCH * kSampleThreads) {
-    uint4 r[BATCH];
+  // (every load is made, that of the last unit behind the row's end: where they were conditional, each waited for the one before it)
+  typedef __attribute__((address_space(1))) const u32x4_t global_unit_t;
+  const global_unit_t* at = (const global_unit_t*)(row + head * ES);
+  const auto load = [&](uint4 (&r)[BATCH], int base) {
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
-      const int unit = base + b * kSampleThreads + tid;
-      if (unit < units) r[b] = at[unit];
+      const u32x4_t x = at[min(base + b * kSampleThreads + tid, units - 1)];
+      r[b] = make_uint4(x.x, x.y, x.z, x.w);
     }
+  };
+  const auto work = [&](const uint4 (&r)[BATCH], int base) {
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
       const int unit = base + b * kSampleThreads + tid;
       if (unit < units) unit_of(r[b], head + unit * EPU);
+    }
+  };
+  constexpr int STEP = BATCH * kSampleThreads;
+  if (units == 0) return;
+  if constexpr (!AHEAD) {
+    for (int base = 0; base < units; base += STEP) {
+      uint4 r[BATCH];
+      load(r, base);
+      work(r, base);
+    }
+  } else {
+    uint4 r[BATCH], n[BATCH];
+    load(r, 0);
+    for (int base = 0; base < units; base += 2 * STEP) {
+      load(n, base + STEP);
+      work(r, base);
+      load(r, base + 2 * STEP);
+      work(n, base + STEP);
     }
   }
 }
 // f(z, token) of every logit
 template <typename T, typename F>
 __device__ __forceinline__ void each_logit(const char* row, int32_t V, const F& f) {
-  each_unit<T>(row, V, [&](uint32_t bits, int token) { f(sample_value(bits, T{}), token); }, [&](const uint4& r, int token) {
+  each_unit<T, 4, false>(row, V, [&](uint32_t bits, int token) { f(sample_value(bits, T{}), token); }, [&](const uint4& r, int token) {
     float x[Elem<T>::per16];
     unpack16(r, x, T{});
 #pragma unroll
@@ -164,7 +189,7 @@ struct Line {
 struct SampleLds {
   union {
     struct { u64 mass[kSteps]; uint32_t count[kSteps]; };
-    uint32_t value_count[kValues];
+    uint32_t value_count[(kValues + kNowhere) * kCopies];
   };
   u64 list[kListed];
   u64 wave64[kSampleWaves];
@@ -176,23 +201,40 @@ struct SampleLds {
   uint32_t found_count, found_kind;
 };
 
-__device__ __forceinline__ u64 shuffle_up(u64 x, int by) {
-  const uint32_t lo = __shfl_up((uint32_t)x, by, 64), hi = __shfl_up((uint32_t)(x >> 32), by, 64);
-  return (u64)hi << 32 | lo;
+// x of the lane whose number differs in bit J (of 64 lanes), by the vector units: through LDS (two shuffles for 64 bits) a sort of 512 took 10 us, 3 so.
+template <int J>
+__device__ __forceinline__ uint32_t across(uint32_t x) {
+  if constexpr (J == 1) return __builtin_amdgcn_update_dpp(x, x, kDppXor1, 0xf, 0xf, true);
+  else if constexpr (J == 2) return __builtin_amdgcn_update_dpp(x, x, kDppXor2, 0xf, 0xf, true);
+  else if constexpr (J == 4) {           // 7 - i, then 3 - i inside a quad
+    const uint32_t y = __builtin_amdgcn_update_dpp(x, x, kDppHalfMirror, 0xf, 0xf, true);
+    return __builtin_amdgcn_update_dpp(y, y, 0x1B, 0xf, 0xf, true);
+  } else if constexpr (J == 8) return __builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xf, true);      // turned by eight of sixteen
+  else if constexpr (J == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
 }
-__device__ __forceinline__ u64 shuffle_xor(u64 x, int by) {
-  const uint32_t lo = __shfl_xor((uint32_t)x, by, 64), hi = __shfl_xor((uint32_t)(x >> 32), by, 64);
-  return (u64)hi << 32 | lo;
+template <int J>
+__device__ __forceinline__ u64 across64(u64 x) { return (u64)across<J>((uint32_t)(x >> 32)) << 32 | across<J>((uint32_t)x); }
+// x of another lane, zero where there is none (row: 16 lanes; mask: rows that take it)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_before(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 from_before(u64 x) {
+  return (u64)from_before<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | from_before<CTRL, ROWS>((uint32_t)x);
 }
 template <typename N>
 __device__ __forceinline__ N wave_scan(N x) {          // sum of this lane's and all before it
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    N y;
-    if constexpr (sizeof(N) == 8) y = shuffle_up(x, o); else y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
+  x += from_before<0x111, 0xf>(x);                      // 1, 2, 4, 8 lanes back inside a row,
+  x += from_before<0x112, 0xf>(x);
+  x += from_before<0x114, 0xf>(x);
+  x += from_before<0x118, 0xf>(x);
+  x += from_before<0x142, 0xa>(x);                      // the last of a row to the next, of two rows to the next two
+  x += from_before<0x143, 0xc>(x);
   return x;
 }
 // The same over the workgroup; `waves`: kSampleWaves in LDS.
@@ -258,10 +300,10 @@ struct Scale {
   double rate;                 // log2(e) / temperature
   float steps;                 // steps of the histogram per unit of (max - z) / 2
   double temperature;
-  float rate_hi, rate_lo;      // twice the rate: for (max - z) / 2, which does not overflow
+  float rate_hi, offset;       // the rate in 32 bits, max times it
   __device__ __forceinline__ Scale(float m, double t) : max(m), rate(1.4426950408889634074 / t), temperature(t) {
-    rate_hi = (float)(2.0 * rate);
-    rate_lo = (float)(2.0 * rate - (double)rate_hi);
+    rate_hi = (float)rate;
+    offset = max * rate_hi;
     steps = (float)fmin(rate * (2 * kSteps / kSpan), 1e30);       // (finite: max - z may be zero)
   }
   // step of a logit; kSteps and more: it weighs nothing (-inf too).  Rises with max - z whatever is rounded.
@@ -287,16 +329,30 @@ struct Scale {
     const double two = __longlong_as_double((long long)(1023 + (int)whole) << 52);
     return (u64)__double_as_longlong(__builtin_fma(y, two, 4503599627370496.0)) & 0xfffffffffffffull;
   }
-  // exp((z - max) / temperature) in 32 bits: the exponent's product with its rounding put back, so that what is left is the
-  // instruction's own (2^-23), that of max - z (kSpan * 2^-24 * ln 2 < 2^-19) and of sums of eight (3 * 2^-24): kTailBound covers them twice.
-  __device__ __forceinline__ float tail_weight(float z) const {
-    const float d = __builtin_fmaf(z, 0.5f, -0.5f * max), y = d * rate_hi, e = __builtin_fmaf(d, rate_hi, -y) + d * rate_lo, w = fast_exp2(y);
-    return y > -kSpan ? __builtin_fmaf(w, e * 0.69314718f, w) : 0.f;
+  // exp((z - max) / temperature) in 32 bits, but for factors that all have in common: its exponent is z * rate_hi - offset, rounded once
+  // (kSpan * 2^-24 * ln 2), and tail_sum() puts right what the rounding of rate and offset did to it, the former (kSpan * 2^-24 * ln 2 at most) from some of the
+  // exponents.  With the instruction's 2^-23 and sums of eight, 3 * 2^-24, below 2^-18: kTailBound is twice that.  (Weights beyond kSpan, which round to nothing,
+  // stay in: less than V altogether.)
+  __device__ __forceinline__ float tail_exponent(float z) const { return __builtin_fmaf(z, rate_hi, -offset); }
+  __device__ __forceinline__ bool tail_fits() const { return fabsf(offset) < 1e30f; }
+  __device__ __forceinline__ double tail_sum(double weights, double mean_exponent) const {
+    return weights * exp2((double)offset - (double)max * (double)rate_hi) * (1.0 + 0.69314718055994531 * mean_exponent * ((rate - (double)rate_hi) / rate));
   }
   __device__ __forceinline__ bool above(float z, double log_min) const { return ((double)z - (double)max) / temperature >= log_min; }
 };
 
-// The listed items in order, one a thread: bitonic, in registers inside a wave.
+// The listed items in order, one a thread: bitonic, in registers inside a wave.  Waves without items keep to the barriers.
+template <int J>
+__device__ __forceinline__ void sort_step(u64& x, bool falling) {
+  const u64 y = across64<J>(x);
+  const bool keep_small = ((threadIdx.x & J) == 0) != falling;
+  x = (y < x) == keep_small ? y : x;
+}
+template <int J>
+__device__ __forceinline__ void sort_steps(u64& x, bool falling) {      // J, J / 2 ... 1
+  sort_step<J>(x, falling);
+  if constexpr (J > 1) sort_steps<J / 2>(x, falling);
+}
 template <bool WAVE>
 __device__ __forceinline__ u64 sort_list(SampleLds& s, int n) {
   const int tid = threadIdx.x;
@@ -304,20 +360,27 @@ __device__ __forceinline__ u64 sort_list(SampleLds& s, int n) {
   int size = 64;
   if constexpr (!WAVE)
     while (size < n) size <<= 1;
-  for (int k = 2; k <= size; k <<= 1)
-    for (int j = k >> 1; j >= 1; j >>= 1) {
-      u64 y;
-      if (!WAVE && j >= 64) {
+  const bool mine = (tid & ~63) < size;                  // (a wave's)
+  if (mine) {
+    sort_steps<1>(x, tid & 2);
+    sort_steps<2>(x, tid & 4);
+    sort_steps<4>(x, tid & 8);
+    sort_steps<8>(x, tid & 16);
+    sort_steps<16>(x, tid & 32);
+    sort_steps<32>(x, !WAVE && (tid & 64));
+  }
+  if constexpr (!WAVE) {
+    for (int k = 128; k <= size; k <<= 1) {
+      for (int j = k >> 1; j >= 64; j >>= 1) {
         __syncthreads();
         s.list[tid] = x;
         __syncthreads();
-        y = s.list[tid ^ j];
-      } else {
-        y = shuffle_xor(x, j);
+        const u64 y = s.list[tid ^ j];
+        x = (y < x) == (((tid & j) == 0) == ((tid & k) == 0)) ? y : x;
       }
-      const bool keep_small = ((tid & j) == 0) == ((tid & k) == 0);
-      x = (y < x) == keep_small ? y : x;
+      if (mine) sort_steps<32>(x, tid & k);
     }
+  }
   return x;
 }
 
@@ -491,6 +554,12 @@ __device__ __noinline__ Found look_up(SampleLds& s, const char* row, int32_t V, 
   return f;
 }
 
+// a / b of a quotient below 2^32, by 64-bit floating point and what that is off
+__device__ __forceinline__ u64 quotient(u64 a, u64 b) {
+  u64 q = (u64)((double)a / (double)b);
+  if (q * b > a) --q;
+  return (q + 1) * b <= a ? q + 1 : q;
+}
 // floor(u * mass), below it
 __device__ __forceinline__ u64 part_of(float u, u64 mass) {
   const double x = (double)u * (double)mass;
@@ -522,9 +591,11 @@ __device__ __forceinline__ Drawn draw_from_list(SampleLds& s, int listed, const 
   // the mass of all lies from lo to hi
   u64 lo = list.all, hi = list.all;
   if (!complete) {
-    lo += (u64)(tail * (1.0 - kTailBound));
-    hi += (u64)(tail * (1.0 + kTailBound)) + (u64)V;           // (and the weights' rounding to integers)
+    // (and the weights' rounding to integers, and sums of eight that held listed ones)
+    const u64 off = (u64)(tail * kTailBound) + (list.all >> 21) + (u64)V;
     d.kept = list.all + (u64)tail;
+    lo = d.kept > list.all + off ? d.kept - off : list.all;
+    hi = d.kept + off;
   } else {
     d.kept = list.all;
   }
@@ -587,7 +658,7 @@ struct ValueSums {
     return At{s.found_kind, s.found_count, s.found_mass, s.found_weight};
   }
 };
-__device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, int32_t V, float max, double temperature, Wish w) {
+__device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row, int32_t V, float max, double temperature, Wish w) {
   const Scale sc(max, temperature);
   const int tid = threadIdx.x;
   Drawn d{0, 0, false};
@@ -595,15 +666,26 @@ __device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, in
   const float lowest = (float)fmax((double)max - (double)kSpan / sc.rate, -3.4028234663852886e38);
   const uint32_t top = __float_as_uint(fmaxf(fabsf(max), fabsf(lowest))) >> 23, a0 = top > 15 ? (top - 15) << 7 : 1;        // (zeros are equal whatever their sign: never a place of their own)
   __syncthreads();
-  for (int i = tid; i < kValues; i += kSampleThreads) s.value_count[i] = 0;
+  for (int i = tid; i < (kValues + kNowhere) * kCopies; i += kSampleThreads) s.value_count[i] = 0;
   if (tid == 0) s.n = 0;
   __syncthreads();
-  const auto add = [&](uint32_t h, int token) {      // (h: 16 bits)
-    const uint32_t v = (h & 0x7fffu) - a0;
-    if (v < kValues / 2) {
-      if (!(h & 0x8000u)) atomicAdd(&s.value_count[v ^ 0x7ffu], 1u);
-      else if (__uint_as_float(h << 16) >= lowest) atomicAdd(&s.value_count[v ^ 0x800u], 1u);
-    } else if ((int32_t)v < 0) {
+  // place of a value, less than kValues for one of the binades and only for those: magnitude less a0, turned for a positive one, then the lane's count there as
+  // bytes (two values at a time).  Places below the lowest logit are counted, and weigh nothing.
+  const auto packed = [](int x) { return (uint32_t)x * 0x10001u; };
+  const upair16_t from = __builtin_bit_cast(upair16_t, packed(a0)), nowhere = __builtin_bit_cast(upair16_t, packed(kValues + (tid & (kNowhere - 1))));
+  const uint32_t copy = packed(4 * (tid & (kCopies - 1)));
+  const auto places = [&](uint32_t x, uint32_t magnitude) {
+    const upair16_t v = __builtin_bit_cast(upair16_t, magnitude) - from;
+    const uint32_t sign = __builtin_bit_cast(uint32_t, __builtin_bit_cast(pair16_t, x) >> 15);
+    const upair16_t turned = __builtin_bit_cast(upair16_t, __builtin_bit_cast(uint32_t, v) ^ (~sign & 0x07ff07ffu));
+    const upair16_t at = __builtin_elementwise_min(__builtin_elementwise_add_sat(turned, __builtin_bit_cast(upair16_t, sign & 0x08000800u)), nowhere);
+    static_assert((kValues + kNowhere) * kCopies * 4 <= 65536 && kCopies == 2, "bytes of a place");
+    return __builtin_bit_cast(uint32_t, at << (unsigned short)3) | copy;
+  };
+  char* const counts = reinterpret_cast<char*>(s.value_count);
+  const auto count = [&](uint32_t at) { atomicAdd(reinterpret_cast<uint32_t*>(counts + at), 1u); };
+  const auto near_zero = [&](uint32_t h, int token) {
+    if ((h & 0x7fffu) < a0) {
       const float z = __uint_as_float(h << 16);
       if (z >= lowest) {
         const uint32_t n = atomicAdd(&s.n, 1u);
@@ -611,13 +693,25 @@ __device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, in
       }
     }
   };
-  each_unit<bf16_t>(row, V, add, [&](const uint4& r, int token) {
+  each_unit<bf16_t, 5, true>(row, V, [&](uint32_t h, int token) {
+    count(places(h, h & 0x7fffu) & 0xffffu);
+    near_zero(h, token);
+  }, [&](const uint4& r, int token) {
     const uint32_t x[4] = {r.x, r.y, r.z, r.w};
+    upair16_t least = {0xffff, 0xffff};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      add(x[e] & 0xffffu, token + 2 * e);
-      add(x[e] >> 16, token + 2 * e + 1);
+      const uint32_t magnitude = x[e] & 0x7fff7fffu, at = places(x[e], magnitude);
+      least = __builtin_elementwise_min(least, __builtin_bit_cast(upair16_t, magnitude));
+      count(at & 0xffffu);
+      count(at >> 16);
     }
+    if (least.x < a0 || least.y < a0)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        near_zero(x[e] & 0xffffu, token + 2 * e);
+        near_zero(x[e] >> 16, token + 2 * e + 1);
+      }
   });
   __syncthreads();
   const int listed = (int)s.n;
@@ -633,7 +727,9 @@ __device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, in
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int place = 4 * tid + e;
-    x.c[e] = s.value_count[place];
+    x.c[e] = 0;
+#pragma unroll
+    for (int n = 0; n < kCopies; ++n) x.c[e] += s.value_count[place * kCopies + n];
     x.w[e] = x.c[e] ? sc.weight(value_at(place)) : 0;
     cc += x.c[e];
     m += x.c[e] * x.w[e];
@@ -667,7 +763,7 @@ __device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, in
       return at.before_mass + near.mass_at(place);
     }
     return t.by_count ? at.before_mass + (u64)(t.count - at.before_count) * at.weight
-                      : at.before_mass + ((t.mass - at.before_mass) / at.weight + 1) * at.weight;
+                      : at.before_mass + (quotient(t.mass - at.before_mass, at.weight) + 1) * at.weight;
   };
   d.kept = x.all_mass;
   if (w.by_k && (uint32_t)w.k < x.all_count) d.kept = mass_at(Target{true, (uint32_t)w.k, 0});
@@ -687,8 +783,11 @@ __device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, in
     return d;
   }
   // which of the equal ones: by id
-  const uint32_t count = s.value_count[at.place], h = __float_as_uint(value_at((int)at.place)) >> 16;
-  if (count > kListed) return d;
+  uint32_t equal = 0;
+#pragma unroll
+  for (int n = 0; n < kCopies; ++n) equal += s.value_count[at.place * kCopies + n];
+  const uint32_t h = __float_as_uint(value_at((int)at.place)) >> 16;
+  if (equal > kListed) return d;
   __syncthreads();
   if (tid == 0) s.n = 0;
   __syncthreads();
@@ -699,15 +798,12 @@ __device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, in
     }
   };
   const uint32_t both = h * 0x10001u;
-  each_unit<bf16_t>(row, V, note, [&](const uint4& r, int token) {
+  each_unit<bf16_t, kAtOnce, false>(row, V, note, [&](const uint4& r, int token) {
     const uint32_t x[4] = {r.x, r.y, r.z, r.w};
-    bool any = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t y = x[e] ^ both;                 // a half that is equal is zero
-      any = any || !(y & 0xffffu) || !(y >> 16);
-    }
-    if (any)
+    // (a half that is equal is zero: the smaller ones of two and two)
+    const auto diff = [&](int e) { return __builtin_bit_cast(upair16_t, x[e] ^ both); };
+    const upair16_t least = __builtin_elementwise_min(__builtin_elementwise_min(diff(0), diff(1)), __builtin_elementwise_min(diff(2), diff(3)));
+    if (least.x == 0 || least.y == 0)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         note(x[e] & 0xffffu, token + 2 * e);
@@ -715,9 +811,9 @@ __device__ __noinline__ Drawn draw_from_values(SampleLds& s, const char* row, in
       }
   });
   __syncthreads();
-  const u64 items = sort_list<false>(s, (int)count);
+  const u64 items = sort_list<false>(s, (int)equal);
   __syncthreads();
-  if (tid == (int)((mass - at.before_mass) / at.weight)) s.found_item = items;
+  if (tid == (int)quotient(mass - at.before_mass, at.weight)) s.found_item = items;
   __syncthreads();
   d.item = s.found_item;
   d.settled = true;
@@ -771,13 +867,13 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
   w.u = p.u[b];
   for (int i = threadIdx.x; i < kSteps; i += kSampleThreads) s.count[i] = 0;
   if (threadIdx.x == 0) { s.n = 0; s.found_first = kSteps - 1; }
-  if (t >= 0.f && t < 1.17549435e-38f) { t = 1.f; w.k = 1; }      // the largest alone (2 log2(e) / t fits 32 bits otherwise)
+  if (t >= 0.f && t < 1.17549435e-38f) { t = 1.f; w.k = 1; }      // the largest alone (log2(e) / t fits 32 bits otherwise)
 
   // A
   float mine;
   bool bad;
   Ends<T> ends;
-  each_unit<T>(row, p.V, [&](uint32_t bits, int) { ends.one(bits); }, [&](const uint4& r, int) { ends.add(r); });
+  each_unit<T, kAtOnce, false>(row, p.V, [&](uint32_t bits, int) { ends.one(bits); }, [&](const uint4& r, int) { ends.add(r); });
   ends.finish(mine, bad);
   bad = bad || !(t > 0.f && t < __builtin_inff()) || w.u != w.u;
   const float max = block_max(mine, s.wavef) + 0.f;      // (-0 is 0)
@@ -810,6 +906,26 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
   const float depth = 2.f * (float)(step + 1) / sc.steps;
   const Line line(fmaxf(max - depth - 1e-6f * (fabsf(max) + depth), -3.4028235e38f), T{});
 
+  // Rows so flat that the list would not hold what is drawn from: left to D.  The threads' maxima above the line say about what it holds (half
+  // as much again), 16 bytes a thread from the middle of the row what lies below.  (A wrong guess costs time alone.)
+  const bool sum = !w.by_k && (w.by_p || !w.by_m) && !complete;
+  bool flat = sum && !sc.tail_fits();
+  if (sum && !w.by_m && !flat) {
+    float in = mine >= line.z ? fast_exp2(sc.tail_exponent(mine)) : 0.f, out = 0.f;
+    constexpr int EPU = Elem<T>::per16;
+    const int units = (p.V - EPU) / EPU;                 // (whole ones there are wherever the row starts)
+    if (units >= kSampleThreads) {
+      const char* at = row + ((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) + (int64_t)((units - kSampleThreads) / 2 + threadIdx.x) * 16;
+      float x[EPU];
+      unpack16(*reinterpret_cast<const uint4*>(at), x, T{});
+#pragma unroll
+      for (int e = 0; e < EPU; ++e) out += x[e] < line.z ? fast_exp2(sc.tail_exponent(x[e])) : 0.f;
+      const double above = 1.5 * block_sum_double((double)in, s.waved);
+      const double below = block_sum_double((double)out, s.waved) * ((double)units / kSampleThreads);
+      flat = above < 0.85 * (w.by_p ? w.top_p : w.u) * (above + below);
+    }
+  }
+
   // B
   double tail = 0.0;
   const auto note = [&](float z, int token) {
@@ -818,26 +934,38 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
       if (n < kListed) s.list[n] = item_of(z, token);
     }
   };
-  if (!w.by_k && (w.by_p || !w.by_m) && !complete) {
+  if (flat) {
+  } else if (sum) {
     double part = 0.0;
-    each_unit<T>(row, p.V, [&](uint32_t bits, int token) {
+    float some = 0.f, weighted = 0.f;                    // of every unit's first: weight, weight times exponent
+    const auto listed_too = [&](float z, int token) {    // (its weight has been added: taken away as it was)
+      if (z >= line.z) {
+        part -= (double)fast_exp2(sc.tail_exponent(z));
+        note(z, token);
+      }
+    };
+    each_unit<T, 5, true>(row, p.V, [&](uint32_t bits, int token) {
       const float z = sample_value(bits, T{});
-      note(z, token);
-      if (z < line.z) part += sc.tail_weight(z);
+      part += (double)fast_exp2(sc.tail_exponent(z));
+      listed_too(z, token);
     }, [&](const uint4& r, int token) {
-      float x[Elem<T>::per16], y[Elem<T>::per16];
-      unpack16(r, x, T{});
+      float z[Elem<T>::per16], x[Elem<T>::per16];
+      unpack16(r, z, T{});
 #pragma unroll
-      for (int e = 0; e < Elem<T>::per16; ++e) y[e] = x[e] < line.z ? sc.tail_weight(x[e]) : 0.f;
-      if constexpr (Elem<T>::per16 == 8) part += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
-      else part += (y[0] + y[1]) + (y[2] + y[3]);
+      for (int e = 0; e < Elem<T>::per16; ++e) x[e] = fast_exp2(sc.tail_exponent(z[e]));
+      some += x[0];
+      weighted = __builtin_fmaf(x[0], fmaxf(sc.tail_exponent(z[0]), -1000.f), weighted);      // (-inf: no NaN)
+      if constexpr (Elem<T>::per16 == 8) part += (double)(((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])));
+      else part += (double)((x[0] + x[1]) + (x[2] + x[3]));
       if (line.reached(r, T{}))
 #pragma unroll
-        for (int e = 0; e < Elem<T>::per16; ++e) note(x[e], token + e);
+        for (int e = 0; e < Elem<T>::per16; ++e) listed_too(z[e], token + e);
     });
-    tail = block_sum_double(part, s.waved) * (double)(1ull << kWeightBits);
+    const double weights = block_sum_double(part, s.waved);
+    const double of = block_sum_double((double)some, s.waved), exponents = block_sum_double((double)weighted, s.waved);
+    tail = fmax(sc.tail_sum(weights, of > 0.0 ? exponents / of : 0.0), 0.0) * (double)(1ull << kWeightBits);
   } else {
-    each_unit<T>(row, p.V, [&](uint32_t bits, int token) { note(sample_value(bits, T{}), token); }, [&](const uint4& r, int token) {
+    each_unit<T, kAtOnce, false>(row, p.V, [&](uint32_t bits, int token) { note(sample_value(bits, T{}), token); }, [&](const uint4& r, int token) {
       if (line.reached(r, T{})) {
         float x[Elem<T>::per16];
         unpack16(r, x, T{});
@@ -851,7 +979,8 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
 
   // C
   Drawn d{0, 0, false};
-  if (listed <= 64) {
+  if (flat) {
+  } else if (listed <= 64) {
     if (threadIdx.x < 64) {
       d = draw_from_list<true>(s, listed, sc, w, complete, tail, p.V);
       if (threadIdx.x == 0) { s.found_item = d.item; s.found_mass = d.kept; s.found_kind = d.settled; }
