@@ -609,22 +609,33 @@ class Runtime:
         off = np.ascontiguousarray(row_offsets, dtype=np.int64)
         if off.shape != (self.B + 1,):
             raise BcError("row_offsets must have B + 1 entries")
-        n = np.diff(off)
         rows, dev = q.shape[0], q.device
-        if n.min() < 0 or off[0] < 0 or off[-1] > rows:
+        first, end = int(off[0]), int(off[-1])
+        if self.B == 1:
+            least = most = end - first
+        else:
+            n = off[1:] - off[:-1]
+            least, most = int(n.min()), int(n.max())
+        if least < 0 or first < 0 or end > rows:
             raise BcError("row_offsets must not decrease and end within the %d rows" % rows)
-        for name, t, h in (("q", q, self.Hq), ("k", k, self.Hkv), ("v", v, self.Hkv)):
-            _is(t, name, self.elem_dtype, (rows, h, self.d), dev)
+        d, dtype = self.d, self.elem_dtype
+        _is(q, "q", dtype, (rows, self.Hq, d), dev)
+        _is(k, "k", dtype, (rows, self.Hkv, d), dev)
+        _is(v, "v", dtype, (rows, self.Hkv, d), dev)
         if a is not None:
             _is(a, "active", torch.uint8, (self.B,), dev)
         if out is None:
-            out = torch.empty(rows, self.Hq, self.d, dtype=torch.float32, device=dev)
+            out = torch.empty((rows, self.Hq, d), dtype=torch.float32, device=dev)
         else:
-            _is(out, "out", torch.float32, (rows, self.Hq, self.d), dev)
-        nbytes = int(bc_prompt_workspace_bytes(self.shape, int(n.max()), int(off[-1] - off[0]), self.max_cap))
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        _check(bc_prompt_step(self.shape, self.cache, _ptr(k), _ptr(v), _ptr(q), off.ctypes.data, _ptr(out), _ptr(a), _ptr(ws),
-                              nbytes, _stream_ptr()))
+            _is(out, "out", torch.float32, (rows, self.Hq, d), dev)
+        lib = _lib or load()
+        shape = C.byref(self.shape)
+        nbytes = lib.bc_prompt_workspace_bytes(shape, most, end - first, self.max_cap)
+        ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+        st = lib.bc_prompt_step(shape, C.byref(self.cache), k.data_ptr(), v.data_ptr(), q.data_ptr(), off.ctypes.data, out.data_ptr(), _ptr(a),
+                                ws.data_ptr(), nbytes, _stream_ptr())
+        if st != BC_OK:
+            _check(st)
         self._prompt_moved = True
         return out
 
@@ -809,18 +820,18 @@ def _is(t, name, dtype, shape, device):
 
 def _rope_rows(qkv, positions, inv_freq, Hq, Hkv, d, q_weight, k_weight):
     """Checks what both calls take; -> (shape, rows, row stride, rotated elements)."""
+    rows, width = qkv.shape if qkv.dim() == 2 else (0, 0)
+    if width != (Hq + 2 * Hkv) * d or (rows and qkv.stride(1) != 1) or not qkv.is_cuda:
+        raise BcError("qkv must be a device tensor [rows, (Hq + 2 * Hkv) * d] with elements of a row back to back")
     import torch
-    if qkv.dim() != 2 or qkv.shape[1] != (Hq + 2 * Hkv) * d or (qkv.numel() and qkv.stride(1) != 1):
-        raise BcError("qkv must be [rows, (Hq + 2 * Hkv) * d] with elements of a row back to back")
-    rows, dev = qkv.shape[0], qkv.device
-    if not qkv.is_cuda:
-        raise BcError("qkv must be a device tensor")
+    dev = qkv.device
     _is(positions, "positions", torch.int32, (rows,), dev)
     _is(inv_freq, "inv_freq", torch.float32, (inv_freq.numel(),), dev)
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _is(w, name, qkv.dtype, (d,), dev)
-    return bc_shape(1, Hq, Hkv, d, _logits_code(qkv), 1.0), rows, qkv.stride(0) if rows > 1 else qkv.shape[1], 2 * inv_freq.numel()
+    if q_weight is not None:
+        _is(q_weight, "q_weight", qkv.dtype, (d,), dev)
+    if k_weight is not None:
+        _is(k_weight, "k_weight", qkv.dtype, (d,), dev)
+    return bc_shape(1, Hq, Hkv, d, _logits_code(qkv), 1.0), rows, qkv.stride(0) if rows > 1 else width, 2 * inv_freq.numel()
 
 
 @_on_its_device
@@ -829,11 +840,16 @@ def qk_norm_rope(qkv, positions, inv_freq, Hq, Hkv, d, q_weight=None, k_weight=N
     inv_freq [rot / 2] fp32, weights [d] of qkv's dtype or None (no norm).  Returns (q [R, Hq, d], k, v [R, Hkv, d]), which the
     current stream works on."""
     import torch
-    load()
+    lib = _lib or load()
     shape, rows, stride, rot = _rope_rows(qkv, positions, inv_freq, Hq, Hkv, d, q_weight, k_weight)
-    q, k, v = (torch.empty(rows, h, d, dtype=qkv.dtype, device=qkv.device) for h in (Hq, Hkv, Hkv))
-    _check(bc_qk_norm_rope(shape, rows, _ptr(qkv), stride, _ptr(positions), _ptr(inv_freq), rot, _ptr(q_weight), _ptr(k_weight),
-                           float(eps), _ptr(q), _ptr(k), _ptr(v), _stream_ptr()))
+    dtype, dev = qkv.dtype, qkv.device
+    q = torch.empty((rows, Hq, d), dtype=dtype, device=dev)
+    k = torch.empty((rows, Hkv, d), dtype=dtype, device=dev)
+    v = torch.empty((rows, Hkv, d), dtype=dtype, device=dev)
+    st = lib.bc_qk_norm_rope(C.byref(shape), rows, qkv.data_ptr(), stride, positions.data_ptr(), inv_freq.data_ptr(), rot, _ptr(q_weight),
+                             _ptr(k_weight), eps, q.data_ptr(), k.data_ptr(), v.data_ptr(), _stream_ptr())
+    if st != BC_OK:
+        _check(st)
     _used_here(qkv, positions, inv_freq, q_weight, k_weight)
     return q, k, v
 

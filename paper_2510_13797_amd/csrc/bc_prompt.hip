@@ -133,7 +133,8 @@ struct Columns {
   }
   // One tile (K, then V behind it).  `next` asks for further tiles, behind the scores' products.  The order is written out as in
   // the prefill kernels: operands are asked for several instructions ahead.
-  template <bool MASKED, typename F>
+  // THIRD: what two parts of a weight leave (below 2^-17 of it) is a third one, half as many products again.
+  template <bool MASKED, bool THIRD, typename F>
   __device__ __forceinline__ void tile(const char* tile, int koff, int voff, uint32_t see, float qscale, const F& next) {
     float pe[16], psum;
     auto weights = [&](const f32x16_t& s) BC_INLINE {
@@ -188,11 +189,24 @@ struct Columns {
     for (int k = 0; k < 4 * NJ; ++k) {
       const int n = k / 2;
       O[n % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[n], y.operand(k & 1, n / NJ), O[n % NJ], 0, 0, 0);
-      if (k % 2 == 0 && n + NJ < 2 * NJ) c[n + NJ] = col_of(n + NJ);
+      if (!THIRD && k % 2 == 0 && n + NJ < 2 * NJ) c[n + NJ] = col_of(n + NJ);
+      if (THIRD && k % 2 == 0 && n < NJ) c[n + NJ] = col_of(n + NJ);
 #pragma unroll
       for (int g = 4; g < 8; ++g)
         if (k == (g - 4) * NJ / 2) y.split(g, pe[2 * g], pe[2 * g + 1]);
       step_fence();
+    }
+    if constexpr (THIRD) {
+      uint32_t rest[8];
+#pragma unroll
+      for (int g = 0; g < 8; ++g)
+        rest[g] = pack2_bf16(pe[2 * g] - __uint_as_float(y.h[g] << 16) - __uint_as_float(y.l[g] << 16),
+                             pe[2 * g + 1] - __uint_as_float(y.h[g] & 0xffff0000u) - __uint_as_float(y.l[g] & 0xffff0000u));
+#pragma unroll
+      for (int n = 0; n < 2 * NJ; ++n) {
+        const uint32_t* r = rest + 4 * (n / NJ);
+        O[n % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[n], __builtin_bit_cast(bf16x8_t, make_uint4(r[0], r[1], r[2], r[3])), O[n % NJ], 0, 0, 0);
+      }
     }
   }
 };
@@ -315,12 +329,12 @@ __global__ __launch_bounds__(kTileWaves * 64, 3) void prompt_attn_kernel(PromptP
   auto end_pass = [&]() BC_INLINE { stage = stage + 1 == kTileStages ? 0 : stage + 1; };
   for (const int dense = min(tiles.dense(), mine); t < dense; ++t) {
     begin_pass();
-    x.template tile<false>(lds + stage * (2 * TILE), koff, voff, ~0u, p.qscale, next);
+    x.template tile<false, false>(lds + stage * (2 * TILE), koff, voff, ~0u, p.qscale, next);
     end_pass();
   }
   for (; t < mine; ++t) {
     begin_pass();
-    x.template tile<true>(lds + stage * (2 * TILE), koff, voff, tiles.visible(t, i) >> (4 * half), p.qscale, next);
+    x.template tile<true, false>(lds + stage * (2 * TILE), koff, voff, tiles.visible(t, i) >> (4 * half), p.qscale, next);
     end_pass();
   }
   for (; t < wk.t1; ++t) {
@@ -401,9 +415,9 @@ __global__ __launch_bounds__(kTileWaves * 64, 1) void prompt_few_kernel(PromptPa
     const char* at = own + stage * (2 * TILE);
     auto nothing = [] {};
     if (t < tiles.dense())
-      x.template tile<false>(at, koff, voff, ~0u, p.qscale, nothing);
+      x.template tile<false, true>(at, koff, voff, ~0u, p.qscale, nothing);
     else
-      x.template tile<true>(at, koff, voff, tiles.visible(t, i) >> (4 * half), p.qscale, nothing);
+      x.template tile<true, true>(at, koff, voff, tiles.visible(t, i) >> (4 * half), p.qscale, nothing);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // the stage has been read
     if (t + 2 * kTileWaves < wk.t1) issue_tile(t + 2 * kTileWaves, stage);
     stage ^= 1;
