@@ -609,7 +609,10 @@ class Runtime:
         off = np.ascontiguousarray(row_offsets, dtype=np.int64)
         if off.shape != (self.B + 1,):
             raise BcError("row_offsets must have B + 1 entries")
-        rows, dev = q.shape[0], q.device
+        rows, dev = q.shape[0], self.k_slab.device
+        if dev.index != torch.cuda.current_device():           # the stream, and the workspace's, are that device's
+            with torch.cuda.device(dev):
+                return self.prompt_step(k, v, q, row_offsets, a, out)
         first, end = int(off[0]), int(off[-1])
         if self.B == 1:
             least = most = end - first
@@ -636,6 +639,7 @@ class Runtime:
                                 ws.data_ptr(), nbytes, _stream_ptr())
         if st != BC_OK:
             _check(st)
+        _used_here(k, v, q, a)
         self._prompt_moved = True
         return out
 
@@ -894,5 +898,5 @@ def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     logprob = torch.empty(B, dtype=f32, device=dev) if want_logprob else None
     _check(bc_sample_tokens(B, V, _ptr(logits), _logits_code(logits), logits.stride(0) if B > 1 else V, _ptr(temperature), _ptr(top_k),
                             _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(active), _ptr(tokens), _ptr(logprob), _stream_ptr()))
-    _used_here(logits, u, temperature, top_k, top_p, min_p, active)
+    _used_here(logits, u, temperature, top_k, top_p, min_p, active, tokens)
     return (tokens, logprob) if want_logprob else tokens

@@ -658,8 +658,8 @@ struct ValueSums {
     return At{s.found_kind, s.found_count, s.found_mass, s.found_weight};
   }
 };
-__device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row, int32_t V, float max, double temperature, Wish w) {
-  const Scale sc(max, temperature);
+__device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row, int32_t V, const Scale& sc, const Wish& w) {
+  const float max = sc.max;
   const int tid = threadIdx.x;
   Drawn d{0, 0, false};
   // the lowest logit that weighs anything, and the binades: down from the larger magnitude of it and the largest
@@ -820,7 +820,8 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
   return d;
 }
 
-// D for any logits.
+// D for any logits.  It and look_up() are functions of their own: inline, their registers cost the other ways (one row 12.8 -> 14.8 us) and each other (a
+// flat fp32 row 109 -> 129); a call saves a hundred registers a thread in memory, which is little beside their passes (and was a third of draw_from_values()).
 template <typename T>
 __device__ __noinline__ Drawn draw_from_steps(SampleLds& s, const char* row, int32_t V, float max, double temperature, Wish w) {
   const Scale sc(max, temperature);
@@ -834,22 +835,34 @@ __device__ __noinline__ Drawn draw_from_steps(SampleLds& s, const char* row, int
   });
   const Totals total = sum_steps(s);
   Drawn d{0, total.mass, true};
-  if (w.by_k && (uint32_t)w.k < total.count) d.kept = look_up<T>(s, row, V, max, temperature, total, Target{true, (uint32_t)w.k, 0}).mass;
-  if (w.by_p) d.kept = look_up<T>(s, row, V, max, temperature, total, Target{false, 0, cut_of(w.top_p, d.kept)}).mass;
-  if (w.by_m) {
-    // whole steps in front of the one the limit falls into, give or take one, and what of those three is above it
-    const double limit = -0.5 * w.log_min * sc.temperature * (double)sc.steps;
-    const int near = (int)fmin(fmax(limit, 0.0), (double)kSteps), from = near > 0 ? near - 1 : 0;
-    u64 m = 0;
-    each_logit<T>(row, V, [&](float z, int) {
-      const int step = sc.step(z);
-      if (step >= from && step <= near + 1 && step < kSteps && sc.above(z, w.log_min)) m += sc.weight(z);
-    });
-    m = block_sum(m, s.wave64) + (from < kSteps ? s.mass[from] : total.mass);
-    m = m < 1ull << kWeightBits ? 1ull << kWeightBits : m;
-    d.kept = m < d.kept ? m : d.kept;
+  // top-k's last token, top-p's, the draw: one after the other
+#pragma clang loop unroll(disable)
+  for (int stage = 0; stage < 3; ++stage) {
+    Target t{stage == 0, (uint32_t)w.k, 0};
+    if (stage == 0) {
+      if (!w.by_k || (uint32_t)w.k >= total.count) continue;
+    } else if (stage == 1) {
+      if (!w.by_p) continue;
+      t.mass = cut_of(w.top_p, d.kept);
+    } else {
+      if (w.by_m) {
+        // whole steps in front of the one the limit falls into, give or take one, and what of those three is above it
+        const double limit = -0.5 * w.log_min * sc.temperature * (double)sc.steps;
+        const int near = (int)fmin(fmax(limit, 0.0), (double)kSteps), from = near > 0 ? near - 1 : 0;
+        u64 m = 0;
+        each_logit<T>(row, V, [&](float z, int) {
+          const int step = sc.step(z);
+          if (step >= from && step <= near + 1 && step < kSteps && sc.above(z, w.log_min)) m += sc.weight(z);
+        });
+        m = block_sum(m, s.wave64) + (from < kSteps ? s.mass[from] : total.mass);
+        m = m < 1ull << kWeightBits ? 1ull << kWeightBits : m;
+        d.kept = m < d.kept ? m : d.kept;
+      }
+      t.mass = part_of(w.u, d.kept);
+    }
+    const Found f = look_up<T>(s, row, V, max, temperature, total, t);
+    if (stage < 2) d.kept = f.mass; else d.item = f.item;
   }
-  d.item = look_up<T>(s, row, V, max, temperature, total, Target{false, 0, part_of(w.u, d.kept)}).item;
   return d;
 }
 
@@ -991,7 +1004,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
     d = draw_from_list<false>(s, listed, sc, w, complete, tail, p.V);
   }
   if constexpr (std::is_same<T, bf16_t>::value)
-    if (!d.settled) d = draw_from_values(s, row, p.V, max, (double)t, w);
+    if (!d.settled) d = draw_from_values(s, row, p.V, sc, w);
   if (!d.settled) d = draw_from_steps<T>(s, row, p.V, max, (double)t, w);
   if (threadIdx.x == 0) {
     p.token[b] = (int32_t)(uint32_t)d.item;

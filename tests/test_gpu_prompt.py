@@ -122,6 +122,18 @@ def test_ragged_chunks_in_parts(dev):
             _check(dev, 4, 4, 64, lens, n, cap=cap, every=13)
 
 
+def test_rows_behind_the_last_sequence_are_left_as_they_were(dev):
+    import torch
+    for n in (3, 40):
+        rt = _runtime(dev, 4, 1, 64, [(20, 0, 0)], np.array([200]))
+        k, v, q = _rows(dev, rt, n + 9)
+        k[n:], v[n:], q[n:] = float("nan"), float("nan"), float("nan")
+        out = torch.full((n + 9, 4, 64), 7.0, device=dev)
+        rt.prompt_step(k, v, q, [0, n], out=out)
+        assert (out[n:] == 7).all() and torch.isfinite(out[:n]).all() and rt.P.item() == 20 + n
+        assert torch.isnan(rt.k_slab.view(200, 64)[20 + n:]).all() and torch.isfinite(rt.k_slab.view(200, 64)[:20 + n]).all()
+
+
 def test_rows_in_front_and_idle_sequences(dev):
     _check(dev, 8, 2, 128, [(40, 2, 1), (9, 0, 0), (60, 0, 3)], [20, 11, 30], active=np.array([1, 0, 1], np.uint8), first=5, every=2)
 
