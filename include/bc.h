@@ -400,8 +400,8 @@ int32_t bc_topk_kl_loss_bwd(int64_t T, int32_t V, int32_t k, const void *student
  *   out[i] = y[i] cos a_i - y[i+h] sin a_i,  out[i+h] = y[i+h] cos a_i + y[i] sin a_i  (i < h);  out[i] = y[i]  (i >= rot).
  * shape: Hq, Hkv, d and kv_dtype, the type of qkv, the weights and q, k, v (B and scale are not read); Hq + 2 Hkv <= 65536.
  * qkv: device [rows, Hq + 2 Hkv, d], rows qkv_row_stride elements apart (16 bytes' multiple); positions: device [rows] int32;
- * inv_freq: device [rot / 2] fp32, rot a multiple of 8 from 0 to d.  q [rows, Hq, d], k and v [rows, Hkv, d]: dense; v NULL: not
- * copied.  eps >= 0 and finite.  Arithmetic in fp32 (the angles' products in fp64), rounded once.  Rows of a decode step
+ * inv_freq: device [rot / 2] fp32, rot a multiple of 8 from 0 to d.  q [rows, Hq, d], k and v [rows, Hkv, d]: dense, apart from
+ * qkv; v NULL: not copied.  eps >= 0 and finite.  Arithmetic in fp32 (the angles' products in fp64), rounded once.  Rows of a decode step
  * (rows = B) and of a prefill are the same call.  Pointers 16-byte aligned (positions, inv_freq: 4). */
 int32_t bc_qk_norm_rope(const bc_shape *shape, int64_t rows, const void *qkv, int64_t qkv_row_stride,
                         const int32_t *positions, const float *inv_freq, int32_t rot, const void *q_weight,
@@ -428,7 +428,8 @@ int32_t bc_qk_norm_rope_bwd(const bc_shape *shape, int64_t rows, const void *qkv
  *   min_p[b] > 0: those of at least min_p[b] times the first one's weight.
  * tokens[b] is the first kept token up to and with which there is more than u[b] times the weight of all kept ones (u in [0, 1);
  * 1 and more: the last that weighs anything).  temperature[b] = 0 (or below 2^-126) takes the first token.  Weights are rounded to multiples of 2^-42
- * of the largest one, sums of them are exact.  logprob (nullable): natural log of the token's share of the kept weight.
+ * of the largest one, sums of them are exact.  logprob (nullable): natural log of the token's share of the kept weight,
+ * off by its rounding and less than 1e-7.
  * logits: device, rows of V <= 2^20 elements, row_stride elements apart, at any element, logits_dtype BC_BF16 or BC_F32;
  * -infinity is a token that is never drawn.  temperature, top_k (int32), top_p, min_p: device [B] fp32 or NULL (1, and no filter);
  * u: device [B] fp32.  A row with a NaN or +infinity, no finite logit, a temperature that is negative or not finite or a u that is

@@ -768,13 +768,13 @@ def prefill_attn_bwd(q, k, v, out, lse, dout, row_offsets, P, c, Hq, Hkv, d, sca
     return dq, dk, dv
 
 
-def _logits_code(t):
+def _logits_code(t, name="logits"):
     import torch
     if t.dtype == torch.bfloat16:
         return BC_BF16
     if t.dtype == torch.float32:
         return BC_F32
-    raise BcError("logits must be bf16 or fp32 device tensors")
+    raise BcError("%s must be bf16 or fp32 device tensors" % name)
 
 
 @_on_its_device
@@ -835,7 +835,7 @@ def _rope_rows(qkv, positions, inv_freq, Hq, Hkv, d, q_weight, k_weight):
         _is(q_weight, "q_weight", qkv.dtype, (d,), dev)
     if k_weight is not None:
         _is(k_weight, "k_weight", qkv.dtype, (d,), dev)
-    return bc_shape(1, Hq, Hkv, d, _logits_code(qkv), 1.0), rows, qkv.stride(0) if rows > 1 else width, 2 * inv_freq.numel()
+    return bc_shape(1, Hq, Hkv, d, _logits_code(qkv, "qkv"), 1.0), rows, qkv.stride(0) if rows > 1 else width, 2 * inv_freq.numel()
 
 
 @_on_its_device

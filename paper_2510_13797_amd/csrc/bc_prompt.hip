@@ -6,12 +6,15 @@
 // The query heads of a KV head see the same keys, so (row, head) pairs are the columns of the products: column i * g + h, with the
 // causal limit by i alone.  Tiles of 32 keys come from two places, first the slab's rows [0, L), then the new rows as the call got
 // them (the append need not be over), and go through LDS into 32x32x16 MFMA as in the prefill kernels: S^T = K.Q^T, O^T += V^T.P^T
-// with P in two bf16 parts (16 bits: what a decode step over the same rows gives), softmax online in registers.
+// with P in two bf16 parts (17 bits: what a decode step over the same rows gives; in fp32 sums) or three, softmax online in registers.
 //
 // Two kernels share a wave's work on a tile:
-//   many columns: a workgroup's four waves have 32 columns each and share the tiles (3-stage ring, a barrier a tile);
-//   32 columns or fewer: all four waves have the same columns and every fourth tile each, in a ring of their own without barriers,
-//   and are merged through LDS.
+//   many columns: a workgroup's four waves have 32 columns each and share the tiles (3-stage ring, a barrier a tile).  Bound by the matrix cores:
+//   4 x 2048 rows over 30,000, 32/8 heads, d = 128, 5.25 to 5.5 ms, 4.16 TFLOP of the definition (0.77 PFLOP/s), 6.25 of products issued (1.16; a library
+//   product of 16384^3 reaches 1.35).  Weights in three parts would leave 2.4e-7 of an output's error in place of 2.5e-6 (plain fp32: 1.6e-6) and take
+//   7.9 ms; 512 rows over 7680, 118 us and 163;
+//   32 columns or fewer: all four waves have the same columns and every fourth tile each, in a ring of their own without barriers, and are merged through
+//   LDS.  Bound by memory: 7 rows over 16,000, 65 MB, 17.5 us (3.7 TB/s) and 4 for the fold; there the third part costs nothing, and is taken.
 // Where that leaves compute units idle the keys are cut into parts, each of which leaves its sums in the workspace (plan_prompt()).
 // A second launch folds the parts in order, appends the rows to the slab and moves the tables: the first launch reads them.
 #include <vector>
@@ -390,8 +393,9 @@ __global__ __launch_bounds__(kTileWaves * 64, 1) void prompt_few_kernel(PromptPa
       const uint32_t vo = (uint32_t)(vl.row < ld.valid ? vl.row : 0) * ld.step + vl.in_row;
 #pragma unroll
       for (int n = 0; n < D / 64; ++n) {
-        issue_block<false>(ld.k + 128 * n, ko, own_at + stage * (2 * TILE) + n * 4096 + rg * 1024);
-        issue_block<false>(ld.v + 128 * n, vo, own_at + stage * (2 * TILE) + TILE + n * 4096 + rg * 1024);
+        // (read once: out of the way of the caches)
+        lds_dma16_s<true>(ko, (uint64_t)(ld.k + 128 * n), own_at + stage * (2 * TILE) + n * 4096 + rg * 1024);
+        lds_dma16_s<true>(vo, (uint64_t)(ld.v + 128 * n), own_at + stage * (2 * TILE) + TILE + n * 4096 + rg * 1024);
       }
     }
   };
@@ -473,8 +477,8 @@ __device__ __forceinline__ PartWeight part_weight(float2 ml) {
   return {f, 1.0f / sum};
 }
 
-// Many parts of few columns: four groups of threads share a column's parts, eight loads of each together (one column's parts one after the other
-// by 32 threads: 7 rows over 16,000, 32 parts, 26 us; 4 so).
+// Many parts of few columns: four groups of threads share a column's parts, eight loads of each together (one column's parts one after the other by
+// 32 threads: 7 rows over 16,000, 32 parts, 26 us; 4 so).
 template <int D>
 __device__ __forceinline__ void fold_many_parts(const PromptParams& p, int block) {
   constexpr int UNITS = D / 4, COLS = 256 / UNITS / kFoldGroups;

@@ -211,6 +211,24 @@ def test_pieces_give_what_the_whole_prompt_gives(dev):
     assert [list(y) for y in rt.tables()[:2]] == [list(y) for y in other.tables()[:2]] == [[2], [2]]
 
 
+def test_decode_steps_behind_a_chunk_in_a_uniform_layout(dev):
+    # equal prompts and capacities are told the library, which asks for prompt rows before the tables: chunks move the tables away from that
+    import torch
+    from paper_2510_13797_amd import bc
+    Hq, Hkv, d, n = 12, 2, 128, [30, 7]
+    rt = _runtime(dev, Hq, Hkv, d, [(40, 0, 0), (40, 0, 0)], np.array([200, 200]), c=4)
+    assert rt.cache.uniform_P == 40
+    k, v, q = _rows(dev, rt, sum(n))
+    rt.prompt_step(k, v, q, [0, n[0], sum(n)])
+    K, V = zip(*(rt.resident(s) for s in range(2)))
+    other = bc.Runtime(2, Hq, Hkv, d, "bf16", rt.shape.scale, [70, 47], [4, 4], [200, 200], dev)
+    other.cache_init(list(K), list(V))
+    for t in range(9):
+        x, b = _rows(dev, rt, 2, seed=50 + t), _rows(dev, rt, 2, seed=80 + t)
+        assert torch.equal(rt.decode_step(*x, *b[:2]).clone(), other.decode_step(*x, *b[:2]).clone()), t
+    assert rt.tables()[2] == other.tables()[2] == 0
+
+
 def test_captured_and_replayed(dev):
     import torch
     lens = [(100, 3, 2), (5, 0, 0)]

@@ -13,7 +13,7 @@ def shape(Hq=4, Hkv=2, d=64, dtype=bc.BC_BF16, B=1, scale=1.0):
     return bc.bc_shape(B, Hq, Hkv, d, dtype, scale)
 
 
-def _rope(s=None, rows=3, qkv=PTR, stride=512, pos=PTR, freq=PTR, rot=64, qw=PTR, kw=PTR, eps=1e-6, q=PTR, k=PTR, v=PTR):
+def _rope(s=None, rows=3, qkv=PTR - 4096, stride=512, pos=PTR, freq=PTR, rot=64, qw=PTR, kw=PTR, eps=1e-6, q=PTR, k=PTR, v=PTR):
     return bc.bc_qk_norm_rope(s or shape(), rows, qkv, stride, pos, freq, rot, qw, kw, eps, q, k, v, None)
 
 
@@ -39,10 +39,12 @@ def test_rope_refusals_of_both_directions(call):
 
 
 def test_rope_refusals_of_one_direction():
-    for kw in (dict(q=None), dict(k=None), dict(q=ODD), dict(k=ODD), dict(v=ODD)):
+    other = PTR + 4096
+    for kw in (dict(q=None), dict(k=None), dict(q=ODD), dict(k=ODD), dict(v=ODD), dict(qkv=other, q=other), dict(qkv=other, k=other),
+               dict(qkv=other, v=other)):
         assert _rope(**kw) == bc.BC_ERR_ARG, kw
     for kw in (dict(dq=None), dict(dk=None), dict(dqkv=None), dict(dq=ODD), dict(dk=ODD), dict(dv=ODD), dict(dqkv=ODD), dict(dstride=510),
-               dict(dstride=516), dict(qw=None), dict(kw=None)):
+               dict(dstride=516), dict(dstride=520), dict(qw=None), dict(kw=None)):
         assert _rope_bwd(**kw) == bc.BC_ERR_ARG, kw
     need = bc.bc_qk_norm_rope_bwd_workspace_bytes(shape())
     assert need > 0 and bc.bc_qk_norm_rope_bwd_workspace_bytes(shape(d=96)) == 0
