@@ -392,12 +392,17 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+_streams = {}                          # torch's objects of the streams that calls have run on
+
+
 def _used_here(*tensors):
     """The current stream uses these tensors, which the caller may free as soon as the call returns: memory that
     came from another stream is not given out again before this one is done with it.  (Behind a call that has asked for
     the stream.)"""
-    stream_id, device_index, device_type = _torch_c._cuda_getCurrentStream(_torch_c._cuda_getDevice())
-    stream = _torch_stream(stream_id=stream_id, device_index=device_index, device_type=device_type)
+    at = _torch_c._cuda_getCurrentStream(_torch_c._cuda_getDevice())
+    stream = _streams.get(at)
+    if stream is None:
+        stream = _streams[at] = _torch_stream(stream_id=at[0], device_index=at[1], device_type=at[2])
     for t in tensors:
         if t is None:
             continue

@@ -232,19 +232,31 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_bwd_kernel(RopePara
   }
 }
 
-// dw from the workgroups' sums, in a fixed order: 16 columns a workgroup, 16 slices of the workgroups.
+// dw from the workgroups' sums, in a fixed order: 16 columns a workgroup, 64 slices of the workgroups, whose sums a thread asks for all together
+// (16 slices, one load after the other: 22 us for 1024 workgroups, 3 so).
+constexpr int kRopeBwdMost = 1024;       // workgroups of the gradient, each with its sums of dw
 template <int D>
-__global__ void __launch_bounds__(256) rope_weight_sum_kernel(const float* partial, int n, float* dqw, float* dkw) {
-  __shared__ double part[16][17];
+__global__ void __launch_bounds__(1024) rope_weight_sum_kernel(const float* partial, int n, float* dqw, float* dkw) {
+  constexpr int SLICES = 64, EACH = kRopeBwdMost / SLICES;
+  __shared__ double part[SLICES][17];
   const int c = threadIdx.x & 15, slice = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+  float x[EACH];
+#pragma unroll
+  for (int k = 0; k < EACH; ++k) {
+    const int i = slice + k * SLICES;
+    x[k] = partial[(int64_t)(i < n ? i : 0) * 2 * D + col];
+  }
   double t = 0.0;
-  for (int i = slice; i < n; i += 16) t += partial[(int64_t)i * 2 * D + col];
+#pragma unroll
+  for (int k = 0; k < EACH; ++k) t += slice + k * SLICES < n ? (double)x[k] : 0.0;
   part[slice][c] = t;
-  __syncthreads();
+  for (int half = SLICES / 2; half >= 1; half >>= 1) {
+    __syncthreads();
+    if (slice < half) part[slice][c] += part[slice + half][c];
+  }
   if (slice == 0) {
-    for (int i = 1; i < 16; ++i) t += part[i][c];
     float* to = col < D ? dqw : dkw;
-    if (to) to[col & (D - 1)] = (float)t;
+    if (to) to[col & (D - 1)] = (float)part[0][c];
   }
 }
 
@@ -257,7 +269,6 @@ void deal_heads(RopeParams& p) {
   p.per_item = (int)(n < 1 ? 1 : n < p.heads ? n : p.heads);
   p.chunks = (p.heads + p.per_item - 1) / p.per_item;
 }
-constexpr int kRopeBwdMost = 1024;       // workgroups of the gradient, each with its sums of dw
 int64_t rope_groups(const RopeParams& p, int d) {
   const int64_t per = kRopeThreads / (d / 8);
   return (p.rows * p.chunks + per - 1) / per;
@@ -297,7 +308,7 @@ void launch_rope_bwd(const RopeParams& p, float* dqw, float* dkw, hipStream_t s)
   if (n == 0) {                            // (no rows: dw is zero)
   } else if (p.qw || p.kw) qk_norm_rope_bwd_kernel<T, D, true><<<n, kRopeThreads, 0, s>>>(p);
   else qk_norm_rope_bwd_kernel<T, D, false><<<n, kRopeThreads, 0, s>>>(p);
-  if (p.partial) rope_weight_sum_kernel<D><<<2 * D / 16, 256, 0, s>>>(p.partial, n, dqw, dkw);
+  if (p.partial) rope_weight_sum_kernel<D><<<2 * D / 16, 1024, 0, s>>>(p.partial, n, dqw, dkw);
 }
 
 }  // namespace

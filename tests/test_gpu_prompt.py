@@ -229,6 +229,28 @@ def test_decode_steps_behind_a_chunk_in_a_uniform_layout(dev):
     assert rt.tables()[2] == other.tables()[2] == 0
 
 
+def test_two_calls_at_once(dev):
+    # two batches of caches on two streams, each with a workspace of its own
+    import torch
+    for n in (3, 60):
+        lens = [(700, 0, 0), (30, 2, 1)]
+        rts = [_runtime(dev, 12, 2, 128, lens, np.array([1500, 1500]), seed=i) for i in range(2)]
+        k, v, q = _rows(dev, rts[0], 2 * n)
+        want = []
+        for rt in rts:
+            start = [t.clone() for t in (rt.P, rt.nb, rt.w)]
+            want.append(rt.prompt_step(k, v, q, [0, n, 2 * n]).clone())
+            for t, s in zip((rt.P, rt.nb, rt.w), start):
+                t.copy_(s)
+        torch.cuda.synchronize()
+        got = []
+        for rt in rts:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                got.append(rt.prompt_step(k, v, q, [0, n, 2 * n]))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_captured_and_replayed(dev):
     import torch
     lens = [(100, 3, 2), (5, 0, 0)]

@@ -141,6 +141,36 @@ def test_extreme_scales(dev):
     _check(dev, z, "f32", r.random(4), temperature=1e30, top_p=0.5)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_vocabulary(dev, dtype):
+    r = np.random.default_rng(12)
+    z = np.concatenate([_peaked(r, 2, 1 << 20), 2 * r.standard_normal((2, 1 << 20))])
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=60), dict(min_p=0.01)):
+        _check(dev, z, dtype, r.random(4), **kw)
+
+
+def test_two_calls_at_once_and_tensors_of_another_stream(dev):
+    import torch
+    from paper_2510_13797_amd import bc
+    g = torch.Generator(device=dev).manual_seed(8)
+    p = torch.full((40,), 0.95, device=dev)
+    want = []
+    for i in range(6):
+        z, u = (2 * torch.randn(40, 60000, generator=g, device=dev)).bfloat16(), torch.rand(40, generator=g, device=dev)
+        want.append((z, u, bc.sample_tokens(z, u, top_p=p)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for i, (z, u, _) in enumerate(want):
+        with torch.cuda.stream(streams[i % 2]):
+            copy = z.clone()                                   # freed, and its memory asked for again, while the call may not have begun
+            got.append(bc.sample_tokens(copy, u, top_p=p))
+            del copy
+            z.clone().zero_()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, (_, _, b) in zip(got, want))
+
+
 def test_idle_rows_and_given_tensors(dev):
     import torch
     from paper_2510_13797_amd import bc
