@@ -5,7 +5,7 @@
 //   o_i = y_i cos a_i - y_{i+h} sin a_i,  o_{i+h} = y_{i+h} cos a_i + y_i sin a_i  (i < h),  o_i = y_i  (i >= rot)
 //   gradient: dy = o's rotated back,  dw = sum dy x r,  dx = r (w dy - x r^2 mean(w dy x))
 //
-// Bound by memory: every element in and out once.  139,008 rows of 12/2 heads, d = 128, bf16: 1.14 GB in 222 us, the gradient's 2.21 GB in 465 (5.1 and 4.75 TB/s; a copy of
+// Bound by memory: every element in and out once.  139,008 rows of 12/2 heads, d = 128, bf16: 1.14 GB in 203 us, the gradient's 2.21 GB in 420 (5.6 and 5.3 TB/s; torch's copy of
 // 2 GiB reaches 4.9); a token of 32/8 heads 3 us beside the call's 13.  d / 8 lanes work on a head, eight elements a lane, in two pieces of four that
 // are each other's partners in the rotation: both halves of a pair are in one lane, and an instruction still asks for whole
 // 128-byte lines.  A lane's four angles serve all heads of its row that are its item.  All arithmetic in fp32, rounded once
@@ -40,22 +40,37 @@ struct RopeParams {
   float eps;
 };
 
-// four elements <-> floats
+// four elements <-> floats.  STREAM: past the caches (rope_streams())
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load_from(const char* at) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const V*>(at));
+  else return *reinterpret_cast<const V*>(at);
+}
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store_to(char* at, const V& x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<V*>(at));
+  else *reinterpret_cast<V*>(at) = x;
+}
+template <bool STREAM = false>
 __device__ __forceinline__ void load4(const char* at, float (&x)[4], float) {
-  const f32x4_t r = *reinterpret_cast<const f32x4_t*>(at);
+  const f32x4_t r = load_from<STREAM, f32x4_t>(at);
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] = r[e];
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void load4(const char* at, float (&x)[4], bf16_t) {
-  const uint2 r = *reinterpret_cast<const uint2*>(at);
+  const u32x2_t r = load_from<STREAM, u32x2_t>(at);
   x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
   x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xffff0000u);
 }
+template <bool STREAM>
 __device__ __forceinline__ void store4(char* at, const float (&x)[4], float) {
-  *reinterpret_cast<f32x4_t*>(at) = f32x4_t{x[0], x[1], x[2], x[3]};
+  store_to<STREAM>(at, f32x4_t{x[0], x[1], x[2], x[3]});
 }
+template <bool STREAM>
 __device__ __forceinline__ void store4(char* at, const float (&x)[4], bf16_t) {
-  *reinterpret_cast<uint2*>(at) = make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]));
+  store_to<STREAM>(at, u32x2_t{pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3])});
 }
 
 // cos and sin of position * inv_freq.  The product and its remainder of quarter turns in 64 bits: a position of a million times a
@@ -102,7 +117,7 @@ struct RopeLane {
   }
 };
 
-template <typename T, int D, bool NORM, int U>
+template <typename T, int D, bool NORM, bool STREAM, int U>
 __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(RopeParams p) {
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES;
   const int lane = threadIdx.x % LPH;
@@ -121,8 +136,8 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(RopeParams p
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int h = min(h0 + u, last - 1);
-      load4(in + (int64_t)h * HEAD + ln.o1 * ES, x[u][0], T{});
-      load4(in + (int64_t)h * HEAD + ln.o2 * ES, x[u][1], T{});
+      load4<STREAM>(in + (int64_t)h * HEAD + ln.o1 * ES, x[u][0], T{});
+      load4<STREAM>(in + (int64_t)h * HEAD + ln.o2 * ES, x[u][1], T{});
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -144,13 +159,13 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(RopeParams p
         }
         ln.template turn<false>(x[u][0], x[u][1]);
       }
-      store4(out + ln.o1 * ES, x[u][0], T{});
-      store4(out + ln.o2 * ES, x[u][1], T{});
+      store4<STREAM>(out + ln.o1 * ES, x[u][0], T{});
+      store4<STREAM>(out + ln.o2 * ES, x[u][1], T{});
     }
   }
 }
 
-template <typename T, int D, bool NORM>
+template <typename T, int D, bool NORM, bool STREAM>
 __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_bwd_kernel(RopeParams p) {
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES, GROUPS = kRopeThreads / LPH;
   __shared__ float sums[NORM ? GROUPS : 1][NORM ? D : 1];
@@ -173,12 +188,12 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_bwd_kernel(RopePara
       const float* g = isq ? p.dq + (row * p.Hq + h) * D
                            : h < p.Hq + p.Hkv ? p.dk + (row * p.Hkv + h - p.Hq) * D : p.dv + (row * p.Hkv + h - p.Hq - p.Hkv) * D;
       float dy[2][4], x[2][4];
-      load4(reinterpret_cast<const char*>(g + o1), dy[0], 0.f);
-      load4(reinterpret_cast<const char*>(g + o2), dy[1], 0.f);
+      load4<STREAM>(reinterpret_cast<const char*>(g + o1), dy[0], 0.f);
+      load4<STREAM>(reinterpret_cast<const char*>(g + o2), dy[1], 0.f);
       if (norm) {
         const char* in = p.qkv + row * p.row_bytes + (int64_t)h * HEAD;
-        load4(in + o1 * ES, x[0], T{});
-        load4(in + o2 * ES, x[1], T{});
+        load4<STREAM>(in + o1 * ES, x[0], T{});
+        load4<STREAM>(in + o2 * ES, x[1], T{});
       }
       if (h < p.Hq + p.Hkv) ln.template turn<true>(dy[0], dy[1]);
       if (norm) {
@@ -204,8 +219,8 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_bwd_kernel(RopePara
           }
       }
       char* out = p.dqkv + row * p.drow_bytes + (int64_t)h * HEAD;
-      store4(out + o1 * ES, dy[0], T{});
-      store4(out + o2 * ES, dy[1], T{});
+      store4<STREAM>(out + o1 * ES, dy[0], T{});
+      store4<STREAM>(out + o2 * ES, dy[1], T{});
     }
   }
   if constexpr (NORM) {
@@ -295,20 +310,34 @@ void fill_rope(RopeParams& p, const bc_shape* sh, int64_t rows, const void* qkv,
   p.rows = rows; p.Hq = sh->Hq; p.Hkv = sh->Hkv; p.half = rot / 2; p.eps = eps;
 }
 
-template <typename T, int D>
+// Packed rows beyond the 256 MB of the Infinity Cache go past it, in and out: 139,008 rows of 12/2 heads, d = 128, forward and gradients 678 -> 633 us.  Smaller ones
+// leave their results there for the attention that reads them next: forward and attention of 24,000 rows 113 us, streamed 133 (139,008: 772 and 766).
+bool rope_streams(const RopeParams& p, int d, int es) { return p.rows * (p.Hq + 2 * (int64_t)p.Hkv) * d * es > (256LL << 20); }
+
+template <typename T, int D, bool STREAM>
 void launch_rope(const RopeParams& p, hipStream_t s) {
   const dim3 grid((unsigned)rope_groups(p, D));
-  if (p.qw || p.kw) qk_norm_rope_kernel<T, D, true, 4><<<grid, kRopeThreads, 0, s>>>(p);
-  else qk_norm_rope_kernel<T, D, false, 4><<<grid, kRopeThreads, 0, s>>>(p);
+  if (p.qw || p.kw) qk_norm_rope_kernel<T, D, true, STREAM, 4><<<grid, kRopeThreads, 0, s>>>(p);
+  else qk_norm_rope_kernel<T, D, false, STREAM, 4><<<grid, kRopeThreads, 0, s>>>(p);
 }
 template <typename T, int D>
+void launch_rope(const RopeParams& p, hipStream_t s) {
+  if (rope_streams(p, D, Elem<T>::size)) launch_rope<T, D, true>(p, s);
+  else launch_rope<T, D, false>(p, s);
+}
+template <typename T, int D, bool STREAM>
 void launch_rope_bwd(const RopeParams& p, float* dqw, float* dkw, hipStream_t s) {
   const int64_t want = rope_groups(p, D);
   const int n = (int)(want < kRopeBwdMost ? want : kRopeBwdMost);
   if (n == 0) {                            // (no rows: dw is zero)
-  } else if (p.qw || p.kw) qk_norm_rope_bwd_kernel<T, D, true><<<n, kRopeThreads, 0, s>>>(p);
-  else qk_norm_rope_bwd_kernel<T, D, false><<<n, kRopeThreads, 0, s>>>(p);
+  } else if (p.qw || p.kw) qk_norm_rope_bwd_kernel<T, D, true, STREAM><<<n, kRopeThreads, 0, s>>>(p);
+  else qk_norm_rope_bwd_kernel<T, D, false, STREAM><<<n, kRopeThreads, 0, s>>>(p);
   if (p.partial) rope_weight_sum_kernel<D><<<2 * D / 16, 1024, 0, s>>>(p.partial, n, dqw, dkw);
+}
+template <typename T, int D>
+void launch_rope_bwd(const RopeParams& p, float* dqw, float* dkw, hipStream_t s) {
+  if (rope_streams(p, D, Elem<T>::size)) launch_rope_bwd<T, D, true>(p, dqw, dkw, s);
+  else launch_rope_bwd<T, D, false>(p, dqw, dkw, s);
 }
 
 }  // namespace

@@ -110,6 +110,32 @@ def test_whole_rows_as_items(dev):
     _check(dev, 33000, 4, 1, 64, "bf16", 64)
 
 
+@pytest.mark.parametrize("dtype,R", [("bf16", 360000), ("f32", 180000)])
+def test_rows_beyond_the_caches_are_those_of_smaller_calls(dev, dtype, R):
+    # more than 256 MB of packed rows: the same arithmetic, past the caches
+    import torch
+    from paper_2510_13797_amd import bc
+    Hq, Hkv, d = 4, 1, 64
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device=dev).manual_seed(3)
+    qkv = torch.randn(R, 384, generator=g, device=dev).to(tdt)
+    pos = torch.randint(0, 9000, (R,), generator=g, device=dev, dtype=torch.int32)
+    freq = torch.tensor([1e4 ** (-i / 24.0) for i in range(24)], device=dev)
+    w = [(1 + 0.2 * torch.randn(d, generator=g, device=dev)).to(tdt) for _ in range(2)]
+    grads = [torch.randn(R, h, d, generator=g, device=dev) for h in (Hq, Hkv, Hkv)]
+    whole = bc.qk_norm_rope(qkv, pos, freq, Hq, Hkv, d, *w) + bc.qk_norm_rope_bwd(qkv, *grads, pos, freq, Hq, Hkv, d, *w)
+    dw = [torch.zeros(d, dtype=torch.float64, device=dev) for _ in range(2)]
+    for lo in range(0, R, 90001):
+        rows = slice(lo, min(lo + 90001, R))
+        part = bc.qk_norm_rope(qkv[rows], pos[rows], freq, Hq, Hkv, d, *w)
+        part += bc.qk_norm_rope_bwd(qkv[rows], *(x[rows] for x in grads), pos[rows], freq, Hq, Hkv, d, *w)
+        assert all(torch.equal(a[rows], b) for a, b in zip(whole[:4], part))
+        dw = [a + b.double() for a, b in zip(dw, part[4:])]
+    for a, b in zip(whole[4:], dw):
+        # sums of up to 1.4 million terms of a magnitude near one, by lanes of some hundred each: (100 + 60) * 2^-24 of the sum of magnitudes, both
+        assert (a.double() - b).abs().max() <= 2 * 160 * 2.0 ** -24 * 1.5 * R * Hq
+
+
 def test_small_and_large_values(dev):
     _check(dev, 20, 4, 1, 128, "f32", 128, scale=1e-12)          # the mean square far below eps
     _check(dev, 20, 4, 1, 128, "f32", 128, scale=1e-6, eps=0.0)
