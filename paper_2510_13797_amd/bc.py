@@ -435,7 +435,7 @@ def _on_its_device(call):
 class Runtime:
     """Owns slabs, tables and workspace of one batch of caches; calls the C ABI."""
 
-    _prompt_moved = False         # whether P on the device has left P_host behind
+    _prompt_moved = False         # P on the device may have left P_host behind (a captured call moves it with every replay)
 
     def __init__(self, B, Hq, Hkv, d, dtype, scale, P, c, cap, device):
         import torch
@@ -636,6 +636,7 @@ class Runtime:
             out = torch.empty((rows, self.Hq, d), dtype=torch.float32, device=dev)
         else:
             _is(out, "out", torch.float32, (rows, self.Hq, d), dev)
+            _used_here(out)
         lib = _lib or load()
         shape = C.byref(self.shape)
         nbytes = lib.bc_prompt_workspace_bytes(shape, most, end - first, self.max_cap)
@@ -683,7 +684,7 @@ class Runtime:
             nbs, ws, _ = self.tables()
             nb, w = int(nbs[s]), int(ws[s])
         if self._prompt_moved:
-            self.P_host, self._prompt_moved = self.P.cpu().numpy().astype(np.int32), False
+            self.P_host = self.P.cpu().numpy().astype(np.int32)
         L = int(self.P_host[s]) + nb + w
         cap = int(self.cap_host[s])
         E = self.Hkv * self.d

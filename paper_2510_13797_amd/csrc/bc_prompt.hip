@@ -663,14 +663,17 @@ void launch_finish(const PromptParams& p, const PromptPlan& pl, int64_t total, h
   prompt_finish_kernel<D, PARTS><<<(unsigned)(p.table_blocks + (int64_t)p.copy_blocks * p.B + fold), 256, 0, s>>>(p);
 }
 template <int D>
-void launch_prompt(const PromptParams& p, const PromptPlan& pl, int64_t total, hipStream_t s) {
+int32_t launch_prompt(const PromptParams& p, const PromptPlan& pl, int64_t total, hipStream_t s) {
   const dim3 grid(p.pstride * p.parts, pl.blocks);
   if (pl.few) prompt_few_kernel<D><<<grid, kTileWaves * 64, 0, s>>>(p);
   else prompt_attn_kernel<D><<<grid, kTileWaves * 64, 0, s>>>(p);
+  const int32_t st = launch_status();       // (the second launch goes by what the first one leaves)
+  if (st != BC_OK) return st;
   if (p.parts <= 2) launch_finish<D, 2>(p, pl, total, s);
   else if (p.parts <= 4) launch_finish<D, 4>(p, pl, total, s);
   else if (p.parts <= 8) launch_finish<D, 8>(p, pl, total, s);
   else launch_finish<D, 0>(p, pl, total, s);
+  return launch_status();
 }
 
 }  // namespace
@@ -702,7 +705,9 @@ extern "C" int32_t bc_prompt_step(const bc_shape* shape, const bc_cache* cache, 
   const int64_t total = row_offsets[shape->B] - row_offsets[0];
   if (total == 0) return BC_OK;
   if (!k || !v || !q || !out || !aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(out)) return BC_ERR_ARG;
-  if (max_new * shape->Hq >= (1LL << 31) || total >= (1LL << 31) || (int64_t)shape->B * shape->Hkv > (1 << 24)) return BC_ERR_SHAPE;
+  // (offsets inside a tile of 32 rows are of 32 bits, and so are the threads of a grid's row)
+  if (shape->Hq > 65536 || (int64_t)shape->B * shape->Hkv > (1 << 23)) return BC_ERR_SHAPE;
+  if (max_new * shape->Hq >= (1LL << 31) || total >= (1LL << 31)) return BC_ERR_SHAPE;
   const PromptPlan pl = plan_prompt(shape, max_new, total, cache->max_cap);
   if (pl.blocks > 65535) return BC_ERR_SHAPE;
   if (!workspace || !aligned16(workspace) || workspace_bytes < pl.bytes) return BC_ERR_WORKSPACE;
@@ -749,7 +754,5 @@ extern "C" int32_t bc_prompt_step(const bc_shape* shape, const bc_cache* cache, 
   p.copy_blocks = (int32_t)(copies < share ? copies : share);
   p.qscale = shape->scale * kLog2e;
   hipStream_t s = as_stream(stream);
-  if (shape->d == 128) launch_prompt<128>(p, pl, total, s);
-  else launch_prompt<64>(p, pl, total, s);
-  return launch_status();
+  return shape->d == 128 ? launch_prompt<128>(p, pl, total, s) : launch_prompt<64>(p, pl, total, s);
 }

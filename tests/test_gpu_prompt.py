@@ -278,3 +278,24 @@ def test_captured_and_replayed(dev):
                 rt.decode_attn(q[:2])                          # eager work between replays
                 st.synchronize()
             assert rt.tables()[2] == 0
+
+
+def test_resident_rows_behind_replays(dev):
+    # every replay of a captured call appends its rows; `out` on another stream than its own
+    import torch
+    rt = _runtime(dev, 12, 2, 128, [(100, 0, 0)], np.array([400]))
+    k, v, q = _rows(dev, rt, 5)
+    out = torch.zeros(5, 12, 128, dtype=torch.float32, device=dev)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            rt.prompt_step(k, v, q, [0, 5], out=out)
+        for n in (1, 2, 3):
+            graph.replay()
+            st.synchronize()
+            K, V = rt.resident(0)
+            assert K.shape[0] == 100 + 5 * n
+            assert np.array_equal(K[-5:], k.float().cpu().numpy()) and np.array_equal(V[-5:], v.float().cpu().numpy())
+    assert rt.tables()[2] == 0

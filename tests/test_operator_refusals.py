@@ -96,6 +96,15 @@ def test_prompt_refusals():
     assert bc.bc_prompt_workspace_bytes(shape(), 5, 8, 0) == 0
 
 
+def test_prompt_refuses_what_grids_and_32_bit_offsets_do_not_hold():
+    # (2^23 + 1 sequences; rows of 131,072 heads, 32 of which pass 32 bits at 2^19)
+    off = np.ones((1 << 23) + 2, np.int64)
+    off[0] = 0
+    assert _prompt(s=shape(B=(1 << 23) + 1, Hq=1, Hkv=1), off=off) == bc.BC_ERR_SHAPE
+    for B in (2, 1 << 21):
+        assert _prompt(s=shape(B=B, Hq=1 << 17, Hkv=1 << 14), off=np.arange(B + 1)) == bc.BC_ERR_SHAPE
+
+
 def _sample(B=2, V=100, z=PTR, dtype=bc.BC_BF16, stride=100, t=None, k=None, p=None, m=None, u=PTR, active=None, tokens=PTR, logprob=None):
     return bc.bc_sample_tokens(B, V, z, dtype, stride, t, k, p, m, u, active, tokens, logprob, None)
 
