@@ -4,17 +4,18 @@
 // filters keep are first parts of that order, and the draw takes the first token at which the sum of the weights so far exceeds u
 // times the sum of all that is kept.  Sums have to be right to the last token: a row may hold 150,000 tokens of like weight, and
 // an error of 1e-7 of the sum would draw another one now and then.  Weights are therefore whole multiples of 2^-42 of the largest one
-// (from a series in 64 bits, weight_of()), and every sum is one of integers: exact, and the same in any order, atomics
+// (from a series in 64 bits, Scale::weight()), and every sum is one of integers: exact, and the same in any order, atomics
 // included.  A token below 2^-43 of the largest weight weighs nothing.
 //
 // A workgroup of 1024 threads has a row:
 //   A  the maximum; of the threads' own maxima the k-th largest (without top-k the 200th) gives a line above which all tokens
 //      that matter usually lie, and not many more than that;
 //   B  a second pass lists the tokens above the line (in LDS, 1024 at most).  Where the sum of all weights is asked for, it adds up those below
-//      the line in 32 bits, with a bound on how far off that is (tail_weight());
+//      the line in 32 bits, with a bound on how far off that is (Scale::tail_sum());
 //   C  the list is sorted and its sums formed: counts, masses and the draw are looked up, at both ends of the bound where there is one.
 // Rows that this does not settle (nearly flat ones, where hundreds of tokens are kept, many equal ones, a border inside the bound) go by
-//   D  sums of whole rows.  bf16 logits have few values: their counts are taken in LDS, and a value weighs its count times its weight.  fp32 logits go by a
+//   D  sums of whole rows.  bf16 logits have few values: their counts are taken in LDS, and a value weighs its count times its weight (151,936 equal logits
+//      129 us, zeros 80; zeros by the fp32 way 377).  fp32 logits go by a
 //      histogram of counts and masses over 2048 equal steps of (max - z) / temperature; where a count or mass falls, the step's
 //      tokens are listed and sorted as in C, after further histograms of it where there are too many.
 //
@@ -35,6 +36,7 @@ constexpr float kSpan = 43.5f;             // base-2 exponents a histogram cover
 constexpr int kUsualLine = 200;            // thread maxima above the line without top-k: some 220 tokens
 constexpr int kValues = 4096;              // bf16 values counted: 16 binades of either sign,
 constexpr int kCopies = 2;                 // odd and even lanes apart, so that fewer meet at a count
+constexpr int kZeros = kValues + 1;         // (a place in name alone)
 constexpr int kNowhere = 64;               // counts for logits of no place, a lane's own each
 
 struct SampleParams {
@@ -629,15 +631,18 @@ __device__ __forceinline__ Drawn draw_from_list(SampleLds& s, int listed, const 
 }
 
 // D for bf16 logits.  Values of 16 binades of either sign stand in falling order at 4096 places; those nearer to zero, which come between the signs, in
-// a list.  Not settled: too many of those, or of equal ones where the draw falls.
+// a list, and zeros, between its signs, as a count.  Not settled: too many in the list.
 struct ValueSums {
   SampleLds& s;
   uint32_t c[4];               // this thread's four places
   u64 w[4];
-  uint32_t before_count, near_count, all_count;
+  uint32_t before_count, near_count, all_count;        // near: list and zeros
   u64 before_mass, near_mass, all_mass, half_mass;
   uint32_t half_count;
-  // place, its first token's count and mass, and what each of its tokens weighs, for every thread; place kValues: the list near zero
+  uint32_t zeros, over_count;  // over: of the list, above zero
+  u64 zero_weight, over_mass;
+  // place, its first token's count and mass, and what each of its tokens weighs, for every thread; kValues: the list near zero (zeros in front of what is below
+  // them), kZeros
   struct At { uint32_t place, before_count; u64 before_mass, weight; };
   __device__ __forceinline__ At find(const Target& t) {
     __syncthreads();
@@ -650,9 +655,20 @@ struct ValueSums {
       cc += c[e];
       m += c[e] * w[e];
     }
-    if (threadIdx.x == 0 && (t.by_count ? half_count < t.count && t.count <= half_count + near_count
-                                        : half_mass <= t.mass && t.mass < half_mass + near_mass)) {
-      s.found_kind = kValues; s.found_count = half_count; s.found_mass = half_mass; s.found_weight = 0;
+    if (threadIdx.x == 0) {
+      const auto within = [&](uint32_t c0, uint32_t c1, u64 m0, u64 m1) {
+        return t.by_count ? c0 < t.count && t.count <= c1 : m0 <= t.mass && t.mass < m1;
+      };
+      const u64 zero_mass = zeros * zero_weight;
+      if (within(half_count, half_count + near_count, half_mass, half_mass + near_mass)) {
+        const uint32_t c0 = half_count + over_count;
+        const u64 m0 = half_mass + over_mass;
+        const bool zero = within(c0, c0 + zeros, m0, m0 + zero_mass), over = within(half_count, c0, half_mass, m0);
+        s.found_kind = zero ? kZeros : kValues;
+        s.found_count = zero ? c0 : half_count + (over ? 0 : zeros);
+        s.found_mass = zero ? m0 : half_mass + (over ? 0 : zero_mass);
+        s.found_weight = zero ? zero_weight : 0;
+      }
     }
     __syncthreads();
     return At{s.found_kind, s.found_count, s.found_mass, s.found_weight};
@@ -667,7 +683,7 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
   const uint32_t top = __float_as_uint(fmaxf(fabsf(max), fabsf(lowest))) >> 23, a0 = top > 15 ? (top - 15) << 7 : 1;        // (zeros are equal whatever their sign: never a place of their own)
   __syncthreads();
   for (int i = tid; i < (kValues + kNowhere) * kCopies; i += kSampleThreads) s.value_count[i] = 0;
-  if (tid == 0) s.n = 0;
+  if (tid == 0) s.n = s.found_count = 0;
   __syncthreads();
   // place of a value, less than kValues for one of the binades and only for those: magnitude less a0, turned for a positive one, then the lane's count there as
   // bytes (two values at a time).  Places below the lowest logit are counted, and weigh nothing.
@@ -684,10 +700,13 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
   };
   char* const counts = reinterpret_cast<char*>(s.value_count);
   const auto count = [&](uint32_t at) { atomicAdd(reinterpret_cast<uint32_t*>(counts + at), 1u); };
+  uint32_t zero = 0;
   const auto near_zero = [&](uint32_t h, int token) {
     if ((h & 0x7fffu) < a0) {
       const float z = __uint_as_float(h << 16);
-      if (z >= lowest) {
+      if (z == 0.f) {
+        ++zero;
+      } else if (z >= lowest) {
         const uint32_t n = atomicAdd(&s.n, 1u);
         if (n < kListed) s.list[n] = item_of(z, token);
       }
@@ -713,8 +732,10 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
         near_zero(x[e] >> 16, token + 2 * e + 1);
       }
   });
+  if (zero != 0) atomicAdd(&s.found_count, zero);
   __syncthreads();
   const int listed = (int)s.n;
+  const uint32_t zeros = lowest <= 0.f ? s.found_count : 0;
   if (listed > kListed) return d;
   const Sorted<false> near(s, listed, sc);
   const auto value_at = [&](int place) {
@@ -735,8 +756,12 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
     m += x.c[e] * x.w[e];
     if (w.by_m && x.c[e] && sc.above(value_at(place), w.log_min)) above += x.c[e] * x.w[e];
   }
-  x.near_count = (uint32_t)listed;
-  x.near_mass = near.all;
+  x.zeros = zeros;
+  x.zero_weight = x.zeros ? sc.weight(0.f) : 0;
+  x.over_count = x.zeros ? (uint32_t)near.how_many(tid < listed && logit_of(near.item) > 0.f) : (uint32_t)listed;
+  x.over_mass = !x.zeros ? near.all : x.over_count ? near.mass_at((int)x.over_count - 1) : 0;
+  x.near_count = (uint32_t)listed + x.zeros;
+  x.near_mass = near.all + x.zeros * x.zero_weight;
   const uint32_t upto_count = block_scan(cc, s.wave32);
   x.half_count = 0; x.all_count = x.near_count;
 #pragma unroll
@@ -770,6 +795,7 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
   if (w.by_p) d.kept = mass_at(Target{false, 0, cut_of(w.top_p, d.kept)});
   if (w.by_m) {
     if (tid < listed && sc.above(logit_of(near.item), w.log_min)) above += near.weight;
+    if (tid == 0 && x.zeros && sc.above(0.f, w.log_min)) above += x.zeros * x.zero_weight;
     u64 least = block_sum(above, s.wave64);
     least = least < 1ull << kWeightBits ? 1ull << kWeightBits : least;
     d.kept = least < d.kept ? least : d.kept;
@@ -783,37 +809,66 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
     return d;
   }
   // which of the equal ones: by id
-  uint32_t equal = 0;
+  const bool is_zero = at.place == kZeros;
+  uint32_t equal = is_zero ? x.zeros : 0;
+  if (!is_zero)
 #pragma unroll
-  for (int n = 0; n < kCopies; ++n) equal += s.value_count[at.place * kCopies + n];
-  const uint32_t h = __float_as_uint(value_at((int)at.place)) >> 16;
-  if (equal > kListed) return d;
+    for (int n = 0; n < kCopies; ++n) equal += s.value_count[at.place * kCopies + n];
+  const uint32_t h = is_zero ? 0u : __float_as_uint(value_at((int)at.place)) >> 16, both = h * 0x10001u;
+  const uint32_t bits_of = is_zero ? 0x7fff7fffu : ~0u;        // (a zero's sign does not count)
+  uint32_t rank = (uint32_t)quotient(mass - at.before_mass, at.weight);
+  // f(a token, or the first of a unit that has some; how many; the unit) of those
+  const auto each_equal = [&](const auto& single, const auto& some) {
+    each_unit<bf16_t, kAtOnce, false>(row, V, [&](uint32_t bits, int token) {
+      if ((bits & bits_of) == h) single(token);
+    }, [&](const uint4& r, int token) {
+      const uint32_t x[4] = {r.x & bits_of, r.y & bits_of, r.z & bits_of, r.w & bits_of};
+      // (a half that is equal is zero: the smaller ones of two and two)
+      const auto diff = [&](int e) { return __builtin_bit_cast(upair16_t, x[e] ^ both); };
+      const upair16_t least = __builtin_elementwise_min(__builtin_elementwise_min(diff(0), diff(1)), __builtin_elementwise_min(diff(2), diff(3)));
+      if (least.x == 0 || least.y == 0) some(x, token);
+    });
+  };
   __syncthreads();
+  int stretch = -1;
+  if (equal > kListed) {       // too many for the list: those of the 512 tokens among which it is (a unit goes by its first)
+    for (int i = tid; i < kSteps; i += kSampleThreads) s.count[i] = 0;
+    __syncthreads();
+    each_equal([&](int token) { atomicAdd(&s.count[token >> 9], 1u); }, [&](const uint32_t (&x)[4], int token) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) n += ((x[e] & 0xffffu) == h) + (x[e] >> 16 == h);
+      atomicAdd(&s.count[token >> 9], n);
+    });
+    __syncthreads();
+    const uint32_t c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1], upto = block_scan(c0 + c1, s.wave32), before = upto - c0 - c1;
+    if (before <= rank && rank < upto) {
+      const bool second = rank >= before + c0;
+      s.found_kind = 2 * tid + (second ? 1 : 0);
+      s.found_count = before + (second ? c0 : 0);
+    }
+    __syncthreads();
+    stretch = (int)s.found_kind;
+    rank -= s.found_count;
+  }
   if (tid == 0) s.n = 0;
   __syncthreads();
-  const auto note = [&](uint32_t bits, int token) {
-    if (bits == h) {
-      const uint32_t n = atomicAdd(&s.n, 1u);
-      if (n < kListed) s.list[n] = item_of(__uint_as_float(h << 16), token);
-    }
+  const auto note = [&](int token) {
+    const uint32_t n = atomicAdd(&s.n, 1u);
+    if (n < kListed) s.list[n] = item_of(__uint_as_float(h << 16), token);
   };
-  const uint32_t both = h * 0x10001u;
-  each_unit<bf16_t, kAtOnce, false>(row, V, note, [&](const uint4& r, int token) {
-    const uint32_t x[4] = {r.x, r.y, r.z, r.w};
-    // (a half that is equal is zero: the smaller ones of two and two)
-    const auto diff = [&](int e) { return __builtin_bit_cast(upair16_t, x[e] ^ both); };
-    const upair16_t least = __builtin_elementwise_min(__builtin_elementwise_min(diff(0), diff(1)), __builtin_elementwise_min(diff(2), diff(3)));
-    if (least.x == 0 || least.y == 0)
+  each_equal([&](int token) { if (stretch < 0 || token >> 9 == stretch) note(token); }, [&](const uint32_t (&x)[4], int token) {
+    if (stretch < 0 || token >> 9 == stretch)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        note(x[e] & 0xffffu, token + 2 * e);
-        note(x[e] >> 16, token + 2 * e + 1);
+        if ((x[e] & 0xffffu) == h) note(token + 2 * e);
+        if (x[e] >> 16 == h) note(token + 2 * e + 1);
       }
   });
   __syncthreads();
-  const u64 items = sort_list<false>(s, (int)equal);
+  const u64 items = sort_list<false>(s, (int)s.n);
   __syncthreads();
-  if (tid == (int)quotient(mass - at.before_mass, at.weight)) s.found_item = items;
+  if (tid == (int)rank) s.found_item = items;
   __syncthreads();
   d.item = s.found_item;
   d.settled = true;
@@ -829,8 +884,17 @@ __device__ __noinline__ Drawn draw_from_steps(SampleLds& s, const char* row, int
   each_logit<T>(row, V, [&](float z, int) {
     const int step = sc.step(z);
     if (step < kSteps) {
-      atomicAdd(&s.count[step], 1u);
-      atomicAdd(&s.mass[step], sc.weight(z));
+      const u64 same = __ballot(z == __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(z)))), all = __ballot(true);
+      if (same == all) {       // (one value throughout: once for all lanes, which would meet at one step)
+        if ((threadIdx.x & 63) == __builtin_ctzll(all)) {
+          const uint32_t n = (uint32_t)__popcll(all);
+          atomicAdd(&s.count[step], n);
+          atomicAdd(&s.mass[step], sc.weight(z) * n);
+        }
+      } else {
+        atomicAdd(&s.count[step], 1u);
+        atomicAdd(&s.mass[step], sc.weight(z));
+      }
     }
   });
   const Totals total = sum_steps(s);

@@ -98,6 +98,26 @@ def test_many_equal_logits(dev):
                 _check(dev, z, "f32", u if u else 1e-7, **kw)
 
 
+def _about_zero(r, V):
+    """Rows with zeros of both signs among values of either sign near to zero, ordinary ones in front and behind."""
+    zeros = np.where(r.random(V) < 0.5, 0.0, -0.0)
+    near = r.integers(-40, 41, V) * 2.0 ** -17
+    few = np.where(r.random(V) < 400 / V, near, zeros)
+    return [few, np.where(r.random(V) < 0.3, r.integers(-2, 3, V) * 0.25, few), np.where(np.arange(V) == V // 3, 3.0, few),
+            np.where(r.random(V) < 0.5, -1.0, few), np.where(r.random(V) < 0.5, 1.5, few), np.where(r.random(V) < 0.9, -np.inf, zeros)]
+
+
+def test_many_equal_bf16_logits(dev):
+    # thousands of one value at the cut and at the draw, zeros too, which have either sign
+    r = np.random.default_rng(21)
+    for V in (900, 5000, 151936, 1 << 20):
+        rows = [np.full(V, -3.5), np.full(V, 1.5), r.integers(0, 3, V) * 0.5, np.where(np.arange(V) % 7 == 0, 2.0, -1.0)] + _about_zero(r, V)
+        z = np.stack(rows)
+        for kw in (dict(), dict(top_k=V // 3), dict(top_p=0.4), dict(min_p=0.9), dict(top_k=V // 2, top_p=0.6, min_p=0.1)):
+            for u in (1e-7, 0.37337, 0.99987) if V < 1 << 20 else (0.61803,):
+                _check(dev, z, "bf16", u, shift=3, pad=5, **kw)
+
+
 def test_ends_of_the_random_number(dev):
     import torch
     from paper_2510_13797_amd import bc
