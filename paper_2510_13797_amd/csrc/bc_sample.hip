@@ -120,7 +120,7 @@ __device__ __forceinline__ void each_logit(const char* row, int32_t V, const F& 
 }
 
 // Logits as signed integers: not negative ones rise with the value, negative ones fall.  The largest and smallest integer of some logits tell their
-// maximum, the largest unsigned one whether a NaN with a sign is among them.
+// maximum, the largest unsigned one whether a NaN with a sign is among them, and the lowest if one has a sign.
 typedef __attribute__((ext_vector_type(2))) short pair16_t;
 typedef __attribute__((ext_vector_type(2))) unsigned short upair16_t;
 struct Ends16 {                // of bf16, packed
@@ -134,11 +134,12 @@ struct Ends16 {                // of bf16, packed
   }
   __device__ __forceinline__ void add(const uint4& r) { add(r.x); add(r.y); add(r.z); add(r.w); }
   __device__ __forceinline__ void one(uint32_t bits) { add(bits * 0x10001u); }
-  __device__ __forceinline__ void finish(float& max, bool& bad) const {
+  __device__ __forceinline__ void finish(float& max, float& low, bool& bad) const {
     const int hi = most.x > most.y ? most.x : most.y, lo = least.x < least.y ? least.x : least.y;
     const uint32_t u = umost.x > umost.y ? umost.x : umost.y;
     const bool any = hi >= lo;
     max = any ? __uint_as_float((uint32_t)(hi >= 0 ? hi : lo & 0xffff) << 16) : -__builtin_inff();
+    low = any ? __uint_as_float((u >= 0x8000u ? u : (uint32_t)lo) << 16) : __builtin_inff();
     bad = any && (hi >= 0x7f80 || u > 0xff80u);
   }
 };
@@ -151,9 +152,10 @@ struct Ends32 {
     umost = max(umost, bits);
   }
   __device__ __forceinline__ void add(const uint4& r) { one(r.x); one(r.y); one(r.z); one(r.w); }
-  __device__ __forceinline__ void finish(float& max, bool& bad) const {
+  __device__ __forceinline__ void finish(float& max, float& low, bool& bad) const {
     const bool any = most >= least;
     max = any ? __uint_as_float((uint32_t)(most >= 0 ? most : least)) : -__builtin_inff();
+    low = any ? __uint_as_float(umost >= 0x80000000u ? umost : (uint32_t)least) : __builtin_inff();
     bad = any && (most >= 0x7f800000 || umost > 0xff800000u);
   }
 };
@@ -191,6 +193,7 @@ struct Line {
 struct SampleLds {
   union {
     struct { u64 mass[kSteps]; uint32_t count[kSteps]; };
+    float lows[kSampleThreads];                          // (in place of masses)
     uint32_t value_count[(kValues + kNowhere) * kCopies];
   };
   u64 list[kListed];
@@ -285,6 +288,9 @@ __device__ __forceinline__ float block_max(float x, float* waves) {
   return all;
 }
 
+// The row's lowest logit.
+__device__ __forceinline__ float lowest_of(SampleLds& s) { return -block_max(-s.lows[threadIdx.x], s.wavef); }
+
 // Place of a token in the order as one number, smaller in front: the logit's bits turned so that they fall with it, then the id.
 __device__ __forceinline__ u64 item_of(float z, int token) {
   const uint32_t b = __float_as_uint(z + 0.f);                // (-0 is 0)
@@ -303,10 +309,11 @@ struct Scale {
   float steps;                 // steps of the histogram per unit of (max - z) / 2
   double temperature;
   float rate_hi, offset;       // the rate in 32 bits, max times it
-  __device__ __forceinline__ Scale(float m, double t) : max(m), rate(1.4426950408889634074 / t), temperature(t) {
+  // low: the row's lowest logit, below which steps need not reach (151,936 normal logits of 0.001, which are within a few steps of kSpan: 610 us, 123 so)
+  __device__ __forceinline__ Scale(float m, double t, float low = -__builtin_inff()) : max(m), rate(1.4426950408889634074 / t), temperature(t) {
     rate_hi = (float)rate;
     offset = max * rate_hi;
-    steps = (float)fmin(rate * (2 * kSteps / kSpan), 1e30);       // (finite: max - z may be zero)
+    steps = (float)fmin(fmax(rate * (2 * kSteps / kSpan), 0.999 * 2 * kSteps / ((double)m - (double)low)), 1e30);       // (finite: max - z may be zero)
   }
   // step of a logit; kSteps and more: it weighs nothing (-inf too).  Rises with max - z whatever is rounded.
   __device__ __forceinline__ int step(float z) const { return (int)fminf((0.5f * max - 0.5f * z) * steps, (float)kSteps); }
@@ -489,8 +496,8 @@ struct Found { u64 item, mass; };       // mass: up to and with it
 
 // Looks a target up in a row whose first histogram (sc.step()) is in `s`, as sum_steps() leaves it, and keeps it there.
 template <typename T>
-__device__ __noinline__ Found look_up(SampleLds& s, const char* row, int32_t V, float max, double temperature, Totals all, Target t) {
-  const Scale sc(max, temperature);
+__device__ __noinline__ Found look_up(SampleLds& s, const char* row, int32_t V, float max, float low, double temperature, Totals all, Target t) {
+  const Scale sc(max, temperature, low);
   // the first histogram is put by: two counts and masses a thread
   Place at = step_of(s, t, all, 0, 0);
   const int i = 2 * threadIdx.x;
@@ -674,12 +681,12 @@ struct ValueSums {
     return At{s.found_kind, s.found_count, s.found_mass, s.found_weight};
   }
 };
-__device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row, int32_t V, const Scale& sc, const Wish& w) {
+__device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row, int32_t V, const Scale& sc, float low, const Wish& w) {
   const float max = sc.max;
   const int tid = threadIdx.x;
   Drawn d{0, 0, false};
-  // the lowest logit that weighs anything, and the binades: down from the larger magnitude of it and the largest
-  const float lowest = (float)fmax((double)max - (double)kSpan / sc.rate, -3.4028234663852886e38);
+  // the lowest logit that weighs anything (or that there is: 151,936 normal ones of 0.001 would not fit the list, 622 us for 64), and the binades: down from the larger magnitude of it and the largest
+  const float lowest = fmaxf((float)fmax((double)max - (double)kSpan / sc.rate, -3.4028234663852886e38), low);
   const uint32_t top = __float_as_uint(fmaxf(fabsf(max), fabsf(lowest))) >> 23, a0 = top > 15 ? (top - 15) << 7 : 1;        // (zeros are equal whatever their sign: never a place of their own)
   __syncthreads();
   for (int i = tid; i < (kValues + kNowhere) * kCopies; i += kSampleThreads) s.value_count[i] = 0;
@@ -879,7 +886,9 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
 // flat fp32 row 109 -> 129); a call saves a hundred registers a thread in memory, which is little beside their passes (and was a third of draw_from_values()).
 template <typename T>
 __device__ __noinline__ Drawn draw_from_steps(SampleLds& s, const char* row, int32_t V, float max, double temperature, Wish w) {
-  const Scale sc(max, temperature);
+  // (bf16: draw_from_values() has written over them)
+  const float low = std::is_same<T, float>::value ? lowest_of(s) : -__builtin_inff();
+  const Scale sc(max, temperature, low);
   clear_steps(s, true);
   each_logit<T>(row, V, [&](float z, int) {
     const int step = sc.step(z);
@@ -924,7 +933,7 @@ __device__ __noinline__ Drawn draw_from_steps(SampleLds& s, const char* row, int
       }
       t.mass = part_of(w.u, d.kept);
     }
-    const Found f = look_up<T>(s, row, V, max, temperature, total, t);
+    const Found f = look_up<T>(s, row, V, max, low, temperature, total, t);
     if (stage < 2) d.kept = f.mass; else d.item = f.item;
   }
   return d;
@@ -947,11 +956,12 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
   if (t >= 0.f && t < 1.17549435e-38f) { t = 1.f; w.k = 1; }      // the largest alone (log2(e) / t fits 32 bits otherwise)
 
   // A
-  float mine;
+  float mine, low;
   bool bad;
   Ends<T> ends;
   each_unit<T, kAtOnce, false>(row, p.V, [&](uint32_t bits, int) { ends.one(bits); }, [&](const uint4& r, int) { ends.add(r); });
-  ends.finish(mine, bad);
+  ends.finish(mine, low, bad);
+  s.lows[threadIdx.x] = low;                             // (of use to D alone: kept in a register, 17.6 us of an fp32 row were 18.7)
   bad = bad || !(t > 0.f && t < __builtin_inff()) || w.u != w.u;
   const float max = block_max(mine, s.wavef) + 0.f;      // (-0 is 0)
   if (__syncthreads_or(bad) || !(max > -__builtin_inff())) {
@@ -1067,9 +1077,14 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleParams p) 
   } else if (listed <= kListed) {
     d = draw_from_list<false>(s, listed, sc, w, complete, tail, p.V);
   }
-  if constexpr (std::is_same<T, bf16_t>::value)
-    if (!d.settled) d = draw_from_values(s, row, p.V, sc, w);
-  if (!d.settled) d = draw_from_steps<T>(s, row, p.V, max, (double)t, w);
+  if constexpr (std::is_same<T, bf16_t>::value) {
+    if (!d.settled) {
+      d = draw_from_values(s, row, p.V, sc, lowest_of(s), w);
+      if (!d.settled) d = draw_from_steps<T>(s, row, p.V, max, (double)t, w);
+    }
+  } else {
+    if (!d.settled) d = draw_from_steps<T>(s, row, p.V, max, (double)t, w);
+  }
   if (threadIdx.x == 0) {
     p.token[b] = (int32_t)(uint32_t)d.item;
     if (p.logprob)

@@ -118,6 +118,20 @@ def test_many_equal_bf16_logits(dev):
                 _check(dev, z, "bf16", u, shift=3, pad=5, **kw)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_a_narrow_range(dev, dtype):
+    # all of a row within a small part of what weighs anything: about zero, far from it, with masked tokens, next to denormals
+    r = np.random.default_rng(33)
+    for V in (1300, 151936):
+        n = r.standard_normal((8, V))
+        z = np.stack([1e-4 * n[0], 1e-3 * n[1], 2e-2 * n[2], 0.1 * n[3], 1000 + 1e-3 * n[4], -1000 + n[5], np.where(r.random(V) < 0.5, -np.inf, 1e-3 * n[6]),
+                      1e-40 * n[7]])
+        for kw in (dict(), dict(top_k=V // 3), dict(top_p=0.4), dict(min_p=0.9999), dict(temperature=0.3, top_k=V // 2, top_p=0.6, min_p=0.1),
+                   dict(temperature=50.0, top_p=0.9)):
+            for u in (1e-7, 0.37337, 0.99987):
+                _check(dev, z, dtype, u, shift=3, pad=5, **kw)
+
+
 def test_ends_of_the_random_number(dev):
     import torch
     from paper_2510_13797_amd import bc
