@@ -47,12 +47,12 @@ struct PromptParams {
   const uint8_t* active;
   float* out;                  // [total, Hq, d]
   int32_t* resident;           // [B] rows in front of the chunk, -1: the sequence takes no part
-  float2* ml;                  // [parts][npairs][columns] maximum (log2) and sum of a part
-  float* sums;                 // [parts][npairs][columns][d]
+  float2* ml;                  // [parts][rows * Hq] maximum (log2) and sum of a part: a sequence's columns behind those of the ones in front
+  float* sums;                 // [parts][rows * Hq][d]                                of it, in it a pair's behind the pair's in front of it
   const int64_t* row_off;      // [B + 1], null: `inl`
   int32_t B, Hq, Hkv, g;
   int32_t npairs, pstride, turn, parts;      // as in the prefill kernels
-  int32_t columns;             // most columns of a pair, padded to a workgroup's
+  int64_t first_row, slots;    // the first sequence's first row; columns of a part
   int32_t table_blocks, copy_blocks;      // of the second launch
   float qscale;
   InlineOffsets inl;
@@ -77,6 +77,12 @@ __device__ __forceinline__ Chunk chunk_of(const PromptParams& p, int s) {       
   const_offsets_t* in = (const_offsets_t*)((const_char_t*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(PromptParams, inl));
   const int at = in->from[s];
   return {in->first + at, in->from[s + 1] - at};
+}
+
+// Where a pair's sums start inside a part's: columns take the room of the rows that there are (a pair's place by the longest chunk's columns took
+// gigabytes where one chunk was long and many short).
+__device__ __forceinline__ int64_t first_slot(const PromptParams& p, const Chunk& c, int kvh) {
+  return (c.off0 - p.first_row) * p.Hq + (int64_t)kvh * c.rows * p.g;
 }
 
 // What a sequence's tables say: rows in front of the chunk, or -1 and the error bit to set.
@@ -234,7 +240,7 @@ __device__ __forceinline__ void issue_columns(const PromptParams& p, int64_t off
 // The workgroup's place and its sequence; false: nothing to do.
 struct PromptWork {
   int part, pair, kvh, s, n, columns, first;
-  int64_t off0;
+  int64_t off0, slot0;
   PromptTiles tiles;
   int t0, t1;                  // tiles of this part
   template <int D, int WIDE>
@@ -248,6 +254,7 @@ struct PromptWork {
     const Chunk chunk = chunk_of(p, s);
     off0 = chunk.off0;
     n = chunk.rows;
+    slot0 = part * p.slots + first_slot(p, chunk, kvh);
     const int block = gridDim.y - 1 - blockIdx.y;              // long ones first
     const Resident r = resident_rows(p, s, n);
     if (block == 0 && part == 0 && kvh == 0 && threadIdx.x == 0) {
@@ -273,9 +280,7 @@ struct PromptWork {
     return true;
   }
   // where a column's sums of this part go
-  __device__ __forceinline__ int64_t slot(const PromptParams& p, int column) const {
-    return ((int64_t)part * p.npairs + pair) * p.columns + column;
-  }
+  __device__ __forceinline__ int64_t slot(int column) const { return slot0 + column; }
 };
 
 template <int D> constexpr int prompt_lds() { return kTileStages * 2 * kTileRows * D * 2; }
@@ -360,11 +365,11 @@ __global__ __launch_bounds__(kTileWaves * 64, 3) void prompt_attn_kernel(PromptP
         return t < left ? r * p.Hq + c - r * p.g : -1;
       });
   } else {
-    if (half == 0 && col < left) p.ml[wk.slot(p, first + col)] = make_float2(x.m, l);
+    if (half == 0 && col < left) p.ml[wk.slot(first + col)] = make_float2(x.m, l);
     if (wk.t0 >= wk.t1) return;
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass)
-      store_rows<D, false>(my, x.O, 1.f, pass, lane, p.sums + wk.slot(p, first) * D, D, [&](int t) { return t < left ? t : -1; });
+      store_rows<D, false>(my, x.O, 1.f, pass, lane, p.sums + wk.slot(first) * D, D, [&](int t) { return t < left ? t : -1; });
   }
 }
 
@@ -456,7 +461,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 1) void prompt_few_kernel(PromptPa
       float* to = p.out + ((wk.off0 + r) * p.Hq + wk.kvh * p.g + c - r * p.g) * D;
       *reinterpret_cast<f32x4_t*>(to + 4 * unit) = o * (1.0f / sum);
     } else {
-      const int64_t slot = wk.slot(p, c);
+      const int64_t slot = wk.slot(c);
       if (unit == 0) p.ml[slot] = make_float2(M, sum);
       if (wk.t0 < wk.t1) *reinterpret_cast<f32x4_t*>(p.sums + slot * D + 4 * unit) = o;
     }
@@ -490,7 +495,7 @@ __device__ __forceinline__ void fold_many_parts(const PromptParams& p, int block
   __shared__ float weight[COLS][kMostParts];
   __shared__ float inv[COLS];
   __shared__ f32x4_t some[kFoldGroups][COLS * UNITS];
-  const int64_t slot0 = (int64_t)pair * p.columns + first, step = (int64_t)p.npairs * p.columns;
+  const int64_t slot0 = first_slot(p, chunk, pair % p.Hkv) + first, step = p.slots;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (wave < COLS) {
     const int64_t slot = slot0 + min(wave, columns - 1 - first);
@@ -547,7 +552,7 @@ __device__ __forceinline__ void fold_few_parts(const PromptParams& p, int block)
   const Chunk chunk = chunk_of(p, s);
   const int first = (int)(block - fold_start<PER>(chunk.off0 - off, s, p.Hq)) * PER + threadIdx.x / UNITS, unit = threadIdx.x % UNITS;
   const int last = chunk.rows * p.Hq - 1;
-  const int64_t step = (int64_t)p.npairs * p.columns;
+  const int64_t step = p.slots;
   int64_t slot[COLS];
   f32x4_t x[COLS][PARTS];
   float2 ml[COLS];
@@ -555,7 +560,7 @@ __device__ __forceinline__ void fold_few_parts(const PromptParams& p, int block)
 #pragma unroll
   for (int c = 0; c < COLS; ++c) {
     const int at = min(first + c * APART, last), i = at / p.Hq, head = at - i * p.Hq, kvh = head / p.g;
-    slot[c] = ((int64_t)s * p.Hkv + kvh) * p.columns + i * p.g + head - kvh * p.g;
+    slot[c] = first_slot(p, chunk, kvh) + i * p.g + head - kvh * p.g;
     ml[c] = lane < p.parts ? p.ml[slot[c] + lane * step] : make_float2(kNegBig, 0.f);
 #pragma unroll
     for (int n = 0; n < PARTS; ++n)
@@ -625,7 +630,7 @@ struct PromptPlan {
   bool few;
   int blocks;                  // workgroups along a pair's columns
   int parts;
-  int64_t columns;             // of a pair, padded
+  int64_t columns;             // of a pair, at most
   size_t bytes, ml_at, sums_at, tables_at;
 };
 PromptPlan plan_prompt(const bc_shape* sh, int64_t max_new, int64_t total, int32_t max_cap) {
@@ -647,9 +652,10 @@ PromptPlan plan_prompt(const bc_shape* sh, int64_t max_new, int64_t total, int32
   pl.tables_at = at;
   if (sh->B > kInlineChunks) at += ((size_t)sh->B * 16 + 8 + 15) & ~(size_t)15;
   pl.ml_at = at;
-  if (pl.parts > 1) at += (size_t)pl.parts * npairs * pl.columns * sizeof(float2);
+  const size_t slots = pl.parts > 1 ? (size_t)pl.parts * total * sh->Hq : 0;
+  at += (slots * sizeof(float2) + 15) & ~(size_t)15;
   pl.sums_at = at;
-  if (pl.parts > 1) at += (size_t)pl.parts * npairs * pl.columns * sh->d * sizeof(float);
+  at += slots * sh->d * sizeof(float);
   pl.bytes = at;
   return pl;
 }
@@ -747,7 +753,8 @@ extern "C" int32_t bc_prompt_step(const bc_shape* shape, const bc_cache* cache, 
   p.pstride = roam ? p.npairs | 1 : pair_stride(p.npairs);
   p.turn = roam ? 0 : pair_turn(p.pstride);
   p.parts = pl.parts;
-  p.columns = (int32_t)pl.columns;
+  p.first_row = row_offsets[0];
+  p.slots = total * shape->Hq;
   p.table_blocks = (shape->B + 255) / 256;
   const int64_t units = max_new * shape->Hkv * (shape->d / 8);
   const int64_t copies = (units + 1023) / 1024, share = 4096 / shape->B + 1;

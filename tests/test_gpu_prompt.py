@@ -299,3 +299,35 @@ def test_resident_rows_behind_replays(dev):
             assert K.shape[0] == 100 + 5 * n
             assert np.array_equal(K[-5:], k.float().cpu().numpy()) and np.array_equal(V[-5:], v.float().cpu().numpy())
     assert rt.tables()[2] == 0
+
+
+@pytest.mark.parametrize("n", [[0] * 9 + [200] + [0] * 30, [1] * 9 + [300] + [2] * 30, [0] * 20 + [5] + [0] * 19, [3] * 10 + [0, 4, 1] + [0] * 27])
+def test_few_of_many_sequences_within_the_workspace(dev, n):
+    # one long chunk among short ones or none, few rows for few sequences; the workspace as large as asked for, and what lies behind it
+    import torch
+    from paper_2510_13797_amd import bc
+    r = np.random.default_rng(6)
+    B, Hq, Hkv, d = len(n), 12, 2, 64
+    lens = [(int(x), 0, 0) for x in r.integers(0, 300, B)]
+    for cap in (700, 9000):
+        rt = _runtime(dev, Hq, Hkv, d, lens, np.full(B, cap))
+        off = np.concatenate([[0], np.cumsum(n)]).astype(np.int64) + 3
+        total = int(off[-1] - off[0])
+        k, v, q = _rows(dev, rt, int(off[-1]))
+        before = [rt.resident(s) for s in range(B)]
+        nbytes = bc.bc_prompt_workspace_bytes(rt.shape, max(n), total, cap)
+        ws = torch.full((nbytes + 4096,), 0x5a, dtype=torch.uint8, device=dev)
+        out = torch.full((int(off[-1]), Hq, d), 7.0, device=dev)
+        st = bc.bc_prompt_step(rt.shape, rt.cache, k.data_ptr(), v.data_ptr(), q.data_ptr(), off.ctypes.data, out.data_ptr(), None,
+                               ws.data_ptr(), nbytes, torch.cuda.current_stream().cuda_stream)
+        assert st == bc.BC_OK
+        torch.cuda.synchronize()
+        assert (ws[nbytes:] == 0x5a).all() and (out[:3] == 7).all() and rt.tables()[2] == 0
+        kn, vn, qn, got = _np(k), _np(v), _np(q), _np(out)
+        for s in range(B):
+            K, V = before[s]
+            rows = slice(int(off[s]), int(off[s + 1]))
+            K, V = np.concatenate([K, kn[rows]]), np.concatenate([V, vn[rows]])
+            for i in range(0, n[s], 1 if n[s] < 9 else 17):
+                ref = OA.decode_attention(qn[off[s] + i], K[:lens[s][0] + i + 1], V[:lens[s][0] + i + 1], rt.shape.scale)
+                assert np.abs(got[off[s] + i] - ref).max() <= TOL, (s, i)

@@ -120,3 +120,16 @@ def test_sample_refusals():
     for args in ((z, u), (z[0], u), (z.t(), u)):               # (on the host, wrong orders)
         with pytest.raises(bc.BcError):
             bc.sample_tokens(*args)
+
+
+def test_prompt_workspace_goes_by_the_rows_there_are():
+    # one long chunk among short ones or among slots without rows: no more than the long one's own call, the tables and the short rows' share
+    for B, Hq, Hkv, n in ((128, 4, 1, 4096), (64, 8, 1, 2048), (50, 12, 2, 4096), (64, 12, 2, 512), (256, 4, 1, 10000), (64, 32, 8, 7)):
+        for d in (64, 128):
+            for short in (0, 1):
+                total = n + short * (B - 1)
+                alone = bc.bc_prompt_workspace_bytes(shape(Hq=Hq, Hkv=Hkv, d=d), n, n, 32768)
+                got = bc.bc_prompt_workspace_bytes(shape(Hq=Hq, Hkv=Hkv, d=d, B=B), n, total, 32768)
+                # (sums, a maximum and a sum for every part of a row and head; several sequences are cut into half as many parts again, and into two
+                # where the one alone is not cut; 20 bytes a sequence of tables, ends of 16)
+                assert got <= 1.5 * alone * total / n + 2 * 4 * total * Hq * (d + 2) + 20 * B + 64, (B, Hq, Hkv, n, d, short, got, alone)
