@@ -282,7 +282,8 @@ int32_t bc_decode_step_budget(const bc_shape *shape, const bc_cache *cache, cons
  * with a beacon at the tail (w == c + 1) the state bit; both are left alone.  k and v are finite: a product with an entry that
  * is not may show in rows of its sequence that do not see it.  No atomics on results: they are reproducible.
  * workspace: bc_prompt_workspace_bytes() of the longest chunk, the sum of all and max_cap, 16-byte aligned, no initialisation;
- * calls that overlap in time need one each.  scale must be > 0 and finite; Hq <= 65536, B * Hkv <= 2^23. */
+ * calls that overlap in time need one each.  scale must be > 0 and finite.  Limits (else BC_ERR_SHAPE, and 0 bytes): Hq <= 65536,
+ * B * Hkv <= 2^23, fewer than 2^31 rows in all, a sequence's rows times Hq below 2^31, times Hq / Hkv at most 65535 * 128. */
 size_t bc_prompt_workspace_bytes(const bc_shape *shape, int32_t max_new, int64_t total_new, int32_t max_cap);
 int32_t bc_prompt_step(const bc_shape *shape, const bc_cache *cache, const void *k, const void *v, const void *q,
                        const int64_t *row_offsets, float *out, const uint8_t *active, void *workspace,

@@ -633,6 +633,13 @@ struct PromptPlan {
   int64_t columns;             // of a pair, at most
   size_t bytes, ml_at, sums_at, tables_at;
 };
+// What the kernels and their grids hold: offsets inside a tile of 32 rows and a sequence's (row, head) pairs are of 32 bits, and so are the threads of a
+// grid's row; its rows are 65535 blocks of columns at most.
+bool prompt_fits(const bc_shape* sh, int64_t max_new, int64_t total) {
+  if (sh->kv_dtype != BC_BF16 || sh->Hq > 65536 || (int64_t)sh->B * sh->Hkv > (1 << 23)) return false;
+  if (max_new >= (1LL << 31) || max_new * sh->Hq >= (1LL << 31) || total >= (1LL << 31)) return false;
+  return max_new * (sh->Hq / sh->Hkv) <= 65535LL * kColumns;
+}
 PromptPlan plan_prompt(const bc_shape* sh, int64_t max_new, int64_t total, int32_t max_cap) {
   const int64_t g = sh->Hq / sh->Hkv, npairs = (int64_t)sh->B * sh->Hkv;
   PromptPlan pl;
@@ -688,7 +695,7 @@ int32_t launch_prompt(const PromptParams& p, const PromptPlan& pl, int64_t total
 using namespace bc;
 
 extern "C" size_t bc_prompt_workspace_bytes(const bc_shape* shape, int32_t max_new, int64_t total_new, int32_t max_cap) {
-  if (check_shape(shape) != BC_OK || max_new < 0 || total_new < 0 || max_cap < 1) return 0;
+  if (check_shape(shape) != BC_OK || max_new < 0 || total_new < 0 || max_cap < 1 || !prompt_fits(shape, max_new, total_new)) return 0;
   return plan_prompt(shape, max_new, total_new, max_cap).bytes;
 }
 
@@ -711,11 +718,8 @@ extern "C" int32_t bc_prompt_step(const bc_shape* shape, const bc_cache* cache, 
   const int64_t total = row_offsets[shape->B] - row_offsets[0];
   if (total == 0) return BC_OK;
   if (!k || !v || !q || !out || !aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(out)) return BC_ERR_ARG;
-  // (offsets inside a tile of 32 rows are of 32 bits, and so are the threads of a grid's row)
-  if (shape->Hq > 65536 || (int64_t)shape->B * shape->Hkv > (1 << 23)) return BC_ERR_SHAPE;
-  if (max_new * shape->Hq >= (1LL << 31) || total >= (1LL << 31)) return BC_ERR_SHAPE;
+  if (!prompt_fits(shape, max_new, total)) return BC_ERR_SHAPE;
   const PromptPlan pl = plan_prompt(shape, max_new, total, cache->max_cap);
-  if (pl.blocks > 65535) return BC_ERR_SHAPE;
   if (!workspace || !aligned16(workspace) || workspace_bytes < pl.bytes) return BC_ERR_WORKSPACE;
   PromptParams p{};
   char* ws = static_cast<char*>(workspace);

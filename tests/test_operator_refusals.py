@@ -133,3 +133,18 @@ def test_prompt_workspace_goes_by_the_rows_there_are():
                 # (sums, a maximum and a sum for every part of a row and head; several sequences are cut into half as many parts again, and into two
                 # where the one alone is not cut; 20 bytes a sequence of tables, ends of 16)
                 assert got <= 1.5 * alone * total / n + 2 * 4 * total * Hq * (d + 2) + 20 * B + 64, (B, Hq, Hkv, n, d, short, got, alone)
+
+
+def test_prompt_limits_are_those_of_its_workspace():
+    # chunks on either side of a limit: no size for what the step refuses
+    most = 65535 * 128
+    for s, n, total, fits in ((shape(Hq=8, Hkv=1), most // 8, most // 8, True), (shape(Hq=8, Hkv=1), most // 8 + 1, most // 8 + 1, False),
+                              (shape(Hq=512, Hkv=512), (1 << 22) - 1, 1 << 22, True), (shape(Hq=512, Hkv=512), 1 << 22, 1 << 22, False),
+                              (shape(B=400), most // 2, (1 << 31) - 1, True), (shape(B=400), most // 2, 1 << 31, False),
+                              (shape(Hq=1 << 16, Hkv=1 << 13), 5, 5, True), (shape(Hq=1 << 17, Hkv=1 << 14), 5, 5, False),
+                              (shape(Hq=1, Hkv=1, B=1 << 23), 1, 1 << 23, True), (shape(Hq=1, Hkv=1, B=(1 << 23) + 1), 1, (1 << 23) + 1, False),
+                              (shape(dtype=bc.BC_F32), 5, 5, False), (shape(), 1 << 62, 1 << 62, False)):
+        got = bc.bc_prompt_workspace_bytes(s, n, total, 64)
+        assert (got > 0) == fits, (s.B, s.Hq, s.Hkv, n, total, got)
+        if s.B == 1 and s.kv_dtype == bc.BC_BF16 and n < 1 << 60:     # (what fits goes on to the check of the workspace)
+            assert _prompt(s=s, off=(0, n), nbytes=0) == (bc.BC_ERR_WORKSPACE if fits else bc.BC_ERR_SHAPE)
