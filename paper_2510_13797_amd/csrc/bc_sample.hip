@@ -339,11 +339,12 @@ struct Scale {
     return (u64)__double_as_longlong(__builtin_fma(y, two, 4503599627370496.0)) & 0xfffffffffffffull;
   }
   // exp((z - max) / temperature) in 32 bits, but for factors that all have in common: its exponent is z * rate_hi - offset, rounded once
-  // (kSpan * 2^-24 * ln 2), and tail_sum() puts right what the rounding of rate and offset did to it, the former (kSpan * 2^-24 * ln 2 at most) from some of the
-  // exponents.  With the instruction's 2^-23 and sums of eight, 3 * 2^-24, below 2^-18: kTailBound is twice that.  (Weights beyond kSpan, which round to nothing,
-  // stay in: less than V altogether.)
+  // (half a step of less than 2^6, 2^-19 * ln 2), and tail_sum() puts right what the rounding of rate and offset did to it, the former (kSpan * 2^-24 * ln 2 at most) from
+  // some of the exponents.  With the instruction's 2^-23 and sums of eight, 3 * 2^-24, below 2^-18: kTailBound is twice that.  (Weights beyond kSpan, which round to
+  // nothing, stay in: less than V altogether.)  The offset's rounding moves all exponents by half a step of it: where that is more than a half, as for logits
+  // of 20 and a temperature of 1e-6, rows are left to D (beyond offsets of 2^31 it was more than 126, and weights and their sums not finite).
   __device__ __forceinline__ float tail_exponent(float z) const { return __builtin_fmaf(z, rate_hi, -offset); }
-  __device__ __forceinline__ bool tail_fits() const { return fabsf(offset) < 1e30f; }
+  __device__ __forceinline__ bool tail_fits() const { return fabsf(offset) < 16777216.f; }
   __device__ __forceinline__ double tail_sum(double weights, double mean_exponent) const {
     return weights * exp2((double)offset - (double)max * (double)rate_hi) * (1.0 + 0.69314718055994531 * mean_exponent * ((rate - (double)rate_hi) / rate));
   }

@@ -236,3 +236,23 @@ def test_captured_and_replayed(dev):
             graph.replay()
             st.synchronize()
             assert torch.equal(got, bc.sample_tokens(z, u, top_p=p)), i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_near_greedy_temperatures(dev, dtype):
+    # max / temperature of 1e6 to 2e10, whose own rounding in 32 bits is a half to hundreds: more equal maxima than make a line, some in runs
+    # of a load's length, over logits that weigh nothing; tokens just below the maxima where the temperature lets them weigh
+    r = np.random.default_rng(40)
+    V = 40000
+    for m, t in ((20.125, 1.1878648287222404e-08), (31.875, 1.5443692547023602e-08), (17.375, 2.7561490867356042e-09),
+                 (28.375, 5.293514071524896e-09), (20.0, 1e-6), (20.0, 2.5e-6), (-20.0, 1e-6), (16.0, 1e-4), (1.0, 0.125)):
+        rows = []
+        for below in (m - 1.0, m - 0.125):
+            z = np.full(V, below)
+            z[r.permutation(V // 16)[:260] * 16 + 3] = m
+            for i in r.permutation(V // 16)[:60]:
+                z[i * 16:i * 16 + 8] = m
+            rows.append(z)
+        for kw in (dict(), dict(top_p=0.7), dict(top_p=0.7, min_p=0.5)):
+            for u in (1e-7, 0.37337, 0.99987):
+                _check(dev, np.stack(rows), dtype, u, temperature=t, **kw)
