@@ -429,8 +429,9 @@ int32_t bc_qk_norm_rope_bwd(const bc_shape *shape, int64_t rows, const void *qkv
  *   min_p[b] > 0: those of at least min_p[b] times the first one's weight.
  * tokens[b] is the first kept token up to and with which there is more than u[b] times the weight of all kept ones (u in [0, 1);
  * 1 and more: the last that weighs anything).  temperature[b] = 0 (or below 2^-126) takes the first token.  Weights are rounded to multiples of 2^-42
- * of the largest one, sums of them are exact.  logprob (nullable): natural log of the token's share of the kept weight,
- * off by its rounding and less than 1e-7.
+ * of the largest one, and the token is that of their exact sums.  logprob (nullable): natural log of the token's share of the kept weight, off by
+ * its rounding and less than 1e-7 where a filter cuts the row; where none does, small weights may be summed in 32 bits: less than 3e-6 (6e-7 measured,
+ * where most of a row is one value).
  * logits: device, rows of V <= 2^20 elements, row_stride elements apart, at any element, logits_dtype BC_BF16 or BC_F32;
  * -infinity is a token that is never drawn.  temperature, top_k (int32), top_p, min_p: device [B] fp32 or NULL (1, and no filter);
  * u: device [B] fp32.  A row with a NaN or +infinity, no finite logit, a temperature that is negative or not finite or a u that is

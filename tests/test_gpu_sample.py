@@ -256,3 +256,27 @@ def test_near_greedy_temperatures(dev, dtype):
         for kw in (dict(), dict(top_p=0.7), dict(top_p=0.7, min_p=0.5)):
             for u in (1e-7, 0.37337, 0.99987):
                 _check(dev, np.stack(rows), dtype, u, temperature=t, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_shares_over_one_value(dev, dtype):
+    # a largest logit and 300 others above one value throughout the rest, whose roundings do not even out, drawn without a filter: the small
+    # weights' sum in 32 bits has exponents to half a step below 2^5, the rate to 2^-24 of 2^5, 2^-23 of the instruction and three roundings of a sum of eight,
+    # (2^-20 + 2^-19) ln 2 + 2^-23 + 3 * 2^-24 = 2.3e-6 of it, and V * 2^-43 for the weights' own rounding.  With a filter that cuts, 1e-7.
+    import torch
+    from paper_2510_13797_amd import bc
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    for V, rows in ((151936, [(27.375, 23.625, 20.5, 0.6175395250320435), (26.625, 22.5, 19.0, 0.6868405938148499),
+                              (4.21875, 0.86328125, -2.0, 0.5594238042831421), (27.125, 19.0, 12.0, 1.3616269826889038)]),
+                    (1 << 20, [(26.75, 18.625, 10.75, 1.348808765411377), (24.125, 19.875, 15.75, 0.7026007771492004)])):
+        for most, mid, rest, t in rows:
+            z = torch.full((1, V), rest, dtype=tdt, device=dev)
+            z[0, torch.arange(300, device=dev) * (V // 300) + 5] = mid
+            z[0, V // 2] = most
+            ex = z[0].double().cpu().numpy()
+            col = lambda x: torch.tensor([x], dtype=torch.float32, device=dev)
+            for kw, bound in ((dict(), 2.3e-6 + V * 2.0 ** -43), (dict(min_p=1e-12), 1e-7), (dict(top_p=0.5), 1e-7)):
+                tok, lp = bc.sample_tokens(z, col(0.05), col(t), want_logprob=True, **{n: col(x) for n, x in kw.items()})
+                want, wlp, margin = OS.sample(ex, float(np.float32(0.05)), float(np.float32(t)), **{n: float(np.float32(x)) for n, x in kw.items()})
+                assert margin > 1e-6 and tok.item() == want == V // 2
+                assert abs(lp.double().item() - wlp) <= 2.0 ** -24 * abs(wlp) + bound, (V, most, kw, lp.item(), wlp)
