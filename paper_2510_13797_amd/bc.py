@@ -392,7 +392,8 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-_streams = {}                          # torch's objects of the streams that calls have run on
+_streams = {}                          # torch's objects of streams that calls have run on,
+_MOST_STREAMS = 64                     # so many at most: a caller may make one for every request
 
 
 def _used_here(*tensors):
@@ -402,6 +403,8 @@ def _used_here(*tensors):
     at = _torch_c._cuda_getCurrentStream(_torch_c._cuda_getDevice())
     stream = _streams.get(at)
     if stream is None:
+        if len(_streams) >= _MOST_STREAMS:
+            _streams.clear()
         stream = _streams[at] = _torch_stream(stream_id=at[0], device_index=at[1], device_type=at[2])
     for t in tensors:
         if t is None:

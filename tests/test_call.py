@@ -101,3 +101,33 @@ def test_build_without_a_compiler_or_headers_leaves_no_old_module(monkeypatch, t
             m.setattr(G.shutil if name == "which" else G.os.path, name, value)
             assert G.build_call_module() is False
         assert not lib.exists() and "ctypes" in capsys.readouterr().out
+
+
+def test_streams_that_calls_ran_on_are_not_kept_without_end(monkeypatch):
+    # (torch's side stands in: the stream asked for is another one every time, its tensors note it)
+    class Torch:
+        n = 0
+
+        def _cuda_getDevice(self):
+            return 0
+
+        def _cuda_getCurrentStream(self, device):
+            return (self.n, device, 1)
+
+    class Tensor:
+        is_cuda = True
+
+        def record_stream(self, stream):
+            self.seen = stream
+
+    class Stream:
+        def __init__(self, stream_id, device_index, device_type):
+            self.id = stream_id
+
+    torch, tensor = Torch(), Tensor()
+    monkeypatch.setattr(bc, "_torch_c", torch)
+    monkeypatch.setattr(bc, "_torch_stream", Stream)
+    monkeypatch.setattr(bc, "_streams", {})
+    for torch.n in list(range(1000)) + [999, 3]:
+        bc._used_here(None, tensor)
+        assert tensor.seen.id == torch.n and len(bc._streams) <= 64
