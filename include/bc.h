@@ -281,6 +281,9 @@ int32_t bc_decode_step_budget(const bc_shape *shape, const bc_cache *cache, cons
  * left alone, their rows of out with them.  A sequence whose rows do not fit its slab (L + n > cap) sets the capacity bit, one
  * with a beacon at the tail (w == c + 1) the state bit; both are left alone.  k and v are finite: a product with an entry that
  * is not may show in rows of its sequence that do not see it.  No atomics on results: they are reproducible.
+ * A softmax weight enters its product with V in two bf16 parts (17 bits, as in a decode step), or in three (24 bits) where no sequence has more than
+ * 32 new rows times Hq / Hkv: outputs are off by up to 2^-17 of the values' magnitude, or about an fp32 rounding, and so the same row may differ by
+ * the former between chunks of different lengths.
  * workspace: bc_prompt_workspace_bytes() of the longest chunk, the sum of all and max_cap, 16-byte aligned, no initialisation;
  * calls that overlap in time need one each.  scale must be > 0 and finite.  Limits (else BC_ERR_SHAPE, and 0 bytes): Hq <= 65536,
  * B * Hkv <= 2^23, fewer than 2^31 rows in all, a sequence's rows times Hq below 2^31, times Hq / Hkv at most 65535 * 128. */

@@ -331,3 +331,29 @@ def test_few_of_many_sequences_within_the_workspace(dev, n):
             for i in range(0, n[s], 1 if n[s] < 9 else 17):
                 ref = OA.decode_attention(qn[off[s] + i], K[:lens[s][0] + i + 1], V[:lens[s][0] + i + 1], rt.shape.scale)
                 assert np.abs(got[off[s] + i] - ref).max() <= TOL, (s, i)
+
+
+@pytest.mark.parametrize("s", [11.1875, 11.3125, 12.375, 12.5, 14.125])
+def test_parts_of_the_weights(dev, s):
+    """Values of one everywhere, one key of weight 1 and three of a weight that two bf16 parts leave most of (an output is one but for that).  Up to 32 columns: three parts
+    and fp32 sums of four keys, a step of 2^-23 for each addition of the parts' products, half a step for seven others: 31 * 2^-24; more columns: 2^-17 too."""
+    import torch
+    from paper_2510_13797_amd import bc
+    few, many = 31 * 2.0 ** -24, 31 * 2.0 ** -24 + 2.0 ** -17
+    bf = lambda x: torch.tensor(x, dtype=torch.float64).bfloat16().double().item()
+    w = float(np.float32(2.0 ** ((s - 16.0) * 0.125 * np.log2(np.e))))
+    left = w - bf(w) - bf(w - bf(w))
+    assert few < 3 * abs(left) / (1 + 3 * w) < 2.0 ** -17              # two parts alone do not pass as three
+    for n, bound in ((1, few), (8, few), (9, many), (70, many)):
+        rt = bc.Runtime(1, 4, 1, 64, "bf16", 0.125, [3], [0], [100], dev)
+        assert bc.bc_prompt_workspace_bytes(rt.shape, n, n, 100) <= 64          # (one part: nothing is folded)
+        rt.k_slab.view(100, 64)[:3] = 0
+        rt.k_slab.view(100, 64)[:3, 0] = s
+        rt.v_slab.view(100, 64)[:3] = 1
+        q = torch.zeros(n, 4, 64, dtype=torch.bfloat16, device=dev)
+        q[..., 0] = 1
+        k = torch.zeros(n, 1, 64, dtype=torch.bfloat16, device=dev)
+        k[..., 0] = -4096                                              # (a weight of nothing,
+        k[0, 0, 0] = 16                                                # the first one's is 1)
+        got = rt.prompt_step(k, torch.ones_like(k), q, [0, n])
+        assert (got.double() - 1).abs().max().item() <= bound, n
