@@ -211,3 +211,39 @@ def test_results_are_the_same_again_and_in_a_graph(dev):
             assert all(torch.equal(a, b) for a, b in zip(got, want))
             again = bc.qk_norm_rope(qkv, pos, freq, 12, 2, 128, *w)
             assert all(torch.equal(a, b) for a, b in zip(again, want))
+
+
+@pytest.mark.parametrize("dtype,R", [("bf16", 360000), ("f32", 180000)])
+def test_weight_gradients_of_many_rows(dev, dtype, R):
+    """Against sums in 64 bits.  A row is an item and there are 32 * 1024 groups of lanes: a lane adds the terms of ceil(R / 32768) rows and of a row's
+    heads, a workgroup those of 32 lanes, in 32 bits; a term carries the twenty roundings above.  Magnitudes: a term's are |p| + |q| of two normal
+    numbers times |x| of a third, 1.6 * 0.8 at the mean: 10.5 in all for 360,000 rows of four heads.  A workgroup's own sum, of R * heads / 1024 products of
+    variance one, would be missed: its deviation is three times the bound and more."""
+    import torch
+    from paper_2510_13797_amd import bc
+    Hq, Hkv, d, rot = 4, 1, 64, 48
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device=dev).manual_seed(4)
+    qkv = torch.randn(R, 384, generator=g, device=dev).to(tdt)
+    pos = torch.randint(0, 9000, (R,), generator=g, device=dev, dtype=torch.int32)
+    freq = torch.tensor([1e4 ** (-i / 24.0) for i in range(24)], device=dev)
+    w = [(1 + 0.2 * torch.randn(d, generator=g, device=dev)).to(tdt) for _ in range(2)]
+    grads = [torch.randn(R, h, d, generator=g, device=dev) for h in (Hq, Hkv, Hkv)]
+    got = bc.qk_norm_rope_bwd(qkv, *grads, pos, freq, Hq, Hkv, d, *w)[1:]
+    first = 0
+    for heads, dwi, gi in zip((Hq, Hkv), got, grads):
+        want, mag = (torch.zeros(d, dtype=torch.float64, device=dev) for _ in range(2))
+        for lo in range(0, R, 60000):
+            rows = slice(lo, min(lo + 60000, R))
+            a = (pos[rows].double()[:, None] * freq.double())[:, None]
+            x = qkv[rows].double().unflatten(1, (Hq + 2 * Hkv, d))[:, first:first + heads]
+            x = x / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt()
+            do = gi[rows].double()
+            p, q, rest = do[..., :rot // 2], do[..., rot // 2:rot], do[..., rot:]
+            want += (torch.cat([p * a.cos() + q * a.sin(), q * a.cos() - p * a.sin(), rest], -1) * x).sum((0, 1))
+            mag += (torch.cat([p.abs() + q.abs(), p.abs() + q.abs(), rest.abs()], -1) * x.abs()).sum((0, 1))
+        first += heads
+        bound = (-(-R // 32768) * heads + 32 + 20) * 2.0 ** -24 * mag
+        err = (dwi.double() - want).abs()
+        assert (err <= bound).all(), (heads, err.max().item(), bound.max().item())
+        assert bound.max().item() < (R * heads / 1024) ** 0.5 / 3
