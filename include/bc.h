@@ -435,7 +435,7 @@ int32_t bc_qk_norm_rope_bwd(const bc_shape *shape, int64_t rows, const void *qkv
  * of the largest one, and the token is that of their exact sums.  logprob (nullable): natural log of the token's share of the kept weight, off by
  * its rounding and less than 1e-7 where a filter cuts the row; where none does, small weights may be summed in 32 bits: less than 3e-6 (6e-7 measured,
  * where most of a row is one value).
- * logits: device, rows of V <= 2^20 elements, row_stride elements apart, at any element, logits_dtype BC_BF16 or BC_F32;
+ * logits: device, B < 2^22 rows of V <= 2^20 elements, row_stride elements apart, at any element, logits_dtype BC_BF16 or BC_F32;
  * -infinity is a token that is never drawn.  temperature, top_k (int32), top_p, min_p: device [B] fp32 or NULL (1, and no filter);
  * u: device [B] fp32.  A row with a NaN or +infinity, no finite logit, a temperature that is negative or not finite or a u that is
  * NaN gets token -1 and a logprob of NaN.  active: [B] bytes or NULL; rows of others are left as they were. */

@@ -892,7 +892,8 @@ def qk_norm_rope_bwd(qkv, dq, dk, dv, positions, inv_freq, Hq, Hkv, d, q_weight=
 def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, active=None, tokens=None, want_logprob=False):
     """bc_sample_tokens on device tensors: logits [B, V] bf16/fp32 (rows may lie apart), u, temperature, top_p, min_p [B] fp32,
     top_k [B] int32, active [B] uint8; all but logits and u may be None.  Returns tokens [B] int32, and with want_logprob
-    (tokens, logprob [B] fp32), which the current stream works on; tokens=: where they go (rows that are not active stay)."""
+    (tokens, logprob [B] fp32), which the current stream works on; tokens=: where they go (rows that are not active stay; in a new tensor
+    they are unspecified)."""
     import torch
     load()
     if logits.dim() != 2 or (logits.numel() and logits.stride(1) != 1) or not logits.is_cuda:

@@ -1106,7 +1106,7 @@ extern "C" int32_t bc_sample_tokens(int32_t B, int32_t V, const void* logits, in
                                     const int32_t* top_k, const float* top_p, const float* min_p, const float* u, const uint8_t* active,
                                     int32_t* tokens, float* logprob, void* stream) {
   if (logits_dtype != BC_F32 && logits_dtype != BC_BF16) return BC_ERR_SHAPE;
-  if (B < 0 || V < 1 || V > (1 << 20)) return BC_ERR_SHAPE;
+  if (B < 0 || (int64_t)B * kSampleThreads > 0xffffffffLL || V < 1 || V > (1 << 20)) return BC_ERR_SHAPE;      // (threads of a grid: 32 bits)
   if (B == 0) return BC_OK;
   const int es = elem_size(logits_dtype);
   if (!logits || !u || !tokens || (reinterpret_cast<uintptr_t>(logits) & (es - 1))) return BC_ERR_ARG;

@@ -280,3 +280,18 @@ def test_shares_over_one_value(dev, dtype):
                 want, wlp, margin = OS.sample(ex, float(np.float32(0.05)), float(np.float32(t)), **{n: float(np.float32(x)) for n, x in kw.items()})
                 assert margin > 1e-6 and tok.item() == want == V // 2
                 assert abs(lp.double().item() - wlp) <= 2.0 ** -24 * abs(wlp) + bound, (V, most, kw, lp.item(), wlp)
+
+
+def test_as_many_rows_as_a_grid_holds(dev):
+    import torch
+    from paper_2510_13797_amd import bc
+    B = (1 << 22) - 1
+    g = torch.Generator(device=dev).manual_seed(15)
+    z, u = torch.randn(B, 3, generator=g, device=dev), torch.rand(B, generator=g, device=dev)
+    token = bc.sample_tokens(z, u)
+    x, order = torch.sort(z.double(), dim=1, descending=True, stable=True)
+    upto = (x - x[:, :1]).exp().cumsum(1)
+    share = upto / upto[:, 2:]
+    pick = (share[:, :2] <= u.double()[:, None]).sum(1, keepdim=True)
+    clear = (share[:, :2] - u.double()[:, None]).abs().amin(1) > 1e-9           # (of a border; V * 2^-43 and 2^-53 are less)
+    assert (~clear).sum().item() <= 3 and torch.equal(token[clear].long(), order.gather(1, pick)[clear, 0])

@@ -148,3 +148,8 @@ def test_prompt_limits_are_those_of_its_workspace():
         assert (got > 0) == fits, (s.B, s.Hq, s.Hkv, n, total, got)
         if s.B == 1 and s.kv_dtype == bc.BC_BF16 and n < 1 << 60:     # (what fits goes on to the check of the workspace)
             assert _prompt(s=s, off=(0, n), nbytes=0) == (bc.BC_ERR_WORKSPACE if fits else bc.BC_ERR_SHAPE)
+
+
+def test_sample_refuses_more_rows_than_a_grid_holds():
+    assert _sample(B=1 << 22, V=1, stride=1) == bc.BC_ERR_SHAPE
+    assert _sample(B=(1 << 22) - 1, V=1, stride=1, u=None) == bc.BC_ERR_ARG            # (goes on to what follows)
