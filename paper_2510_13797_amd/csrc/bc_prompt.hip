@@ -11,8 +11,8 @@
 // Two kernels share a wave's work on a tile:
 //   many columns: a workgroup's four waves have 32 columns each and share the tiles (3-stage ring, a barrier a tile).  Bound by the matrix cores:
 //   4 x 2048 rows over 30,000, 32/8 heads, d = 128, 5.25 to 5.5 ms, 4.16 TFLOP of the definition (0.77 PFLOP/s), 6.25 of products issued (1.16; a library
-//   product of 16384^3 reaches 1.35).  Weights in three parts would leave 2.4e-7 of an output's error in place of 2.5e-6 (plain fp32: 1.6e-6) and take
-//   7.9 ms; 512 rows over 7680, 118 us and 163;
+//   product of 16384^3 reaches 1.35).  Weights in three parts would leave 2.4e-7 of an output's error in place of 2.2e-6 to 3.0e-6 (plain fp32: 0.5e-6 to
+//   2.1e-6) and take 7.9 ms; 512 rows over 7680, which take 107 us, went from 118 to 163 in an earlier session;
 //   32 columns or fewer: all four waves have the same columns and every fourth tile each, in a ring of their own without barriers, and are merged through
 //   LDS.  Bound by memory: 7 rows over 16,000, 65 MB, 17.5 us (3.7 TB/s) and 4 for the fold; there the third part costs nothing, and is taken.
 // Where that leaves compute units idle the keys are cut into parts, each of which leaves its sums in the workspace (plan_prompt()).
@@ -620,6 +620,7 @@ __global__ __launch_bounds__(256) void prompt_finish_kernel(PromptParams p) {
 // How a call is cut.  Lengths of the caches are on the device; the capacity stands for them.  Many columns: as many workgroups as run at once (three
 // a compute unit), half as many again for several sequences, whose lengths differ, in parts of 16 tiles and more; 32 columns: one a
 // compute unit (its LDS), four tiles and more.  One, two, three, four, six, eight parts in us, with the rule's in brackets:
+//   (one earlier session; the first line's six parts now take 107)
 //   512 rows over 7680, 32/8 heads      242 151 141 124 [120] 127
 //   700 over 3000, 12/2                 112  67  55  55 [46] 47
 //   8 x 64 over 2000, 32/8               74  52  52 [49] 51  61

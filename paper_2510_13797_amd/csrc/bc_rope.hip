@@ -165,6 +165,8 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(RopeParams p
   }
 }
 
+// (The sums of dw are of 32 bits over a lane's items and a workgroup's lanes, some hundred terms, and of 64 behind that: 360,000 rows of four heads, whose sums are about a
+// thousand, are off by 5e-4 at most.)
 template <typename T, int D, bool NORM, bool STREAM>
 __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_bwd_kernel(RopeParams p) {
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES, GROUPS = kRopeThreads / LPH;

@@ -15,7 +15,7 @@
 //   C  the list is sorted and its sums formed: counts, masses and the draw are looked up, at both ends of the bound where there is one.
 // Rows that this does not settle (nearly flat ones, where hundreds of tokens are kept, many equal ones, a border inside the bound) go by
 //   D  sums of whole rows.  bf16 logits have few values: their counts are taken in LDS, and a value weighs its count times its weight (151,936 equal logits
-//      129 us, zeros 80; zeros by the fp32 way 377).  fp32 logits go by a
+//      131 us, zeros 87; zeros by the fp32 way 377).  fp32 logits go by a
 //      histogram of counts and masses over 2048 equal steps of (max - z) / temperature; where a count or mass falls, the step's
 //      tokens are listed and sorted as in C, after further histograms of it where there are too many.
 //
@@ -309,7 +309,7 @@ struct Scale {
   float steps;                 // steps of the histogram per unit of (max - z) / 2
   double temperature;
   float rate_hi, offset;       // the rate in 32 bits, max times it
-  // low: the row's lowest logit, below which steps need not reach (151,936 normal logits of 0.001, which are within a few steps of kSpan: 610 us, 123 so)
+  // low: the row's lowest logit, below which steps need not reach (151,936 normal logits of 0.001, which are within a few steps of kSpan: 610 us, 127 so)
   __device__ __forceinline__ Scale(float m, double t, float low = -__builtin_inff()) : max(m), rate(1.4426950408889634074 / t), temperature(t) {
     rate_hi = (float)rate;
     offset = max * rate_hi;
@@ -690,7 +690,7 @@ __device__ __forceinline__ Drawn draw_from_values(SampleLds& s, const char* row,
   const float max = sc.max;
   const int tid = threadIdx.x;
   Drawn d{0, 0, false};
-  // the lowest logit that weighs anything (or that there is: 151,936 normal ones of 0.001 would not fit the list, 622 us for 64), and the binades: down from the larger magnitude of it and the largest
+  // the lowest logit that weighs anything (or that there is: 151,936 normal ones of 0.001 would not fit the list, 622 us for 60), and the binades: down from the larger magnitude of it and the largest
   const float lowest = fmaxf((float)fmax((double)max - (double)kSpan / sc.rate, -3.4028234663852886e38), low);
   const uint32_t top = __float_as_uint(fmaxf(fabsf(max), fabsf(lowest))) >> 23, a0 = top > 15 ? (top - 15) << 7 : 1;        // (zeros are equal whatever their sign: never a place of their own)
   __syncthreads();
