@@ -43,6 +43,7 @@ EXPORTS = [
     "bc_prompt_workspace_bytes", "bc_prompt_step",
     "bc_sample_tokens",
     "bc_qk_norm_rope", "bc_qk_norm_rope_bwd_workspace_bytes", "bc_qk_norm_rope_bwd",
+    "bc_paged_append", "bc_paged_workspace_bytes", "bc_paged_attend",
 ]
 DIAG_EXPORTS = ["bc_diag_stream_read"]
 
@@ -59,6 +60,12 @@ class bc_cache(C.Structure):
                 ("max_cap", C.c_int32), ("order", C.c_void_p),
                 ("uniform_P", C.c_int32), ("uniform_cap", C.c_int32),
                 ("rows_per_workgroup", C.c_int32), ("plan", C.c_int32)]
+
+
+class bc_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("table", C.c_void_p), ("len", C.c_void_p), ("err", C.c_void_p), ("arrivals", C.c_void_p),
+                ("pages", C.c_int32), ("page_rows", C.c_int32), ("table_pages", C.c_int32), ("max_len", C.c_int32)]
 
 
 class BcError(RuntimeError):
@@ -147,6 +154,13 @@ def load():
     lib.bc_qk_norm_rope_bwd_workspace_bytes.argtypes = [sp]
     lib.bc_qk_norm_rope_bwd.restype = i32
     lib.bc_qk_norm_rope_bwd.argtypes = [sp, i64, vp, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    pp = C.POINTER(bc_pages)
+    lib.bc_paged_append.restype = i32
+    lib.bc_paged_append.argtypes = [sp, pp, i64, vp, i32, vp, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, vp, vp]
+    lib.bc_paged_workspace_bytes.restype = sz
+    lib.bc_paged_workspace_bytes.argtypes = [sp, i32, i32]
+    lib.bc_paged_attend.restype = i32
+    lib.bc_paged_attend.argtypes = [sp, pp, i64, vp, i32, vp, vp, vp, vp, sz, vp]
     lib.bc_tables_to_host.restype = i32
     lib.bc_tables_to_host.argtypes = [sp, cp, vp, vp, vp, vp]
     call = at = None
@@ -345,6 +359,20 @@ def bc_qk_norm_rope_bwd(shape, rows, qkv, qkv_row_stride, positions, inv_freq, r
     return load().bc_qk_norm_rope_bwd(C.byref(shape), rows, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight,
                                       k_weight, eps, dq, dk, dv, dqkv, dqkv_row_stride, dq_weight, dk_weight, ws,
                                       ws_bytes, stream)
+
+
+def bc_paged_append(shape, pages, rows, row_offsets, max_new, qkv, qkv_row_stride, positions, inv_freq, rot, q_weight, k_weight, eps,
+                    keep, active, q, stream):
+    return load().bc_paged_append(C.byref(shape), C.byref(pages), rows, row_offsets, max_new, qkv, qkv_row_stride, positions,
+                                  inv_freq, rot, q_weight, k_weight, eps, keep, active, q, stream)
+
+
+def bc_paged_workspace_bytes(shape, max_new, max_len):
+    return load().bc_paged_workspace_bytes(C.byref(shape), max_new, max_len)
+
+
+def bc_paged_attend(shape, pages, rows, row_offsets, max_new, q, out, active, ws, ws_bytes, stream):
+    return load().bc_paged_attend(C.byref(shape), C.byref(pages), rows, row_offsets, max_new, q, out, active, ws, ws_bytes, stream)
 
 
 def bc_tables_to_host(shape, cache, nb_host, w_host, err_host, stream):
@@ -697,6 +725,141 @@ class Runtime:
             blk = slab[lo:lo + cap * E].view(self.Hkv, cap, self.d)[:, :L, :]
             out.append(blk.permute(1, 0, 2).float().cpu().numpy())
         return out[0], out[1]
+
+
+class PagedCache:
+    """One layer's cache in pages of 8-bit entries (bc_pages in include/bc.h): owns the pool, its scales, the lengths and a table.
+
+    Which pages a sequence has is the caller's business: `table` [B, table_pages] int32 is a tensor to write to (one passed in may be shared by the layers of a
+    model; the lengths are each layer's own).  A page that is appended to belongs to one sequence, whole ones in front of it may be shared.  Entries that have not
+    been written are NaN."""
+
+    def __init__(self, B, Hq, Hkv, d, pages, page_rows, table_pages, device, dtype="bf16", scale=None, table=None):
+        import torch
+        load()
+        self.torch = torch
+        self.B, self.Hq, self.Hkv, self.d = int(B), int(Hq), int(Hkv), int(d)
+        self.pages, self.page_rows, self.table_pages = int(pages), int(page_rows), int(table_pages)
+        self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.shape = bc_shape(self.B, self.Hq, self.Hkv, self.d, _np_dtype_code(dtype), float(scale if scale is not None else self.d ** -0.5))
+        if self.page_rows < 16 or self.page_rows & (self.page_rows - 1) or min(self.B, self.Hkv, self.d, self.pages, self.table_pages) < 1:
+            raise BcError("a paged cache has pages of 16, 32, ... rows and at least one of everything")
+        size = (self.pages, self.Hkv, self.page_rows, self.d)
+        self.k_pages, self.v_pages = (torch.full(size, 0x7f, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
+        self.k_scale, self.v_scale = (torch.full((self.pages, self.Hkv, self.page_rows // 16), float("nan"), device=device) for _ in range(2))
+        self.device = self.k_pages.device
+        if table is None:
+            table = torch.zeros(self.B, self.table_pages, dtype=torch.int32, device=device)
+        else:
+            _is(table, "table", torch.int32, (self.B, self.table_pages), self.device)
+        self.table = table
+        self.lengths = torch.zeros(self.B, dtype=torch.int32, device=device)
+        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        self._arrivals = torch.zeros(self.B * self.Hkv, dtype=torch.int32, device=device)
+        self._c = bc_pages(*(t.data_ptr() for t in self._own()), self.pages, self.page_rows, self.table_pages, 0)
+        self._refs = C.byref(self.shape), C.byref(self._c)
+        self._home = _stream_ptr() if self.device.type == "cuda" else None
+
+    def _own(self):
+        return self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.table, self.lengths, self.err, self._arrivals
+
+    def _rows(self, x, row_offsets, max_new, active):
+        """Checks what both calls take; -> (row_offsets on the device or None, max_new)."""
+        torch, rows, dev = self.torch, x.shape[0], self.device
+        if active is not None:
+            _is(active, "active", torch.uint8, (self.B,), dev)
+        if row_offsets is None:
+            if rows != self.B:
+                raise BcError("without row_offsets there is one row for each of the %d sequences" % self.B)
+            return None, 1
+        if isinstance(row_offsets, torch.Tensor) and row_offsets.is_cuda:
+            _is(row_offsets, "row_offsets", torch.int64, (self.B + 1,), dev)
+            return row_offsets, rows if max_new is None else int(max_new)
+        off = np.ascontiguousarray(row_offsets, dtype=np.int64)
+        if off.shape != (self.B + 1,):
+            raise BcError("row_offsets must have B + 1 entries")
+        n = off[1:] - off[:-1]
+        if off[0] < 0 or n.min() < 0 or off[-1] > rows:
+            raise BcError("row_offsets must not decrease and end within the %d rows" % rows)
+        # (the values travel in kernel arguments: nothing waits)
+        on_device = torch.empty(2 * self.B + 1, dtype=torch.int64, device=dev)
+        zeros = np.zeros(self.B, dtype=np.int32)
+        _check(bc_trajectory_tables(off.ctypes.data, zeros.ctypes.data, zeros.ctypes.data, self.B, on_device.data_ptr(), _stream_ptr()))
+        return on_device, int(n.max())
+
+    def append(self, qkv, positions, inv_freq, row_offsets=None, max_new=None, q_weight=None, k_weight=None, eps=1e-6, keep=None,
+               active=None, q=None):
+        """bc_paged_append: qkv [rows, (Hq + 2 Hkv) d] (rows may lie apart), positions [rows] int32, inv_freq [rot / 2] fp32, weights [d] or None, keep [B]
+        int32 or None, active [B] uint8 or None.  row_offsets [B + 1]: None (a row a sequence), host integers, or an int64 device tensor with max_new, the longest span.
+        Returns q [rows, Hq, d] bf16 (rows of sequences that take no part: as they were, in a new tensor unspecified)."""
+        torch, dev = self.torch, self.device
+        if dev.index != torch.cuda.current_device():           # the stream is that device's
+            with torch.cuda.device(dev):
+                return self.append(qkv, positions, inv_freq, row_offsets, max_new, q_weight, k_weight, eps, keep, active, q)
+        Hq, Hkv, d = self.Hq, self.Hkv, self.d
+        _, rows, stride, rot = _rope_rows(qkv, positions, inv_freq, Hq, Hkv, d, q_weight, k_weight)
+        if qkv.dtype != self.dtype or qkv.device != dev:
+            raise BcError("qkv must be a %s tensor on %s" % (self.dtype, dev))
+        offsets, most = self._rows(qkv, row_offsets, max_new, active)
+        if keep is not None:
+            _is(keep, "keep", torch.int32, (self.B,), dev)
+        given = q
+        if q is None:
+            q = torch.empty((rows, Hq, d), dtype=torch.bfloat16, device=dev)
+        else:
+            _is(q, "q", torch.bfloat16, (rows, Hq, d), dev)
+        stream = _stream_ptr()
+        st = (_lib or load()).bc_paged_append(*self._refs, rows, _ptr(offsets), most, qkv.data_ptr(), stride, positions.data_ptr(), inv_freq.data_ptr(),
+                                              rot, _ptr(q_weight), _ptr(k_weight), eps, _ptr(keep), _ptr(active), q.data_ptr(), stream)
+        if st != BC_OK:
+            _check(st)
+        _used_here(qkv, positions, inv_freq, q_weight, k_weight, keep, active, given, offsets)
+        if stream != self._home:
+            _used_here(*self._own())
+        return q
+
+    def attend(self, q, row_offsets=None, max_new=None, max_len=None, active=None, out=None):
+        """bc_paged_attend: q [rows, Hq, d] bf16, the rows of the newest entries; row_offsets, max_new, active as for append; max_len: no sequence is longer
+        (None: what the table holds).  Returns out [rows, Hq, d] fp32 (rows of sequences that take no part: as they were, in a new tensor unspecified)."""
+        torch, dev = self.torch, self.device
+        if dev.index != torch.cuda.current_device():           # the stream, and the workspace's, are that device's
+            with torch.cuda.device(dev):
+                return self.attend(q, row_offsets, max_new, max_len, active, out)
+        size = (q.shape[0], self.Hq, self.d)
+        _is(q, "q", torch.bfloat16, size, dev)
+        offsets, most = self._rows(q, row_offsets, max_new, active)
+        given = out
+        if out is None:
+            out = torch.empty(size, dtype=torch.float32, device=dev)
+        else:
+            _is(out, "out", torch.float32, size, dev)
+        longest = self.table_pages * self.page_rows
+        if max_len is not None:
+            longest = max(1, min(int(max_len), longest))
+        self._c.max_len = longest
+        lib, (shape, pages) = _lib or load(), self._refs
+        nbytes = lib.bc_paged_workspace_bytes(shape, most, longest)
+        ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+        stream = _stream_ptr()
+        st = lib.bc_paged_attend(shape, pages, size[0], _ptr(offsets), most, q.data_ptr(), out.data_ptr(), _ptr(active), ws.data_ptr(), nbytes, stream)
+        if st != BC_OK:
+            _check(st)
+        _used_here(q, active, given, offsets)
+        if stream != self._home:
+            _used_here(*self._own())
+        return out
+
+    def entries(self, s):
+        """(K, V) [length, Hkv, d] fp32 NumPy copies of the entries of sequence s."""
+        n, R, d = int(self.lengths[s]), self.page_rows, self.d
+        pages = self.table[s, :-(-n // R)].long()
+        got = []
+        for pool, scale, form in ((self.k_pages, self.k_scale, (d // 64, 4, 64)), (self.v_pages, self.v_scale, (d, 4))):
+            x = pool.view(self.torch.uint8)[pages].view(self.torch.float8_e4m3fn).float().view(-1, self.Hkv, R // 4, *form)
+            x = x.permute(0, 2, 4, 1, 3, 5) if len(form) == 3 else x.permute(0, 2, 4, 1, 3)
+            x = x.reshape(-1, self.Hkv, d) * scale[pages].transpose(1, 2).repeat_interleave(16, dim=1).reshape(-1, self.Hkv, 1)
+            got.append(x[:n].cpu().numpy())
+        return got[0], got[1]
 
 
 BC_INLINE_TRAJECTORIES = 16

@@ -10,7 +10,7 @@
 // are each other's partners in the rotation: both halves of a pair are in one lane, and an instruction still asks for whole
 // 128-byte lines.  A lane's four angles serve all heads of its row that are its item.  All arithmetic in fp32, rounded once
 // (angles: angle_of()).
-#include "bc_common.h"
+#include "bc_rope_lane.h"
 
 namespace bc {
 namespace {
@@ -40,83 +40,6 @@ struct RopeParams {
   float eps;
 };
 
-// four elements <-> floats.  STREAM: past the caches (rope_streams())
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-template <bool STREAM, typename V>
-__device__ __forceinline__ V load_from(const char* at) {
-  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const V*>(at));
-  else return *reinterpret_cast<const V*>(at);
-}
-template <bool STREAM, typename V>
-__device__ __forceinline__ void store_to(char* at, const V& x) {
-  if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<V*>(at));
-  else *reinterpret_cast<V*>(at) = x;
-}
-template <bool STREAM = false>
-__device__ __forceinline__ void load4(const char* at, float (&x)[4], float) {
-  const f32x4_t r = load_from<STREAM, f32x4_t>(at);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = r[e];
-}
-template <bool STREAM = false>
-__device__ __forceinline__ void load4(const char* at, float (&x)[4], bf16_t) {
-  const u32x2_t r = load_from<STREAM, u32x2_t>(at);
-  x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
-  x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xffff0000u);
-}
-template <bool STREAM>
-__device__ __forceinline__ void store4(char* at, const float (&x)[4], float) {
-  store_to<STREAM>(at, f32x4_t{x[0], x[1], x[2], x[3]});
-}
-template <bool STREAM>
-__device__ __forceinline__ void store4(char* at, const float (&x)[4], bf16_t) {
-  store_to<STREAM>(at, u32x2_t{pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3])});
-}
-
-// cos and sin of position * inv_freq.  The product and its remainder of quarter turns in 64 bits: a position of a million times a
-// frequency near one is off by 0.03 in 32.  What is left, at most an eighth of a turn, by the series in 32 bits (next term
-// below 2e-9).
-__device__ __forceinline__ void angle_of(int32_t position, float inv_freq, float& c, float& s) {
-  const double quarters = (double)position * ((double)inv_freq * 0.63661977236758134308);      // 2 / pi
-  const double whole = __builtin_rint(quarters);
-  const float x = (float)(quarters - whole) * 1.57079632679489661923f, xx = x * x;
-  const int n = (int)(int64_t)whole;
-  const float sn = x + x * xx * (-1.f / 6 + xx * (1.f / 120 + xx * (-1.f / 5040 + xx * (1.f / 362880))));
-  const float cs = 1.f + xx * (-0.5f + xx * (1.f / 24 + xx * (-1.f / 720 + xx * (1.f / 40320 + xx * (-1.f / 3628800)))));
-  const float a = n & 1 ? sn : cs, b = n & 1 ? cs : sn;
-  c = (n + 1) & 2 ? -a : a;
-  s = n & 2 ? -b : b;
-}
-
-// Where a lane's two pieces of a head stand, and its angles.
-template <int D>
-struct RopeLane {
-  int o1, o2;                  // elements
-  bool turns;
-  float c[4], s[4];
-  __device__ __forceinline__ RopeLane(const RopeParams& p, int lane, int32_t position) {
-    const int at = 4 * lane;
-    turns = at < p.half;
-    o1 = turns ? at : 2 * at;               // (behind the rotated part eight in a row: 2 * half + 8 * (lane - half / 4))
-    o2 = turns ? p.half + at : o1 + 4;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      c[e] = 1.f; s[e] = 0.f;
-      if (turns) angle_of(position, p.inv_freq[at + e], c[e], s[e]);
-    }
-  }
-  // by the angles, or (BACK) against them
-  template <bool BACK>
-  __device__ __forceinline__ void turn(float (&a)[4], float (&b)[4]) const {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float sn = BACK ? -s[e] : s[e], x = fmaf(a[e], c[e], -b[e] * sn), y = fmaf(b[e], c[e], a[e] * sn);
-      a[e] = turns ? x : a[e];              // (not by a product with zero: the partner may be infinite)
-      b[e] = turns ? y : b[e];
-    }
-  }
-};
-
 template <typename T, int D, bool NORM, bool STREAM, int U>
 __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(RopeParams p) {
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES;
@@ -125,7 +48,7 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_kernel(RopeParams p
   const int64_t row = at;
   if (row >= p.rows) return;
   const int first = (int)(item - at * p.chunks) * p.per_item, last = min(first + p.per_item, p.heads);
-  const RopeLane<D> ln(p, lane, p.positions[row]);
+  const RopeLane<D> ln(p.half, p.inv_freq, lane, p.positions[row]);
   float wq[2][4], wk[2][4];
   const bool nq = NORM && p.qw != nullptr, nk = NORM && p.kw != nullptr;
   if (nq) { load4(p.qw + ln.o1 * ES, wq[0], T{}); load4(p.qw + ln.o2 * ES, wq[1], T{}); }
@@ -180,7 +103,7 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_bwd_kernel(RopePara
     const int64_t row = at;
     if (row >= p.rows) break;
     const int first = (int)(item - at * p.chunks) * p.per_item, last = min(first + p.per_item, p.heads);
-    const RopeLane<D> ln(p, lane, p.positions[row]);
+    const RopeLane<D> ln(p.half, p.inv_freq, lane, p.positions[row]);
     o1 = ln.o1; o2 = ln.o2;
     float wq[2][4], wk[2][4];
     if (nq) { load4(p.qw + o1 * ES, wq[0], T{}); load4(p.qw + o2 * ES, wq[1], T{}); }
