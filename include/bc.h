@@ -487,8 +487,8 @@ int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t ro
  * state bit and is left alone; one with an invalid page for its entries sets the state bit, nothing is read out of range, and its rows of out are unspecified.
  * Entries that a row sees, and those of its sequence behind it, are finite: a product with one that is not may show in rows that do not see it.  What lies behind the
  * last entry may be anything.  No atomics on results: they are reproducible.
- * workspace: bc_paged_workspace_bytes() of the longest span and max_len (16-byte aligned, no initialisation).  Calls that share workspace or arrivals must not overlap in time. */
-size_t bc_paged_workspace_bytes(const bc_shape *shape, int32_t max_new, int32_t max_len);
+ * workspace: bc_paged_workspace_bytes() of the call's rows, max_new and max_len (16-byte aligned, no initialisation).  Calls that share workspace or arrivals must not overlap in time. */
+size_t bc_paged_workspace_bytes(const bc_shape *shape, int64_t rows, int32_t max_new, int32_t max_len);
 int32_t bc_paged_attend(const bc_shape *shape, const bc_pages *pages, int64_t rows, const int64_t *row_offsets,
                         int32_t max_new, const void *q, float *out, const uint8_t *active, void *workspace,
                         size_t workspace_bytes, void *stream);

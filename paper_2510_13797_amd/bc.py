@@ -158,7 +158,7 @@ def load():
     lib.bc_paged_append.restype = i32
     lib.bc_paged_append.argtypes = [sp, pp, i64, vp, i32, vp, i64, vp, vp, i32, vp, vp, C.c_float, vp, vp, vp, vp]
     lib.bc_paged_workspace_bytes.restype = sz
-    lib.bc_paged_workspace_bytes.argtypes = [sp, i32, i32]
+    lib.bc_paged_workspace_bytes.argtypes = [sp, i64, i32, i32]
     lib.bc_paged_attend.restype = i32
     lib.bc_paged_attend.argtypes = [sp, pp, i64, vp, i32, vp, vp, vp, vp, sz, vp]
     lib.bc_tables_to_host.restype = i32
@@ -367,8 +367,8 @@ def bc_paged_append(shape, pages, rows, row_offsets, max_new, qkv, qkv_row_strid
                                   inv_freq, rot, q_weight, k_weight, eps, keep, active, q, stream)
 
 
-def bc_paged_workspace_bytes(shape, max_new, max_len):
-    return load().bc_paged_workspace_bytes(C.byref(shape), max_new, max_len)
+def bc_paged_workspace_bytes(shape, rows, max_new, max_len):
+    return load().bc_paged_workspace_bytes(C.byref(shape), rows, max_new, max_len)
 
 
 def bc_paged_attend(shape, pages, rows, row_offsets, max_new, q, out, active, ws, ws_bytes, stream):
@@ -838,7 +838,7 @@ class PagedCache:
             longest = max(1, min(int(max_len), longest))
         self._c.max_len = longest
         lib, (shape, pages) = _lib or load(), self._refs
-        nbytes = lib.bc_paged_workspace_bytes(shape, most, longest)
+        nbytes = lib.bc_paged_workspace_bytes(shape, size[0], most, longest)
         ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
         stream = _stream_ptr()
         st = lib.bc_paged_attend(shape, pages, size[0], _ptr(offsets), most, q.data_ptr(), out.data_ptr(), _ptr(active), ws.data_ptr(), nbytes, stream)

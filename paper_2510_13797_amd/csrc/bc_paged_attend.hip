@@ -7,7 +7,7 @@
 // The query heads of a KV head see the same entries, so (row, head) pairs are the columns of the products: column i * g + h.  A tile is two blocks of 16 entries, which
 // come from memory as operands (bc_paged.h) and become bf16 by the hardware's conversion, exactly: S^T = K.Q^T by 16x16x32 MFMA, whose result has four entries of a
 // column in a lane; a word of values is those four entries of one element, so O^T += V^T.P^T takes both as they are.  A block's key scale is a factor of its scores, its
-// value scale one of its weights (in fp32, in front of their split into two bf16 parts, 17 bits).  Softmax online, sums in fp32.
+// value scale one of its weights (in fp32, in front of their split into three bf16 parts, 24 bits).  Softmax online, sums in fp32.
 #include "bc_paged.h"
 
 namespace bc {
@@ -24,21 +24,29 @@ struct AttendParams {
   const float* ks;             // [pages, Hkv, page_rows / 16]
   const float* vs;
   int32_t* arrivals;           // [B * Hkv] zero between launches
-  float* part;                 // [pair][chunk][columns][d + 2]
+  float* part;                 // sums of parts; many columns: [parts][rows * Hq][d], and
+  float2* part_ml;             // [parts][rows * Hq] their maximum (log2) and sum
   int32_t Hq, Hkv, g, max_len;
-  int32_t column_blocks, max_chunks, chunk_tiles;
+  uint32_t max_chunks, chunk_tiles;     // few columns
+  int32_t blocks, parts;       // many: workgroups along a pair's columns, parts of its entries
   float qs;                    // scale * log2 e
 };
 
-// Partial results go past the caches in both directions: the L2s of the XCDs do not see each other's lines.
-__device__ __forceinline__ void store2_past(float* a, float x, float y) {
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(a), (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+// Partial results go past the caches in both directions (the L2s of the XCDs do not see each other's lines): buffer accesses of system scope.
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_v;
+typedef __attribute__((ext_vector_type(2))) float f32x2_v;
+constexpr int kPast = 1 | 16;                  // sc0, sc1
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t parts_of(float* part) { return __builtin_amdgcn_make_buffer_rsrc(part, 0, 0x7fffffff, 0x27000); }
+__device__ __forceinline__ void store16_past(__amdgpu_buffer_rsrc_t parts, uint32_t at, const f32x4_t& x) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), parts, at, 0, kPast);
 }
-__device__ __forceinline__ uint64_t load2_past(const float* a) {
-  return __hip_atomic_load(reinterpret_cast<const uint64_t*>(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+__device__ __forceinline__ void store8_past(__amdgpu_buffer_rsrc_t parts, uint32_t at, float x, float y) {
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2_v{__float_as_uint(x), __float_as_uint(y)}, parts, at, 0, kPast);
 }
-__device__ __forceinline__ float low_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
-__device__ __forceinline__ float high_of(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ f32x4_t load16_past(__amdgpu_buffer_rsrc_t parts, uint32_t at) {
+  return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(parts, at, 0, kPast));
+}
+__device__ __forceinline__ u32x2_v load8_past(__amdgpu_buffer_rsrc_t parts, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b64(parts, at, 0, kPast); }
 
 __device__ __forceinline__ uint32_t bf16_of(uint32_t w, bool high) {
   return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true))
@@ -53,293 +61,590 @@ __device__ __forceinline__ f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, 
 }
 __device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// A tile as it comes from memory: 16 bytes a lane for 64 elements of a block of keys, and of values.
-template <int D> struct Tile { u32x4_t k[2][D / 64], v[2][D / 64]; };
+// Waves a SIMD has room for.
+constexpr int few_waves(int ct, int nw) { return ct == 1 && nw == 4 ? 4 : 2; }
 
-template <int D, int CT, int NW>
-__global__ void __launch_bounds__(64 * NW) paged_few_kernel(AttendParams p) {
-  constexpr int H = D / 64, COLS = 16 * CT, PITCH = D + 4, BLOCK_BYTES = kPagedBlock * D;
+// What a sequence of the call is, the same wherever it is asked for.
+struct AttendSpan { int64_t row; int n, L; bool bad; };
+__device__ __forceinline__ AttendSpan attend_span(const AttendParams& p, int s) {
+  const PagedSpan span = paged_span(p.t, s);
+  const int L = p.t.len[s];
+  const bool bad = span.n < 0 || (span.n > 0 && (L < span.n || L > p.max_len));
+  return {span.row, bad ? 0 : span.n, L, bad};
+}
+
+// Up to 16 * CT columns a KV head.  The waves of a workgroup have the tiles of its chunk of a (sequence, KV head) pair by turns.  Where a pair has several chunks, each leaves its
+// sums in the workspace, and the workgroup that is the last to arrive adds them up in their order.
+template <int D, int CT, int NW, bool STREAM>
+__global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(AttendParams p) {
+  constexpr int H = D / 64, COLS = 16 * CT, PITCH = D + 4, BLOCK_BYTES = kPagedBlock * D, SUMS = COLS * (D + 2);
   __shared__ __attribute__((aligned(16))) float s_o[NW][COLS][PITCH];
   __shared__ float s_ml[NW][COLS][2];
+  __shared__ float s_team[256 * NW / D][2];      // (a team and a column: d / 4 threads)
   __shared__ int s_last;
+  const auto parts = parts_of(p.part);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
-  uint32_t id = blockIdx.x;
-  const int kvh = id % p.Hkv; id /= p.Hkv;
-  const int s = id % p.t.B; id /= p.t.B;
-  const int cb = id % p.column_blocks, chunk = id / p.column_blocks;
-  const bool herald = chunk == 0 && cb == 0 && kvh == 0 && tid == 0;
-  const PagedSpan span = paged_span(p.t, s);
-  if (span.n == 0) return;
-  const int n = span.n, L = p.t.len[s];
-  if (n < 0 || L < n || L > p.max_len) {
-    if (herald) atomicOr(p.t.err, BC_ERRBIT_STATE);
-    return;
-  }
-  const int columns = n * p.g, col0 = cb * COLS;                       // (host: no more than 2^31)
-  if (col0 >= columns) return;
-  const int own = min(COLS, columns - col0);
-  const int first_row = col0 / p.g, last_row = (col0 + own - 1) / p.g;
-  const int seen_by_all = L - n + 1 + first_row, lim = L - n + 1 + last_row;
-  const int tiles = (lim + 31) >> 5;
-  const int want = min(p.max_chunks, (tiles + p.chunk_tiles - 1) / p.chunk_tiles), per = (tiles + want - 1) / want, chunks = (tiles + per - 1) / per;
-  if (chunk >= chunks) return;
-  const int t0 = chunk * per, t1 = min(tiles, t0 + per);
+  const int per_page = p.t.page_shift - 4;
 
-  bf16x8_t q[CT][2 * H];
-  int key_lim[CT];
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const int col = min(col0 + 16 * ct + c16, columns - 1), i = col / p.g;
-    key_lim[ct] = L - n + 1 + i;
-    const char* at = p.q + ((span.row + i) * p.Hq + kvh * p.g + (col - i * p.g)) * (2 * D) + 32 * g4;
-#pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) q[ct][2 * h + e] = *reinterpret_cast<const bf16x8_t*>(at + 128 * h + 16 * e);
-  }
-  f32x4_t o[CT][4 * H];
-  float m[CT], l[CT];
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    m[ct] = kNegBig; l[ct] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4 * H; ++i) o[ct][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  const uint32_t pairs = (uint32_t)p.t.B * p.Hkv, chunk = blockIdx.x / pairs;
+  const int pair = blockIdx.x - chunk * pairs, s = pair / p.Hkv, kvh = pair - s * p.Hkv;
+  // 32 tiles of the wave at a time: lane 2 i + b has block b of the i-th.  (Which ones they are follows from the chunk's number alone: the table is asked for together with the
+  // length.)
+  const uint32_t t0 = chunk * p.chunk_tiles;
+  const int most = (p.t.table_pages << per_page) - 1;
+  auto page_of = [&](uint32_t tb) { return p.t.table[(int64_t)s * p.t.table_pages + (min(2 * (int)(tb + NW * (lane >> 1)) + (lane & 1), most) >> per_page)]; };
+  int page = page_of(t0 + wave);
+  const AttendSpan span = attend_span(p, s);
+  if (span.bad && chunk == 0 && kvh == 0 && tid == 0) atomicOr(p.t.err, BC_ERRBIT_STATE);
+  const uint32_t tiles = span.n > 0 ? (uint32_t)(span.L + 31) >> 5 : 0, count = (tiles + p.chunk_tiles - 1) / p.chunk_tiles;
+  if (chunk >= count) return;
+  const uint32_t t1 = min(t0 + p.chunk_tiles, tiles);
+  {
+    const int n = span.n, L = span.L, own = n * p.g, seen_by_all = L - n + 1;
 
-  const uint32_t k_lane = (c16 >> 2) * 4 * D + (c16 & 3) * 64 + g4 * 16, v_lane = g4 * 4 * D + c16 * 16;
-  // 32 tiles of the wave at a time: lane 2 i + b has block b of the i-th
-  for (int tb = t0 + wave; tb < t1; tb += 32 * NW) {
-    const int count = min(32, (t1 - tb + NW - 1) / NW);
-    const int block = min(2 * (tb + NW * min(lane >> 1, count - 1)) + (lane & 1), (lim - 1) >> 4);   // (one behind the last is the last)
-    int page = p.t.table[(int64_t)s * p.t.table_pages + (block >> (p.t.page_shift - 4))];
-    if (page < 0 || page >= p.t.pages) {
-      atomicOr(p.t.err, BC_ERRBIT_STATE);
-      page = 0;
-    }
-    const int per_page = p.t.page_shift - 4;
-    const uint32_t unit = (((uint32_t)page * p.Hkv + kvh) << per_page) + (block & ((1 << per_page) - 1));
-    const float k_scale = p.ks[unit] * p.qs, v_scale = p.vs[unit];
-
-    auto load = [&](Tile<D>& x, int i) {
+    bf16x8_t q[CT][2 * H];
+    int key_lim[CT];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint64_t at = (uint64_t)lane_value(unit, 2 * i + b) * BLOCK_BYTES;
-#pragma unroll
-        for (int h = 0; h < H; ++h) x.k[b][h] = *reinterpret_cast<const u32x4_t*>(p.k + at + (k_lane + 256 * h));
-      }
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint64_t at = (uint64_t)lane_value(unit, 2 * i + b) * BLOCK_BYTES;
-#pragma unroll
-        for (int h = 0; h < H; ++h) x.v[b][h] = *reinterpret_cast<const u32x4_t*>(p.v + at + (v_lane + 256 * h));
-      }
-    };
-    auto work = [&](Tile<D>& x, int i) {
-      const int key0 = 32 * (tb + NW * i);
-      f32x4_t sc[CT][2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) sc[ct][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int h = 0; h < H; ++h)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const bf16x8_t a = operand_of(x.k[b][h][2 * e], x.k[b][h][2 * e + 1]);
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) sc[ct][b] = mfma16(a, q[ct][2 * h + e], sc[ct][b]);
-          }
-      }
-      const bool ends = key0 + 32 > seen_by_all;
-      bf16x8_t hi[CT], lo[CT];
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        float z[8];
-        float top = kMasked;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float f = __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) z[4 * b + r] = sc[ct][b][r] * f;
-        }
-        if (ends) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (key0 + 16 * b + 4 * g4 + r >= key_lim[ct]) z[4 * b + r] = kMasked;
-        }
-#pragma unroll
-        for (int r = 0; r < 8; ++r) top = fmaxf(top, z[r]);
-        top = fmaxf(rows_allreduce_max(top), m[ct]);
-        if (__any(top > m[ct])) {
-          const float was = fast_exp2(m[ct] - top);
-          l[ct] *= was;
-#pragma unroll
-          for (int j = 0; j < 4 * H; ++j) o[ct][j] *= was;
-          m[ct] = top;
-        }
-        float w[8];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float f = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + b));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float e = fast_exp2(z[4 * b + r] - m[ct]);
-            l[ct] += e;
-            w[4 * b + r] = e * f;
-          }
-        }
-        u32x4_t wh, wl;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          wh[r] = pack2_bf16(w[2 * r], w[2 * r + 1]);
-          wl[r] = pack2_bf16(w[2 * r] - __uint_as_float(wh[r] << 16), w[2 * r + 1] - __uint_as_float(wh[r] & 0xffff0000u));
-        }
-        hi[ct] = __builtin_bit_cast(bf16x8_t, wh);
-        lo[ct] = __builtin_bit_cast(bf16x8_t, wl);
-      }
-      if (key0 + 32 > L) {                     // bytes behind the last entry may be anything: zeros, not a product with a weight of zero
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int there = L - (key0 + 16 * b + 4 * g4);
-          const uint32_t mask = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
-#pragma unroll
-          for (int h = 0; h < H; ++h)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x.v[b][h][j] &= mask;
-        }
-      }
+    for (int ct = 0; ct < CT; ++ct) {
+      const int col = min(16 * ct + c16, own - 1), i = col / p.g;
+      key_lim[ct] = L - n + 1 + i;
+      const char* at = p.q + ((span.row + i) * p.Hq + kvh * p.g + (col - i * p.g)) * (2 * D) + 32 * g4;
 #pragma unroll
       for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bf16x8_t a = operand_of(x.v[0][h][j], x.v[1][h][j]);
+        for (int e = 0; e < 2; ++e) q[ct][2 * h + e] = *reinterpret_cast<const bf16x8_t*>(at + 128 * h + 16 * e);
+    }
+    f32x4_t o[CT][4 * H];
+    float m[CT], l[CT];
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            o[ct][4 * h + j] = mfma16(a, hi[ct], o[ct][4 * h + j]);
-            o[ct][4 * h + j] = mfma16(a, lo[ct], o[ct][4 * h + j]);
+    for (int ct = 0; ct < CT; ++ct) {
+      m[ct] = kNegBig; l[ct] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4 * H; ++i) o[ct][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const uint32_t k_lane = (c16 >> 2) * 4 * D + (c16 & 3) * 64 + g4 * 16, v_lane = g4 * 4 * D + c16 * 16;
+    for (uint32_t tb = t0 + wave; tb < t1; tb += 32 * NW) {
+      const int count = min(32, (int)(t1 - tb + NW - 1) / NW), block = 2 * (int)(tb + NW * (lane >> 1)) + (lane & 1), last = (L - 1) >> 4;
+      if (tb != t0 + wave) page = page_of(tb);
+      // (a tile's second block may lie behind the last one: the first in its place; other lanes' blocks are nobody's)
+      const int first_of = __builtin_amdgcn_update_dpp(page, page, 0xA0, 0xf, 0xf, true);        // quad_perm [0, 0, 2, 2]
+      const int at_block = block > last ? block & ~1 : block;
+      if (block > last) page = first_of;
+      if (page < 0 || page >= p.t.pages) {
+        if (at_block <= last && (lane >> 1) < count) atomicOr(p.t.err, BC_ERRBIT_STATE);
+        page = 0;
+      }
+      const uint32_t unit = (((uint32_t)page * p.Hkv + kvh) << per_page) + (at_block & ((1 << per_page) - 1));
+      const float k_scale = p.ks[unit] * p.qs, v_scale = p.vs[unit];
+
+      // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are formed, its values
+      // behind the weights' product.
+      u32x4_t key[2][H], value[2][H];
+      auto load = [&](u32x4_t (&x)[2][H], const uint8_t* pool, uint32_t at_lane, int i) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint8_t* at = pool + (uint64_t)lane_value(unit, 2 * i + b) * BLOCK_BYTES;
+#pragma unroll
+          for (int h = 0; h < H; ++h) {
+            const u32x4_t* from = reinterpret_cast<const u32x4_t*>(at + (at_lane + 256 * h));
+            x[b][h] = STREAM ? __builtin_nontemporal_load(from) : *from;
           }
         }
-    };
-    Tile<D> a, b;
-    load(a, 0);
-    for (int i = 0; i < count; i += 2) {
-      load(b, min(i + 1, count - 1));
-      work(a, i);
-      if (i + 1 >= count) break;
-      load(a, min(i + 2, count - 1));
-      work(b, i + 1);
+      };
+      load(key, p.k, k_lane, 0);
+      load(value, p.v, v_lane, 0);
+      for (int i = 0; i < count; ++i) {
+        const int key0 = 32 * (tb + NW * i);
+        f32x4_t sc[CT][2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) sc[ct][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const bf16x8_t a = operand_of(key[b][h][2 * e], key[b][h][2 * e + 1]);
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) sc[ct][b] = mfma16(a, q[ct][2 * h + e], sc[ct][b]);
+            }
+        }
+        if (i + 1 < count) load(key, p.k, k_lane, i + 1);
+        const bool ends = key0 + 32 > seen_by_all;
+        bf16x8_t part[CT][3];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          float z[8];
+          float top = kMasked;
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const float f = __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z[4 * b + r] = sc[ct][b][r] * f;
+          }
+          if (ends) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (key0 + 16 * b + 4 * g4 + r >= key_lim[ct]) z[4 * b + r] = kMasked;
+          }
+#pragma unroll
+          for (int r = 0; r < 8; ++r) top = fmaxf(top, z[r]);
+          top = fmaxf(rows_allreduce_max(top), m[ct]);
+          if (__any(top > m[ct])) {
+            const float was = fast_exp2(m[ct] - top);
+            l[ct] *= was;
+#pragma unroll
+            for (int j = 0; j < 4 * H; ++j) o[ct][j] *= was;
+            m[ct] = top;
+          }
+          float w[8];
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const float f = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + b));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float e = fast_exp2(z[4 * b + r] - m[ct]);
+              l[ct] += e;
+              w[4 * b + r] = e * f;
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            u32x4_t x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              x[r] = pack2_bf16(w[2 * r], w[2 * r + 1]);
+              w[2 * r] -= __uint_as_float(x[r] << 16);
+              w[2 * r + 1] -= __uint_as_float(x[r] & 0xffff0000u);
+            }
+            part[ct][k] = __builtin_bit_cast(bf16x8_t, x);
+          }
+        }
+        if (key0 + 32 > L) {                     // bytes behind the last entry may be anything: zeros, not a product with a weight of zero
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const int there = L - (key0 + 16 * b + 4 * g4);
+            const uint32_t mask = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) value[b][h][j] &= mask;
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bf16x8_t a = operand_of(value[0][h][j], value[1][h][j]);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+              for (int k = 0; k < 3; ++k) o[ct][4 * h + j] = mfma16(a, part[ct][k], o[ct][4 * h + j]);
+          }
+        if (i + 1 < count) load(value, p.v, v_lane, i + 1);
+      }
     }
-  }
 
-  // the waves' sums: a lane has elements 64 h + 16 g4 + 4 r + j of its column
+    // the waves' sums: a lane has elements 64 h + 16 g4 + 4 r + j of its column
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const float sum = rows_allreduce_sum(l[ct]);
-    if (g4 == 0) { s_ml[wave][16 * ct + c16][0] = m[ct]; s_ml[wave][16 * ct + c16][1] = sum; }
+    for (int ct = 0; ct < CT; ++ct) {
+      const float sum = rows_allreduce_sum(l[ct]);
+      if (g4 == 0) { s_ml[wave][16 * ct + c16][0] = m[ct]; s_ml[wave][16 * ct + c16][1] = sum; }
 #pragma unroll
-    for (int h = 0; h < H; ++h)
+      for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        *reinterpret_cast<f32x4_t*>(&s_o[wave][16 * ct + c16][64 * h + 16 * g4 + 4 * r]) =
-            f32x4_t{o[ct][4 * h][r], o[ct][4 * h + 1][r], o[ct][4 * h + 2][r], o[ct][4 * h + 3][r]};
-  }
-  __syncthreads();
-  const int pair = s * p.Hkv + kvh;
-  float* mine = p.part + ((int64_t)pair * p.max_chunks + chunk) * COLS * (D + 2);
-  for (int at = tid; at < own * (D / 4); at += 64 * NW) {
-    const int c = at / (D / 4), x = 4 * (at % (D / 4));
-    float top = kNegBig;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, s_ml[w][c][0]);
-    float sum = 0.f;
-    f32x4_t r{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float f = fast_exp2(s_ml[w][c][0] - top);
-      sum += f * s_ml[w][c][1];
-      r += f * *reinterpret_cast<const f32x4_t*>(&s_o[w][c][x]);
+        for (int r = 0; r < 4; ++r)
+          *reinterpret_cast<f32x4_t*>(&s_o[wave][16 * ct + c16][64 * h + 16 * g4 + 4 * r]) =
+              f32x4_t{o[ct][4 * h][r], o[ct][4 * h + 1][r], o[ct][4 * h + 2][r], o[ct][4 * h + 3][r]};
     }
-    if (chunks == 1) {
-      const int i = (col0 + c) / p.g;
-      float* to = p.out + ((span.row + i) * p.Hq + kvh * p.g + (col0 + c - i * p.g)) * D + x;
-      *reinterpret_cast<f32x4_t*>(to) = r * (1.f / sum);
-    } else {
-      store2_past(mine + c * D + x, r[0], r[1]);
-      store2_past(mine + c * D + x + 2, r[2], r[3]);
-      if (x == 0) store2_past(mine + COLS * D + 2 * c, top, sum);
-    }
-  }
-  if (chunks == 1) return;
-  // the workgroup that arrives last adds the parts up, in their order
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (tid == 0) s_last = __hip_atomic_fetch_add(p.arrivals + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (s_last != chunks - 1) return;
-  if (tid == 0) __hip_atomic_store(p.arrivals + pair, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const float* parts = p.part + (int64_t)pair * p.max_chunks * COLS * (D + 2);
-  for (int at = tid; at < own * (D / 2); at += 64 * NW) {
-    const int c = at / (D / 2), x = 2 * (at % (D / 2));
-    float top = kNegBig, sum = 0.f, r0 = 0.f, r1 = 0.f;
-    for (int k0 = 0; k0 < chunks; k0 += 8) {
-      uint64_t ml[8], r[8];
+    __syncthreads();
+    const bool whole = count == 1;
+    const uint32_t mine = (pair * p.max_chunks + chunk) * (SUMS * 4);
+    auto result = [&](int c, int x) {            // where element x of a column goes
+      const int i = c / p.g;
+      return reinterpret_cast<f32x4_t*>(p.out + ((span.row + i) * p.Hq + kvh * p.g + (c - i * p.g)) * D + x);
+    };
+    for (int at = tid; at < own * (D / 4); at += 64 * NW) {
+      const int c = at / (D / 4), x = 4 * (at % (D / 4));
+      float top = kNegBig;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float* one = parts + (int64_t)min(k0 + k, chunks - 1) * COLS * (D + 2);
-        ml[k] = load2_past(one + COLS * D + 2 * c);
-        r[k] = load2_past(one + c * D + x);
+      for (int w = 0; w < NW; ++w) top = fmaxf(top, s_ml[w][c][0]);
+      float sum = 0.f;
+      f32x4_t r{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float f = fast_exp2(s_ml[w][c][0] - top);
+        sum += f * s_ml[w][c][1];
+        r += f * *reinterpret_cast<const f32x4_t*>(&s_o[w][c][x]);
       }
-      float high = top;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) high = fmaxf(high, low_of(ml[k]));
-      const float was = fast_exp2(top - high);
-      top = high; sum *= was; r0 *= was; r1 *= was;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float f = k0 + k < chunks ? fast_exp2(low_of(ml[k]) - top) : 0.f;
-        sum += f * high_of(ml[k]); r0 += f * low_of(r[k]); r1 += f * high_of(r[k]);
+      if (whole) *result(c, x) = r * (1.f / sum);
+      else {
+        store16_past(parts, mine + 4 * (c * D + x), r);
+        if (x == 0) store8_past(parts, mine + 4 * (COLS * D + 2 * c), top, sum);
       }
     }
-    const int i = (col0 + c) / p.g;
-    float* to = p.out + ((span.row + i) * p.Hq + kvh * p.g + (col0 + c - i * p.g)) * D + x;
-    const float f = 1.f / sum;
-    to[0] = r0 * f; to[1] = r1 * f;
+    if (whole) return;
+    // the workgroup that arrives last adds the parts up, in their order
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) s_last = __hip_atomic_fetch_add(p.arrivals + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (s_last != (int)count - 1) return;
+    if (tid == 0) __hip_atomic_store(p.arrivals + pair, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // A column's piece of four elements is a thread's, or (few columns) several threads' by turns; their sums meet in LDS.
+    const int pieces = own * (D / 4);
+    int teams = 1;
+    while (2 * teams * pieces <= 64 * NW) teams *= 2;
+    const int team = teams > 1 ? tid / pieces : 0;             // (threads behind the last team have nothing to do)
+    auto add_up = [&](auto together) {
+      constexpr int N = decltype(together)::value;             // parts that a thread asks for at once
+      for (int at = tid - team * pieces; at < pieces && team < teams; at += 64 * NW) {
+        const int c = at / (D / 4), x = 4 * (at % (D / 4));
+        float top = kNegBig, sum = 0.f;
+        f32x4_t r{0.f, 0.f, 0.f, 0.f};
+        for (uint32_t k0 = team; k0 < count; k0 += N * teams) {
+          u32x2_v ml[N];
+          f32x4_t part[N];
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            const uint32_t place = (pair * p.max_chunks + min(k0 + k * teams, count - 1)) * (SUMS * 4);
+            ml[k] = load8_past(parts, place + 4 * (COLS * D + 2 * c));
+            part[k] = load16_past(parts, place + 4 * (c * D + x));
+          }
+          float high = top;
+#pragma unroll
+          for (int k = 0; k < N; ++k) high = fmaxf(high, __uint_as_float(ml[k][0]));
+          const float was = fast_exp2(top - high);
+          top = high; sum *= was; r *= was;
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            const float f = k0 + k * teams < count ? fast_exp2(__uint_as_float(ml[k][0]) - top) : 0.f;
+            sum += f * __uint_as_float(ml[k][1]);
+            r += f * part[k];
+          }
+        }
+        if (teams == 1) *result(c, x) = r * (1.f / sum);
+        else {
+          *reinterpret_cast<f32x4_t*>(&s_o[0][0][0] + (team * pieces + at) * 4) = r;
+          if (x == 0) { s_team[team * own + c][0] = top; s_team[team * own + c][1] = sum; }
+        }
+      }
+    };
+    if (count <= 4u * teams) add_up(std::integral_constant<int, 4>{});
+    else if (count <= 8u * teams) add_up(std::integral_constant<int, 8>{});
+    else add_up(std::integral_constant<int, 16>{});
+    if (teams > 1) {
+      __syncthreads();
+      if (tid < pieces) {
+        const int c = tid / (D / 4), x = 4 * (tid % (D / 4));
+        float top = kNegBig, sum = 0.f;
+        for (int k = 0; k < teams; ++k) top = fmaxf(top, s_team[k * own + c][0]);
+        f32x4_t r{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < teams; ++k) {
+          const float f = fast_exp2(s_team[k * own + c][0] - top);
+          sum += f * s_team[k * own + c][1];
+          r += f * *reinterpret_cast<const f32x4_t*>(&s_o[0][0][0] + (k * pieces + tid) * 4);
+        }
+        *result(c, x) = r * (1.f / sum);
+      }
+    }
   }
 }
 
-struct AttendLaunch {
-  int ct, waves, column_blocks, max_chunks, chunk_tiles;
-  size_t part_bytes;
-  bool fits;
-};
-AttendLaunch plan_attend(const bc_shape* sh, int64_t max_new, int64_t max_len) {
-  AttendLaunch a{};
-  const int64_t g = sh->Hq / sh->Hkv, columns = max_new * g, pairs = (int64_t)sh->B * sh->Hkv;
-  a.ct = columns <= 16 ? 1 : 2;
-  a.waves = 4;
-  const int64_t blocks = (columns + 16 * a.ct - 1) / (16 * a.ct), tiles = (max_len + 31) / 32;
-  int64_t chunks = 1;
-  a.chunk_tiles = 4;
-  if (blocks == 1) {
-    chunks = (1024 + pairs - 1) / pairs;
-    if (chunks > 64) chunks = 64;
-    if (chunks > (tiles + 3) / 4) chunks = (tiles + 3) / 4;
-    if (chunks < 1) chunks = 1;
-  }
-  a.max_chunks = (int)chunks;
-  a.fits = columns <= 0x7fffffff && pairs * blocks * chunks <= 0x7fffffff;
-  a.column_blocks = (int)blocks;
-  a.part_bytes = chunks > 1 ? (size_t)(pairs * chunks * 16 * a.ct * (sh->d + 2)) * 4 : 0;
-  return a;
+
+// ---------------------------------------------------------------------------
+// Many columns: 32 a wave, the workgroup's four share the tiles of 32 entries.  A tile comes as bytes, 16 a lane and a kilobyte a wave in a row, becomes bf16 once and goes
+// to LDS as the operands of 32x32x16 products: keys [d / 16][half][key], element 16 i + 8 half + e of a key; values [block][16 keys][half][element], the block's
+// elements four apart, so that a word's four keys are half of an operand and results have four elements in a row.
+// ---------------------------------------------------------------------------
+constexpr int kManyWaves = 4, kManyColumns = 32 * kManyWaves;
+constexpr float kRedo = 256.f;      // a lane's 16 weights may sum to this before the reference moves
+constexpr float kLazy = 2.f;        // ... where a column's maximum is this much (log2) above it
+
+// Tiles of a block of columns, and those of one of its parts.
+struct ManyCut { int tiles, t0, t1, parts; };
+__device__ __forceinline__ ManyCut many_cut(int parts, int lim, int part) {
+  const int tiles = (lim + 31) >> 5, most = max(1, tiles >> 3), n = min(parts, most);      // (no part of fewer than eight tiles)
+  return {tiles, (int)((int64_t)tiles * part / n), (int)((int64_t)tiles * (part + 1) / n), n};
 }
 
 template <int D>
+__global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendParams p) {
+  constexpr int KS = D / 16, NJ = D / 32, K_BYTES = 32 * D * 2, STAGE = 2 * K_BYTES, LOADS = D / 64, BLOCK_BYTES = kPagedBlock * D;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+  __shared__ float2 s_scale[2][2];                               // [stage][block] of keys (with scale * log2 e) and of values
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+  const uint32_t pairs = (uint32_t)p.t.B * p.Hkv;
+  uint32_t id = blockIdx.x;
+  const int pair = id % pairs; id /= pairs;
+  const int part = id % p.parts, block = p.blocks - 1 - id / p.parts;          // (the longest ones first)
+  const int s = pair / p.Hkv, kvh = pair - s * p.Hkv;
+  const AttendSpan span = attend_span(p, s);
+  if (span.bad && block == 0 && part == 0 && kvh == 0 && tid == 0) atomicOr(p.t.err, BC_ERRBIT_STATE);
+  const int n = span.n, L = span.L, columns = n * p.g, first = block * kManyColumns;
+  if (first >= columns) return;
+  const int last_row = (min(first + kManyColumns, columns) - 1) / p.g;
+  const ManyCut cut = many_cut(p.parts, L - n + 1 + last_row, part);
+  if (part >= cut.parts) return;
+
+  const int mine = first + 32 * wave, c = min(mine + col, columns - 1), i = c / p.g;
+  const int lim = L - n + 1 + i;                                 // entries that this lane's column sees
+  const int free_tiles = (L - n + 1 + min(mine, columns - 1) / p.g) >> 5;      // tiles that all of the wave's columns see whole
+  bf16x8_t qb[KS];
+  {
+    const char* at = p.q + ((span.row + i) * p.Hq + kvh * p.g + (c - i * p.g)) * (2 * D) + 16 * half;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) qb[k] = *reinterpret_cast<const bf16x8_t*>(at + 32 * k);
+  }
+  f32x16_t O[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) O[j] = f32x16_t{0.f};
+  float m = kNegBig, l = 0.f;
+
+  // A tile's bytes: LOADS of keys and of values a wave, each a kilobyte of one block (d = 64: two waves have the keys, two the values).
+  const int per_page = p.t.page_shift - 4;
+  const uint32_t unit_of_last = (L - 1) >> 4;
+  auto unit_at = [&](int b) -> uint32_t {                        // block b of the sequence: where its bytes and scales are
+    b = min(b, (int)unit_of_last);
+    int page = p.t.table[(int64_t)s * p.t.table_pages + (b >> per_page)];
+    if ((uint32_t)page >= (uint32_t)p.t.pages) {
+      if (lane == 0) atomicOr(p.t.err, BC_ERRBIT_STATE);
+      page = 0;
+    }
+    return (((uint32_t)page * p.Hkv + kvh) << per_page) + (b & ((1 << per_page) - 1));
+  };
+  u32x4_t bytes[LOADS];
+  float2 scales{0.f, 0.f};
+  auto fetch = [&](int t) {
+    if (D == 128) {
+      const uint32_t u = unit_at(2 * t + (wave >> 1));
+      const uint64_t at = (uint64_t)u * BLOCK_BYTES + (wave & 1) * 1024 + lane * 16;
+      bytes[0] = *reinterpret_cast<const u32x4_t*>(p.k + at);
+      bytes[LOADS - 1] = *reinterpret_cast<const u32x4_t*>(p.v + at);
+      scales = make_float2(p.ks[u] * p.qs, p.vs[u]);
+    } else {
+      const uint32_t u = unit_at(2 * t + (wave & 1));
+      bytes[0] = *reinterpret_cast<const u32x4_t*>((wave < 2 ? p.k : p.v) + (uint64_t)u * BLOCK_BYTES + lane * 16);
+      scales = make_float2(p.ks[u] * p.qs, p.vs[u]);
+    }
+  };
+  auto put_keys = [&](char* to, const u32x4_t& x, int at) {      // at: the lane's 16 bytes of the tile
+    const int group = at / (D / 4), h = at / 16 % (D / 64), row = 4 * group + at / 4 % 4, k = 4 * h + at % 4;
+    char* place = to + k * 1024 + ((row ^ (2 * (k & 3))) * 16);
+    *reinterpret_cast<bf16x8_t*>(place) = operand_of(x[0], x[1]);
+    *reinterpret_cast<bf16x8_t*>(place + 512) = operand_of(x[2], x[3]);
+  };
+  auto put_values = [&](char* to, u32x4_t x, int at, int t) {
+    const int group = at / (D / 4), e = at % (D / 4);
+    if (32 * t + 32 > L) {                                       // bytes behind the last entry may be anything
+      const int there = L - 32 * t - 4 * group;
+      const uint32_t keep = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] &= keep;
+    }
+    // group: (16 keys, second half of the operand, half of the wave)
+    char* place = to + (group >> 2) * 1024 + (group & 1) * 512 + (group >> 1 & 1) * 8;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t w = (uint64_t)bf16_of(x[j], true) << 32 | bf16_of(x[j], false);
+      const int blk = D == 128 ? j : j & 1, row = D == 128 ? e : (j >> 1) * 16 + e;
+      *reinterpret_cast<uint64_t*>(place + blk * 2048 + row * 16) = w;
+    }
+  };
+  auto put = [&](int t, int stage) {
+    char* to = lds + stage * STAGE;
+    if (D == 128) {
+      put_keys(to, bytes[0], wave * 64 + lane);
+      put_values(to + K_BYTES, bytes[LOADS - 1], wave * 64 + lane, t);
+      if ((wave & 1) == 0 && lane == 0) s_scale[stage][wave >> 1] = scales;
+    } else {
+      if (wave < 2) put_keys(to, bytes[0], wave * 64 + lane);
+      else put_values(to + K_BYTES, bytes[0], (wave - 2) * 64 + lane, t);
+      if (wave < 2 && lane == 0) s_scale[stage][wave] = scales;
+    }
+  };
+
+  fetch(cut.t0);
+  put(cut.t0, 0);
+  if (cut.t0 + 1 < cut.t1) fetch(cut.t0 + 1);
+  __syncthreads();
+  const int seen = mine < columns ? (L - n + 1 + (min(mine + 32, columns) - 1) / p.g + 31) >> 5 : 0;        // tiles that the wave works on
+  for (int t = cut.t0, stage = 0; t < cut.t1; ++t, stage ^= 1) {
+    if (t + 1 < cut.t1) put(t + 1, stage ^ 1);
+    if (t + 2 < cut.t1) fetch(t + 2);
+    if (t < seen) {
+      const char* tile = lds + stage * STAGE;
+      f32x16_t sc = f32x16_t{0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_t*>(tile + k * 1024 + half * 512 + ((col ^ (2 * (k & 3))) * 16)), qb[k], sc, 0, 0, 0);
+      const float2 f0 = s_scale[stage][0], f1 = s_scale[stage][1];
+      // result e: entry 8 (e / 4) + 4 half + e % 4 of the tile
+      if (t >= free_tiles) {
+        const int there = lim - 32 * t - 4 * half;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = 8 * (e >> 2) + (e & 3) < there ? sc[e] * (e < 8 ? f0.x : f1.x) : kMasked;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] *= e < 8 ? f0.x : f1.x;
+      }
+      float pe[16], psum;
+      auto weights = [&]() {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) pe[e] = fast_exp2(sc[e] - m);
+        psum = (((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]))) +
+               (((pe[8] + pe[9]) + (pe[10] + pe[11])) + ((pe[12] + pe[13]) + (pe[14] + pe[15])));
+      };
+      weights();
+      if (__builtin_expect(__any(psum > kRedo), 0)) {
+        float top = kMasked;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[e]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float to = top > m + kLazy ? top : m, was = fast_exp2(m - to);
+        m = to; l *= was;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) O[j] *= was;
+        weights();
+      }
+      l += psum;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) pe[e] *= e < 8 ? f0.y : f1.y;
+      u32x4_t hi[2], lo[2];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const uint32_t h = pack2_bf16(pe[2 * x], pe[2 * x + 1]);
+        hi[x >> 2][x & 3] = h;
+        lo[x >> 2][x & 3] = pack2_bf16(pe[2 * x] - __uint_as_float(h << 16), pe[2 * x + 1] - __uint_as_float(h & 0xffff0000u));
+      }
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(tile + K_BYTES + j * 2048 + kk * 1024 + half * 512 + col * 16);
+          O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8_t, hi[kk]), O[j], 0, 0, 0);
+          O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8_t, lo[kk]), O[j], 0, 0, 0);
+        }
+    }
+    __syncthreads();
+  }
+  if (mine + col >= columns) return;
+  l += __shfl_xor(l, 32, 64);
+  const int64_t at = (span.row + i) * p.Hq + kvh * p.g + (c - i * p.g);
+  const bool whole = cut.parts == 1;
+  float* to = whole ? p.out + at * D : p.part + (part * (p.t.rows * p.Hq) + at) * D;
+  const float f = whole ? 1.f / l : 1.f;
+  if (!whole && half == 0) p.part_ml[part * (p.t.rows * p.Hq) + at] = make_float2(m, l);
+  // result e of block j: its row 8 (e / 4) + 4 half + e % 4
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int row = 8 * (e >> 2) + 4 * half + (e & 3);
+    if constexpr (D == 128) *reinterpret_cast<f32x4_t*>(to + 4 * row) = f32x4_t{O[0][e] * f, O[1][e] * f, O[NJ - 2][e] * f, O[NJ - 1][e] * f};
+    else *reinterpret_cast<f32x2_v*>(to + 4 * (row & 15) + 2 * (row >> 4)) = f32x2_v{O[0][e] * f, O[1][e] * f};
+  }
+}
+
+// The parts of many columns: a column's pieces of four elements a thread each.
+template <int D>
+__global__ void __launch_bounds__(256) paged_fold_kernel(AttendParams p) {
+  constexpr int UNITS = D / 4, PER = 256 / UNITS;
+  const int64_t pairs = (int64_t)p.t.B * p.Hkv;
+  const int pair = blockIdx.x % pairs, s = pair / p.Hkv, kvh = pair - s * p.Hkv;
+  const int c = (int)(blockIdx.x / pairs) * PER + threadIdx.x / UNITS, unit = threadIdx.x % UNITS;
+  const AttendSpan span = attend_span(p, s);
+  const int columns = span.n * p.g;
+  if (c >= columns) return;
+  const int i = c / p.g, last_row = (min(c / kManyColumns * kManyColumns + kManyColumns, columns) - 1) / p.g;
+  const ManyCut cut = many_cut(p.parts, span.L - span.n + 1 + last_row, 0);
+  if (cut.parts == 1) return;
+  const int64_t at = (span.row + i) * p.Hq + kvh * p.g + (c - i * p.g), step = p.t.rows * p.Hq;
+  float top = kNegBig, sum = 0.f;
+  f32x4_t r{0.f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < cut.parts; k0 += 8) {
+    float2 ml[8];
+    f32x4_t x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t from = min(k0 + k, cut.parts - 1) * step + at;
+      ml[k] = p.part_ml[from];
+      x[k] = *reinterpret_cast<const f32x4_t*>(p.part + from * D + 4 * unit);
+    }
+    float high = top;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) high = fmaxf(high, ml[k].x);
+    const float was = fast_exp2(top - high);
+    top = high; sum *= was; r *= was;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float f = k0 + k < cut.parts ? fast_exp2(ml[k].x - top) : 0.f;
+      sum += f * ml[k].y; r += f * x[k];
+    }
+  }
+  *reinterpret_cast<f32x4_t*>(p.out + at * D + 4 * unit) = r * (1.f / sum);
+}
+
+struct AttendLaunch {
+  int ct, waves, max_chunks, chunk_tiles;      // few columns
+  bool stream;
+  int blocks, parts;           // many
+  size_t part_bytes, ml_at;
+  bool fits;
+};
+constexpr int kMostParts = 16, kManyGroups = 512;
+constexpr int64_t kStreamBytes = 96 << 20;
+AttendLaunch plan_attend(const bc_shape* sh, int64_t rows, int64_t max_new, int64_t max_len) {
+  AttendLaunch a{};
+  const int64_t g = sh->Hq / sh->Hkv, columns = max_new * g, pairs = (int64_t)sh->B * sh->Hkv, tiles = (max_len + 31) / 32;
+  if (columns > 0x7fffffff) return a;
+  if (columns <= 32) {
+    a.ct = columns <= 16 ? 1 : 2;
+    a.waves = pairs <= 256 && tiles >= (a.ct == 1 ? 62 : 32) ? 8 : 4;
+    a.stream = pairs * max_len * 2 * sh->d > kStreamBytes;
+    const int64_t groups = a.waves == 8 ? 256 : 512, most = groups / pairs < 1 ? 1 : groups / pairs, each = (tiles + most - 1) / most;
+    a.chunk_tiles = (int)(each < a.waves ? a.waves : each);
+    a.max_chunks = (int)((tiles + a.chunk_tiles - 1) / a.chunk_tiles);
+    a.part_bytes = a.max_chunks > 1 ? (size_t)(pairs * a.max_chunks) * 16 * a.ct * (sh->d + 2) * 4 : 0;
+    a.fits = true;
+    return a;
+  }
+  a.blocks = (int)((columns + kManyColumns - 1) / kManyColumns);
+  const int64_t groups = pairs * a.blocks;
+  int64_t parts = kManyGroups / groups;
+  if (parts > kMostParts) parts = kMostParts;
+  if (parts > tiles / 8) parts = tiles / 8;
+  if (parts < 1) parts = 1;
+  a.parts = (int)parts;
+  const int64_t fold = pairs * ((columns + 1024 / sh->d - 1) / (1024 / sh->d));
+  a.fits = groups * parts <= 0x7fffffff && fold <= 0x7fffffff;
+  if (parts > 1) {
+    a.ml_at = (size_t)(parts * rows * sh->Hq) * sh->d * 4;
+    a.part_bytes = a.ml_at + (size_t)(parts * rows * sh->Hq) * 8;
+  }
+  return a;
+}
+
+template <int D, int CT, int NW>
+void launch_few(const AttendParams& p, const AttendLaunch& a, hipStream_t s) {
+  const unsigned groups = (unsigned)((int64_t)p.t.B * p.Hkv * a.max_chunks);
+  if (a.stream) paged_few_kernel<D, CT, NW, true><<<groups, 64 * NW, 0, s>>>(p);
+  else paged_few_kernel<D, CT, NW, false><<<groups, 64 * NW, 0, s>>>(p);
+}
+template <int D>
 void launch_attend(const AttendParams& p, const AttendLaunch& a, hipStream_t s) {
-  const unsigned grid = (unsigned)((int64_t)p.t.B * p.Hkv * a.column_blocks * a.max_chunks);
-  if (a.ct == 1) paged_few_kernel<D, 1, 4><<<grid, 256, 0, s>>>(p);
-  else paged_few_kernel<D, 2, 4><<<grid, 256, 0, s>>>(p);
+  if (a.ct) {
+    if (a.ct == 1) { if (a.waves == 8) launch_few<D, 1, 8>(p, a, s); else launch_few<D, 1, 4>(p, a, s); }
+    else { if (a.waves == 8) launch_few<D, 2, 8>(p, a, s); else launch_few<D, 2, 4>(p, a, s); }
+    return;
+  }
+  const int64_t pairs = (int64_t)p.t.B * p.Hkv;
+  paged_many_kernel<D><<<(unsigned)(pairs * a.blocks * a.parts), 64 * kManyWaves, 0, s>>>(p);
+  if (a.parts > 1) {
+    const int64_t columns = (int64_t)p.t.max_new * p.g, per = 1024 / D;
+    paged_fold_kernel<D><<<(unsigned)(pairs * ((columns + per - 1) / per)), 256, 0, s>>>(p);
+  }
 }
 
 int64_t longest(const bc_pages* pg) {
@@ -352,17 +657,11 @@ int64_t longest(const bc_pages* pg) {
 
 using namespace bc;
 
-extern "C" size_t bc_paged_workspace_bytes(const bc_shape* shape, int32_t max_new, int32_t max_len) {
-  if (check_shape(shape) != BC_OK || max_new < 0 || max_len < 1 || (int64_t)shape->B * shape->Hkv > (1 << 23)) return 0;
-  if (!plan_attend(shape, max_new, max_len).fits) return 0;
-  // (fewer rows may be cut where more are not)
-  size_t most = 0;
-  const int64_t g = shape->Hq / shape->Hkv;
-  for (int64_t n : {(int64_t)1, 16 / g, 32 / g, (int64_t)max_new}) {
-    const AttendLaunch a = plan_attend(shape, n < max_new ? n : max_new, max_len);
-    if (a.fits && a.part_bytes > most) most = a.part_bytes;
-  }
-  return most + 16;
+extern "C" size_t bc_paged_workspace_bytes(const bc_shape* shape, int64_t rows, int32_t max_new, int32_t max_len) {
+  if (check_shape(shape) != BC_OK || rows < 0 || rows > 0x7fffffff || max_new < 0 || max_len < 1 || (int64_t)shape->B * shape->Hkv > (1 << 23)) return 0;
+  const int64_t most = max_new < rows ? max_new : rows;
+  const AttendLaunch a = plan_attend(shape, rows, most < max_len ? most : max_len, max_len);
+  return a.fits ? a.part_bytes + 16 : 0;
 }
 
 extern "C" int32_t bc_paged_attend(const bc_shape* shape, const bc_pages* pages, int64_t rows, const int64_t* row_offsets, int32_t max_new,
@@ -377,7 +676,7 @@ extern "C" int32_t bc_paged_attend(const bc_shape* shape, const bc_pages* pages,
   // (a sequence cannot have more new rows than there are, nor than entries)
   int64_t most = max_new < rows ? max_new : rows;
   if (most > max_len) most = max_len;
-  const AttendLaunch a = plan_attend(shape, most, max_len);
+  const AttendLaunch a = plan_attend(shape, rows, most, max_len);
   if (!a.fits) return BC_ERR_SHAPE;
   if (a.part_bytes && (!workspace || !aligned16(workspace) || workspace_bytes < a.part_bytes)) return BC_ERR_WORKSPACE;
   AttendParams p{};
@@ -385,8 +684,9 @@ extern "C" int32_t bc_paged_attend(const bc_shape* shape, const bc_pages* pages,
   p.q = static_cast<const char*>(q); p.out = out;
   p.k = static_cast<const uint8_t*>(pages->k); p.v = static_cast<const uint8_t*>(pages->v); p.ks = pages->k_scale; p.vs = pages->v_scale;
   p.arrivals = pages->arrivals; p.part = static_cast<float*>(workspace);
+  p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + a.ml_at);
   p.Hq = shape->Hq; p.Hkv = shape->Hkv; p.g = shape->Hq / shape->Hkv; p.max_len = (int32_t)max_len;
-  p.column_blocks = a.column_blocks; p.max_chunks = a.max_chunks; p.chunk_tiles = a.chunk_tiles;
+  p.max_chunks = a.max_chunks; p.chunk_tiles = a.chunk_tiles; p.blocks = a.blocks; p.parts = a.parts;
   p.qs = shape->scale * kLog2e;
   if (shape->d == 128) launch_attend<128>(p, a, as_stream(stream)); else launch_attend<64>(p, a, as_stream(stream));
   return launch_status();
