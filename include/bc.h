@@ -455,7 +455,7 @@ typedef struct {
   const int32_t *table;    /* [B, table_pages] pages of every sequence              */
   int32_t *len;            /* [B] entries of every sequence (updated by bc_paged_append) */
   int32_t *err;            /* [1] sticky error bits                                 */
-  int32_t *arrivals;       /* [B * Hkv] counters of bc_paged_attend: zero at first, left at zero */
+  int32_t *arrivals;       /* [B * Hkv] counters of the calls: zero at first, left at zero */
   int32_t pages;           /* HOST values: pages of the pool                        */
   int32_t page_rows;       /* a power of two from 16 to 1024                        */
   int32_t table_pages;     /* entries of a row of the table                         */
@@ -472,7 +472,7 @@ typedef struct {
  * What is not finite is stored as a NaN and does not count for the scale.  Bytes behind the last entry stay as they were.
  * A sequence that is not active or has no rows is left alone, and its rows of q with it; so is one with an invalid span, length, keep (0 .. len) or page, which sets
  * the state bit, and one that its row of the table cannot hold, which sets the capacity bit.  A page that is written to belongs to one sequence
- * (shared pages are whole ones in front of it).  No limits beyond bc_qk_norm_rope's but B * Hkv <= 2^23, fewer than 2^31 rows, blocks of 16 in a pool (of a head) and
+ * (shared pages are whole ones in front of it).  Calls that share arrivals must not overlap in time.  No limits beyond bc_qk_norm_rope's but B * Hkv <= 2^23, fewer than 2^31 rows, blocks of 16 in a pool (of a head) and
  * entries in a table's row. */
 int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t rows, const int64_t *row_offsets,
                         int32_t max_new, const void *qkv, int64_t qkv_row_stride, const int32_t *positions,

@@ -76,11 +76,12 @@ _lib = None
 _call = None                  # the function of csrc/bc_call.cpp (None where there is no such module), with
 _call_lib = None              # the library whose entry point it calls, and
 _decode_step_at = None        # its address there
+_paged_calls = None           # (append, its entry point's address, attend, its), where there is such a module
 
 
 def load():
     """Load libbc.so and declare the signatures; raises if the library or a symbol is missing."""
-    global _lib, _call, _call_lib, _decode_step_at
+    global _lib, _call, _call_lib, _decode_step_at, _paged_calls
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -170,6 +171,9 @@ def load():
         pass
     else:
         call, at = _bc_call.decode_step, C.cast(lib.bc_decode_step, C.c_void_p).value
+        if hasattr(_bc_call, "paged_append"):
+            _paged_calls = (_bc_call.paged_append, C.cast(lib.bc_paged_append, C.c_void_p).value,
+                            _bc_call.paged_attend, C.cast(lib.bc_paged_attend, C.c_void_p).value)
     # (another thread may be in a step already: nothing it uses is taken away)
     _call, _decode_step_at, _call_lib = call, at, lib if call else None
     _lib = lib
@@ -414,6 +418,13 @@ def _stream_ptr():
         _torch_stream = torch.Stream
         _torch_c = torch._C
     return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice())
+
+
+def _current_device():
+    if _torch_c is not None:
+        return _torch_c._cuda_getDevice()
+    import torch
+    return torch.cuda.current_device()
 
 
 def _ptr(t):
@@ -748,6 +759,7 @@ class PagedCache:
         self.k_pages, self.v_pages = (torch.full(size, 0x7f, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
         self.k_scale, self.v_scale = (torch.full((self.pages, self.Hkv, self.page_rows // 16), float("nan"), device=device) for _ in range(2))
         self.device = self.k_pages.device
+        self._width = (self.Hq + 2 * self.Hkv) * self.d
         if table is None:
             table = torch.zeros(self.B, self.table_pages, dtype=torch.int32, device=device)
         else:
@@ -763,9 +775,9 @@ class PagedCache:
     def _own(self):
         return self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.table, self.lengths, self.err, self._arrivals
 
-    def _rows(self, x, row_offsets, max_new, active):
+    def _rows(self, rows, row_offsets, max_new, active):
         """Checks what both calls take; -> (row_offsets on the device or None, max_new)."""
-        torch, rows, dev = self.torch, x.shape[0], self.device
+        torch, dev = self.torch, self.device
         if active is not None:
             _is(active, "active", torch.uint8, (self.B,), dev)
         if row_offsets is None:
@@ -787,33 +799,50 @@ class PagedCache:
         _check(bc_trajectory_tables(off.ctypes.data, zeros.ctypes.data, zeros.ctypes.data, self.B, on_device.data_ptr(), _stream_ptr()))
         return on_device, int(n.max())
 
+    # (A step's kernels take 4 us and up and its calls took 11 and 9: as for Runtime.decode_step, by functions of csrc/bc_call.cpp where they are there.)
     def append(self, qkv, positions, inv_freq, row_offsets=None, max_new=None, q_weight=None, k_weight=None, eps=1e-6, keep=None,
                active=None, q=None):
         """bc_paged_append: qkv [rows, (Hq + 2 Hkv) d] (rows may lie apart), positions [rows] int32, inv_freq [rot / 2] fp32, weights [d] or None, keep [B]
         int32 or None, active [B] uint8 or None.  row_offsets [B + 1]: None (a row a sequence), host integers, or an int64 device tensor with max_new, the longest span.
         Returns q [rows, Hq, d] bf16 (rows of sequences that take no part: as they were, in a new tensor unspecified)."""
         torch, dev = self.torch, self.device
-        if dev.index != torch.cuda.current_device():           # the stream is that device's
+        if dev.index != _current_device():                     # the stream is that device's
             with torch.cuda.device(dev):
                 return self.append(qkv, positions, inv_freq, row_offsets, max_new, q_weight, k_weight, eps, keep, active, q)
-        Hq, Hkv, d = self.Hq, self.Hkv, self.d
-        _, rows, stride, rot = _rope_rows(qkv, positions, inv_freq, Hq, Hkv, d, q_weight, k_weight)
-        if qkv.dtype != self.dtype or qkv.device != dev:
-            raise BcError("qkv must be a %s tensor on %s" % (self.dtype, dev))
-        offsets, most = self._rows(qkv, row_offsets, max_new, active)
+        d, dtype, i32 = self.d, self.dtype, torch.int32
+        rows, width = qkv.shape if qkv.dim() == 2 else (0, 0)
+        if width != self._width or qkv.dtype != dtype or qkv.device != dev or not qkv.is_cuda:
+            raise BcError("qkv must be a %s tensor [rows, %d] on %s" % (dtype, self._width, dev))
+        stride, inner = qkv.stride()
+        if rows and inner != 1:
+            raise BcError("elements of a row of qkv must lie back to back")
+        _is(positions, "positions", i32, (rows,), dev)
+        half = inv_freq.numel()
+        _is(inv_freq, "inv_freq", torch.float32, (half,), dev)
+        if q_weight is not None:
+            _is(q_weight, "q_weight", dtype, (d,), dev)
+        if k_weight is not None:
+            _is(k_weight, "k_weight", dtype, (d,), dev)
+        offsets, most = self._rows(rows, row_offsets, max_new, active)
         if keep is not None:
-            _is(keep, "keep", torch.int32, (self.B,), dev)
+            _is(keep, "keep", i32, (self.B,), dev)
         given = q
         if q is None:
-            q = torch.empty((rows, Hq, d), dtype=torch.bfloat16, device=dev)
+            q = torch.empty((rows, self.Hq, d), dtype=torch.bfloat16, device=dev)
         else:
-            _is(q, "q", torch.bfloat16, (rows, Hq, d), dev)
+            _is(q, "q", torch.bfloat16, (rows, self.Hq, d), dev)
         stream = _stream_ptr()
-        st = (_lib or load()).bc_paged_append(*self._refs, rows, _ptr(offsets), most, qkv.data_ptr(), stride, positions.data_ptr(), inv_freq.data_ptr(),
-                                              rot, _ptr(q_weight), _ptr(k_weight), eps, _ptr(keep), _ptr(active), q.data_ptr(), stream)
+        if rows <= 1:
+            stride = width
+        if _paged_calls is not None:
+            st = _paged_calls[0](_paged_calls[1], self.shape, self._c, rows, offsets, most, qkv, stride, positions, inv_freq, 2 * half, q_weight, k_weight,
+                                 eps, keep, active, q, stream)
+        else:
+            st = (_lib or load()).bc_paged_append(*self._refs, rows, _ptr(offsets), most, qkv.data_ptr(), stride, positions.data_ptr(), inv_freq.data_ptr(),
+                                                  2 * half, _ptr(q_weight), _ptr(k_weight), eps, _ptr(keep), _ptr(active), q.data_ptr(), stream)
         if st != BC_OK:
             _check(st)
-        _used_here(qkv, positions, inv_freq, q_weight, k_weight, keep, active, given, offsets)
+        _used_here(qkv, positions, inv_freq, q_weight, k_weight, keep, active, given, offsets if offsets is row_offsets else None)
         if stream != self._home:
             _used_here(*self._own())
         return q
@@ -822,12 +851,13 @@ class PagedCache:
         """bc_paged_attend: q [rows, Hq, d] bf16, the rows of the newest entries; row_offsets, max_new, active as for append; max_len: no sequence is longer
         (None: what the table holds).  Returns out [rows, Hq, d] fp32 (rows of sequences that take no part: as they were, in a new tensor unspecified)."""
         torch, dev = self.torch, self.device
-        if dev.index != torch.cuda.current_device():           # the stream, and the workspace's, are that device's
+        if dev.index != _current_device():                     # the stream, and the workspace's, are that device's
             with torch.cuda.device(dev):
                 return self.attend(q, row_offsets, max_new, max_len, active, out)
-        size = (q.shape[0], self.Hq, self.d)
+        rows = q.shape[0]
+        size = (rows, self.Hq, self.d)
         _is(q, "q", torch.bfloat16, size, dev)
-        offsets, most = self._rows(q, row_offsets, max_new, active)
+        offsets, most = self._rows(rows, row_offsets, max_new, active)
         given = out
         if out is None:
             out = torch.empty(size, dtype=torch.float32, device=dev)
@@ -838,13 +868,16 @@ class PagedCache:
             longest = max(1, min(int(max_len), longest))
         self._c.max_len = longest
         lib, (shape, pages) = _lib or load(), self._refs
-        nbytes = lib.bc_paged_workspace_bytes(shape, size[0], most, longest)
+        nbytes = lib.bc_paged_workspace_bytes(shape, rows, most, longest)
         ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
         stream = _stream_ptr()
-        st = lib.bc_paged_attend(shape, pages, size[0], _ptr(offsets), most, q.data_ptr(), out.data_ptr(), _ptr(active), ws.data_ptr(), nbytes, stream)
+        if _paged_calls is not None:
+            st = _paged_calls[2](_paged_calls[3], self.shape, self._c, rows, offsets, most, q, out, active, ws, nbytes, stream)
+        else:
+            st = lib.bc_paged_attend(shape, pages, rows, _ptr(offsets), most, q.data_ptr(), out.data_ptr(), _ptr(active), ws.data_ptr(), nbytes, stream)
         if st != BC_OK:
             _check(st)
-        _used_here(q, active, given, offsets)
+        _used_here(q, active, given, offsets if offsets is row_offsets else None)
         if stream != self._home:
             _used_here(*self._own())
         return out

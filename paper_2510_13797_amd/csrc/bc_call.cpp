@@ -1,4 +1,4 @@
-// The Python decode step's call of the C ABI, as a CPython function: addresses of tensors and structures to the entry point without a Python
+// The Python calls of a decode step (over slabs; over pages, append and attention) of the C ABI, as CPython functions: addresses of tensors and structures to the entry point without a Python
 // frame or a ctypes conversion for each.  What it gives is host time: the conversions were 2.1 us of a call of 6.7, now 0.9.  (A pass of 16 small steps, called one by
 // one, 98 to 109 us, differs from run to run by more than that.)  The entry point's address comes with every call: nothing is kept here.
 #define PY_SSIZE_T_CLEAN
@@ -57,7 +57,101 @@ PyObject* decode_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
+using PagedAppend = int32_t (*)(const void*, const void*, int64_t, const int64_t*, int32_t, const void*, int64_t, const int32_t*, const float*, int32_t,
+                                const void*, const void*, float, const int32_t*, const uint8_t*, void*, void*);
+using PagedAttend = int32_t (*)(const void*, const void*, int64_t, const int64_t*, int32_t, const void*, float*, const uint8_t*, void*, size_t, void*);
+
+// An argument that is an entry point.
+template <typename Call>
+Call entry_point(PyObject* x) {
+  const Call call = reinterpret_cast<Call>(PyLong_AsVoidPtr(x));
+  if (call == nullptr && !PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no entry point");
+  return call;
+}
+bool number(PyObject* x, int64_t* to) {
+  *to = PyLong_AsLongLong(x);
+  return *to != -1 || PyErr_Occurred() == nullptr;
+}
+bool number32(PyObject* x, int32_t* to) {
+  int64_t n;
+  if (!number(x, &n)) return false;
+  if (n != static_cast<int32_t>(n)) {
+    PyErr_SetString(PyExc_OverflowError, "a number does not fit 32 bits");
+    return false;
+  }
+  *to = static_cast<int32_t>(n);
+  return true;
+}
+bool stream_of(PyObject* x, void** to) {
+  *to = PyLong_AsVoidPtr(x);
+  return *to != nullptr || PyErr_Occurred() == nullptr;
+}
+// Two ctypes structures, held while a call runs.
+struct Structures {
+  Py_buffer a{}, b{};
+  int held = 0;
+  bool get(PyObject* x, PyObject* y) {
+    if (PyObject_GetBuffer(x, &a, PyBUF_SIMPLE) != 0) return false;
+    held = 1;
+    if (PyObject_GetBuffer(y, &b, PyBUF_SIMPLE) != 0) return false;
+    held = 2;
+    return true;
+  }
+  ~Structures() {
+    if (held > 1) PyBuffer_Release(&b);
+    if (held > 0) PyBuffer_Release(&a);
+  }
+};
+
+// paged_append(entry point, shape, pages, rows, row_offsets, max_new, qkv, stride, positions, inv_freq, rot, q_weight, k_weight, eps, keep, active, q, stream) -> status
+PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 18) return PyErr_Format(PyExc_TypeError, "paged_append takes 18 arguments (%zd given)", n);
+  const auto call = entry_point<PagedAppend>(args[0]);
+  int64_t rows, stride;
+  int32_t max_new, rot;
+  void *off, *qkv, *positions, *inv_freq, *qw, *kw, *keep, *active, *q, *stream;
+  const double eps = PyFloat_AsDouble(args[13]);
+  if (call == nullptr || (eps == -1.0 && PyErr_Occurred()) || !number(args[3], &rows) || !tensor_address(args[4], &off) || !number32(args[5], &max_new) ||
+      !tensor_address(args[6], &qkv) || !number(args[7], &stride) || !tensor_address(args[8], &positions) || !tensor_address(args[9], &inv_freq) ||
+      !number32(args[10], &rot) || !tensor_address(args[11], &qw) || !tensor_address(args[12], &kw) || !tensor_address(args[14], &keep) ||
+      !tensor_address(args[15], &active) || !tensor_address(args[16], &q) || !stream_of(args[17], &stream))
+    return nullptr;
+  Structures s;
+  if (!s.get(args[1], args[2])) return nullptr;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = call(s.a.buf, s.b.buf, rows, static_cast<const int64_t*>(off), max_new, qkv, stride, static_cast<const int32_t*>(positions),
+                static_cast<const float*>(inv_freq), rot, qw, kw, static_cast<float>(eps), static_cast<const int32_t*>(keep),
+                static_cast<const uint8_t*>(active), q, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// paged_attend(entry point, shape, pages, rows, row_offsets, max_new, q, out, active, workspace, workspace_bytes, stream) -> status
+PyObject* paged_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 12) return PyErr_Format(PyExc_TypeError, "paged_attend takes 12 arguments (%zd given)", n);
+  const auto call = entry_point<PagedAttend>(args[0]);
+  int64_t rows, bytes;
+  int32_t max_new;
+  void *off, *q, *out, *active, *workspace, *stream;
+  if (call == nullptr || !number(args[3], &rows) || !tensor_address(args[4], &off) || !number32(args[5], &max_new) || !tensor_address(args[6], &q) ||
+      !tensor_address(args[7], &out) || !tensor_address(args[8], &active) || !tensor_address(args[9], &workspace) || !number(args[10], &bytes) ||
+      !stream_of(args[11], &stream))
+    return nullptr;
+  if (bytes < 0) return PyErr_Format(PyExc_OverflowError, "workspace_bytes is negative");
+  Structures s;
+  if (!s.get(args[1], args[2])) return nullptr;
+  int32_t status;
+  Py_BEGIN_ALLOW_THREADS
+  status = call(s.a.buf, s.b.buf, rows, static_cast<const int64_t*>(off), max_new, q, static_cast<float*>(out), static_cast<const uint8_t*>(active), workspace,
+                static_cast<size_t>(bytes), stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
 PyMethodDef methods[] = {
+    {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
+    {"paged_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attend)), METH_FASTCALL, nullptr},
     {"decode_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_step)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bc_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -21,14 +21,15 @@ struct PagedTables {
   int32_t B, pages, page_shift, table_pages, max_new;
 };
 
-// New rows of a sequence: [row, row + n).  n = 0: left alone; n < 0: not a span of the call (the caller sets the state bit).
-struct PagedSpan { int64_t row; int n; };
+// New rows of a sequence: [row, row + n), and its length.  n = 0: left alone; n < 0: not a span of the call (the caller sets the state bit).
+// (All that the tables say is asked for together.)
+struct PagedSpan { int64_t row; int n, len; };
 __device__ __forceinline__ PagedSpan paged_span(const PagedTables& t, int s) {
-  if (t.active && !t.active[s]) return {0, 0};
-  if (!t.off) return {s, 1};
-  const int64_t a = t.off[s], b = t.off[s + 1];
-  if (a < 0 || b < a || b > t.rows || b - a > t.max_new) return {0, -1};
-  return {a, (int)(b - a)};
+  const int64_t a = t.off ? t.off[s] : s, b = t.off ? t.off[s + 1] : s + 1;
+  const int len = t.len[s];
+  const bool active = t.active ? t.active[s] != 0 : true;
+  const bool bad = a < 0 || b < a || b > t.rows || b - a > t.max_new;
+  return {a, !active ? 0 : bad ? -1 : (int)(b - a), len};
 }
 
 // the four e4m3 values of a word

@@ -9,7 +9,7 @@
 // rounding, 2^-4 of its value, that any scale would leave.
 //
 // Bound by memory where rows are many, by the latency of tables and loads where they are few.  Two kernels:
-//   a block of 16 entries a workgroup, d / 8 lanes a row, as many rows as the block has: the block's largest magnitude goes through LDS;
+//   a block of 16 entries a workgroup (few rows: several, which share the queries' heads), d / 8 lanes a row: the block's largest magnitude goes through LDS;
 //   one new row a sequence at most (a decode step): a workgroup a sequence, a wave for the key or the value of a head; the rest of the block is touched only where its scale grows.
 #include "bc_paged.h"
 #include "bc_rope_lane.h"
@@ -32,7 +32,8 @@ struct AppendParams {
   float* ks;                   // [pages, Hkv, page_rows / 16]
   float* vs;
   int32_t Hq, Hkv, half;
-  uint32_t blocks;             // workgroups of a sequence (block kernel)
+  int32_t* arrivals;           // [B * Hkv] zero between launches
+  uint32_t blocks, turns;      // block kernel: blocks of a sequence, workgroups of a block
   float eps;
 };
 
@@ -68,8 +69,8 @@ template <int D> __device__ __forceinline__ int value_at(int r, int o) { return 
 struct AppendPlan { int64_t row; int n, start; };
 __device__ __forceinline__ AppendPlan append_plan(const AppendParams& p, int s, int lane, bool herald) {
   const PagedSpan span = paged_span(p.t, s);
+  const int L = span.len, start = p.keep ? p.keep[s] : L;
   if (span.n == 0) return {0, 0, 0};
-  const int L = p.t.len[s], start = p.keep ? p.keep[s] : L;
   int bad = span.n < 0 || L < 0 || start < 0 || start > L ? BC_ERRBIT_STATE : 0;
   if (!bad && (int64_t)start + span.n > (int64_t)p.t.table_pages << p.t.page_shift) bad = BC_ERRBIT_CAPACITY;
   if (!bad) {
@@ -98,134 +99,146 @@ __device__ __forceinline__ void norm_head(float (&x)[2][4], const float (&w)[2][
   for (int e = 0; e < 4; ++e) { x[0][e] *= r * w[0][e]; x[1][e] *= r * w[1][e]; }
 }
 
-// (16 rows' lanes: 256 threads, 128 for d = 64)
-template <typename T, int D, bool NORM>
+// 16 rows' lanes: 256 threads, 128 for d = 64.  A block has p.turns workgroups: the first has the keys and values, and the queries' heads where it is alone; the others share those heads.
+template <typename T, int D, bool NORM, bool STREAM>
 __global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES, U = 4;
   __shared__ float s_most[U][kPagedBlock];
   const int lane = threadIdx.x % LPH, mine = threadIdx.x / LPH;      // a row of the block
-  const int s = blockIdx.x / p.blocks, j = blockIdx.x - s * p.blocks;
-  const AppendPlan plan = append_plan(p, s, threadIdx.x & 63, j == 0 && threadIdx.x < 64);
+  const uint32_t of_sequence = p.blocks * p.turns;
+  const int s = blockIdx.x / of_sequence, at_block = blockIdx.x - s * of_sequence, j = at_block / p.turns, turn = at_block - j * p.turns;
+  const AppendPlan plan = append_plan(p, s, threadIdx.x & 63, at_block == 0 && threadIdx.x < 64);
   if (plan.n == 0) return;
   const int start = plan.start, end = start + plan.n, first = ((start >> 4) + j) << 4, slot = first + mine;
-  if (first >= end) return;
+  // The length moves when all of the sequence's workgroups have read it, those without rows among them.
+  // (The count's answer is looked at behind the work.)
+  __syncthreads();
+  int arrived = -1;
+  if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(p.arrivals + s * p.Hkv, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  auto leave = [&] {
+    if (arrived != (int)of_sequence - 1) return;
+    __hip_atomic_store(p.arrivals + s * p.Hkv, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    p.t.len[s] = end;
+  };
+  if (first >= end) return leave();
   const bool fresh = slot >= start && slot < end, stays = slot < start, staying = first < start;
-  const int page = p.t.table[(int64_t)s * p.t.table_pages + (first >> p.t.page_shift)];
-  const int r = slot & ((1 << p.t.page_shift) - 1), per_page = 1 << (p.t.page_shift - 4);
   const int64_t row = plan.row + (fresh ? slot - start : 0);         // (other rows' lanes look at the first one)
   const char* in = p.qkv + row * p.row_bytes;
   const RopeLane<D> ln(p.half, p.inv_freq, lane, p.positions[row]);
-  if (p.q && fresh) {
+  if (p.q && fresh && (turn > 0 || p.turns == 1)) {
     float w[2][4];
     const bool norm = NORM && p.qw != nullptr;
     if (norm) { load4(p.qw + ln.o1 * ES, w[0], T{}); load4(p.qw + ln.o2 * ES, w[1], T{}); }
-    for (int h0 = 0; h0 < p.Hq; h0 += U) {
+    const int shares = p.turns > 1 ? (int)p.turns - 1 : 1, share = p.turns > 1 ? turn - 1 : 0;
+    const int h_first = p.Hq * share / shares, h_end = p.Hq * (share + 1) / shares;
+    for (int h0 = h_first; h0 < h_end; h0 += U) {
       float x[U][2][4];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int h = min(h0 + u, p.Hq - 1);
-        load4(in + (int64_t)h * HEAD + ln.o1 * ES, x[u][0], T{});
-        load4(in + (int64_t)h * HEAD + ln.o2 * ES, x[u][1], T{});
+        const int h = min(h0 + u, h_end - 1);
+        load4<STREAM>(in + (int64_t)h * HEAD + ln.o1 * ES, x[u][0], T{});
+        load4<STREAM>(in + (int64_t)h * HEAD + ln.o2 * ES, x[u][1], T{});
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (h0 + u >= p.Hq) break;
+        if (h0 + u >= h_end) break;
         if (norm) norm_head<T, D, NORM>(x[u], w, p.eps);
         ln.template turn<false>(x[u][0], x[u][1]);
         char* out = p.q + (row * p.Hq + h0 + u) * (D * 2);
-        store4<false>(out + ln.o1 * 2, x[u][0], bf16_t{});
-        store4<false>(out + ln.o2 * 2, x[u][1], bf16_t{});
+        store4<STREAM>(out + ln.o1 * 2, x[u][0], bf16_t{});
+        store4<STREAM>(out + ln.o2 * 2, x[u][1], bf16_t{});
       }
     }
   }
+  if (turn > 0) return leave();
+  const int page = p.t.table[(int64_t)s * p.t.table_pages + (first >> p.t.page_shift)];
+  const int r = slot & ((1 << p.t.page_shift) - 1), per_page = 1 << (p.t.page_shift - 4), block = (first >> 4) & (per_page - 1);
   // keys, then values
   float w[2][4];
   const bool norm = NORM && p.kw != nullptr;
   if (norm) { load4(p.kw + ln.o1 * ES, w[0], T{}); load4(p.kw + ln.o2 * ES, w[1], T{}); }
+  for (int it = 0; it < 2 * p.Hkv; it += U) {
+    float x[U][2][4], was[U];
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    uint8_t* pool = which ? p.v : p.k;
-    float* scales = which ? p.vs : p.ks;
-    const int o1 = which ? 8 * lane : ln.o1, o2 = which ? o1 + 4 : ln.o2;    // (values are not turned: eight in a row)
-    const char* at = in + (int64_t)(p.Hq + which * p.Hkv) * HEAD;
-    for (int h0 = 0; h0 < p.Hkv; h0 += U) {
-      float x[U][2][4], was[U];
+    for (int u = 0; u < U; ++u) {
+      const int item = min(it + u, 2 * p.Hkv - 1), value = item >= p.Hkv, h = item - value * p.Hkv;
+      const int o1 = value ? 8 * lane : ln.o1, o2 = value ? 8 * lane + 4 : ln.o2;       // (values are not turned: eight in a row)
+      load4<STREAM>(in + (int64_t)(p.Hq + item) * HEAD + o1 * ES, x[u][0], T{});
+      load4<STREAM>(in + (int64_t)(p.Hq + item) * HEAD + o2 * ES, x[u][1], T{});
+      was[u] = staying ? (value ? p.vs : p.ks)[((int64_t)page * p.Hkv + h) * per_page + block] : 0.f;
+    }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = min(h0 + u, p.Hkv - 1);
-        const int64_t head = (int64_t)page * p.Hkv + h;
-        was[u] = staying ? scales[head * per_page + ((first & ((1 << p.t.page_shift) - 1)) >> 4)] : 0.f;
-        load4(at + (int64_t)h * HEAD + o1 * ES, x[u][0], T{});
-        load4(at + (int64_t)h * HEAD + o2 * ES, x[u][1], T{});
-        if (stays) {                       // what it holds, for the case that the scale grows
-          const uint8_t* old = pool + (head << p.t.page_shift) * D;
-          if (which) {
+    for (int u = 0; u < U; ++u) {
+      const int item = min(it + u, 2 * p.Hkv - 1), value = item >= p.Hkv, h = item - value * p.Hkv;
+      if (stays) {                         // what it holds, for the case that the scale grows
+        const uint8_t* old = (value ? p.v : p.k) + ((((int64_t)page * p.Hkv + h) << p.t.page_shift) * D);
+        if (value) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float a[4], b[4];
-              unpack_e4m3(old[value_at<D>(r, o1 + e)], a);
-              unpack_e4m3(old[value_at<D>(r, o2 + e)], b);
-              x[u][0][e] = a[0] * was[u]; x[u][1][e] = b[0] * was[u];
-            }
-          } else {
-            unpack_e4m3(*reinterpret_cast<const uint32_t*>(old + key_at<D>(r, o1)), x[u][0]);
-            unpack_e4m3(*reinterpret_cast<const uint32_t*>(old + key_at<D>(r, o2)), x[u][1]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { x[u][0][e] *= was[u]; x[u][1][e] *= was[u]; }
-          }
-        } else if (!which) {
-          if (norm) norm_head<T, D, NORM>(x[u], w, p.eps);
-          ln.template turn<false>(x[u][0], x[u][1]);
-        }
-        const float most = fresh ? largest(x[u]) : 0.f;
-        const float all = group_allreduce_max<LPH>(most);
-        if (lane == 0) s_most[u][mine] = all;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (h0 + u >= p.Hkv) break;
-        float most = 0.f;
-#pragma unroll
-        for (int i = 0; i < kPagedBlock; ++i) most = fmaxf(most, s_most[u][i]);
-        const float scale = fmaxf(power_of_two(scale_exponent(most)), was[u]), inv = inverse_of(scale);
-        const int64_t head = (int64_t)page * p.Hkv + h0 + u;
-        if (threadIdx.x == 0) scales[head * per_page + ((first & ((1 << p.t.page_shift) - 1)) >> 4)] = scale;
-        uint8_t* to = pool + (head << p.t.page_shift) * D;
-        uint32_t a = quantise(x[u][0], inv), b = quantise(x[u][1], inv);
-        if (!which) {
-          if (fresh || (stays && scale != was[u])) {
-            *reinterpret_cast<uint32_t*>(to + key_at<D>(r, o1)) = a;
-            *reinterpret_cast<uint32_t*>(to + key_at<D>(r, o2)) = b;
+          for (int e = 0; e < 4; ++e) {
+            float a[4], b[4];
+            unpack_e4m3(old[value_at<D>(r, 8 * lane + e)], a);
+            unpack_e4m3(old[value_at<D>(r, 8 * lane + 4 + e)], b);
+            x[u][0][e] = a[0]; x[u][1][e] = b[0];
           }
         } else {
-          // four rows' words of four elements each -> four elements' words of four rows each: rows r ^ 1, then r ^ 2 (v_perm: bytes 0..3 of the second
-          // operand, 4..7 of the first)
-          const bool odd = r & 1, high = r & 2;
-          auto turned = [&](uint32_t x0) {
-            const uint32_t y = __shfl_xor(x0, LPH, 64);
-            const uint32_t x1 = odd ? __builtin_amdgcn_perm(x0, y, 0x07030501) : __builtin_amdgcn_perm(y, x0, 0x06020400);
-            const uint32_t z = __shfl_xor(x1, 2 * LPH, 64);
-            return high ? __builtin_amdgcn_perm(x1, z, 0x07060302) : __builtin_amdgcn_perm(z, x1, 0x05040100);
-          };
-          a = turned(a); b = turned(b);
-          // entries behind the last one keep their bytes
-          const int group = slot & ~3, whole = end - group;           // rows of the group in front of the end
-          if (whole > 0 && (group + 4 > start || scale != was[u])) {
-            uint32_t* wa = reinterpret_cast<uint32_t*>(to + value_at<D>(r & ~3, o1 + (r & 3)));
-            uint32_t* wb = reinterpret_cast<uint32_t*>(to + value_at<D>(r & ~3, o2 + (r & 3)));
-            if (whole < 4) {
-              const uint32_t ours = (1u << (8 * whole)) - 1;
-              a = (a & ours) | (*wa & ~ours);
-              b = (b & ours) | (*wb & ~ours);
-            }
-            *wa = a; *wb = b;
+          unpack_e4m3(*reinterpret_cast<const uint32_t*>(old + key_at<D>(r, ln.o1)), x[u][0]);
+          unpack_e4m3(*reinterpret_cast<const uint32_t*>(old + key_at<D>(r, ln.o2)), x[u][1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[u][0][e] *= was[u]; x[u][1][e] *= was[u]; }
+      } else if (!value) {
+        if (norm) norm_head<T, D, NORM>(x[u], w, p.eps);
+        ln.template turn<false>(x[u][0], x[u][1]);
+      }
+      const float most = group_allreduce_max<LPH>(fresh ? largest(x[u]) : 0.f);
+      if (lane == 0) s_most[u][mine] = most;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int item = it + u, value = item >= p.Hkv, h = item - value * p.Hkv;
+      if (item >= 2 * p.Hkv) break;
+      float most = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPagedBlock; ++i) most = fmaxf(most, s_most[u][i]);
+      const float scale = fmaxf(power_of_two(scale_exponent(most)), was[u]), inv = inverse_of(scale);
+      const int64_t head = (int64_t)page * p.Hkv + h;
+      if (threadIdx.x == 0) (value ? p.vs : p.ks)[head * per_page + block] = scale;
+      uint8_t* to = (value ? p.v : p.k) + (head << p.t.page_shift) * D;
+      uint32_t a = quantise(x[u][0], inv), b = quantise(x[u][1], inv);
+      if (!value) {
+        if (fresh || (stays && scale != was[u])) {
+          *reinterpret_cast<uint32_t*>(to + key_at<D>(r, ln.o1)) = a;
+          *reinterpret_cast<uint32_t*>(to + key_at<D>(r, ln.o2)) = b;
+        }
+      } else {
+        // four rows' words of four elements each -> four elements' words of four rows each: rows r ^ 1, then r ^ 2 (v_perm: bytes 0..3 of the second
+        // operand, 4..7 of the first)
+        const bool odd = r & 1, high = r & 2;
+        auto turned = [&](uint32_t x0) {
+          const uint32_t y = __shfl_xor(x0, LPH, 64);
+          const uint32_t x1 = odd ? __builtin_amdgcn_perm(x0, y, 0x07030501) : __builtin_amdgcn_perm(y, x0, 0x06020400);
+          const uint32_t z = __shfl_xor(x1, 2 * LPH, 64);
+          return high ? __builtin_amdgcn_perm(x1, z, 0x07060302) : __builtin_amdgcn_perm(z, x1, 0x05040100);
+        };
+        a = turned(a); b = turned(b);
+        // entries behind the last one keep their bytes
+        const int group = slot & ~3, whole = end - group;             // rows of the group in front of the end
+        if (whole > 0 && (group + 4 > start || scale != was[u])) {
+          uint32_t* wa = reinterpret_cast<uint32_t*>(to + value_at<D>(r & ~3, 8 * lane + (r & 3)));
+          uint32_t* wb = reinterpret_cast<uint32_t*>(to + value_at<D>(r & ~3, 8 * lane + 4 + (r & 3)));
+          if (whole < 4) {
+            const uint32_t ours = (1u << (8 * whole)) - 1;
+            a = (a & ours) | (*wa & ~ours);
+            b = (b & ours) | (*wb & ~ours);
           }
+          *wa = a; *wb = b;
         }
       }
-      __syncthreads();
     }
+    __syncthreads();
   }
+  leave();
 }
 
 // One new row at most: a workgroup a sequence, whose waves take the keys' and values' heads and then the queries' by turns, and at the end the length.
@@ -315,30 +328,31 @@ __global__ void __launch_bounds__(1024) paged_append_one_kernel(AppendParams p) 
   if (threadIdx.x == 0) p.t.len[s] = start + 1;
 }
 
-// The lengths, behind the block kernel: a wave a sequence, which comes to the same plan.
-__global__ void __launch_bounds__(256) paged_length_kernel(AppendParams p) {
-  const int s = (blockIdx.x * 256 + threadIdx.x) >> 6, lane = threadIdx.x & 63;
-  if (s >= p.t.B) return;
-  const AppendPlan plan = append_plan(p, s, lane, false);
-  if (plan.n > 0 && lane == 0) p.t.len[s] = plan.start + plan.n;
+// Workgroups of a block: more where there are few rows.
+constexpr int64_t kAppendGroups = 1024;
+void deal_blocks(AppendParams& p, int64_t rows) {
+  const int64_t blocks = (rows + kPagedBlock - 1) / kPagedBlock + p.t.B, heads = p.q ? p.Hq : 0, most = (heads + 3) / 4 + 1;
+  const int64_t want = heads ? kAppendGroups / blocks : 1;
+  p.turns = (uint32_t)(want < 1 ? 1 : want > most ? most : want);
 }
-
+// Packed rows beyond the 256 MB of the Infinity Cache go past it, as in bc_qk_norm_rope.
 template <typename T, int D, bool NORM>
-void launch_append(AppendParams& p, hipStream_t s) {
+void launch_append(AppendParams& p, int64_t rows, hipStream_t s) {
   if (p.t.max_new <= 1) {
     constexpr int PER = 64 / (D / 8);
     const int tasks = 2 * p.Hkv + (p.q ? (p.Hq + PER - 1) / PER : 0);
     paged_append_one_kernel<T, D, NORM><<<p.t.B, 64 * (tasks < 16 ? tasks : 16), 0, s>>>(p);
     return;
   }
-  paged_append_kernel<T, D, NORM><<<(unsigned)((int64_t)p.t.B * p.blocks), 2 * D, 0, s>>>(p);
-  paged_length_kernel<<<(p.t.B + 3) / 4, 256, 0, s>>>(p);
+  const unsigned grid = (unsigned)((int64_t)p.t.B * p.blocks * p.turns);
+  if (rows * (p.Hq + 2 * (int64_t)p.Hkv) * D * Elem<T>::size > (256LL << 20)) paged_append_kernel<T, D, NORM, true><<<grid, 2 * D, 0, s>>>(p);
+  else paged_append_kernel<T, D, NORM, false><<<grid, 2 * D, 0, s>>>(p);
 }
 template <typename T>
-void launch_append(AppendParams& p, int d, hipStream_t s) {
+void launch_append(AppendParams& p, int64_t rows, int d, hipStream_t s) {
   const bool norm = p.qw || p.kw;
-  if (d == 128) { if (norm) launch_append<T, 128, true>(p, s); else launch_append<T, 128, false>(p, s); }
-  else { if (norm) launch_append<T, 64, true>(p, s); else launch_append<T, 64, false>(p, s); }
+  if (d == 128) { if (norm) launch_append<T, 128, true>(p, rows, s); else launch_append<T, 128, false>(p, rows, s); }
+  else { if (norm) launch_append<T, 64, true>(p, rows, s); else launch_append<T, 64, false>(p, rows, s); }
 }
 
 }  // namespace
@@ -358,7 +372,7 @@ extern "C" int32_t bc_paged_append(const bc_shape* shape, const bc_pages* pages,
   // (a sequence cannot have more new rows than there are)
   const int64_t most = max_new < rows ? max_new : rows, blocks = (most + 14) / kPagedBlock + 1;
   if (shape->B * blocks > 0x7fffffff) return BC_ERR_SHAPE;
-  if (!qkv || !positions || (rot > 0 && !inv_freq) || !aligned16(qkv) || !aligned16(q) || !aligned16(q_weight) || !aligned16(k_weight)) return BC_ERR_ARG;
+  if (!qkv || !positions || (rot > 0 && !inv_freq) || !aligned16(qkv) || !aligned16(q) || !aligned16(q_weight) || !aligned16(k_weight) || !pages->arrivals) return BC_ERR_ARG;
   if (qkv_row_stride < (int64_t)(shape->Hq + 2 * (int64_t)shape->Hkv) * shape->d || qkv_row_stride > (1LL << 31) ||
       qkv_row_stride * elem_size(shape->kv_dtype) % 16 != 0 || q == qkv)
     return BC_ERR_ARG;
@@ -369,8 +383,10 @@ extern "C" int32_t bc_paged_append(const bc_shape* shape, const bc_pages* pages,
   p.qw = static_cast<const char*>(q_weight); p.kw = static_cast<const char*>(k_weight); p.eps = eps;
   p.keep = keep; p.q = static_cast<char*>(q);
   p.k = static_cast<uint8_t*>(pages->k); p.v = static_cast<uint8_t*>(pages->v); p.ks = pages->k_scale; p.vs = pages->v_scale;
-  p.Hq = shape->Hq; p.Hkv = shape->Hkv; p.blocks = (uint32_t)blocks;
+  p.Hq = shape->Hq; p.Hkv = shape->Hkv; p.blocks = (uint32_t)blocks; p.arrivals = pages->arrivals;
+  deal_blocks(p, rows);
+  if (shape->B * blocks * p.turns > 0x7fffffff) return BC_ERR_SHAPE;
   hipStream_t s = as_stream(stream);
-  if (shape->kv_dtype == BC_BF16) launch_append<bf16_t>(p, shape->d, s); else launch_append<float>(p, shape->d, s);
+  if (shape->kv_dtype == BC_BF16) launch_append<bf16_t>(p, rows, shape->d, s); else launch_append<float>(p, rows, shape->d, s);
   return launch_status();
 }

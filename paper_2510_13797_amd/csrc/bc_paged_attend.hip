@@ -68,7 +68,7 @@ constexpr int few_waves(int ct, int nw) { return ct == 1 && nw == 4 ? 4 : 2; }
 struct AttendSpan { int64_t row; int n, L; bool bad; };
 __device__ __forceinline__ AttendSpan attend_span(const AttendParams& p, int s) {
   const PagedSpan span = paged_span(p.t, s);
-  const int L = p.t.len[s];
+  const int L = span.len;
   const bool bad = span.n < 0 || (span.n > 0 && (L < span.n || L > p.max_len));
   return {span.row, bad ? 0 : span.n, L, bad};
 }

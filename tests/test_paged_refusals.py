@@ -56,7 +56,7 @@ def test_append_refusals():
     for eps in (-1e-6, float("nan"), float("inf")):
         assert _append(eps=eps) == bc.BC_ERR_ARG
     for kw in (dict(qkv=None), dict(qkv=ODD), dict(pos=None), dict(freq=None), dict(q=ODD), dict(qw=ODD), dict(kw=ODD), dict(stride=511), dict(stride=516), dict(stride=504),
-               dict(stride=-512), dict(stride=1 << 40), dict(q=PTR)):
+               dict(stride=-512), dict(stride=1 << 40), dict(q=PTR), dict(pg=_pages(arrivals=None))):
         assert _append(**kw) == bc.BC_ERR_ARG, kw
     # (more blocks than a grid holds)
     assert _append(s=shape(B=1 << 21, Hkv=4), rows=1 << 30, max_new=1 << 20) == bc.BC_ERR_SHAPE
@@ -69,28 +69,25 @@ def test_attend_refusals():
     for kw in (dict(q=None), dict(out=None), dict(q=ODD), dict(out=ODD), dict(pg=_pages(arrivals=None))):
         assert _attend(**kw) == bc.BC_ERR_ARG, kw
     long = _pages(pages=1000, table_pages=1000)
-    need = bc.bc_paged_workspace_bytes(shape(), 5, 32000)
+    need = bc.bc_paged_workspace_bytes(shape(), 5, 5, 32000)
     assert need > 1000
-    for kw in (dict(ws=None), dict(ws=ODD), dict(nbytes=1000)):
+    for kw in (dict(ws=None), dict(ws=ODD), dict(nbytes=1000), dict(nbytes=need - 17)):
         assert _attend(pg=long, **kw) == bc.BC_ERR_WORKSPACE, kw
-    assert bc.bc_paged_workspace_bytes(shape(d=96), 5, 100) == 0 and bc.bc_paged_workspace_bytes(shape(), -1, 100) == 0
-    assert bc.bc_paged_workspace_bytes(shape(), 5, 0) == 0 and bc.bc_paged_workspace_bytes(shape(B=(1 << 23) + 1), 5, 100) == 0
+    size = bc.bc_paged_workspace_bytes
+    assert size(shape(d=96), 5, 5, 100) == 0 and size(shape(), 5, -1, 100) == 0 and size(shape(), -1, 5, 100) == 0 and size(shape(), 1 << 31, 5, 100) == 0
+    assert size(shape(), 5, 5, 0) == 0 and size(shape(B=(1 << 23) + 1), 5, 5, 100) == 0
     # (more columns than 31 bits count)
-    assert bc.bc_paged_workspace_bytes(shape(Hq=8, Hkv=1), 1 << 29, 1 << 30) == 0
+    assert size(shape(Hq=8, Hkv=1), 1 << 30, 1 << 29, 1 << 30) == 0
     assert _attend(s=shape(Hq=8, Hkv=1), rows=1 << 30, max_new=1 << 29, pg=_pages(pages=1, table_pages=1 << 24, page_rows=64)) == bc.BC_ERR_SHAPE
 
 
-def test_workspace_covers_what_the_call_needs():
-    # the call cuts the longest span to the rows and entries there are: it asks for no more than the size for what it was given
-    for B, Hq, Hkv, d in ((1, 32, 8, 128), (64, 12, 2, 128), (24, 14, 2, 64), (300, 4, 1, 128)):
-        for new in (1, 2, 3, 5, 8, 9, 64, 700):
-            for n in (31, 100, 5000, 32768):
-                s = shape(Hq, Hkv, d, B=B)
-                need = bc.bc_paged_workspace_bytes(s, new, n)
-                assert need >= 16
-                for fewer in (1, new // 2, new):
-                    if fewer:
-                        assert bc.bc_paged_workspace_bytes(s, fewer, n) <= max(need, bc.bc_paged_workspace_bytes(s, new, n))
+def test_workspace_goes_by_the_rows_there_are():
+    # one long chunk among many sequences with a row or none: what its own call needs and the others' share
+    for B, Hq, Hkv, n in ((128, 4, 1, 4096), (64, 12, 2, 512), (64, 32, 8, 40)):
+        for d in (64, 128):
+            alone = bc.bc_paged_workspace_bytes(shape(Hq, Hkv, d), n, n, 8192)
+            got = bc.bc_paged_workspace_bytes(shape(Hq, Hkv, d, B=B), n + B - 1, n, 8192)
+            assert 16 <= got <= max(alone, 16) * (n + B - 1) / n + 64, (B, n, d, got, alone)
 
 
 def test_struct_layout_matches_the_header(tmp_path):
