@@ -110,13 +110,11 @@ __global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
   const AppendPlan plan = append_plan(p, s, threadIdx.x & 63, at_block == 0 && threadIdx.x < 64);
   if (plan.n == 0) return;
   const int start = plan.start, end = start + plan.n, first = ((start >> 4) + j) << 4, slot = first + mine;
-  // The length moves when all of the sequence's workgroups have read it, those without rows among them.
-  // (The count's answer is looked at behind the work.)
-  __syncthreads();
-  int arrived = -1;
-  if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(p.arrivals + s * p.Hkv, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // The length moves when all of the sequence's workgroups have read it, those without rows among them: counted behind the work (in front of it the loads behind the count, which
+  // come back in order, waited for its answer: 2 us).
   auto leave = [&] {
-    if (arrived != (int)of_sequence - 1) return;
+    __syncthreads();
+    if (threadIdx.x != 0 || __hip_atomic_fetch_add(p.arrivals + s * p.Hkv, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (int)of_sequence - 1) return;
     __hip_atomic_store(p.arrivals + s * p.Hkv, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     p.t.len[s] = end;
   };
