@@ -356,26 +356,41 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
 
 
 // ---------------------------------------------------------------------------
-// Many columns: 32 a wave, the workgroup's four share the tiles of 32 entries.  A tile comes as bytes, 16 a lane and a kilobyte a wave in a row, becomes bf16 once and goes
-// to LDS as the operands of 32x32x16 products: keys [d / 16][half][key], element 16 i + 8 half + e of a key; values [block][16 keys][half][element], the block's
-// elements four apart, so that a word's four keys are half of an operand and results have four elements in a row.
+// Many columns: 32 a wave, the workgroup's four share tiles of 64 entries.  A wave brings the bytes of one of a tile's four blocks, makes them bf16 times their scale (the
+// conversion takes a power of two, and is exact) and leaves them in LDS as the operands of 32x32x16 products, 16 bytes a lane: keys [32 entries][d / 16][half][entry],
+// element 16 i + 8 half + e of a key (its place among the 32 turned by i, so that the writes meet no bank twice); values [16 entries][j][half][row], element (d / 32) row + j: a word's four
+// keys are half of an operand, the lane's other word the other half, and results have d / 32 elements in a row.
 // ---------------------------------------------------------------------------
-constexpr int kManyWaves = 4, kManyColumns = 32 * kManyWaves;
-constexpr float kRedo = 256.f;      // a lane's 16 weights may sum to this before the reference moves
+constexpr int kManyWaves = 4, kManyColumns = 32 * kManyWaves, kManyTile = 16 * kManyWaves;
+constexpr float kRedo = 256.f;      // a lane's 32 weights may sum to this before the reference moves
 constexpr float kLazy = 2.f;        // ... where a column's maximum is this much (log2) above it
 
 // Tiles of a block of columns, and those of one of its parts.
 struct ManyCut { int tiles, t0, t1, parts; };
 __device__ __forceinline__ ManyCut many_cut(int parts, int lim, int part) {
-  const int tiles = (lim + 31) >> 5, most = max(1, tiles >> 3), n = min(parts, most);      // (no part of fewer than eight tiles)
+  const int tiles = (lim + kManyTile - 1) / kManyTile, n = min(parts, max(1, tiles >> 2));      // (no part of fewer than four tiles)
   return {tiles, (int)((int64_t)tiles * part / n), (int)((int64_t)tiles * (part + 1) / n), n};
+}
+
+// A scale as the conversion's factor and what is left of it: one for a power of two.
+__device__ __forceinline__ bool power_of_two_scale(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return (u & 0x807fffffu) == 0 && u - 0x00800000u < 0x7f000000u;
+}
+__device__ __forceinline__ uint32_t scaled_bf16(uint32_t w, float scale, bool high) {
+  return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))
+              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+}
+__device__ __forceinline__ u32x4_t scaled_operand(uint32_t a, uint32_t b, float scale) {
+  return u32x4_t{scaled_bf16(a, scale, false), scaled_bf16(a, scale, true), scaled_bf16(b, scale, false), scaled_bf16(b, scale, true)};
 }
 
 template <int D>
 __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendParams p) {
-  constexpr int KS = D / 16, NJ = D / 32, K_BYTES = 32 * D * 2, STAGE = 2 * K_BYTES, LOADS = D / 64, BLOCK_BYTES = kPagedBlock * D;
+  constexpr int KS = D / 16, NJ = D / 32, K_BYTES = kManyTile * D * 2, STAGE = 2 * K_BYTES, BLOCK_BYTES = kPagedBlock * D;
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
-  __shared__ float2 s_scale[2][2];                               // [stage][block] of keys (with scale * log2 e) and of values
+  __shared__ float2 s_rest[2][kManyWaves];                       // what the conversions left of a block's scales, of keys and of values
+  __shared__ int s_uneven;                                       // whether that has been anything but ones
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const uint32_t pairs = (uint32_t)p.t.B * p.Hkv;
   uint32_t id = blockIdx.x;
@@ -392,7 +407,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 
   const int mine = first + 32 * wave, c = min(mine + col, columns - 1), i = c / p.g;
   const int lim = L - n + 1 + i;                                 // entries that this lane's column sees
-  const int free_tiles = (L - n + 1 + min(mine, columns - 1) / p.g) >> 5;      // tiles that all of the wave's columns see whole
+  const int free_tiles = (L - n + 1 + min(mine, columns - 1) / p.g) / kManyTile;        // tiles that all of the wave's columns see whole
+  const int seen = mine < columns ? (L - n + (min(mine + 32, columns) - 1) / p.g) / kManyTile + 1 : 0;         // tiles that the wave works on
   bf16x8_t qb[KS];
   {
     const char* at = p.q + ((span.row + i) * p.Hq + kvh * p.g + (c - i * p.g)) * (2 * D) + 16 * half;
@@ -404,105 +420,117 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   for (int j = 0; j < NJ; ++j) O[j] = f32x16_t{0.f};
   float m = kNegBig, l = 0.f;
 
-  // A tile's bytes: LOADS of keys and of values a wave, each a kilobyte of one block (d = 64: two waves have the keys, two the values).
-  const int per_page = p.t.page_shift - 4;
-  const uint32_t unit_of_last = (L - 1) >> 4;
-  auto unit_at = [&](int b) -> uint32_t {                        // block b of the sequence: where its bytes and scales are
-    b = min(b, (int)unit_of_last);
+  // A tile's bytes on their way: the wave's block of it.
+  const int per_page = p.t.page_shift - 4, last_block = (L - 1) >> 4;
+  u32x4_t kb[D / 64], vb[D / 64];                                // (d = 64: two words of each of two groups of values)
+  float k_scale = 1.f, v_scale = 1.f;
+  auto fetch = [&](int t) {
+    const int b = min(4 * t + wave, last_block);
     int page = p.t.table[(int64_t)s * p.t.table_pages + (b >> per_page)];
     if ((uint32_t)page >= (uint32_t)p.t.pages) {
       if (lane == 0) atomicOr(p.t.err, BC_ERRBIT_STATE);
       page = 0;
     }
-    return (((uint32_t)page * p.Hkv + kvh) << per_page) + (b & ((1 << per_page) - 1));
-  };
-  u32x4_t bytes[LOADS];
-  float2 scales{0.f, 0.f};
-  auto fetch = [&](int t) {
-    if (D == 128) {
-      const uint32_t u = unit_at(2 * t + (wave >> 1));
-      const uint64_t at = (uint64_t)u * BLOCK_BYTES + (wave & 1) * 1024 + lane * 16;
-      bytes[0] = *reinterpret_cast<const u32x4_t*>(p.k + at);
-      bytes[LOADS - 1] = *reinterpret_cast<const u32x4_t*>(p.v + at);
-      scales = make_float2(p.ks[u] * p.qs, p.vs[u]);
+    const uint32_t unit = (((uint32_t)page * p.Hkv + kvh) << per_page) + (b & ((1 << per_page) - 1));
+    const uint8_t *k = p.k + (uint64_t)unit * BLOCK_BYTES, *v = p.v + (uint64_t)unit * BLOCK_BYTES;
+    k_scale = p.ks[unit]; v_scale = p.vs[unit];
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) kb[x] = *reinterpret_cast<const u32x4_t*>(k + (1024 * x + 16 * lane));
+    if constexpr (D == 128) {
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) vb[x] = *reinterpret_cast<const u32x4_t*>(v + (1024 * x + 16 * lane));
     } else {
-      const uint32_t u = unit_at(2 * t + (wave & 1));
-      bytes[0] = *reinterpret_cast<const u32x4_t*>((wave < 2 ? p.k : p.v) + (uint64_t)u * BLOCK_BYTES + lane * 16);
-      scales = make_float2(p.ks[u] * p.qs, p.vs[u]);
-    }
-  };
-  auto put_keys = [&](char* to, const u32x4_t& x, int at) {      // at: the lane's 16 bytes of the tile
-    const int group = at / (D / 4), h = at / 16 % (D / 64), row = 4 * group + at / 4 % 4, k = 4 * h + at % 4;
-    char* place = to + k * 1024 + ((row ^ (2 * (k & 3))) * 16);
-    *reinterpret_cast<bf16x8_t*>(place) = operand_of(x[0], x[1]);
-    *reinterpret_cast<bf16x8_t*>(place + 512) = operand_of(x[2], x[3]);
-  };
-  auto put_values = [&](char* to, u32x4_t x, int at, int t) {
-    const int group = at / (D / 4), e = at % (D / 4);
-    if (32 * t + 32 > L) {                                       // bytes behind the last entry may be anything
-      const int there = L - 32 * t - 4 * group;
-      const uint32_t keep = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] &= keep;
-    }
-    // group: (16 keys, second half of the operand, half of the wave)
-    char* place = to + (group >> 2) * 1024 + (group & 1) * 512 + (group >> 1 & 1) * 8;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint64_t w = (uint64_t)bf16_of(x[j], true) << 32 | bf16_of(x[j], false);
-      const int blk = D == 128 ? j : j & 1, row = D == 128 ? e : (j >> 1) * 16 + e;
-      *reinterpret_cast<uint64_t*>(place + blk * 2048 + row * 16) = w;
+      const u32x2_v a = *reinterpret_cast<const u32x2_v*>(v + (256 * half + 8 * col)), b = *reinterpret_cast<const u32x2_v*>(v + (512 + 256 * half + 8 * col));
+      vb[0] = u32x4_t{a[0], a[1], b[0], b[1]};
     }
   };
   auto put = [&](int t, int stage) {
     char* to = lds + stage * STAGE;
-    if (D == 128) {
-      put_keys(to, bytes[0], wave * 64 + lane);
-      put_values(to + K_BYTES, bytes[LOADS - 1], wave * 64 + lane, t);
-      if ((wave & 1) == 0 && lane == 0) s_scale[stage][wave >> 1] = scales;
-    } else {
-      if (wave < 2) put_keys(to, bytes[0], wave * 64 + lane);
-      else put_values(to + K_BYTES, bytes[0], (wave - 2) * 64 + lane, t);
-      if (wave < 2 && lane == 0) s_scale[stage][wave] = scales;
+    const bool ke = power_of_two_scale(k_scale), ve = power_of_two_scale(v_scale);
+    const float kf = ke ? k_scale : 1.f, vf = ve ? v_scale : 1.f;
+    if (lane == 0) {
+      s_rest[stage][wave] = make_float2(ke ? 1.f : k_scale, ve ? 1.f : v_scale);
+      if (!ke || !ve) s_uneven = 1;
+    }
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) {                           // rows of the block: 4 * group + (lane / 4) % 4
+      const int at = 64 * x + lane, group = at / (D / 4), h = at / 16 % (D / 64), k = 4 * h + lane % 4, row = 16 * (wave & 1) + 4 * group + lane / 4 % 4;
+      char* place = to + (wave >> 1) * (K_BYTES / 2) + k * 1024 + ((row ^ (2 * (k & 3))) * 16);
+      *reinterpret_cast<u32x4_t*>(place) = scaled_operand(kb[x][0], kb[x][1], kf);
+      *reinterpret_cast<u32x4_t*>(place + 512) = scaled_operand(kb[x][2], kb[x][3], kf);
+    }
+    // values: words w of group `half` and of group `half + 2`
+    char* place = to + K_BYTES + wave * (NJ * 1024) + half * 512 + col * 16;
+    uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
+    if (kManyTile * (t + 1) > L) {                               // bytes behind the last entry may be anything
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int there = L - kManyTile * t - 16 * wave - 4 * (half + 2 * x);
+        keep[x] = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const uint32_t a = D == 128 ? vb[0][j] : vb[0][j & 1], b = D == 128 ? vb[D / 64 - 1][j] : vb[0][2 + (j & 1)];
+      *reinterpret_cast<u32x4_t*>(place + j * 1024) = scaled_operand(a & keep[0], b & keep[1], vf);
     }
   };
 
   fetch(cut.t0);
+  if (tid == 0) s_uneven = 0;
+  __syncthreads();
   put(cut.t0, 0);
   if (cut.t0 + 1 < cut.t1) fetch(cut.t0 + 1);
   __syncthreads();
-  const int seen = mine < columns ? (L - n + 1 + (min(mine + 32, columns) - 1) / p.g + 31) >> 5 : 0;        // tiles that the wave works on
   for (int t = cut.t0, stage = 0; t < cut.t1; ++t, stage ^= 1) {
     if (t + 1 < cut.t1) put(t + 1, stage ^ 1);
     if (t + 2 < cut.t1) fetch(t + 2);
     if (t < seen) {
       const char* tile = lds + stage * STAGE;
-      f32x16_t sc = f32x16_t{0.f};
+      f32x16_t sc[2];
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_t*>(tile + k * 1024 + half * 512 + ((col ^ (2 * (k & 3))) * 16)), qb[k], sc, 0, 0, 0);
-      const float2 f0 = s_scale[stage][0], f1 = s_scale[stage][1];
-      // result e: entry 8 (e / 4) + 4 half + e % 4 of the tile
-      if (t >= free_tiles) {
-        const int there = lim - 32 * t - 4 * half;
+      for (int x = 0; x < 2; ++x) {
+        sc[x] = f32x16_t{0.f};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] = 8 * (e >> 2) + (e & 3) < there ? sc[e] * (e < 8 ? f0.x : f1.x) : kMasked;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] *= e < 8 ? f0.x : f1.x;
+        for (int k = 0; k < KS; ++k)
+          sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              *reinterpret_cast<const bf16x8_t*>(tile + x * (K_BYTES / 2) + k * 1024 + half * 512 + ((col ^ (2 * (k & 3))) * 16)), qb[k], sc[x], 0, 0, 0);
       }
-      float pe[16], psum;
-      auto weights = [&]() {
+      const bool uneven = __builtin_amdgcn_readfirstlane(s_uneven) != 0;
+      // result e of sc[x]: entry 32 x + 8 (e / 4) + 4 half + e % 4 of the tile, of its block 2 x + e / 8
+      if (__builtin_expect(uneven, 0)) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) pe[e] = fast_exp2(sc[e] - m);
-        psum = (((pe[0] + pe[1]) + (pe[2] + pe[3])) + ((pe[4] + pe[5]) + (pe[6] + pe[7]))) +
-               (((pe[8] + pe[9]) + (pe[10] + pe[11])) + ((pe[12] + pe[13]) + (pe[14] + pe[15])));
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[x][e] *= s_rest[stage][2 * x + e / 8].x;
+      }
+      if (t >= free_tiles) {
+        const int there = lim - kManyTile * t - 4 * half;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (32 * x + 8 * (e >> 2) + (e & 3) >= there) sc[x][e] = kMasked;
+      }
+      float pe[2][16], psum;
+      auto weights = [&]() __attribute__((always_inline)) {
+        float sum[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) pe[x][e] = fast_exp2(fmaf(sc[x][e], p.qs, -m));
+          sum[x] = (((pe[x][0] + pe[x][1]) + (pe[x][2] + pe[x][3])) + ((pe[x][4] + pe[x][5]) + (pe[x][6] + pe[x][7]))) +
+                   (((pe[x][8] + pe[x][9]) + (pe[x][10] + pe[x][11])) + ((pe[x][12] + pe[x][13]) + (pe[x][14] + pe[x][15])));
+        }
+        psum = sum[0] + sum[1];
       };
       weights();
       if (__builtin_expect(__any(psum > kRedo), 0)) {
         float top = kMasked;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[e]);
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[x][e] > 0.5f * kMasked ? sc[x][e] * p.qs : kMasked);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float to = top > m + kLazy ? top : m, was = fast_exp2(m - to);
         m = to; l *= was;
@@ -511,23 +539,28 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         weights();
       }
       l += psum;
+      if (__builtin_expect(uneven, 0)) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) pe[e] *= e < 8 ? f0.y : f1.y;
-      u32x4_t hi[2], lo[2];
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const uint32_t h = pack2_bf16(pe[2 * x], pe[2 * x + 1]);
-        hi[x >> 2][x & 3] = h;
-        lo[x >> 2][x & 3] = pack2_bf16(pe[2 * x] - __uint_as_float(h << 16), pe[2 * x + 1] - __uint_as_float(h & 0xffff0000u));
+          for (int e = 0; e < 16; ++e) pe[x][e] *= s_rest[stage][2 * x + e / 8].y;
       }
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
+      for (int b = 0; b < 4; ++b) {
+        u32x4_t hi, lo;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float u = pe[b >> 1][8 * (b & 1) + 2 * y], w = pe[b >> 1][8 * (b & 1) + 2 * y + 1];
+          hi[y] = pack2_bf16(u, w);
+          lo[y] = pack2_bf16(u - __uint_as_float(hi[y] << 16), w - __uint_as_float(hi[y] & 0xffff0000u));
+        }
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(tile + K_BYTES + j * 2048 + kk * 1024 + half * 512 + col * 16);
-          O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8_t, hi[kk]), O[j], 0, 0, 0);
-          O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8_t, lo[kk]), O[j], 0, 0, 0);
+          const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(tile + K_BYTES + b * (NJ * 1024) + j * 1024 + half * 512 + col * 16);
+          O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8_t, hi), O[j], 0, 0, 0);
+          O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8_t, lo), O[j], 0, 0, 0);
         }
+      }
     }
     __syncthreads();
   }
@@ -543,7 +576,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   for (int e = 0; e < 16; ++e) {
     const int row = 8 * (e >> 2) + 4 * half + (e & 3);
     if constexpr (D == 128) *reinterpret_cast<f32x4_t*>(to + 4 * row) = f32x4_t{O[0][e] * f, O[1][e] * f, O[NJ - 2][e] * f, O[NJ - 1][e] * f};
-    else *reinterpret_cast<f32x2_v*>(to + 4 * (row & 15) + 2 * (row >> 4)) = f32x2_v{O[0][e] * f, O[1][e] * f};
+    else *reinterpret_cast<f32x2_v*>(to + 2 * row) = f32x2_v{O[0][e] * f, O[1][e] * f};
   }
 }
 
