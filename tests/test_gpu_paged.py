@@ -373,20 +373,23 @@ def test_the_sum_where_the_scale_is_zero_and_where_scores_are_large(dev):
     both.check_attend(q, [1, 1], tol=0.05)
 
 
-def test_scales_of_any_kind(dev):
-    # a cache filled by the caller: scales that are no powers of two, negative ones among them
+@pytest.mark.parametrize("n", [[1, 3], [40, 66]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_of_any_kind(dev, n, d):
+    # a cache filled by the caller: scales that are no powers of two, negative ones and zeros among them
     import torch
-    both = Both(dev, 2, 4, 1, 64, 16, 200)
+    both = Both(dev, 2, 4, 1, d, 16, 250)
     both.append([150, 77])
-    _, q = both.append([1, 3])
+    _, q = both.append(n)
     r = np.random.default_rng(5)
     for s in range(2):
         for seq, scales in ((both.k[s], both.c.k_scale), (both.v[s], both.c.v_scale)):
-            f = r.uniform(0.5, 1.5, seq.scales.shape) * r.choice([-1.0, 1.0], seq.scales.shape)
+            f = r.uniform(0.5, 1.5, seq.scales.shape) * r.choice([-1.0, 1.0, 0.0], seq.scales.shape)
+            f[:, 3] = 1.0
             seq.scales = np.float64(np.float32(seq.scales * f))
             for b in range(seq.scales.shape[1]):
                 scales[int(both.table[s, b]), :, 0] = torch.from_numpy(np.float32(seq.scales[:, b])).to(dev)
-    both.check_attend(q, [1, 3])
+    both.check_attend(q, n)
 
 
 def test_pages_in_common(dev):
