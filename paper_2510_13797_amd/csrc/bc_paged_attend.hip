@@ -6,14 +6,16 @@
 //
 // The query heads of a KV head see the same entries, so (row, head) pairs are the columns of the products: column i * g + h.  A tile is two blocks of 16 entries, which
 // come from memory as operands (bc_paged.h) and become bf16 by the hardware's conversion, exactly: S^T = K.Q^T by 16x16x32 MFMA, whose result has four entries of a
-// column in a lane; a word of values is those four entries of one element, so O^T += V^T.P^T takes both as they are.  A block's key scale is a factor of its scores, its
-// value scale one of its weights (in fp32, in front of their split into three bf16 parts, 24 bits).  Softmax online, sums in fp32.
+// column in a lane; a word of values is those four entries of one element, so O^T += V^T.P^T takes both as they are.  The conversion takes the
+// block's scale along where it is a power of two, exactly (other scales are factors of its scores and weights).  Weights enter their product in bf16 parts, three (24 bits) where there are
+// few columns, two (17 bits) where there are many.  Softmax online, sums in fp32.
 #include "bc_paged.h"
 
 namespace bc {
 namespace {
 
-constexpr float kMasked = 2.f * kNegBig;       // a score that no maximum is below
+constexpr float kRedo = 256.f;                 // a lane's weights of a tile may sum to this before the reference moves,
+constexpr float kLazy = 2.f;                   // and then it moves where a column's maximum is this much (log2) above it
 
 struct AttendParams {
   PagedTables t;
@@ -48,14 +50,19 @@ __device__ __forceinline__ f32x4_t load16_past(__amdgpu_buffer_rsrc_t parts, uin
 }
 __device__ __forceinline__ u32x2_v load8_past(__amdgpu_buffer_rsrc_t parts, uint32_t at) { return __builtin_amdgcn_raw_buffer_load_b64(parts, at, 0, kPast); }
 
-__device__ __forceinline__ uint32_t bf16_of(uint32_t w, bool high) {
-  return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true))
-              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false));
+// A scale as the conversion's factor and what is left of it: one for a power of two.
+__device__ __forceinline__ bool power_of_two_scale(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return (u & 0x807fffffu) == 0 && u - 0x00800000u < 0x7f000000u;
 }
-// eight e4m3 values (two words) as an operand
-__device__ __forceinline__ bf16x8_t operand_of(uint32_t a, uint32_t b) {
-  return __builtin_bit_cast(bf16x8_t, u32x4_t{bf16_of(a, false), bf16_of(a, true), bf16_of(b, false), bf16_of(b, true)});
+__device__ __forceinline__ uint32_t scaled_bf16(uint32_t w, float scale, bool high) {
+  return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))
+              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
 }
+__device__ __forceinline__ u32x4_t scaled_operand(uint32_t a, uint32_t b, float scale) {
+  return u32x4_t{scaled_bf16(a, scale, false), scaled_bf16(a, scale, true), scaled_bf16(b, scale, false), scaled_bf16(b, scale, true)};
+}
+
 __device__ __forceinline__ f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -136,7 +143,9 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
         page = 0;
       }
       const uint32_t unit = (((uint32_t)page * p.Hkv + kvh) << per_page) + (at_block & ((1 << per_page) - 1));
-      const float k_scale = p.ks[unit] * p.qs, v_scale = p.vs[unit];
+      const float qs = CT == 1 ? 1.f : p.qs, k_scale = CT == 1 ? p.ks[unit] * p.qs : p.ks[unit], v_scale = p.vs[unit];
+      // (With one tile of columns scales are always factors of the results: two ways through the code cost a short step half a microsecond, 9.7 -> 10.3 us.)
+      const bool uneven = CT == 1 || __any(at_block <= last && (lane >> 1) < count && !(power_of_two_scale(k_scale) && power_of_two_scale(v_scale)));
 
       // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are formed, its values
       // behind the weights' product.
@@ -159,57 +168,73 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
         f32x4_t sc[CT][2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
+          const float scale = uneven ? 1.f : __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) sc[ct][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const bf16x8_t a = operand_of(key[b][h][2 * e], key[b][h][2 * e + 1]);
+              const bf16x8_t a = __builtin_bit_cast(bf16x8_t, scaled_operand(key[b][h][2 * e], key[b][h][2 * e + 1], scale));
 #pragma unroll
               for (int ct = 0; ct < CT; ++ct) sc[ct][b] = mfma16(a, q[ct][2 * h + e], sc[ct][b]);
             }
         }
         if (i + 1 < count) load(key, p.k, k_lane, i + 1);
-        const bool ends = key0 + 32 > seen_by_all;
+        if (uneven) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) sc[ct][b] *= __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
+        }
+        const bool ends = key0 + 32 > seen_by_all;                   // some columns do not see all of it
+        if (CT == 1 && ends) {
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            if (key0 + 16 * (r >> 2) + 4 * g4 + (r & 3) >= key_lim[0]) sc[0][r >> 2][r & 3] = 2.f * kNegBig;
+        }
         bf16x8_t part[CT][3];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          float z[8];
-          float top = kMasked;
+          float w[8], sum;
+          const int there = key_lim[ct] - key0 - 4 * g4;
+          auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const float f = __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
+            for (int r = 0; r < 8; ++r) w[r] = fast_exp2(fmaf(sc[ct][r >> 2][r & 3], qs, -m[ct]));
+            if (CT > 1 && ends) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) z[4 * b + r] = sc[ct][b][r] * f;
-          }
-          if (ends) {
+              for (int r = 0; r < 8; ++r) w[r] = 16 * (r >> 2) + (r & 3) < there ? w[r] : 0.f;
+            }
+            sum = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+          };
+          auto move = [&]() __attribute__((always_inline)) {   // the reference, to the column's maximum
+            float top = kNegBig;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (key0 + 16 * b + 4 * g4 + r >= key_lim[ct]) z[4 * b + r] = kMasked;
-          }
-#pragma unroll
-          for (int r = 0; r < 8; ++r) top = fmaxf(top, z[r]);
-          top = fmaxf(rows_allreduce_max(top), m[ct]);
-          if (__any(top > m[ct])) {
-            const float was = fast_exp2(m[ct] - top);
-            l[ct] *= was;
+            for (int r = 0; r < 8; ++r) top = fmaxf(top, CT == 1 || 16 * (r >> 2) + (r & 3) < there ? sc[ct][r >> 2][r & 3] * qs : kNegBig);
+            top = rows_allreduce_max(top);
+            const float to = CT == 1 ? fmaxf(top, m[ct]) : top > m[ct] + kLazy ? top : m[ct];
+            if (!__any(to > m[ct])) return;
+            const float was = fast_exp2(m[ct] - to);
+            m[ct] = to; l[ct] *= was;
 #pragma unroll
             for (int j = 0; j < 4 * H; ++j) o[ct][j] *= was;
-            m[ct] = top;
-          }
-          float w[8];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const float f = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + b));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float e = fast_exp2(z[4 * b + r] - m[ct]);
-              l[ct] += e;
-              w[4 * b + r] = e * f;
+          };
+          // With two tiles of columns vector work counts: the maximum is formed only where weights get large (38.7 -> 35.3 us for 16 x 1-8 rows over 900 to 6000,
+          // 32/8 heads).  With one, a wave's two or three tiles would pay for forming the first one's weights twice.
+          if constexpr (CT == 1) {
+            move();
+            weights();
+          } else {
+            weights();
+            if (__builtin_expect(__any(sum > kRedo), 0)) {
+              move();
+              weights();
             }
+          }
+          l[ct] += sum;
+          if (uneven) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) w[r] *= __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + (r >> 2)));
           }
 #pragma unroll
           for (int k = 0; k < 3; ++k) {
@@ -234,11 +259,14 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
               for (int j = 0; j < 4; ++j) value[b][h][j] &= mask;
           }
         }
+        const float v0 = uneven ? 1.f : __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i));
+        const float v1 = uneven ? 1.f : __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + 1));
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const bf16x8_t a = operand_of(value[0][h][j], value[1][h][j]);
+            const uint32_t x = value[0][h][j], y = value[1][h][j];
+            const bf16x8_t a = __builtin_bit_cast(bf16x8_t, u32x4_t{scaled_bf16(x, v0, false), scaled_bf16(x, v0, true), scaled_bf16(y, v1, false), scaled_bf16(y, v1, true)});
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -362,27 +390,11 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
 // keys are half of an operand, the lane's other word the other half, and results have d / 32 elements in a row.
 // ---------------------------------------------------------------------------
 constexpr int kManyWaves = 4, kManyColumns = 32 * kManyWaves, kManyTile = 16 * kManyWaves;
-constexpr float kRedo = 256.f;      // a lane's 32 weights may sum to this before the reference moves
-constexpr float kLazy = 2.f;        // ... where a column's maximum is this much (log2) above it
-
 // Tiles of a block of columns, and those of one of its parts.
 struct ManyCut { int tiles, t0, t1, parts; };
 __device__ __forceinline__ ManyCut many_cut(int parts, int lim, int part) {
   const int tiles = (lim + kManyTile - 1) / kManyTile, n = min(parts, max(1, tiles >> 2));      // (no part of fewer than four tiles)
   return {tiles, (int)((int64_t)tiles * part / n), (int)((int64_t)tiles * (part + 1) / n), n};
-}
-
-// A scale as the conversion's factor and what is left of it: one for a power of two.
-__device__ __forceinline__ bool power_of_two_scale(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return (u & 0x807fffffu) == 0 && u - 0x00800000u < 0x7f000000u;
-}
-__device__ __forceinline__ uint32_t scaled_bf16(uint32_t w, float scale, bool high) {
-  return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))
-              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
-}
-__device__ __forceinline__ u32x4_t scaled_operand(uint32_t a, uint32_t b, float scale) {
-  return u32x4_t{scaled_bf16(a, scale, false), scaled_bf16(a, scale, true), scaled_bf16(b, scale, false), scaled_bf16(b, scale, true)};
 }
 
 template <int D>
@@ -507,14 +519,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 #pragma unroll
           for (int e = 0; e < 16; ++e) sc[x][e] *= s_rest[stage][2 * x + e / 8].x;
       }
-      if (t >= free_tiles) {
-        const int there = lim - kManyTile * t - 4 * half;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (32 * x + 8 * (e >> 2) + (e & 3) >= there) sc[x][e] = kMasked;
-      }
+      const bool ends = t >= free_tiles;                         // some columns do not see all of it
+      const int there = lim - kManyTile * t - 4 * half;
       float pe[2][16], psum;
       auto weights = [&]() __attribute__((always_inline)) {
         float sum[2];
@@ -522,6 +528,10 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         for (int x = 0; x < 2; ++x) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) pe[x][e] = fast_exp2(fmaf(sc[x][e], p.qs, -m));
+          if (ends) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) pe[x][e] = 32 * x + 8 * (e >> 2) + (e & 3) < there ? pe[x][e] : 0.f;
+          }
           sum[x] = (((pe[x][0] + pe[x][1]) + (pe[x][2] + pe[x][3])) + ((pe[x][4] + pe[x][5]) + (pe[x][6] + pe[x][7]))) +
                    (((pe[x][8] + pe[x][9]) + (pe[x][10] + pe[x][11])) + ((pe[x][12] + pe[x][13]) + (pe[x][14] + pe[x][15])));
         }
@@ -529,11 +539,11 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
       };
       weights();
       if (__builtin_expect(__any(psum > kRedo), 0)) {
-        float top = kMasked;
+        float top = kNegBig;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[x][e] > 0.5f * kMasked ? sc[x][e] * p.qs : kMasked);
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, 32 * x + 8 * (e >> 2) + (e & 3) < there ? sc[x][e] * p.qs : kNegBig);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float to = top > m + kLazy ? top : m, was = fast_exp2(m - to);
         m = to; l *= was;

@@ -365,7 +365,13 @@ def test_the_sum_where_the_scale_is_zero_and_where_scores_are_large(dev):
     _, q = both.append([1, 1])
     both.c.shape.scale = 0.0
     both.check_attend(q, [1, 1], scale=0.0)
-    both.c.shape.scale = 128 ** -0.5
+    for n in ([40, 3], [2, 8], [200, 31]):
+        both = Both(dev, 2, 8, 2, 128, 16, 900)
+        both.append([300, 0])
+        _, q = both.append(n)
+        for scale in (0.0, 1e-30, 1e-6):
+            both.c.shape.scale = scale
+            both.check_attend(q, n, scale=scale, every=3)
     # scores of some hundreds: weights of 0 and 1; a score is off by 128 roundings of up to 2^-24 of some 1e4
     both = Both(dev, 2, 8, 2, 128, 16, 300)
     both.append([200, 90], size=20.0)
