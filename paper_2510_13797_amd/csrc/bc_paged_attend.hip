@@ -37,6 +37,8 @@ struct AttendParams {
 // Partial results go past the caches in both directions (the L2s of the XCDs do not see each other's lines): buffer accesses of system scope.
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_v;
 typedef __attribute__((ext_vector_type(2))) float f32x2_v;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_v;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_v;
 constexpr int kPast = 1 | 16;                  // sc0, sc1
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t parts_of(float* part) { return __builtin_amdgcn_make_buffer_rsrc(part, 0, 0x7fffffff, 0x27000); }
 __device__ __forceinline__ void store16_past(__amdgpu_buffer_rsrc_t parts, uint32_t at, const f32x4_t& x) {
@@ -63,6 +65,26 @@ __device__ __forceinline__ u32x4_t scaled_operand(uint32_t a, uint32_t b, float 
   return u32x4_t{scaled_bf16(a, scale, false), scaled_bf16(a, scale, true), scaled_bf16(b, scale, false), scaled_bf16(b, scale, true)};
 }
 
+// eight e4m3 values (two words) as an operand in half precision: exact
+__device__ __forceinline__ u32x4_t half_operand(uint32_t a, uint32_t b) {
+  return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true))};
+}
+// f u, f v -> two pairs in half precision, the second one what the first leaves (22 bits together; the least step is 2^-24)
+__device__ __forceinline__ void split_halves(float u, float v, float f, uint32_t& hi, uint32_t& lo) {
+  const f16x2_v h = __builtin_convertvector(f32x2_v{u * f, v * f}, f16x2_v);
+  hi = __builtin_bit_cast(uint32_t, h);
+  lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_v{fmaf(u, f, -(float)h[0]), fmaf(v, f, -(float)h[1])}, f16x2_v));
+}
+// The level of a column's values.  Weights times their block's value scale enter products in half precision, so what they are brought to has to go with the product: sums
+// are kept as `f` times what they are, f a power of two, so that no factor passes 2^14 and the largest came to 2^8 when f was last set.  What was small beside that is as small
+// in the result.  f starts where nothing is too large and sums are zero.
+constexpr float kLevelMost = 16384.f, kLevelStart = 0x1p127f;
+__device__ __forceinline__ float level_for(float largest) {      // 2^8 over it, as a power of two (up to 2^127)
+  return __uint_as_float(min(254u, 254u + 8u - (__float_as_uint(largest) >> 23)) << 23);
+}
 __device__ __forceinline__ f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -401,8 +423,9 @@ template <int D>
 __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendParams p) {
   constexpr int KS = D / 16, NJ = D / 32, K_BYTES = kManyTile * D * 2, STAGE = 2 * K_BYTES, BLOCK_BYTES = kPagedBlock * D;
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
-  __shared__ float2 s_rest[2][kManyWaves];                       // what the conversions left of a block's scales, of keys and of values
-  __shared__ int s_uneven;                                       // whether that has been anything but ones
+  __shared__ float s_rest[2][kManyWaves];                        // what the conversion left of a block's key scale,
+  __shared__ int s_uneven;                                       // whether that has been anything but ones,
+  __shared__ f32x4_t s_value[2];                                 // value scales
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const uint32_t pairs = (uint32_t)p.t.B * p.Hkv;
   uint32_t id = blockIdx.x;
@@ -430,7 +453,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   f32x16_t O[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) O[j] = f32x16_t{0.f};
-  float m = kNegBig, l = 0.f;
+  float m = kNegBig, l = 0.f, level = kLevelStart;               // m: a whole number, once it has moved
 
   // A tile's bytes on their way: the wave's block of it.
   const int per_page = p.t.page_shift - 4, last_block = (L - 1) >> 4;
@@ -458,11 +481,12 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   };
   auto put = [&](int t, int stage) {
     char* to = lds + stage * STAGE;
-    const bool ke = power_of_two_scale(k_scale), ve = power_of_two_scale(v_scale);
-    const float kf = ke ? k_scale : 1.f, vf = ve ? v_scale : 1.f;
+    const bool ke = power_of_two_scale(k_scale);
+    const float kf = ke ? k_scale : 1.f;
     if (lane == 0) {
-      s_rest[stage][wave] = make_float2(ke ? 1.f : k_scale, ve ? 1.f : v_scale);
-      if (!ke || !ve) s_uneven = 1;
+      s_rest[stage][wave] = ke ? 1.f : k_scale;
+      s_value[stage][wave] = v_scale;
+      if (!ke) s_uneven = 1;
     }
 #pragma unroll
     for (int x = 0; x < D / 64; ++x) {                           // rows of the block: 4 * group + (lane / 4) % 4
@@ -484,7 +508,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const uint32_t a = D == 128 ? vb[0][j] : vb[0][j & 1], b = D == 128 ? vb[D / 64 - 1][j] : vb[0][2 + (j & 1)];
-      *reinterpret_cast<u32x4_t*>(place + j * 1024) = scaled_operand(a & keep[0], b & keep[1], vf);
+      *reinterpret_cast<u32x4_t*>(place + j * 1024) = half_operand(a & keep[0], b & keep[1]);
     }
   };
 
@@ -517,7 +541,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sc[x][e] *= s_rest[stage][2 * x + e / 8].x;
+          for (int e = 0; e < 16; ++e) sc[x][e] *= s_rest[stage][2 * x + e / 8];
       }
       const bool ends = t >= free_tiles;                         // some columns do not see all of it
       const int there = lim - kManyTile * t - 4 * half;
@@ -545,36 +569,43 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 #pragma unroll
           for (int e = 0; e < 16; ++e) top = fmaxf(top, 32 * x + 8 * (e >> 2) + (e & 3) < there ? sc[x][e] * p.qs : kNegBig);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float to = top > m + kLazy ? top : m, was = fast_exp2(m - to);
+        const float to = top > m + kLazy ? ceilf(top) : m, was = fast_exp2(m - to), up = level * fast_exp2(to - m);
         m = to; l *= was;
+        // (sums keep their level, or are nothing beside what there will be)
+        if (!(up <= kLevelStart)) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) O[j] *= was;
+          for (int j = 0; j < NJ; ++j) O[j] = f32x16_t{0.f};
+        }
+        level = fminf(up, kLevelStart);
         weights();
       }
       l += psum;
-      if (__builtin_expect(uneven, 0)) {
+      const f32x4_t scales = s_value[stage];
+      const float largest = psum * fmaxf(fmaxf(fabsf(scales[0]), fabsf(scales[1])), fmaxf(fabsf(scales[2]), fabsf(scales[3])));
+      if (__builtin_expect(__any(largest * level > kLevelMost), 0)) {
+        const float both = fmaxf(largest, __shfl_xor(largest, 32, 64)), to = both * level > kLevelMost ? level_for(both) : level, was = to / level;
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) pe[x][e] *= s_rest[stage][2 * x + e / 8].y;
+        for (int j = 0; j < NJ; ++j) O[j] *= was;
+        level = to;
       }
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         u32x4_t hi, lo;
         if (b == 0) __builtin_amdgcn_s_setprio(1);
+        const float f = scales[b] * level;
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-          const float u = pe[b >> 1][8 * (b & 1) + 2 * y], w = pe[b >> 1][8 * (b & 1) + 2 * y + 1];
-          hi[y] = pack2_bf16(u, w);
-          lo[y] = pack2_bf16(u - __uint_as_float(hi[y] << 16), w - __uint_as_float(hi[y] & 0xffff0000u));
+          uint32_t h, r;
+          split_halves(pe[b >> 1][8 * (b & 1) + 2 * y], pe[b >> 1][8 * (b & 1) + 2 * y + 1], f, h, r);
+          hi[y] = h; lo[y] = r;
         }
-        bf16x8_t a[NJ];
+        f16x8_v a[NJ];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) a[j] = *reinterpret_cast<const bf16x8_t*>(tile + K_BYTES + b * (NJ * 1024) + j * 1024 + half * 512 + col * 16);
+        for (int j = 0; j < NJ; ++j) a[j] = *reinterpret_cast<const f16x8_v*>(tile + K_BYTES + b * (NJ * 1024) + j * 1024 + half * 512 + col * 16);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[j], __builtin_bit_cast(bf16x8_t, hi), O[j], 0, 0, 0);
+        for (int j = 0; j < NJ; ++j) O[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[j], __builtin_bit_cast(f16x8_v, hi), O[j], 0, 0, 0);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[j], __builtin_bit_cast(bf16x8_t, lo), O[j], 0, 0, 0);
+        for (int j = 0; j < NJ; ++j) O[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[j], __builtin_bit_cast(f16x8_v, lo), O[j], 0, 0, 0);
       }
     }
     __builtin_amdgcn_s_setprio(0);
@@ -585,14 +616,14 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   const int64_t at = (span.row + i) * p.Hq + kvh * p.g + (c - i * p.g);
   const bool whole = cut.parts == 1;
   float* to = whole ? p.out + at * D : p.part + (part * (p.t.rows * p.Hq) + at) * D;
-  const float f = whole ? 1.f / l : 1.f;
+  const float f = 1.f / level, inv = whole ? 1.f / l : 1.f;      // (one after the other: their product may be too small)
   if (!whole && half == 0) p.part_ml[part * (p.t.rows * p.Hq) + at] = make_float2(m, l);
   // result e of block j: its row 8 (e / 4) + 4 half + e % 4
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     const int row = 8 * (e >> 2) + 4 * half + (e & 3);
-    if constexpr (D == 128) *reinterpret_cast<f32x4_t*>(to + 4 * row) = f32x4_t{O[0][e] * f, O[1][e] * f, O[NJ - 2][e] * f, O[NJ - 1][e] * f};
-    else *reinterpret_cast<f32x2_v*>(to + 2 * row) = f32x2_v{O[0][e] * f, O[1][e] * f};
+    if constexpr (D == 128) *reinterpret_cast<f32x4_t*>(to + 4 * row) = f32x4_t{O[0][e] * f * inv, O[1][e] * f * inv, O[NJ - 2][e] * f * inv, O[NJ - 1][e] * f * inv};
+    else *reinterpret_cast<f32x2_v*>(to + 2 * row) = f32x2_v{O[0][e] * f * inv, O[1][e] * f * inv};
   }
 }
 
