@@ -482,8 +482,8 @@ int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t ro
 /* Attention of the newest rows, whose keys and values are in the pages already: with L = len[s] entries and n rows of sequence s (spans as for bc_paged_append),
  *   out[i,h,:] = sum_j softmax_j(scale * q[i,h,:] . K_j[kvh,:]) V_j[kvh,:],  j over entries 0 .. L - n + i.
  * One row a sequence is a decode step, a few are drafted tokens that are checked, many a chunk of a prompt.  q: [rows, Hq, d] BF16 (kv_dtype is not read);
- * out: [rows, Hq, d] fp32.  scale finite and >= 0.  Scales of blocks may be any finite numbers.  A softmax weight enters its product with V in two bf16 parts (17 bits).
- * Sequences that are not active or have no rows are left alone, their rows of out with them; one with an invalid span, fewer entries than rows or more than max_len sets the
+ * out: [rows, Hq, d] fp32.  scale finite and >= 0.  Scales of blocks may be any finite numbers.  A softmax weight enters its product with
+ * V in two half-precision parts: 22 bits, and at least 2^-32 of the row's largest product.  Sequences that are not active or have no rows are left alone, their rows of out with them; one with an invalid span, fewer entries than rows or more than max_len sets the
  * state bit and is left alone; one with an invalid page for its entries sets the state bit, nothing is read out of range, and its rows of out are unspecified.
  * Entries that a row sees, and those of its sequence behind it, are finite: a product with one that is not may show in rows that do not see it.  What lies behind the
  * last entry may be anything.  No atomics on results: they are reproducible.

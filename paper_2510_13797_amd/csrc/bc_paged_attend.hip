@@ -5,10 +5,10 @@
 //   K_j = key bytes * their block's scale, V_j likewise
 //
 // The query heads of a KV head see the same entries, so (row, head) pairs are the columns of the products: column i * g + h.  A tile is two blocks of 16 entries, which
-// come from memory as operands (bc_paged.h) and become bf16 by the hardware's conversion, exactly: S^T = K.Q^T by 16x16x32 MFMA, whose result has four entries of a
-// column in a lane; a word of values is those four entries of one element, so O^T += V^T.P^T takes both as they are.  The conversion takes the
-// block's scale along where it is a power of two, exactly (other scales are factors of its scores and weights).  Weights enter their product in bf16 parts, three (24 bits) where there are
-// few columns, two (17 bits) where there are many.  Softmax online, sums in fp32.
+// come from memory as operands (bc_paged.h) and become bf16 or half precision by the hardware's conversions, exactly: S^T = K.Q^T by 16x16x32 MFMA, whose result has four entries of a
+// column in a lane; a word of values is those four entries of one element, so O^T += V^T.P^T takes both as they are.  A key scale that is a power of
+// two goes along with the conversion, exactly; others are factors of their block's scores.  Values become half precision without their scale, which is a factor of the
+// weights; those enter their product in two half-precision parts (22 bits) at a level that goes with the products (kLevelMost).  Softmax online, sums in fp32.
 #include "bc_paged.h"
 
 namespace bc {
@@ -144,10 +144,10 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
         for (int e = 0; e < 2; ++e) q[ct][2 * h + e] = *reinterpret_cast<const bf16x8_t*>(at + 128 * h + 16 * e);
     }
     f32x4_t o[CT][4 * H];
-    float m[CT], l[CT];
+    float m[CT], l[CT], level[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      m[ct] = kNegBig; l[ct] = 0.f;
+      m[ct] = kNegBig; l[ct] = 0.f; level[ct] = kLevelStart;
 #pragma unroll
       for (int i = 0; i < 4 * H; ++i) o[ct][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
       }
       const uint32_t unit = (((uint32_t)page * p.Hkv + kvh) << per_page) + (at_block & ((1 << per_page) - 1));
       const float qs = CT == 1 ? 1.f : p.qs, k_scale = CT == 1 ? p.ks[unit] * p.qs : p.ks[unit], v_scale = p.vs[unit];
-      // (With one tile of columns scales are always factors of the results: two ways through the code cost a short step half a microsecond, 9.7 -> 10.3 us.)
-      const bool uneven = CT == 1 || __any(at_block <= last && (lane >> 1) < count && !(power_of_two_scale(k_scale) && power_of_two_scale(v_scale)));
+      // (With one tile of columns key scales are always factors of the scores: two ways through the code cost a short step half a microsecond, 9.7 -> 10.3 us.)
+      const bool uneven = CT == 1 || __any(at_block <= last && (lane >> 1) < count && !power_of_two_scale(k_scale));
 
       // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are formed, its values
       // behind the weights' product.
@@ -215,10 +215,11 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
           for (int r = 0; r < 8; ++r)
             if (key0 + 16 * (r >> 2) + 4 * g4 + (r & 3) >= key_lim[0]) sc[0][r >> 2][r & 3] = 2.f * kNegBig;
         }
-        bf16x8_t part[CT][3];
+        f16x8_v part[CT][2];
+        const float v0 = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i)), v1 = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + 1));
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          float w[8], sum;
+          float w[8], sums[2], sum;
           const int there = key_lim[ct] - key0 - 4 * g4;
           auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -227,19 +228,25 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
 #pragma unroll
               for (int r = 0; r < 8; ++r) w[r] = 16 * (r >> 2) + (r & 3) < there ? w[r] : 0.f;
             }
-            sum = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+            sums[0] = (w[0] + w[1]) + (w[2] + w[3]); sums[1] = (w[4] + w[5]) + (w[6] + w[7]);
+            sum = sums[0] + sums[1];
           };
           auto move = [&]() __attribute__((always_inline)) {   // the reference, to the column's maximum
             float top = kNegBig;
 #pragma unroll
             for (int r = 0; r < 8; ++r) top = fmaxf(top, CT == 1 || 16 * (r >> 2) + (r & 3) < there ? sc[ct][r >> 2][r & 3] * qs : kNegBig);
             top = rows_allreduce_max(top);
-            const float to = CT == 1 ? fmaxf(top, m[ct]) : top > m[ct] + kLazy ? top : m[ct];
+            const float to = top > m[ct] + (CT == 1 ? 0.f : kLazy) ? ceilf(top) : m[ct];
             if (!__any(to > m[ct])) return;
-            const float was = fast_exp2(m[ct] - to);
-            m[ct] = to; l[ct] *= was;
+            const float up = level[ct] * fast_exp2(to - m[ct]);
+            l[ct] *= fast_exp2(m[ct] - to);
+            m[ct] = to;
+            // (sums keep their level, or are nothing beside what there will be)
+            if (!(up <= kLevelStart)) {
 #pragma unroll
-            for (int j = 0; j < 4 * H; ++j) o[ct][j] *= was;
+              for (int j = 0; j < 4 * H; ++j) o[ct][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+            level[ct] = fminf(up, kLevelStart);
           };
           // With two tiles of columns vector work counts: the maximum is formed only where weights get large (38.7 -> 35.3 us for 16 x 1-8 rows over 900 to 6000,
           // 32/8 heads).  With one, a wave's two or three tiles would pay for forming the first one's weights twice.
@@ -254,21 +261,22 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
             }
           }
           l[ct] += sum;
-          if (uneven) {
+          const float largest = fmaxf(sums[0] * fabsf(v0), sums[1] * fabsf(v1));     // (block by block: a heavy key has nothing to do with another block's scale)
+          if (__builtin_expect(__any(largest * level[ct] > kLevelMost), 0)) {
+            const float all = rows_allreduce_max(largest), to = all * level[ct] > kLevelMost ? level_for(all) : level[ct], was = to / level[ct];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) w[r] *= __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + (r >> 2)));
+            for (int j = 0; j < 4 * H; ++j) o[ct][j] *= was;
+            level[ct] = to;
           }
+          u32x4_t hi, lo;
 #pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            u32x4_t x;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              x[r] = pack2_bf16(w[2 * r], w[2 * r + 1]);
-              w[2 * r] -= __uint_as_float(x[r] << 16);
-              w[2 * r + 1] -= __uint_as_float(x[r] & 0xffff0000u);
-            }
-            part[ct][k] = __builtin_bit_cast(bf16x8_t, x);
+          for (int r = 0; r < 4; ++r) {
+            uint32_t h, x;
+            split_halves(w[2 * r], w[2 * r + 1], (r < 2 ? v0 : v1) * level[ct], h, x);
+            hi[r] = h; lo[r] = x;
           }
+          part[ct][0] = __builtin_bit_cast(f16x8_v, hi);
+          part[ct][1] = __builtin_bit_cast(f16x8_v, lo);
         }
         if (key0 + 32 > L) {                     // bytes behind the last entry may be anything: zeros, not a product with a weight of zero
 #pragma unroll
@@ -281,18 +289,16 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
               for (int j = 0; j < 4; ++j) value[b][h][j] &= mask;
           }
         }
-        const float v0 = uneven ? 1.f : __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i));
-        const float v1 = uneven ? 1.f : __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + 1));
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t x = value[0][h][j], y = value[1][h][j];
-            const bf16x8_t a = __builtin_bit_cast(bf16x8_t, u32x4_t{scaled_bf16(x, v0, false), scaled_bf16(x, v0, true), scaled_bf16(y, v1, false), scaled_bf16(y, v1, true)});
+            const f16x8_v a = __builtin_bit_cast(f16x8_v, half_operand(value[0][h][j], value[1][h][j]));
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-              for (int k = 0; k < 3; ++k) o[ct][4 * h + j] = mfma16(a, part[ct][k], o[ct][4 * h + j]);
+              for (int k = 0; k < 2; ++k)
+                o[ct][4 * h + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, part[ct][k], o[ct][4 * h + j], 0, 0, 0);
           }
         if (i + 1 < count) load(value, p.v, v_lane, i + 1);
       }
@@ -302,13 +308,14 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       const float sum = rows_allreduce_sum(l[ct]);
+      const float f = 1.f / level[ct];
       if (g4 == 0) { s_ml[wave][16 * ct + c16][0] = m[ct]; s_ml[wave][16 * ct + c16][1] = sum; }
 #pragma unroll
       for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           *reinterpret_cast<f32x4_t*>(&s_o[wave][16 * ct + c16][64 * h + 16 * g4 + 4 * r]) =
-              f32x4_t{o[ct][4 * h][r], o[ct][4 * h + 1][r], o[ct][4 * h + 2][r], o[ct][4 * h + 3][r]};
+              f32x4_t{o[ct][4 * h][r], o[ct][4 * h + 1][r], o[ct][4 * h + 2][r], o[ct][4 * h + 3][r]} * f;
     }
     __syncthreads();
     const bool whole = count == 1;
@@ -406,8 +413,8 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
 
 
 // ---------------------------------------------------------------------------
-// Many columns: 32 a wave, the workgroup's four share tiles of 64 entries.  A wave brings the bytes of one of a tile's four blocks, makes them bf16 times their scale (the
-// conversion takes a power of two, and is exact) and leaves them in LDS as the operands of 32x32x16 products, 16 bytes a lane: keys [32 entries][d / 16][half][entry],
+// Many columns: 32 a wave, the workgroup's four share tiles of 64 entries.  A wave brings the bytes of one of a tile's four blocks, converts them (keys
+// to bf16, values to half precision) and leaves them in LDS as the operands of 32x32x16 products, 16 bytes a lane: keys [32 entries][d / 16][half][entry],
 // element 16 i + 8 half + e of a key (its place among the 32 turned by i, so that the writes meet no bank twice); values [16 entries][j][half][row], element (d / 32) row + j: a word's four
 // keys are half of an operand, the lane's other word the other half, and results have d / 32 elements in a row.
 // ---------------------------------------------------------------------------
@@ -545,9 +552,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
       }
       const bool ends = t >= free_tiles;                         // some columns do not see all of it
       const int there = lim - kManyTile * t - 4 * half;
-      float pe[2][16], psum;
+      float pe[2][16], sums[4], psum;                            // sums: of blocks
       auto weights = [&]() __attribute__((always_inline)) {
-        float sum[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
 #pragma unroll
@@ -556,10 +562,10 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 #pragma unroll
             for (int e = 0; e < 16; ++e) pe[x][e] = 32 * x + 8 * (e >> 2) + (e & 3) < there ? pe[x][e] : 0.f;
           }
-          sum[x] = (((pe[x][0] + pe[x][1]) + (pe[x][2] + pe[x][3])) + ((pe[x][4] + pe[x][5]) + (pe[x][6] + pe[x][7]))) +
-                   (((pe[x][8] + pe[x][9]) + (pe[x][10] + pe[x][11])) + ((pe[x][12] + pe[x][13]) + (pe[x][14] + pe[x][15])));
+          sums[2 * x] = ((pe[x][0] + pe[x][1]) + (pe[x][2] + pe[x][3])) + ((pe[x][4] + pe[x][5]) + (pe[x][6] + pe[x][7]));
+          sums[2 * x + 1] = ((pe[x][8] + pe[x][9]) + (pe[x][10] + pe[x][11])) + ((pe[x][12] + pe[x][13]) + (pe[x][14] + pe[x][15]));
         }
-        psum = sum[0] + sum[1];
+        psum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
       };
       weights();
       if (__builtin_expect(__any(psum > kRedo), 0)) {
@@ -581,7 +587,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
       }
       l += psum;
       const f32x4_t scales = s_value[stage];
-      const float largest = psum * fmaxf(fmaxf(fabsf(scales[0]), fabsf(scales[1])), fmaxf(fabsf(scales[2]), fabsf(scales[3])));
+      const float largest = fmaxf(fmaxf(sums[0] * fabsf(scales[0]), sums[1] * fabsf(scales[1])), fmaxf(sums[2] * fabsf(scales[2]), sums[3] * fabsf(scales[3])));
       if (__builtin_expect(__any(largest * level > kLevelMost), 0)) {
         const float both = fmaxf(largest, __shfl_xor(largest, 32, 64)), to = both * level > kLevelMost ? level_for(both) : level, was = to / level;
 #pragma unroll

@@ -3,7 +3,7 @@
 What is appended without norm and rotation is exact: a scale is a power of two, a byte one rounding to nearest.  With them fp32 arithmetic comes first, off by less
 than 2e-6 of the row's largest magnitude (a dozen operations of 2^-24 and a series good to 1e-7), so a value is off by half a step of e4m3 (2^-4 of it, 2^-10 of its scale
 below 2^-6 of that) and 2e-6 of the largest; queries by half a step of bf16 (2^-8 of a value, as torch.finfo counts) and the same.
-Attention reads exact values; a softmax weight enters its product in two bf16 parts (2^-17), scores are fp32 sums of up to 128 products behind a 2^x of one step:
+Attention reads exact values; a softmax weight enters its product in two half-precision parts (2^-22), scores are fp32 sums of up to 128 products behind a 2^x of one step:
 a weight is off by less than 2e-5, outputs of N(0, 1) values (below 5 in magnitude) by less than 1e-4."""
 import numpy as np
 import pytest
@@ -396,6 +396,54 @@ def test_scales_of_any_kind(dev, n, d):
             for b in range(seq.scales.shape[1]):
                 scales[int(both.table[s, b]), :, 0] = torch.from_numpy(np.float32(seq.scales[:, b])).to(dev)
     both.check_attend(q, n)
+
+
+@pytest.mark.parametrize("n", [[1, 2], [6, 8], [40, 66]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_of_very_different_sizes(dev, n, d):
+    # blocks of values from 1e-25 to 1e25, empty ones among them, under scores that let now these, now those weigh something.  A product of a weight and a value is in two
+    # half-precision parts whose least step is 2^-32 of the largest product so far: an output is off by less than 1e-5 of the largest product of its row
+    import torch
+    both = Both(dev, 2, 4, 2, d, 16, 700)
+    r = np.random.default_rng(7)
+    lens = [600, 333]
+    for s in range(2):                                                  # sixteen rows at a time, so that a block has a size of its own
+        for at in range(0, lens[s], 16):
+            m = [0, 0]
+            m[s] = min(16, lens[s] - at)
+            x = both.packed(m[s])
+            size = 10.0 ** r.uniform(-25, 25) if at % 48 else 0.0
+            x[:, (4 + 2) * d:] *= size
+            x[:, 4 * d:6 * d] *= 10.0 ** r.uniform(-1, 0.7)
+            both.append(m, packed=x)
+    x = both.packed(sum(n))
+    x[:, 6 * d:] *= 1e-3
+    both.append(n, packed=x)
+    q = (3.0 * torch.randn(sum(n), 4, d, generator=both.gen, device=dev)).bfloat16()
+    off = np.concatenate([[0], np.cumsum(n)])
+    got, qn = _np(both.c.attend(q, row_offsets=off)), _np(q)
+    for s in range(2):
+        K, V = both.k[s].numbers(), both.v[s].numbers()
+        for i in range(0, n[s], 5):
+            e = len(K) - n[s] + i + 1
+            for h in range(4):
+                z = K[:e, h // 2] @ qn[off[s] + i, h] * both.c.shape.scale
+                p = np.exp(z - z.max())
+                p /= p.sum()
+                products = p[:, None] * V[:e, h // 2]
+                assert np.isfinite(got[off[s] + i, h]).all()
+                assert np.abs(got[off[s] + i, h] - products.sum(axis=0)).max() <= 1e-5 * np.abs(products).max() + 1e-37, (s, i, h)
+
+
+def test_an_empty_cache_of_zeros(dev):
+    both = Both(dev, 2, 8, 2, 128, 16, 400)
+    both.append([300, 5], packed=both.packed(305) * 0)
+    for n in ([1, 1], [8, 3], [70, 40]):
+        x = both.packed(sum(n))
+        x[:, 10 * 128:] = 0
+        _, q = both.append(n, packed=x)
+        out = both.check_attend(q, n, every=7)
+        assert (out[:sum(n)] == 0).all()
 
 
 def test_pages_in_common(dev):
