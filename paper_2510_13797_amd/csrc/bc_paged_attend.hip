@@ -172,13 +172,17 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
       // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are formed, its values
       // behind the weights' product.
       u32x4_t key[2][H], value[2][H];
+      // (Behind the last tile one 16-byte piece of it in every lane's place: without a branch about the loads the compiler knows how many are on their way, and a
+      // tile's scores wait for its keys alone.)
       auto load = [&](u32x4_t (&x)[2][H], const uint8_t* pool, uint32_t at_lane, int i) {
+        const uint32_t lane_at = i < count ? at_lane : 0;
+        i = min(i, count - 1);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           const uint8_t* at = pool + (uint64_t)lane_value(unit, 2 * i + b) * BLOCK_BYTES;
 #pragma unroll
           for (int h = 0; h < H; ++h) {
-            const u32x4_t* from = reinterpret_cast<const u32x4_t*>(at + (at_lane + 256 * h));
+            const u32x4_t* from = reinterpret_cast<const u32x4_t*>(at + (lane_at + 256 * h));
             x[b][h] = STREAM ? __builtin_nontemporal_load(from) : *from;
           }
         }
@@ -202,7 +206,7 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
               for (int ct = 0; ct < CT; ++ct) sc[ct][b] = mfma16(a, q[ct][2 * h + e], sc[ct][b]);
             }
         }
-        if (i + 1 < count) load(key, p.k, k_lane, i + 1);
+        load(key, p.k, k_lane, i + 1);
         if (uneven) {
 #pragma unroll
           for (int b = 0; b < 2; ++b)
@@ -300,7 +304,7 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
               for (int k = 0; k < 2; ++k)
                 o[ct][4 * h + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, part[ct][k], o[ct][4 * h + j], 0, 0, 0);
           }
-        if (i + 1 < count) load(value, p.v, v_lane, i + 1);
+        load(value, p.v, v_lane, i + 1);
       }
     }
 
