@@ -683,6 +683,17 @@ struct AttendLaunch {
   size_t part_bytes, ml_at;
   bool fits;
 };
+// How a call is cut.  Lengths are on the device; the longest that there can be stands for them.
+// Few columns, four waves a workgroup in up to 512 or eight in up to 256 (us, one row a sequence, d = 128):
+//   1 x 16,000 rows, 32/8 heads          17.0, 13.3     64 x 300-1500 (eight share a prompt), 12/2   10.6, 11.2
+//   4 x 2000, 32/8                       11.0, 10.2     1 x 500, 32/8                                 6.4,  7.4
+//   128 x 300-3000, 12/2                 26.0, 24.0     64 x 400, 12/2                                8.4,  8.9
+//   32 x 4000, 32/8                      48.9, 46.9     64 x 1000, 32/8 (more pairs than 256)        26.0, 27.6
+// and two to eight rows: 1 x 8000, 32/8 28.1, 19.1; 64 x 1000, 12/2 16.9, 15.5; 1 x 500, 32/8 9.6, 10.7; 128 x 300, 32/8 26.8, 38.4.  More and smaller workgroups (four waves, 768): 19.8 for
+// the first.  Two tiles of columns leave twice the sums to add up: chunks of at least sixteen tiles (1 x 8000: 19.1 -> 15.9, others as they were).
+// Caches beyond some 100 MB go past the caches: 64 x 1000 rows, 32/8 heads (131 MB) 30.2 -> 26.7; 128 x 300 (79 MB) 17.5 -> 18.3.
+// (Chunks of equal size for all sequences of a batch, worked out by every workgroup from the lengths: 2.3 us more for one tile of columns, nothing gained with two.)
+// Many columns: parts until there are as many workgroups as run at once (two a compute unit): 512 rows over 7680, 32/8 heads, in three, four, five parts 135, 115, 153 us.
 constexpr int kMostParts = 16, kManyGroups = 512;
 constexpr int64_t kStreamBytes = 96 << 20;
 AttendLaunch plan_attend(const bc_shape* sh, int64_t rows, int64_t max_new, int64_t max_len) {
@@ -694,7 +705,8 @@ AttendLaunch plan_attend(const bc_shape* sh, int64_t rows, int64_t max_new, int6
     a.waves = pairs <= 256 && tiles >= (a.ct == 1 ? 62 : 32) ? 8 : 4;
     a.stream = pairs * max_len * 2 * sh->d > kStreamBytes;
     const int64_t groups = a.waves == 8 ? 256 : 512, most = groups / pairs < 1 ? 1 : groups / pairs, each = (tiles + most - 1) / most;
-    a.chunk_tiles = (int)(each < a.waves ? a.waves : each);
+    const int least = a.ct == 1 ? a.waves : 16;
+    a.chunk_tiles = (int)(each < least ? least : each);
     a.max_chunks = (int)((tiles + a.chunk_tiles - 1) / a.chunk_tiles);
     a.part_bytes = a.max_chunks > 1 ? (size_t)(pairs * a.max_chunks) * 16 * a.ct * (sh->d + 2) * 4 : 0;
     a.fits = true;
