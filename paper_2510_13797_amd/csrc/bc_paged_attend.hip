@@ -245,10 +245,10 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
             const float up = level[ct] * fast_exp2(to - m[ct]);
             l[ct] *= fast_exp2(m[ct] - to);
             m[ct] = to;
-            // (sums keep their level, or are nothing beside what there will be)
-            if (!(up <= kLevelStart)) {
+            if (!(up <= kLevelStart)) {        // (as high as it goes: the sums come down instead, to nothing where there are none yet)
+              const float down = kLevelStart / up;
 #pragma unroll
-              for (int j = 0; j < 4 * H; ++j) o[ct][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+              for (int j = 0; j < 4 * H; ++j) o[ct][j] *= down;
             }
             level[ct] = fminf(up, kLevelStart);
           };
@@ -581,10 +581,10 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float to = top > m + kLazy ? ceilf(top) : m, was = fast_exp2(m - to), up = level * fast_exp2(to - m);
         m = to; l *= was;
-        // (sums keep their level, or are nothing beside what there will be)
-        if (!(up <= kLevelStart)) {
+        if (!(up <= kLevelStart)) {            // (as high as it goes: the sums come down instead, to nothing where there are none yet)
+          const float down = kLevelStart / up;
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) O[j] = f32x16_t{0.f};
+          for (int j = 0; j < NJ; ++j) O[j] *= down;
         }
         level = fminf(up, kLevelStart);
         weights();

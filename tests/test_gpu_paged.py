@@ -435,6 +435,37 @@ def test_values_of_very_different_sizes(dev, n, d):
                 assert np.abs(got[off[s] + i, h] - products.sum(axis=0)).max() <= 1e-5 * np.abs(products).max() + 1e-37, (s, i, h)
 
 
+@pytest.mark.parametrize("n", [[1, 2], [6, 8], [40, 66]])
+@pytest.mark.parametrize("size", [1e-33, 1e-30, 1e30])
+def test_values_at_the_ends_of_the_range(dev, n, size):
+    # scores that rise with the entries, so that the reference moves all along, over values whose level is as high, or as low, as it goes
+    import torch
+    d = 128
+    both = Both(dev, 2, 4, 2, d, 16, 500)
+    lens = [400, 260]
+    x = both.packed(sum(lens))
+    x[:, 4 * d:6 * d] = 0.1 * x[:, 4 * d:6 * d]
+    x[:, 4 * d] = torch.cat([torch.arange(k, device=dev) / 8.0 for k in lens]).to(x.dtype)
+    x[:, 5 * d] = x[:, 4 * d]
+    x[:, 6 * d:] *= size
+    both.append(lens, packed=x)
+    x = both.packed(sum(n))
+    x[:, 6 * d:] *= size
+    both.append(n, packed=x)
+    q = torch.randn(sum(n), 4, d, generator=both.gen, device=dev)
+    q[:, :, 0] = 4.0
+    q = q.bfloat16()
+    off = np.concatenate([[0], np.cumsum(n)])
+    got, qn = _np(both.c.attend(q, row_offsets=off)), _np(q)
+    for s in range(2):
+        K, V = both.k[s].numbers(), both.v[s].numbers()
+        for i in range(0, n[s], 5):
+            e = len(K) - n[s] + i + 1
+            ref = OA.decode_attention(qn[off[s] + i], K[:e], V[:e], both.c.shape.scale)
+            # (outputs of N(0, 1) values, off by 1e-4 at most)
+            assert np.abs(got[off[s] + i] - ref).max() <= TOL * size, (s, i)
+
+
 def test_an_empty_cache_of_zeros(dev):
     both = Both(dev, 2, 8, 2, 128, 16, 400)
     both.append([300, 5], packed=both.packed(305) * 0)
