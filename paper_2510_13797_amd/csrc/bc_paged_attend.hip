@@ -9,6 +9,12 @@
 // column in a lane; a word of values is those four entries of one element, so O^T += V^T.P^T takes both as they are.  A key scale that is a power of
 // two goes along with the conversion, exactly; others are factors of their block's scores.  Values become half precision without their scale, which is a factor of the
 // weights; those enter their product in two half-precision parts (22 bits) at a level that goes with the products (kLevelMost).  Softmax online, sums in fp32.
+//
+// Two kernels:
+//   up to 32 columns: bound by memory, and by latency at both ends.  A row over 16,000, 32/8 heads, d = 128 (33 MB): 12.4 us; 64 rows over 4352 to 8704, 12/2 heads (216 MB): 38.6 (6.3 TB/s while it
+//   streams, as 1.07 GB in 171 us; a large read reaches 6.5); 1 to 8 rows of 16 sequences over 900 to 6000, 32/8 heads (121 MB): 28.2;
+//   more: bound by the matrix cores, large ones by the power limit.  4 x 2048 rows over 30,000, 32/8 heads: 4.84 ms, 0.80 PFLOP/s of the definition's products and 1.2 of those issued (a library
+//   product of 16384^3 reaches 1.39), matrix pipe busy 58 % of the cycles at 1.85 GHz; 512 rows over 7680: 103 us.
 #include "bc_paged.h"
 
 namespace bc {
@@ -172,8 +178,8 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
       // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are formed, its values
       // behind the weights' product.
       u32x4_t key[2][H], value[2][H];
-      // (Behind the last tile one 16-byte piece of it in every lane's place: without a branch about the loads the compiler knows how many are on their way, and a
-      // tile's scores wait for its keys alone.)
+      // (Behind the last tile one 16-byte piece of it in every lane's place: with a branch about the loads the compiler did not know how many were on their way, and
+      // waited for all of them in front of the scores: 14.1 us for a row over 16,000, 13.3 so.)
       auto load = [&](u32x4_t (&x)[2][H], const uint8_t* pool, uint32_t at_lane, int i) {
         const uint32_t lane_at = i < count ? at_lane : 0;
         i = min(i, count - 1);
