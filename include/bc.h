@@ -465,14 +465,14 @@ typedef struct {
 /* Rows of a layer's packed projections as new entries, in one pass: the norms and the rotation of bc_qk_norm_rope (same qkv, positions, inv_freq, rot, weights and eps;
  * shape's kv_dtype is their type), the queries to q [rows, Hq, d] in BF16 whatever the type (NULL: not wanted), keys and values into the pages.
  * Sequence s's new rows are [row_offsets[s], row_offsets[s+1]) (row_offsets: DEVICE [B + 1], spans within [0, rows) and of at most max_new rows, a HOST value; NULL: row s,
- * with rows == B).  They become entries start, start + 1, ... and len[s] = start + their number, where start = len[s], or keep[s] where keep (device [B], NULL: none)
+ * with rows == B and max_new 1).  They become entries start, start + 1, ... and len[s] = start + their number, where start = len[s], or keep[s] where keep (device [B], NULL: none)
  * is given: entries from keep[s] on are dropped (a beacon's window, drafted tokens that were not accepted).
  * The scale of a block is the least power of two s >= 2^-120 with |x| <= 448 s for every x written to it since its first entry: it grows with its entries (those that stay
  * are rounded again: exact but for magnitudes below 2^-6 of their new scale) and starts anew with a first one.  The scale of a block that holds entries has to be such a power of two.
  * What is not finite is stored as a NaN and does not count for the scale.  Bytes behind the last entry stay as they were.
  * A sequence that is not active or has no rows is left alone, and its rows of q with it; so is one with an invalid span, length, keep (0 .. len) or page, which sets
- * the state bit, and one that its row of the table cannot hold, which sets the capacity bit.  A page that is written to belongs to one sequence
- * (shared pages are whole ones in front of it).  Calls that share arrivals must not overlap in time.  No limits beyond bc_qk_norm_rope's but B * Hkv <= 2^23, fewer than 2^31 rows, blocks of 16 in a pool (of a head) and
+ * the state bit, and one that its row of the table cannot hold, which sets the capacity bit.  A page that is written to belongs to one sequence, and stands once in its
+ * row of the table (shared pages are whole ones in front of it).  positions may be len itself where row_offsets is NULL; otherwise nothing that the call reads overlaps what it writes.  Calls that share arrivals must not overlap in time.  No limits beyond bc_qk_norm_rope's but B * Hkv <= 2^23, fewer than 2^31 rows, blocks of 16 in a pool (of a head) and
  * entries in a table's row. */
 int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t rows, const int64_t *row_offsets,
                         int32_t max_new, const void *qkv, int64_t qkv_row_stride, const int32_t *positions,
@@ -485,9 +485,9 @@ int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t ro
  * out: [rows, Hq, d] fp32.  scale finite and >= 0.  Scales of blocks may be any finite numbers.  A softmax weight enters its product with
  * V in two half-precision parts: 22 bits, and at least 2^-32 of the row's largest product.  Sequences that are not active or have no rows are left alone, their rows of out with them; one with an invalid span, fewer entries than rows or more than max_len sets the
  * state bit and is left alone; one with an invalid page for its entries sets the state bit, nothing is read out of range, and its rows of out are unspecified.
- * Entries that a row sees, and those of its sequence behind it, are finite: a product with one that is not may show in rows that do not see it.  What lies behind the
- * last entry may be anything.  No atomics on results: they are reproducible.
- * workspace: bc_paged_workspace_bytes() of the call's rows, max_new and max_len (16-byte aligned, no initialisation).  Calls that share workspace or arrivals must not overlap in time. */
+ * What is not finite shows in the rows that see it and nowhere else: a row of a head is NaN throughout for a key or its own query, for a value at its element at least and throughout at
+ * most.  Scores, in log2, are smaller than 1e29.  What lies behind the last entry may be anything.  No atomics on results: they are reproducible.
+ * workspace: bc_paged_workspace_bytes() of the call's rows and max_new and of pages' max_len (table_pages * page_rows where that is 0 or more); 16-byte aligned, no initialisation.  Calls that share workspace or arrivals must not overlap in time. */
 size_t bc_paged_workspace_bytes(const bc_shape *shape, int64_t rows, int32_t max_new, int32_t max_len);
 int32_t bc_paged_attend(const bc_shape *shape, const bc_pages *pages, int64_t rows, const int64_t *row_offsets,
                         int32_t max_new, const void *q, float *out, const uint8_t *active, void *workspace,

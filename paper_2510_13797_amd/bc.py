@@ -743,7 +743,7 @@ class PagedCache:
 
     Which pages a sequence has is the caller's business: `table` [B, table_pages] int32 is a tensor to write to (one passed in may be shared by the layers of a
     model; the lengths are each layer's own).  A page that is appended to belongs to one sequence, whole ones in front of it may be shared.  Entries that have not
-    been written are NaN."""
+    been written are NaN.  One call at a time: what calls of a cache use besides the entries is shared by them."""
 
     def __init__(self, B, Hq, Hkv, d, pages, page_rows, table_pages, device, dtype="bf16", scale=None, table=None):
         import torch

@@ -51,14 +51,14 @@ inline int32_t check_pages(const bc_shape* sh, const bc_pages* pg, int64_t rows,
   // (blocks and entries are counted in 32 bits)
   if ((int64_t)pg->pages * sh->Hkv * (pg->page_rows / kPagedBlock) > 0x7fffffff || (int64_t)pg->table_pages * pg->page_rows > 0x7fffff00) return BC_ERR_SHAPE;
   if (rows < 0 || rows > 0x7fffffff || max_new < 0 || (int64_t)sh->B * sh->Hkv > (1 << 23)) return BC_ERR_SHAPE;
-  if (!off && (rows != sh->B || max_new < 1)) return BC_ERR_ARG;
+  if (!off && (rows != sh->B || max_new != 1)) return BC_ERR_ARG;
   return BC_OK;
 }
 
 inline PagedTables paged_tables(const bc_shape* sh, const bc_pages* pg, int64_t rows, const int64_t* off, int32_t max_new, const uint8_t* active) {
   PagedTables t{};
   t.table = pg->table; t.len = pg->len; t.err = pg->err; t.off = off; t.active = active; t.rows = rows;
-  t.B = sh->B; t.pages = pg->pages; t.table_pages = pg->table_pages; t.max_new = off ? max_new : 1;
+  t.B = sh->B; t.pages = pg->pages; t.table_pages = pg->table_pages; t.max_new = max_new;
   t.page_shift = __builtin_ctz(pg->page_rows);
   return t;
 }

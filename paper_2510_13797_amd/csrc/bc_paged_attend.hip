@@ -84,6 +84,15 @@ __device__ __forceinline__ void split_halves(float u, float v, float f, uint32_t
   hi = __builtin_bit_cast(uint32_t, h);
   lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_v{fmaf(u, f, -(float)h[0]), fmaf(v, f, -(float)h[1])}, f16x2_v));
 }
+// Bit 7 of the bytes that are no number (0x7f or 0xff), other bits anything; and a word with those bytes zero.
+__device__ __forceinline__ uint32_t no_numbers(uint32_t w) { return (w & 0x7f7f7f7fu) + 0x01010101u; }
+__device__ __forceinline__ uint32_t only_numbers(uint32_t w) { return w & ~((no_numbers(w) >> 7 & 0x01010101u) * 0xffu); }
+// A NaN that the compiler, which is told that there are none, does not see.
+__device__ __forceinline__ float no_number() {
+  float x;
+  asm volatile("v_mov_b32 %0, 0x7fc00000" : "=v"(x));
+  return x;
+}
 // The level of a column's values.  Weights times their block's value scale enter products in half precision, so what they are brought to has to go with the product: sums
 // are kept as `f` times what they are, f a power of two, so that no factor passes 2^14 and the largest came to 2^8 when f was last set.  What was small beside that is as small
 // in the result.  f starts where nothing is too large and sums are zero.
@@ -299,6 +308,34 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
               for (int j = 0; j < 4; ++j) value[b][h][j] &= mask;
           }
         }
+        // A value that is no number would reach the columns that do not see it, by a weight of zero: its bytes become zeros, and the columns that do see it get a sum
+        // of weights that is no number.
+        if (n > 1 && ends) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint32_t nans = 0;
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) nans |= no_numbers(value[b][h][j]);
+            if (__builtin_expect(__any((nans & 0x80808080u) != 0), 0)) {
+#pragma unroll 1
+              for (int r = 0; r < 4; ++r, nans >>= 8) {
+                const bool here = (__ballot(nans >> 7 & 1) >> (16 * g4) & 0xffff) != 0;      // entry key0 + 16 b + 4 g4 + r
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                  if (here && key0 + 16 * b + 4 * g4 + r < key_lim[ct]) l[ct] = no_number();
+              }
+#pragma unroll
+              for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  value[b][h][j] = only_numbers(value[b][h][j]);
+                  __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+          }
+        }
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
@@ -442,7 +479,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
   __shared__ float s_rest[2][kManyWaves];                        // what the conversion left of a block's key scale,
   __shared__ int s_uneven;                                       // whether that has been anything but ones,
-  __shared__ f32x4_t s_value[2];                                 // value scales
+  __shared__ f32x4_t s_value[2];                                 // value scales,
+  __shared__ __attribute__((aligned(8))) uint16_t s_no_number[2][kManyWaves];      // entries with a value that is no number
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const uint32_t pairs = (uint32_t)p.t.B * p.Hkv;
   uint32_t id = blockIdx.x;
@@ -459,6 +497,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 
   const int mine = first + 32 * wave, c = min(mine + col, columns - 1), i = c / p.g;
   const int lim = L - n + 1 + i;                                 // entries that this lane's column sees
+  const int all_free = (L - n + 1 + first / p.g) / kManyTile;    // tiles that all columns of the workgroup see whole
   const int free_tiles = (L - n + 1 + min(mine, columns - 1) / p.g) / kManyTile;        // tiles that all of the wave's columns see whole
   const int seen = mine < columns ? (L - n + (min(mine + 32, columns) - 1) / p.g) / kManyTile + 1 : 0;         // tiles that the wave works on
   bf16x8_t qb[KS];
@@ -521,6 +560,28 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         const int there = L - kManyTile * t - 16 * wave - 4 * (half + 2 * x);
         keep[x] = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
       }
+    }
+    if (t >= all_free) {                                         // (as with few columns)
+      uint32_t nans[2] = {0, 0}, entries = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (D == 128) { nans[0] |= no_numbers(vb[0][j] & keep[0]); nans[1] |= no_numbers(vb[D / 64 - 1][j] & keep[1]); }
+        else nans[j >> 1] |= no_numbers(vb[0][j] & keep[j >> 1]);
+      }
+      if (__builtin_expect(__any(((nans[0] | nans[1]) & 0x80808080u) != 0), 0)) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint64_t have = __ballot(nans[x] >> (8 * r + 7) & 1);
+            entries |= ((uint32_t)have != 0 ? 1u : 0u) << (8 * x + r) | ((have >> 32) != 0 ? 1u : 0u) << (8 * x + 4 + r);
+          }
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) vb[x][j] = only_numbers(vb[x][j]);
+      }
+      if (lane == 0) s_no_number[stage][wave] = (uint16_t)entries;
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -596,6 +657,11 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         weights();
       }
       l += psum;
+      if (t >= all_free) {
+        const uint64_t entries = *reinterpret_cast<const uint64_t*>(s_no_number[stage]);
+        const int sees = lim - kManyTile * t;
+        if (sees > 0 && (entries & (sees >= 64 ? ~0ull : (1ull << sees) - 1)) != 0) l = no_number();
+      }
       const f32x4_t scales = s_value[stage];
       const float largest = fmaxf(fmaxf(sums[0] * fabsf(scales[0]), sums[1] * fabsf(scales[1])), fmaxf(sums[2] * fabsf(scales[2]), sums[3] * fabsf(scales[3])));
       if (__builtin_expect(__any(largest * level > kLevelMost), 0)) {
@@ -778,7 +844,6 @@ extern "C" int32_t bc_paged_attend(const bc_shape* shape, const bc_pages* pages,
   if (st != BC_OK) return st;
   if (!nonnegative_finite(shape->scale)) return BC_ERR_ARG;
   if (rows == 0 || max_new == 0) return BC_OK;
-  if (!row_offsets) max_new = 1;
   if (!q || !out || !aligned16(q) || !aligned16(out) || !pages->arrivals) return BC_ERR_ARG;
   const int64_t max_len = longest(pages);
   // (a sequence cannot have more new rows than there are, nor than entries)

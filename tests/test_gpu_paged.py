@@ -466,6 +466,90 @@ def test_values_at_the_ends_of_the_range(dev, n, size):
             assert np.abs(got[off[s] + i] - ref).max() <= TOL * size, (s, i)
 
 
+@pytest.mark.parametrize("n", [[2, 5], [9, 16], [40, 66], [140, 200]])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("before", [[0, 3], [75, 41], [900, 1500]])
+def test_what_a_row_does_not_see_does_not_reach_it(dev, n, d, before):
+    # new rows whose values, keys or query are no numbers: rows in front of them, other heads and other sequences have their results
+    import torch
+    Hq, Hkv = 4, 2
+    both = Both(dev, 2, Hq, Hkv, d, 64, max(b + m for b, m in zip(before, n)))
+    both.append(before)
+    x = both.packed(sum(n))
+    h = x.view(-1, Hq + 2 * Hkv, d)
+    h[n[0] // 2, Hq + Hkv, 5] = float("inf")                 # a value of sequence 0, head 0,
+    h[n[0] - 1, Hq + Hkv + 1, d - 1] = float("nan")          # the last one of head 1,
+    h[n[0] + n[1] - 2, Hq + Hkv + 1, 0] = float("-inf")      # of sequence 1
+    h[n[0] + n[1] - 1, Hq, 3] = float("nan")                 # and a key
+    _, q = both.append(n, packed=x)
+    q[n[0], 3] = float("nan")                                # a query of sequence 1
+    off = np.concatenate([[0], np.cumsum(n)])
+    got, qn, seen = _np(both.c.attend(q, row_offsets=off)), _np(q), 0
+    for s in range(2):
+        K, V = both.k[s].numbers(), both.v[s].numbers()
+        for i in range(n[s]):
+            e = before[s] + i + 1
+            for head in range(Hq):
+                row, kvh = got[off[s] + i, head], head // (Hq // Hkv)
+                k, v, query = K[:e, kvh], V[:e, kvh], qn[off[s] + i, head]
+                if np.isfinite(k).all() and np.isfinite(query).all():
+                    bad = ~np.isfinite(v).all(axis=0)
+                    ref = OA.decode_attention(query[None], k[:, None], np.where(np.isfinite(v), v, 0.0)[:, None], both.c.shape.scale)[0]
+                    assert np.isnan(row[bad]).all()
+                    right = ~bad if not bad.any() else ~bad & ~np.isnan(row)
+                    assert np.abs(row - ref)[right].max(initial=0.0) <= TOL, (s, i, head)
+                    seen += bad.any()
+                else:
+                    assert np.isnan(row).all(), (s, i, head)
+    assert seen >= 4 and both.c.err.item() == 0
+
+
+def test_positions_that_are_the_lengths(dev):
+    # a step's positions are the lengths themselves, the tensor that the call moves
+    import torch
+    both, other = (Both(dev, 5, 12, 2, 128, 16, 80, seed=3) for _ in range(2))
+    freq = 10000.0 ** (-torch.arange(0, 128, 2, device=dev) / 128)
+    for b in (both, other):
+        b.append([30, 0, 16, 15, 1])
+    for _ in range(20):
+        x = both.packed(5)
+        got = both.c.append(x, both.c.lengths, freq)
+        assert torch.equal(got, other.c.append(x, other.c.lengths.clone(), freq))
+    for a, b in zip(both.pool(), other.pool()):
+        assert np.array_equal(a, b, equal_nan=a.dtype.kind == "f")
+
+
+def test_layers_that_share_a_table_and_run_at_once(dev):
+    # two layers' caches over one table, each on a stream of its own
+    import torch
+    from paper_2510_13797_amd import bc
+    B, Hq, Hkv, d, page = 6, 12, 2, 128, 32
+    table = torch.randperm(64, device=dev)[:B * 10].view(B, 10).int()
+    x = torch.randn(2, B * 100, (Hq + 2 * Hkv) * d, device=dev).bfloat16()
+    step = torch.randn(2, 20, B, (Hq + 2 * Hkv) * d, device=dev).bfloat16()
+    pos, none = torch.arange(B * 100, device=dev).int(), torch.zeros(0, device=dev)
+
+    def layer(i, cache):
+        outs = []
+        cache.append(x[i], pos, none, row_offsets=range(0, B * 100 + 1, 100))
+        for t in range(20):
+            outs.append(cache.attend(cache.append(step[i, t], pos[:B], none), max_len=200))
+        return outs
+
+    alone = [layer(i, bc.PagedCache(B, Hq, Hkv, d, 64, page, 10, dev, table=table)) for i in range(2)]
+    caches = [bc.PagedCache(B, Hq, Hkv, d, 64, page, 10, dev, table=table) for _ in range(2)]
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for i in range(2):
+        with torch.cuda.stream(streams[i]):
+            got.append(layer(i, caches[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert caches[i].err.item() == 0 and caches[i].table is table
+        assert all(torch.equal(a, b) for a, b in zip(got[i], alone[i]))
+
+
 def test_an_empty_cache_of_zeros(dev):
     both = Both(dev, 2, 8, 2, 128, 16, 400)
     both.append([300, 5], packed=both.packed(305) * 0)
