@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
         }
         // A value that is no number would reach the columns that do not see it, by a weight of zero: its bytes become zeros, and the columns that do see it get a sum
         // of weights that is no number.
-        if (n > 1 && ends) {
+        if (__builtin_expect(n > 1 && ends, 0)) {
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             uint32_t nans = 0;
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         keep[x] = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
       }
     }
-    if (t >= all_free) {                                         // (as with few columns)
+    if (__builtin_expect(t >= all_free, 0)) {                                         // (as with few columns)
       uint32_t nans[2] = {0, 0}, entries = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -657,7 +657,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         weights();
       }
       l += psum;
-      if (t >= all_free) {
+      if (__builtin_expect(t >= all_free, 0)) {
         const uint64_t entries = *reinterpret_cast<const uint64_t*>(s_no_number[stage]);
         const int sees = lim - kManyTile * t;
         if (sees > 0 && (entries & (sees >= 64 ? ~0ull : (1ull << sees) - 1)) != 0) l = no_number();
