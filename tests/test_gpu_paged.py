@@ -724,6 +724,73 @@ def test_captured_steps(dev):
     assert both.c.err.item() == 0
 
 
+def test_two_graphs_of_one_cache(dev):
+    # a decode step and a check of drafted tokens (a chunk of 40 in the second sequence), captured into one memory pool and replayed by turns
+    import torch
+    both = Both(dev, 3, 12, 2, 128, 32, 1600)
+    both.append([900, 17, 1300])
+    pos = torch.zeros(48, dtype=torch.int32, device=dev)
+    one, many = both.packed(3), both.packed(46)
+    off, accepted = [0, 4, 44, 46], torch.zeros(3, dtype=torch.int32, device=dev)
+
+    def step():
+        return both.c.attend(both.c.append(one, pos[:3], both.empty))
+
+    def check():
+        accepted.copy_(both.c.lengths)
+        accepted.add_(1)
+        out = both.c.attend(both.c.append(many, pos[:46], both.empty, row_offsets=off), row_offsets=off)
+        both.c.lengths.copy_(accepted)                       # one of the drafted tokens is kept
+        return out
+
+    start, pool = both.c.lengths.clone(), [both.c.k_pages.view(torch.uint8), both.c.v_pages.view(torch.uint8), both.c.k_scale, both.c.v_scale]
+    saved = [p.clone() for p in pool]
+
+    def reset():
+        both.c.lengths.copy_(start)
+        for p, x in zip(pool, saved):
+            p.copy_(x)
+
+    eager = [f().clone() for _ in range(3) for f in (step, check)]
+    end = both.c.lengths.clone()
+    reset()
+    stream, graphs, outs, memory = torch.cuda.Stream(), [], [], None
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for f in (step, check):
+            f()
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream, pool=memory):
+                outs.append(f())
+            memory = graph.pool()
+            graphs.append(graph)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        reset()
+        for i in range(6):
+            graphs[i % 2].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i % 2], eager[i]), i
+        assert torch.equal(both.c.lengths, end) and both.c.err.item() == 0
+        reset()
+        assert all(torch.equal(f(), e) for e, f in zip(eager, 3 * (step, check)))
+
+
+def test_without_the_native_module(dev, monkeypatch):
+    import torch
+    from paper_2510_13797_amd import bc
+    got = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(bc, "_paged_calls", None)
+        both = Both(dev, 3, 12, 2, 128, 32, 200, seed=5)
+        both.append([70, 3, 0], keep=[0, 0, 0])
+        _, q = both.append([1, 4, 2], active=[1, 1, 0])
+        got += [both.check_attend(q, [1, 4, 2], active=[1, 1, 0]), both.c.attend(both.c.append(both.packed(3), both.c.lengths, both.empty))]
+    assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3])
+
+
 def test_another_stream(dev):
     import torch
     both = Both(dev, 2, 12, 2, 128, 16, 200)
