@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
   const int s = blockIdx.x / of_sequence, at_block = blockIdx.x - s * of_sequence, j = at_block / p.turns, turn = at_block - j * p.turns;
   const AppendPlan plan = append_plan(p, s, threadIdx.x & 63, at_block == 0 && threadIdx.x < 64);
   if (plan.n == 0) return;
-  const int start = plan.start, end = start + plan.n, first = ((start >> 4) + j) << 4, slot = first + mine;
+  const int start = plan.start, end = start + plan.n;
   // The length moves when all of the sequence's workgroups have read it, those without rows among them: counted behind the work (in front of it the loads behind the count, which
   // come back in order, waited for its answer: 2 us).
   auto leave = [&] {
@@ -119,7 +119,8 @@ __global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
     __hip_atomic_store(p.arrivals + s * p.Hkv, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     p.t.len[s] = end;
   };
-  if (first >= end) return leave();
+  if (j > ((end - 1) >> 4) - (start >> 4)) return leave();            // (counted in blocks: places behind the last one may pass 31 bits)
+  const int first = ((start >> 4) + j) << 4, slot = first + mine;
   const bool fresh = slot >= start && slot < end, stays = slot < start, staying = first < start;
   const int64_t row = plan.row + (fresh ? slot - start : 0);         // (other rows' lanes look at the first one)
   const char* in = p.qkv + row * p.row_bytes;

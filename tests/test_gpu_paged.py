@@ -635,6 +635,35 @@ def test_places_beyond_32_bits(dev):
 
 
 # ------------------------------------------------------------------ together
+def test_the_last_places_of_the_longest_table(dev):
+    # a row of the table that holds 2^31 - 1024 entries, nearly all of them in one page; new rows at its end, in a call for more of them
+    import torch
+    from paper_2510_13797_amd import bc
+    per, page, Hq, Hkv, d = (1 << 21) - 1, 1024, 2, 1, 64
+    c = bc.PagedCache(1, Hq, Hkv, d, 2, page, per, dev)
+    for x in (c.k_pages, c.v_pages):
+        x.view(torch.uint8).zero_()
+    c.k_scale.fill_(OP.LEAST), c.v_scale.fill_(OP.LEAST)
+    c.table[0, -1] = 1
+    start, n = per * page - 130, 90
+    c.lengths.fill_(start)
+    x = torch.randn(2000, (Hq + 2 * Hkv) * d, device=dev).bfloat16()
+    pos, off = torch.zeros(2000, dtype=torch.int32, device=dev), torch.tensor([0, n], device=dev)
+    c.append(x, pos, torch.zeros(0, device=dev), row_offsets=off, max_new=2000)
+    assert c.lengths.item() == start + n and c.err.item() == 0
+    V = c.v_pages.view(torch.uint8)
+    assert (V[0] == 0).all() and (c.v_scale[0] == OP.LEAST).all()
+    seq = OP.Sequence(Hkv, d)
+    seq.append(np.zeros((page - 130, Hkv, d)))
+    seq.append(_np(x[:n]).reshape(n, -1, d)[:, Hq + Hkv:])
+    for j in range(page - 130, page - 130 + n):
+        assert (V[1, 0].reshape(-1).cpu().numpy()[OP.value_place(j, np.arange(d), d)] == OP.e4m3_byte(seq.values[0, j])).all(), j
+    assert (V[1, 0].reshape(page // 4, d, 4)[(page - 130 + n + 3) // 4:] == 0).all()
+    # one more than there is room for
+    c.append(x, pos, torch.zeros(0, device=dev), row_offsets=torch.tensor([0, 41], device=dev), max_new=2000)
+    assert c.err.item() == bc.BC_ERRBIT_CAPACITY and c.lengths.item() == start + n
+
+
 def test_a_generation_with_beacons(dev):
     # Alg. 1 over pages: prompts, tokens, and a beacon in the place of every full window (its own attention over the window first), ratios 4 and 7
     both = Both(dev, 3, 12, 2, 128, 16, 80)
