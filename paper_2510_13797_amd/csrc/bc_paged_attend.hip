@@ -140,324 +140,321 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
   int page = page_of(t0 + wave);
   const AttendSpan span = attend_span(p, s);
   if (span.bad && chunk == 0 && kvh == 0 && tid == 0) atomicOr(p.t.err, BC_ERRBIT_STATE);
-  const uint32_t tiles = span.n > 0 ? (uint32_t)(span.L + 31) >> 5 : 0, count = (tiles + p.chunk_tiles - 1) / p.chunk_tiles;
-  if (chunk >= count) return;
+  const uint32_t tiles = span.n > 0 ? (uint32_t)(span.L + 31) >> 5 : 0, chunks = (tiles + p.chunk_tiles - 1) / p.chunk_tiles;
+  if (chunk >= chunks) return;
   const uint32_t t1 = min(t0 + p.chunk_tiles, tiles);
-  {
-    const int n = span.n, L = span.L, own = n * p.g, seen_by_all = L - n + 1;
+  const int n = span.n, L = span.L, own = n * p.g, seen_by_all = L - n + 1;
 
-    bf16x8_t q[CT][2 * H];
-    int key_lim[CT];
+  bf16x8_t q[CT][2 * H];
+  int key_lim[CT];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      const int col = min(16 * ct + c16, own - 1), i = col / p.g;
-      key_lim[ct] = L - n + 1 + i;
-      const char* at = p.q + ((span.row + i) * p.Hq + kvh * p.g + (col - i * p.g)) * (2 * D) + 32 * g4;
+  for (int ct = 0; ct < CT; ++ct) {
+    const int col = min(16 * ct + c16, own - 1), i = col / p.g;
+    key_lim[ct] = L - n + 1 + i;
+    const char* at = p.q + ((span.row + i) * p.Hq + kvh * p.g + (col - i * p.g)) * (2 * D) + 32 * g4;
 #pragma unroll
-      for (int h = 0; h < H; ++h)
+    for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) q[ct][2 * h + e] = *reinterpret_cast<const bf16x8_t*>(at + 128 * h + 16 * e);
-    }
-    f32x4_t o[CT][4 * H];
-    float m[CT], l[CT], level[CT];
+      for (int e = 0; e < 2; ++e) q[ct][2 * h + e] = *reinterpret_cast<const bf16x8_t*>(at + 128 * h + 16 * e);
+  }
+  f32x4_t o[CT][4 * H];
+  float m[CT], l[CT], level[CT];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      m[ct] = kNegBig; l[ct] = 0.f; level[ct] = kLevelStart;
+  for (int ct = 0; ct < CT; ++ct) {
+    m[ct] = kNegBig; l[ct] = 0.f; level[ct] = kLevelStart;
 #pragma unroll
-      for (int i = 0; i < 4 * H; ++i) o[ct][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int i = 0; i < 4 * H; ++i) o[ct][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
 
-    const uint32_t k_lane = (c16 >> 2) * 4 * D + (c16 & 3) * 64 + g4 * 16, v_lane = g4 * 4 * D + c16 * 16;
-    for (uint32_t tb = t0 + wave; tb < t1; tb += 32 * NW) {
-      const int count = min(32, (int)(t1 - tb + NW - 1) / NW), block = 2 * (int)(tb + NW * (lane >> 1)) + (lane & 1), last = (L - 1) >> 4;
-      if (tb != t0 + wave) page = page_of(tb);
-      // (a tile's second block may lie behind the last one: the first in its place; other lanes' blocks are nobody's)
-      const int first_of = __builtin_amdgcn_update_dpp(page, page, 0xA0, 0xf, 0xf, true);        // quad_perm [0, 0, 2, 2]
-      const int at_block = block > last ? block & ~1 : block;
-      if (block > last) page = first_of;
-      if (page < 0 || page >= p.t.pages) {
-        if (at_block <= last && (lane >> 1) < count) atomicOr(p.t.err, BC_ERRBIT_STATE);
-        page = 0;
+  const uint32_t k_lane = (c16 >> 2) * 4 * D + (c16 & 3) * 64 + g4 * 16, v_lane = g4 * 4 * D + c16 * 16;
+  for (uint32_t tb = t0 + wave; tb < t1; tb += 32 * NW) {
+    const int count = min(32, (int)(t1 - tb + NW - 1) / NW), block = 2 * (int)(tb + NW * (lane >> 1)) + (lane & 1), last = (L - 1) >> 4;
+    if (tb != t0 + wave) page = page_of(tb);
+    // (a tile's second block may lie behind the last one: the first in its place; other lanes' blocks are nobody's)
+    const int first_of = __builtin_amdgcn_update_dpp(page, page, 0xA0, 0xf, 0xf, true);        // quad_perm [0, 0, 2, 2]
+    const int at_block = block > last ? block & ~1 : block;
+    if (block > last) page = first_of;
+    if (page < 0 || page >= p.t.pages) {
+      if (at_block <= last && (lane >> 1) < count) atomicOr(p.t.err, BC_ERRBIT_STATE);
+      page = 0;
+    }
+    const uint32_t unit = (((uint32_t)page * p.Hkv + kvh) << per_page) + (at_block & ((1 << per_page) - 1));
+    const float qs = CT == 1 ? 1.f : p.qs, k_scale = CT == 1 ? p.ks[unit] * p.qs : p.ks[unit], v_scale = p.vs[unit];
+    // (With one tile of columns key scales are always factors of the scores: two ways through the code cost a short step half a microsecond, 9.7 -> 10.3 us.)
+    const bool uneven = CT == 1 || __any(at_block <= last && (lane >> 1) < count && !power_of_two_scale(k_scale));
+
+    // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are formed, its values
+    // behind the weights' product.
+    u32x4_t key[2][H], value[2][H];
+    // (Behind the last tile one 16-byte piece of it in every lane's place: with a branch about the loads the compiler did not know how many were on their way, and
+    // waited for all of them in front of the scores: 14.1 us for a row over 16,000, 13.3 so.)
+    auto load = [&](u32x4_t (&x)[2][H], const uint8_t* pool, uint32_t at_lane, int i) {
+      const uint32_t lane_at = i < count ? at_lane : 0;
+      i = min(i, count - 1);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint8_t* at = pool + (uint64_t)lane_value(unit, 2 * i + b) * BLOCK_BYTES;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          const u32x4_t* from = reinterpret_cast<const u32x4_t*>(at + (lane_at + 256 * h));
+          x[b][h] = STREAM ? __builtin_nontemporal_load(from) : *from;
+        }
       }
-      const uint32_t unit = (((uint32_t)page * p.Hkv + kvh) << per_page) + (at_block & ((1 << per_page) - 1));
-      const float qs = CT == 1 ? 1.f : p.qs, k_scale = CT == 1 ? p.ks[unit] * p.qs : p.ks[unit], v_scale = p.vs[unit];
-      // (With one tile of columns key scales are always factors of the scores: two ways through the code cost a short step half a microsecond, 9.7 -> 10.3 us.)
-      const bool uneven = CT == 1 || __any(at_block <= last && (lane >> 1) < count && !power_of_two_scale(k_scale));
-
-      // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are formed, its values
-      // behind the weights' product.
-      u32x4_t key[2][H], value[2][H];
-      // (Behind the last tile one 16-byte piece of it in every lane's place: with a branch about the loads the compiler did not know how many were on their way, and
-      // waited for all of them in front of the scores: 14.1 us for a row over 16,000, 13.3 so.)
-      auto load = [&](u32x4_t (&x)[2][H], const uint8_t* pool, uint32_t at_lane, int i) {
-        const uint32_t lane_at = i < count ? at_lane : 0;
-        i = min(i, count - 1);
+    };
+    load(key, p.k, k_lane, 0);
+    load(value, p.v, v_lane, 0);
+    for (int i = 0; i < count; ++i) {
+      const int key0 = 32 * (tb + NW * i);
+      f32x4_t sc[CT][2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint8_t* at = pool + (uint64_t)lane_value(unit, 2 * i + b) * BLOCK_BYTES;
+      for (int b = 0; b < 2; ++b) {
+        const float scale = uneven ? 1.f : __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
 #pragma unroll
-          for (int h = 0; h < H; ++h) {
-            const u32x4_t* from = reinterpret_cast<const u32x4_t*>(at + (lane_at + 256 * h));
-            x[b][h] = STREAM ? __builtin_nontemporal_load(from) : *from;
-          }
-        }
-      };
-      load(key, p.k, k_lane, 0);
-      load(value, p.v, v_lane, 0);
-      for (int i = 0; i < count; ++i) {
-        const int key0 = 32 * (tb + NW * i);
-        f32x4_t sc[CT][2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float scale = uneven ? 1.f : __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) sc[ct][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int h = 0; h < H; ++h)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const bf16x8_t a = __builtin_bit_cast(bf16x8_t, scaled_operand(key[b][h][2 * e], key[b][h][2 * e + 1], scale));
-#pragma unroll
-              for (int ct = 0; ct < CT; ++ct) sc[ct][b] = mfma16(a, q[ct][2 * h + e], sc[ct][b]);
-            }
-        }
-        load(key, p.k, k_lane, i + 1);
-        if (uneven) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) sc[ct][b] *= __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
-        }
-        const bool ends = key0 + 32 > seen_by_all;                   // some columns do not see all of it
-        if (CT == 1 && ends) {
-#pragma unroll
-          for (int r = 0; r < 8; ++r)
-            if (key0 + 16 * (r >> 2) + 4 * g4 + (r & 3) >= key_lim[0]) sc[0][r >> 2][r & 3] = 2.f * kNegBig;
-        }
-        f16x8_v part[CT][2];
-        const float v0 = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i)), v1 = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + 1));
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          float w[8], sums[2], sum;
-          const int there = key_lim[ct] - key0 - 4 * g4;
-          auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-            for (int r = 0; r < 8; ++r) w[r] = fast_exp2(fmaf(sc[ct][r >> 2][r & 3], qs, -m[ct]));
-            if (CT > 1 && ends) {
-#pragma unroll
-              for (int r = 0; r < 8; ++r) w[r] = 16 * (r >> 2) + (r & 3) < there ? w[r] : 0.f;
-            }
-            sums[0] = (w[0] + w[1]) + (w[2] + w[3]); sums[1] = (w[4] + w[5]) + (w[6] + w[7]);
-            sum = sums[0] + sums[1];
-          };
-          auto move = [&]() __attribute__((always_inline)) {   // the reference, to the column's maximum
-            float top = kNegBig;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) top = fmaxf(top, CT == 1 || 16 * (r >> 2) + (r & 3) < there ? sc[ct][r >> 2][r & 3] * qs : kNegBig);
-            top = rows_allreduce_max(top);
-            const float to = top > m[ct] + (CT == 1 ? 0.f : kLazy) ? ceilf(top) : m[ct];
-            if (!__any(to > m[ct])) return;
-            const float up = level[ct] * fast_exp2(to - m[ct]);
-            l[ct] *= fast_exp2(m[ct] - to);
-            m[ct] = to;
-            if (!(up <= kLevelStart)) {        // (as high as it goes: the sums come down instead, to nothing where there are none yet)
-              const float down = kLevelStart / up;
-#pragma unroll
-              for (int j = 0; j < 4 * H; ++j) o[ct][j] *= down;
-            }
-            level[ct] = fminf(up, kLevelStart);
-          };
-          // With two tiles of columns vector work counts: the maximum is formed only where weights get large (38.7 -> 35.3 us for 16 x 1-8 rows over 900 to 6000,
-          // 32/8 heads).  With one, a wave's two or three tiles would pay for forming the first one's weights twice.
-          if constexpr (CT == 1) {
-            move();
-            weights();
-          } else {
-            weights();
-            if (__builtin_expect(__any(sum > kRedo), 0)) {
-              move();
-              weights();
-            }
-          }
-          l[ct] += sum;
-          const float largest = fmaxf(sums[0] * fabsf(v0), sums[1] * fabsf(v1));     // (block by block: a heavy key has nothing to do with another block's scale)
-          if (__builtin_expect(__any(largest * level[ct] > kLevelMost), 0)) {
-            const float all = rows_allreduce_max(largest), to = all * level[ct] > kLevelMost ? level_for(all) : level[ct], was = to / level[ct];
-#pragma unroll
-            for (int j = 0; j < 4 * H; ++j) o[ct][j] *= was;
-            level[ct] = to;
-          }
-          u32x4_t hi, lo;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            uint32_t h, x;
-            split_halves(w[2 * r], w[2 * r + 1], (r < 2 ? v0 : v1) * level[ct], h, x);
-            hi[r] = h; lo[r] = x;
-          }
-          part[ct][0] = __builtin_bit_cast(f16x8_v, hi);
-          part[ct][1] = __builtin_bit_cast(f16x8_v, lo);
-        }
-        if (key0 + 32 > L) {                     // bytes behind the last entry may be anything: zeros, not a product with a weight of zero
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int there = L - (key0 + 16 * b + 4 * g4);
-            const uint32_t mask = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
-#pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) value[b][h][j] &= mask;
-          }
-        }
-        // A value that is no number would reach the columns that do not see it, by a weight of zero: its bytes become zeros, and the columns that do see it get a sum
-        // of weights that is no number.
-        if (__builtin_expect(n > 1 && ends, 0)) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            uint32_t nans = 0;
-#pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) nans |= no_numbers(value[b][h][j]);
-            if (__builtin_expect(__any((nans & 0x80808080u) != 0), 0)) {
-#pragma unroll 1
-              for (int r = 0; r < 4; ++r, nans >>= 8) {
-                const bool here = (__ballot(nans >> 7 & 1) >> (16 * g4) & 0xffff) != 0;      // entry key0 + 16 b + 4 g4 + r
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-                  if (here && key0 + 16 * b + 4 * g4 + r < key_lim[ct]) l[ct] = no_number();
-              }
-#pragma unroll
-              for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  value[b][h][j] = only_numbers(value[b][h][j]);
-                  __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-          }
-        }
+        for (int ct = 0; ct < CT; ++ct) sc[ct][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f16x8_v a = __builtin_bit_cast(f16x8_v, half_operand(value[0][h][j], value[1][h][j]));
+          for (int e = 0; e < 2; ++e) {
+            const bf16x8_t a = __builtin_bit_cast(bf16x8_t, scaled_operand(key[b][h][2 * e], key[b][h][2 * e + 1], scale));
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-              for (int k = 0; k < 2; ++k)
-                o[ct][4 * h + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, part[ct][k], o[ct][4 * h + j], 0, 0, 0);
+            for (int ct = 0; ct < CT; ++ct) sc[ct][b] = mfma16(a, q[ct][2 * h + e], sc[ct][b]);
           }
-        load(value, p.v, v_lane, i + 1);
       }
-    }
-
-    // the waves' sums: a lane has elements 64 h + 16 g4 + 4 r + j of its column
+      load(key, p.k, k_lane, i + 1);
+      if (uneven) {
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      const float sum = rows_allreduce_sum(l[ct]);
-      const float f = 1.f / level[ct];
-      if (g4 == 0) { s_ml[wave][16 * ct + c16][0] = m[ct]; s_ml[wave][16 * ct + c16][1] = sum; }
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) sc[ct][b] *= __uint_as_float(lane_value(__float_as_uint(k_scale), 2 * i + b));
+      }
+      const bool ends = key0 + 32 > seen_by_all;                   // some columns do not see all of it
+      if (CT == 1 && ends) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (key0 + 16 * (r >> 2) + 4 * g4 + (r & 3) >= key_lim[0]) sc[0][r >> 2][r & 3] = 2.f * kNegBig;
+      }
+      f16x8_v part[CT][2];
+      const float v0 = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i)), v1 = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + 1));
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        float w[8], sums[2], sum;
+        const int there = key_lim[ct] - key0 - 4 * g4;
+        auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+          for (int r = 0; r < 8; ++r) w[r] = fast_exp2(fmaf(sc[ct][r >> 2][r & 3], qs, -m[ct]));
+          if (CT > 1 && ends) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) w[r] = 16 * (r >> 2) + (r & 3) < there ? w[r] : 0.f;
+          }
+          sums[0] = (w[0] + w[1]) + (w[2] + w[3]); sums[1] = (w[4] + w[5]) + (w[6] + w[7]);
+          sum = sums[0] + sums[1];
+        };
+        auto move = [&]() __attribute__((always_inline)) {   // the reference, to the column's maximum
+          float top = kNegBig;
+#pragma unroll
+          for (int r = 0; r < 8; ++r) top = fmaxf(top, CT == 1 || 16 * (r >> 2) + (r & 3) < there ? sc[ct][r >> 2][r & 3] * qs : kNegBig);
+          top = rows_allreduce_max(top);
+          const float to = top > m[ct] + (CT == 1 ? 0.f : kLazy) ? ceilf(top) : m[ct];
+          if (!__any(to > m[ct])) return;
+          const float up = level[ct] * fast_exp2(to - m[ct]);
+          l[ct] *= fast_exp2(m[ct] - to);
+          m[ct] = to;
+          if (!(up <= kLevelStart)) {        // (as high as it goes: the sums come down instead, to nothing where there are none yet)
+            const float down = kLevelStart / up;
+#pragma unroll
+            for (int j = 0; j < 4 * H; ++j) o[ct][j] *= down;
+          }
+          level[ct] = fminf(up, kLevelStart);
+        };
+        // With two tiles of columns vector work counts: the maximum is formed only where weights get large (38.7 -> 35.3 us for 16 x 1-8 rows over 900 to 6000,
+        // 32/8 heads).  With one, a wave's two or three tiles would pay for forming the first one's weights twice.
+        if constexpr (CT == 1) {
+          move();
+          weights();
+        } else {
+          weights();
+          if (__builtin_expect(__any(sum > kRedo), 0)) {
+            move();
+            weights();
+          }
+        }
+        l[ct] += sum;
+        const float largest = fmaxf(sums[0] * fabsf(v0), sums[1] * fabsf(v1));     // (block by block: a heavy key has nothing to do with another block's scale)
+        if (__builtin_expect(__any(largest * level[ct] > kLevelMost), 0)) {
+          const float all = rows_allreduce_max(largest), to = all * level[ct] > kLevelMost ? level_for(all) : level[ct], was = to / level[ct];
+#pragma unroll
+          for (int j = 0; j < 4 * H; ++j) o[ct][j] *= was;
+          level[ct] = to;
+        }
+        u32x4_t hi, lo;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          uint32_t h, x;
+          split_halves(w[2 * r], w[2 * r + 1], (r < 2 ? v0 : v1) * level[ct], h, x);
+          hi[r] = h; lo[r] = x;
+        }
+        part[ct][0] = __builtin_bit_cast(f16x8_v, hi);
+        part[ct][1] = __builtin_bit_cast(f16x8_v, lo);
+      }
+      if (key0 + 32 > L) {                     // bytes behind the last entry may be anything: zeros, not a product with a weight of zero
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int there = L - (key0 + 16 * b + 4 * g4);
+          const uint32_t mask = there >= 4 ? 0xffffffffu : there <= 0 ? 0u : (1u << (8 * there)) - 1;
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) value[b][h][j] &= mask;
+        }
+      }
+      // A value that is no number would reach the columns that do not see it, by a weight of zero: its bytes become zeros, and the columns that do see it get a sum
+      // of weights that is no number.
+      if (__builtin_expect(n > 1 && ends, 0)) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          uint32_t nans = 0;
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) nans |= no_numbers(value[b][h][j]);
+          if (__builtin_expect(__any((nans & 0x80808080u) != 0), 0)) {
+#pragma unroll 1
+            for (int r = 0; r < 4; ++r, nans >>= 8) {
+              const bool here = (__ballot(nans >> 7 & 1) >> (16 * g4) & 0xffff) != 0;      // entry key0 + 16 b + 4 g4 + r
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct)
+                if (here && key0 + 16 * b + 4 * g4 + r < key_lim[ct]) l[ct] = no_number();
+            }
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                value[b][h][j] = only_numbers(value[b][h][j]);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+          }
+        }
+      }
 #pragma unroll
       for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          *reinterpret_cast<f32x4_t*>(&s_o[wave][16 * ct + c16][64 * h + 16 * g4 + 4 * r]) =
-              f32x4_t{o[ct][4 * h][r], o[ct][4 * h + 1][r], o[ct][4 * h + 2][r], o[ct][4 * h + 3][r]} * f;
+        for (int j = 0; j < 4; ++j) {
+          const f16x8_v a = __builtin_bit_cast(f16x8_v, half_operand(value[0][h][j], value[1][h][j]));
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              o[ct][4 * h + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, part[ct][k], o[ct][4 * h + j], 0, 0, 0);
+        }
+      load(value, p.v, v_lane, i + 1);
     }
-    __syncthreads();
-    const bool whole = count == 1;
-    const uint32_t mine = (pair * p.max_chunks + chunk) * (SUMS * 4);
-    auto result = [&](int c, int x) {            // where element x of a column goes
-      const int i = c / p.g;
-      return reinterpret_cast<f32x4_t*>(p.out + ((span.row + i) * p.Hq + kvh * p.g + (c - i * p.g)) * D + x);
-    };
-    for (int at = tid; at < own * (D / 4); at += 64 * NW) {
+  }
+
+  // the waves' sums: a lane has elements 64 h + 16 g4 + 4 r + j of its column
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const float sum = rows_allreduce_sum(l[ct]);
+    const float f = 1.f / level[ct];
+    if (g4 == 0) { s_ml[wave][16 * ct + c16][0] = m[ct]; s_ml[wave][16 * ct + c16][1] = sum; }
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4_t*>(&s_o[wave][16 * ct + c16][64 * h + 16 * g4 + 4 * r]) =
+            f32x4_t{o[ct][4 * h][r], o[ct][4 * h + 1][r], o[ct][4 * h + 2][r], o[ct][4 * h + 3][r]} * f;
+  }
+  __syncthreads();
+  const bool whole = chunks == 1;
+  const uint32_t mine = (pair * p.max_chunks + chunk) * (SUMS * 4);
+  auto result = [&](int c, int x) {            // where element x of a column goes
+    const int i = c / p.g;
+    return reinterpret_cast<f32x4_t*>(p.out + ((span.row + i) * p.Hq + kvh * p.g + (c - i * p.g)) * D + x);
+  };
+  for (int at = tid; at < own * (D / 4); at += 64 * NW) {
+    const int c = at / (D / 4), x = 4 * (at % (D / 4));
+    float top = kNegBig;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, s_ml[w][c][0]);
+    float sum = 0.f;
+    f32x4_t r{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = fast_exp2(s_ml[w][c][0] - top);
+      sum += f * s_ml[w][c][1];
+      r += f * *reinterpret_cast<const f32x4_t*>(&s_o[w][c][x]);
+    }
+    if (whole) *result(c, x) = r * (1.f / sum);
+    else {
+      store16_past(parts, mine + 4 * (c * D + x), r);
+      if (x == 0) store8_past(parts, mine + 4 * (COLS * D + 2 * c), top, sum);
+    }
+  }
+  if (whole) return;
+  // the workgroup that arrives last adds the parts up, in their order
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) s_last = __hip_atomic_fetch_add(p.arrivals + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (s_last != (int)chunks - 1) return;
+  if (tid == 0) __hip_atomic_store(p.arrivals + pair, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // A column's piece of four elements is a thread's, or (few columns) several threads' by turns; their sums meet in LDS.
+  const int pieces = own * (D / 4);
+  int teams = 1;
+  while (2 * teams * pieces <= 64 * NW) teams *= 2;
+  const int team = teams > 1 ? tid / pieces : 0;             // (threads behind the last team have nothing to do)
+  auto add_up = [&](auto together) {
+    constexpr int N = decltype(together)::value;             // parts that a thread asks for at once
+    for (int at = tid - team * pieces; at < pieces && team < teams; at += 64 * NW) {
       const int c = at / (D / 4), x = 4 * (at % (D / 4));
-      float top = kNegBig;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) top = fmaxf(top, s_ml[w][c][0]);
-      float sum = 0.f;
+      float top = kNegBig, sum = 0.f;
       f32x4_t r{0.f, 0.f, 0.f, 0.f};
+      for (uint32_t k0 = team; k0 < chunks; k0 += N * teams) {
+        u32x2_v ml[N];
+        f32x4_t part[N];
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float f = fast_exp2(s_ml[w][c][0] - top);
-        sum += f * s_ml[w][c][1];
-        r += f * *reinterpret_cast<const f32x4_t*>(&s_o[w][c][x]);
+        for (int k = 0; k < N; ++k) {
+          const uint32_t place = (pair * p.max_chunks + min(k0 + k * teams, chunks - 1)) * (SUMS * 4);
+          ml[k] = load8_past(parts, place + 4 * (COLS * D + 2 * c));
+          part[k] = load16_past(parts, place + 4 * (c * D + x));
+        }
+        float high = top;
+#pragma unroll
+        for (int k = 0; k < N; ++k) high = fmaxf(high, __uint_as_float(ml[k][0]));
+        const float was = fast_exp2(top - high);
+        top = high; sum *= was; r *= was;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float f = k0 + k * teams < chunks ? fast_exp2(__uint_as_float(ml[k][0]) - top) : 0.f;
+          sum += f * __uint_as_float(ml[k][1]);
+          r += f * part[k];
+        }
       }
-      if (whole) *result(c, x) = r * (1.f / sum);
+      if (teams == 1) *result(c, x) = r * (1.f / sum);
       else {
-        store16_past(parts, mine + 4 * (c * D + x), r);
-        if (x == 0) store8_past(parts, mine + 4 * (COLS * D + 2 * c), top, sum);
+        *reinterpret_cast<f32x4_t*>(&s_o[0][0][0] + (team * pieces + at) * 4) = r;
+        if (x == 0) { s_team[team * own + c][0] = top; s_team[team * own + c][1] = sum; }
       }
     }
-    if (whole) return;
-    // the workgroup that arrives last adds the parts up, in their order
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  };
+  if (chunks <= 4u * teams) add_up(std::integral_constant<int, 4>{});
+  else if (chunks <= 8u * teams) add_up(std::integral_constant<int, 8>{});
+  else add_up(std::integral_constant<int, 16>{});
+  if (teams > 1) {
     __syncthreads();
-    if (tid == 0) s_last = __hip_atomic_fetch_add(p.arrivals + pair, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (s_last != (int)count - 1) return;
-    if (tid == 0) __hip_atomic_store(p.arrivals + pair, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // A column's piece of four elements is a thread's, or (few columns) several threads' by turns; their sums meet in LDS.
-    const int pieces = own * (D / 4);
-    int teams = 1;
-    while (2 * teams * pieces <= 64 * NW) teams *= 2;
-    const int team = teams > 1 ? tid / pieces : 0;             // (threads behind the last team have nothing to do)
-    auto add_up = [&](auto together) {
-      constexpr int N = decltype(together)::value;             // parts that a thread asks for at once
-      for (int at = tid - team * pieces; at < pieces && team < teams; at += 64 * NW) {
-        const int c = at / (D / 4), x = 4 * (at % (D / 4));
-        float top = kNegBig, sum = 0.f;
-        f32x4_t r{0.f, 0.f, 0.f, 0.f};
-        for (uint32_t k0 = team; k0 < count; k0 += N * teams) {
-          u32x2_v ml[N];
-          f32x4_t part[N];
-#pragma unroll
-          for (int k = 0; k < N; ++k) {
-            const uint32_t place = (pair * p.max_chunks + min(k0 + k * teams, count - 1)) * (SUMS * 4);
-            ml[k] = load8_past(parts, place + 4 * (COLS * D + 2 * c));
-            part[k] = load16_past(parts, place + 4 * (c * D + x));
-          }
-          float high = top;
-#pragma unroll
-          for (int k = 0; k < N; ++k) high = fmaxf(high, __uint_as_float(ml[k][0]));
-          const float was = fast_exp2(top - high);
-          top = high; sum *= was; r *= was;
-#pragma unroll
-          for (int k = 0; k < N; ++k) {
-            const float f = k0 + k * teams < count ? fast_exp2(__uint_as_float(ml[k][0]) - top) : 0.f;
-            sum += f * __uint_as_float(ml[k][1]);
-            r += f * part[k];
-          }
-        }
-        if (teams == 1) *result(c, x) = r * (1.f / sum);
-        else {
-          *reinterpret_cast<f32x4_t*>(&s_o[0][0][0] + (team * pieces + at) * 4) = r;
-          if (x == 0) { s_team[team * own + c][0] = top; s_team[team * own + c][1] = sum; }
-        }
+    if (tid < pieces) {
+      const int c = tid / (D / 4), x = 4 * (tid % (D / 4));
+      float top = kNegBig, sum = 0.f;
+      for (int k = 0; k < teams; ++k) top = fmaxf(top, s_team[k * own + c][0]);
+      f32x4_t r{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < teams; ++k) {
+        const float f = fast_exp2(s_team[k * own + c][0] - top);
+        sum += f * s_team[k * own + c][1];
+        r += f * *reinterpret_cast<const f32x4_t*>(&s_o[0][0][0] + (k * pieces + tid) * 4);
       }
-    };
-    if (count <= 4u * teams) add_up(std::integral_constant<int, 4>{});
-    else if (count <= 8u * teams) add_up(std::integral_constant<int, 8>{});
-    else add_up(std::integral_constant<int, 16>{});
-    if (teams > 1) {
-      __syncthreads();
-      if (tid < pieces) {
-        const int c = tid / (D / 4), x = 4 * (tid % (D / 4));
-        float top = kNegBig, sum = 0.f;
-        for (int k = 0; k < teams; ++k) top = fmaxf(top, s_team[k * own + c][0]);
-        f32x4_t r{0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < teams; ++k) {
-          const float f = fast_exp2(s_team[k * own + c][0] - top);
-          sum += f * s_team[k * own + c][1];
-          r += f * *reinterpret_cast<const f32x4_t*>(&s_o[0][0][0] + (k * pieces + tid) * 4);
-        }
-        *result(c, x) = r * (1.f / sum);
-      }
+      *result(c, x) = r * (1.f / sum);
     }
   }
 }
-
 
 // ---------------------------------------------------------------------------
 // Many columns: 32 a wave, the workgroup's four share tiles of 64 entries.  A wave brings the bytes of one of a tile's four blocks, converts them (keys
