@@ -10,7 +10,7 @@
 //
 // Bound by memory where rows are many (139,008 rows of 12/2 heads, d = 128, bf16: 1.07 GB in 186 us, 5.7 TB/s; torch's copy of 2 GiB reaches 5.1), by the latency of tables and
 // loads where they are few (24 chunks of up to 130 rows, 14/2 heads, d = 64, fp32: 8.8 us; a row of 32/8 heads: 4.2, beside 9 of the call).  Two kernels:
-//   a block of 16 entries a workgroup (few rows: several, which share the queries' heads), d / 8 lanes a row: the block's largest magnitude goes through LDS;
+//   a block of 16 entries a workgroup (few rows: several, which share the heads), d / 8 lanes a row: the block's largest magnitude goes through LDS;
 //   one new row a sequence at most (a decode step): a workgroup a sequence, a wave for the key or the value of a head; the rest of the block is touched only where its scale grows.
 #include "bc_paged.h"
 #include "bc_rope_lane.h"
@@ -34,7 +34,9 @@ struct AppendParams {
   float* vs;
   int32_t Hq, Hkv, half;
   int32_t* arrivals;           // [B * Hkv] zero between launches
-  uint32_t blocks, turns;      // block kernel: blocks of a sequence, workgroups of a block
+  uint32_t blocks, turns;      // block kernel: blocks of a sequence, workgroups of a block,
+  int32_t kv_turns, kv_share;  // those that share its keys and values, and heads of either that each has;
+  int32_t q_from, q_share;     // the first one that has queries, and heads that each has
   float eps;
 };
 
@@ -100,9 +102,10 @@ __device__ __forceinline__ void norm_head(float (&x)[2][4], const float (&w)[2][
   for (int e = 0; e < 4; ++e) { x[0][e] *= r * w[0][e]; x[1][e] *= r * w[1][e]; }
 }
 
-// 16 rows' lanes: 256 threads, 128 for d = 64.  A block has p.turns workgroups: the first has the keys and values, and the queries' heads where it is alone; the others share those heads.
+// 16 rows' lanes: 256 threads, 128 for d = 64.  A block has p.turns workgroups: the first kv_turns share the heads of keys and of values, the others those of queries; one alone has all.
+// (Five waves a SIMD: 256 x 2-4 rows 29.6 us with four, 28.0.  In fp32 with norms that is two registers short.)
 template <typename T, int D, bool NORM, bool STREAM>
-__global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
+__global__ void __launch_bounds__(2 * D, Elem<T>::size == 2 ? 5 : 4) paged_append_kernel(AppendParams p) {
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES, U = 4;
   __shared__ float s_most[U][kPagedBlock];
   const int lane = threadIdx.x % LPH, mine = threadIdx.x / LPH;      // a row of the block
@@ -125,12 +128,11 @@ __global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
   const int64_t row = plan.row + (fresh ? slot - start : 0);         // (other rows' lanes look at the first one)
   const char* in = p.qkv + row * p.row_bytes;
   const RopeLane<D> ln(p.half, p.inv_freq, lane, p.positions[row]);
-  if (p.q && fresh && (turn > 0 || p.turns == 1)) {
+  if (p.q && fresh && turn >= p.q_from) {
     float w[2][4];
     const bool norm = NORM && p.qw != nullptr;
     if (norm) { load4(p.qw + ln.o1 * ES, w[0], T{}); load4(p.qw + ln.o2 * ES, w[1], T{}); }
-    const int shares = p.turns > 1 ? (int)p.turns - 1 : 1, share = p.turns > 1 ? turn - 1 : 0;
-    const int h_first = p.Hq * share / shares, h_end = p.Hq * (share + 1) / shares;
+    const int h_first = (turn - p.q_from) * p.q_share, h_end = min(h_first + p.q_share, p.Hq);
     for (int h0 = h_first; h0 < h_end; h0 += U) {
       float x[U][2][4];
 #pragma unroll
@@ -150,18 +152,19 @@ __global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
       }
     }
   }
-  if (turn > 0) return leave();
+  if (turn >= p.kv_turns) return leave();
   const int page = p.t.table[(int64_t)s * p.t.table_pages + (first >> p.t.page_shift)];
   const int r = slot & ((1 << p.t.page_shift) - 1), per_page = 1 << (p.t.page_shift - 4), block = (first >> 4) & (per_page - 1);
   // keys, then values
   float w[2][4];
   const bool norm = NORM && p.kw != nullptr;
   if (norm) { load4(p.kw + ln.o1 * ES, w[0], T{}); load4(p.kw + ln.o2 * ES, w[1], T{}); }
-  for (int it = 0; it < 2 * p.Hkv; it += U) {
+  const int it_end = min((turn + 1) * p.kv_share, 2 * p.Hkv);
+  for (int it = turn * p.kv_share; it < it_end; it += U) {
     float x[U][2][4], was[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int item = min(it + u, 2 * p.Hkv - 1), value = item >= p.Hkv, h = item - value * p.Hkv;
+      const int item = min(it + u, it_end - 1), value = item >= p.Hkv, h = item - value * p.Hkv;
       const int o1 = value ? 8 * lane : ln.o1, o2 = value ? 8 * lane + 4 : ln.o2;       // (values are not turned: eight in a row)
       load4<STREAM>(in + (int64_t)(p.Hq + item) * HEAD + o1 * ES, x[u][0], T{});
       load4<STREAM>(in + (int64_t)(p.Hq + item) * HEAD + o2 * ES, x[u][1], T{});
@@ -169,7 +172,7 @@ __global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int item = min(it + u, 2 * p.Hkv - 1), value = item >= p.Hkv, h = item - value * p.Hkv;
+      const int item = min(it + u, it_end - 1), value = item >= p.Hkv, h = item - value * p.Hkv;
       if (stays) {                         // what it holds, for the case that the scale grows
         const uint8_t* old = (value ? p.v : p.k) + ((((int64_t)page * p.Hkv + h) << p.t.page_shift) * D);
         if (value) {
@@ -197,7 +200,7 @@ __global__ void __launch_bounds__(2 * D) paged_append_kernel(AppendParams p) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int item = it + u, value = item >= p.Hkv, h = item - value * p.Hkv;
-      if (item >= 2 * p.Hkv) break;
+      if (item >= it_end) break;
       float most = 0.f;
 #pragma unroll
       for (int i = 0; i < kPagedBlock; ++i) most = fmaxf(most, s_most[u][i]);
@@ -328,12 +331,23 @@ __global__ void __launch_bounds__(1024) paged_append_one_kernel(AppendParams p) 
   if (threadIdx.x == 0) p.t.len[s] = start + 1;
 }
 
-// Workgroups of a block: more where there are few rows.
+// Workgroups of a block: more where there are few rows, of keys and values as of queries.  (us, 32/8 heads, bf16: keys and values all in one workgroup, and shared out)
+//   5 x 1-15 rows 18.0, 8.9     64 x 2-8 19.9, 13.1     1 x 2000 28.7, 19.0     256 x 2-4 27.6, 28.0
+// 1024, 1536, 2048, 4096 workgroups: 1 x 2000 rows 23.3, 28.0, 28.0, 28.0; 400 x 2-4 43.5, 39.5, 72, 80.
 constexpr int64_t kAppendGroups = 1024;
 void deal_blocks(AppendParams& p, int64_t rows) {
-  const int64_t blocks = (rows + kPagedBlock - 1) / kPagedBlock + p.t.B, heads = p.q ? p.Hq : 0, most = (heads + 3) / 4 + 1;
-  const int64_t want = heads ? kAppendGroups / blocks : 1;
-  p.turns = (uint32_t)(want < 1 ? 1 : want > most ? most : want);
+  const int64_t blocks = (rows + kPagedBlock - 1) / kPagedBlock + p.t.B, of_q = p.q ? (p.Hq + 3) / 4 : 0, of_kv = (2 * (int64_t)p.Hkv + 3) / 4;      // (four heads at a time)
+  const int64_t want = kAppendGroups / blocks;
+  // groups of four as `turns` workgroups share them: groups of each; and how many workgroups then have some
+  auto each = [](int64_t of, int64_t turns) { return turns < 2 ? of : turns < of ? (of + turns - 1) / turns : 1; };
+  auto having = [](int64_t of, int64_t each) { return of ? (of + each - 1) / each : 0; };
+  const int64_t kv = each(of_kv, want * of_kv / (of_kv + of_q));
+  p.kv_share = (int32_t)(4 * kv);
+  p.kv_turns = (int32_t)having(of_kv, kv);
+  const int64_t q = each(of_q, want - p.kv_turns);
+  p.q_share = (int32_t)(4 * q);
+  p.q_from = want < 2 ? 0 : p.kv_turns;
+  p.turns = (uint32_t)(want < 2 ? 1 : p.kv_turns + having(of_q, q));
 }
 // Packed rows beyond the 256 MB of the Infinity Cache go past it, as in bc_qk_norm_rope.
 template <typename T, int D, bool NORM>

@@ -142,6 +142,24 @@ def test_append_is_exact_without_norm_and_rotation(dev, Hq, Hkv, d, dtype):
     assert both.c.err.item() == 0
 
 
+@pytest.mark.parametrize("Hq,Hkv,d", [(32, 8, 128), (7, 7, 64), (4, 1, 64)])
+def test_append_without_queries(dev, Hq, Hkv, d):
+    # the entry point itself, q NULL: however workgroups share the heads, the same entries
+    import torch
+    from paper_2510_13797_amd import bc
+    for n in ([5, 30, 0], [300, 1, 17], [1, 1, 1]):
+        both, other = (Both(dev, 3, Hq, Hkv, d, 32, 400, seed=9) for _ in range(2))
+        x, _ = both.append(n)
+        pos = torch.zeros(len(x), dtype=torch.int32, device=dev)
+        off = torch.from_numpy(np.concatenate([[0], np.cumsum(n)])).to(dev)
+        c = other.c
+        assert bc.bc_paged_append(c.shape, c._c, len(x), off.data_ptr(), max(n), x.data_ptr(), x.stride(0), pos.data_ptr(), None, 0, None, None, 1e-6,
+                                  None, None, None, torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(both.c.lengths, c.lengths)
+        for a, b in zip(both.pool(), other.pool()):
+            assert np.array_equal(a, b, equal_nan=a.dtype.kind == "f")
+
+
 @pytest.mark.parametrize("page", [16, 64, 1024])
 def test_append_a_row_each_without_offsets(dev, page):
     import torch
