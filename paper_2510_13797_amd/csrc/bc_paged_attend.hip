@@ -767,8 +767,12 @@ struct AttendLaunch {
 // the first.  Two tiles of columns leave twice the sums to add up: chunks of at least sixteen tiles (1 x 8000: 19.1 -> 15.9, others as they were).
 // Caches beyond some 100 MB go past the caches: 64 x 1000 rows, 32/8 heads (131 MB) 30.2 -> 26.7; 128 x 300 (79 MB) 17.5 -> 18.3.
 // (Chunks of equal size for all sequences of a batch, worked out by every workgroup from the lengths: 2.3 us more for one tile of columns, nothing gained with two.)
-// Many columns: parts until there are as many workgroups as run at once (two a compute unit): 512 rows over 7680, 32/8 heads, in three, four, five parts 135, 115, 153 us.
+// Many columns: as many parts as cost least, in tiles of 64: rounds of the workgroups that run at once (two a compute unit), a workgroup's tiles and its two ends, and parts written and
+// read again.  512 rows over 7680, 32/8 heads, in three, four, five parts 135, 115, 153 us.  One round of workgroups at most, and so:
+//   69 x 15 rows over 1400-27,900, 14/2 heads, d = 64   237, 184     8 x 50-500 over 300-20,000, 12/2   555, 438     9 x 256 over 4000, 32/8   298, 273
+//   the same, all over 27,900                           270, 258     3 x 400 over 6000, 32/8            208, 190     20 x 64 over 3000, 32/8   119, 119 (ends of three tiles: 132)
 constexpr int kMostParts = 16, kManyGroups = 512;
+constexpr double kEndTiles = 5, kFoldTiles = 0.012;
 constexpr int64_t kStreamBytes = 96 << 20;
 AttendLaunch plan_attend(const bc_shape* sh, int64_t rows, int64_t max_new, int64_t max_len) {
   AttendLaunch a{};
@@ -788,11 +792,13 @@ AttendLaunch plan_attend(const bc_shape* sh, int64_t rows, int64_t max_new, int6
   }
   a.blocks = (int)((columns + kManyColumns - 1) / kManyColumns);
   const int64_t groups = pairs * a.blocks;
-  int64_t parts = kManyGroups / groups;
-  if (parts > kMostParts) parts = kMostParts;
-  if (parts > tiles / 8) parts = tiles / 8;
-  if (parts < 1) parts = 1;
-  a.parts = (int)parts;
+  double least = 0;
+  for (int64_t parts = 1; parts <= kMostParts && (parts == 1 || parts <= tiles / 8); ++parts) {
+    const double rounds = (double)((groups * parts + kManyGroups - 1) / kManyGroups), fold = parts > 1 ? kFoldTiles * (double)(groups * parts) : 0;
+    const double cost = rounds * ((double)tiles / 2 / (double)parts + kEndTiles) + fold;
+    if (parts == 1 || cost < least) { least = cost; a.parts = (int)parts; }
+  }
+  const int64_t parts = a.parts;
   const int64_t fold = pairs * ((columns + 1024 / sh->d - 1) / (1024 / sh->d));
   a.fits = groups * parts <= 0x7fffffff && fold <= 0x7fffffff;
   if (parts > 1) {

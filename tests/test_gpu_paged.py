@@ -365,6 +365,20 @@ def test_long_sequences_in_parts(dev):
         assert both.torch.equal(a, b)
 
 
+def test_parts_of_more_workgroups_than_run_at_once(dev):
+    # 138 and 576 blocks of columns, by the longest there may be in seven and three parts; short sequences among long ones have fewer
+    both = Both(dev, 69, 14, 2, 64, 64, 28000)
+    n = np.random.default_rng(8).integers(5, 16, 69)
+    both.append(np.where(np.arange(69) % 3 == 0, 9000, np.where(np.arange(69) % 3 == 1, 1, 500)))
+    _, q = both.append(n)
+    both.check_attend(q, n, every=7)
+    both = Both(dev, 9, 16, 8, 128, 32, 5000)
+    n = np.array([510, 3, 450, 0, 512, 1, 350, 64, 65])
+    both.append(np.full(9, 900))
+    _, q = both.append(n)
+    both.check_attend(q, n, every=251)
+
+
 def test_many_sequences(dev):
     r = np.random.default_rng(3)
     for B, Hq, Hkv, d in ((300, 4, 1, 64), (70, 12, 2, 128), (33, 32, 8, 128)):
