@@ -470,13 +470,15 @@ __device__ __forceinline__ ManyCut many_cut(int parts, int lim, int part) {
   return {tiles, (int)((int64_t)tiles * part / n), (int)((int64_t)tiles * (part + 1) / n), n};
 }
 
-template <int D>
+// Up to 64 columns (HALVES): two waves have a column, and of every tile half of the entries each; their sums meet in LDS at the end.  (With two of the four waves idle, the same
+// SIMDs had all the work of both workgroups: 18 x 2-5 rows over 10,000-30,000, 16/2 heads, 93 -> 71.5 us; 100 x 16 over 500-2000, 32/8, 135 -> 104.)
+template <int D, bool HALVES>
 __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendParams p) {
-  constexpr int KS = D / 16, NJ = D / 32, K_BYTES = kManyTile * D * 2, STAGE = 2 * K_BYTES, BLOCK_BYTES = kPagedBlock * D;
+  constexpr int NX = HALVES ? 1 : 2, KS = D / 16, NJ = D / 32, K_BYTES = kManyTile * D * 2, STAGE = 2 * K_BYTES, BLOCK_BYTES = kPagedBlock * D;
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
   __shared__ float s_rest[2][kManyWaves];                        // what the conversion left of a block's key scale,
   __shared__ int s_uneven;                                       // whether that has been anything but ones,
-  __shared__ f32x4_t s_value[2];                                 // value scales,
+  __shared__ __attribute__((aligned(16))) float s_value[2][kManyWaves];                                 // value scales,
   __shared__ __attribute__((aligned(8))) uint16_t s_no_number[2][kManyWaves];      // entries with a value that is no number
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const uint32_t pairs = (uint32_t)p.t.B * p.Hkv;
@@ -492,7 +494,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   const ManyCut cut = many_cut(p.parts, L - n + 1 + last_row, part);
   if (part >= cut.parts) return;
 
-  const int mine = first + 32 * wave, c = min(mine + col, columns - 1), i = c / p.g;
+  const int x0 = HALVES ? wave >> 1 : 0;                         // (the wave's half)
+  const int mine = first + 32 * (HALVES ? wave & 1 : wave), c = min(mine + col, columns - 1), i = c / p.g;
   const int lim = L - n + 1 + i;                                 // entries that this lane's column sees
   const int all_free = (L - n + 1 + first / p.g) / kManyTile;    // tiles that all columns of the workgroup see whole
   const int free_tiles = (L - n + 1 + min(mine, columns - 1) / p.g) / kManyTile;        // tiles that all of the wave's columns see whole
@@ -600,37 +603,37 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
       const char* tile = lds + stage * STAGE;
       // (The wave that has products to issue goes first: the other of its SIMD forms weights meanwhile.  5.15 -> 4.81 ms; with the weights first 5.16.)
       __builtin_amdgcn_s_setprio(1);
-      f32x16_t sc[2];
+      f32x16_t sc[NX];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < NX; ++x) {
         sc[x] = f32x16_t{0.f};
 #pragma unroll
         for (int k = 0; k < KS; ++k)
           sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              *reinterpret_cast<const bf16x8_t*>(tile + x * (K_BYTES / 2) + k * 1024 + half * 512 + ((col ^ (2 * (k & 3))) * 16)), qb[k], sc[x], 0, 0, 0);
+              *reinterpret_cast<const bf16x8_t*>(tile + (x0 + x) * (K_BYTES / 2) + k * 1024 + half * 512 + ((col ^ (2 * (k & 3))) * 16)), qb[k], sc[x], 0, 0, 0);
       }
       __builtin_amdgcn_s_setprio(0);
       // (A block's values are read in front of the block before it: 111 us for 512 rows over 7680, 110 so.)
       f16x8_v a[2][NJ];
       auto values = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) a[b & 1][j] = *reinterpret_cast<const f16x8_v*>(tile + K_BYTES + b * (NJ * 1024) + j * 1024 + half * 512 + col * 16);
+        for (int j = 0; j < NJ; ++j) a[b & 1][j] = *reinterpret_cast<const f16x8_v*>(tile + K_BYTES + (2 * x0 + b) * (NJ * 1024) + j * 1024 + half * 512 + col * 16);
       };
       values(0);
       const bool uneven = __builtin_amdgcn_readfirstlane(s_uneven) != 0;
-      // result e of sc[x]: entry 32 x + 8 (e / 4) + 4 half + e % 4 of the tile, of its block 2 x + e / 8
+      // result e of sc[x]: entry 32 (x0 + x) + 8 (e / 4) + 4 half + e % 4 of the tile, of its block 2 (x0 + x) + e / 8
       if (__builtin_expect(uneven, 0)) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < NX; ++x)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sc[x][e] *= s_rest[stage][2 * x + e / 8];
+          for (int e = 0; e < 16; ++e) sc[x][e] *= s_rest[stage][2 * (x0 + x) + e / 8];
       }
       const bool ends = t >= free_tiles;                         // some columns do not see all of it
-      const int there = lim - kManyTile * t - 4 * half;
-      float pe[2][16], sums[4], psum;                            // sums: of blocks
+      const int there = lim - kManyTile * t - 32 * x0 - 4 * half;
+      float pe[NX][16], sums[2 * NX], psum;                            // sums: of blocks
       auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < NX; ++x) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) pe[x][e] = fast_exp2(fmaf(sc[x][e], p.qs, -m));
           if (ends) {
@@ -640,13 +643,14 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
           sums[2 * x] = ((pe[x][0] + pe[x][1]) + (pe[x][2] + pe[x][3])) + ((pe[x][4] + pe[x][5]) + (pe[x][6] + pe[x][7]));
           sums[2 * x + 1] = ((pe[x][8] + pe[x][9]) + (pe[x][10] + pe[x][11])) + ((pe[x][12] + pe[x][13]) + (pe[x][14] + pe[x][15]));
         }
-        psum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+        psum = sums[0] + sums[1];
+        if constexpr (NX == 2) psum += sums[2] + sums[3];
       };
       weights();
       if (__builtin_expect(__any(psum > kRedo), 0)) {
         float top = kNegBig;
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < NX; ++x)
 #pragma unroll
           for (int e = 0; e < 16; ++e) top = fmaxf(top, 32 * x + 8 * (e >> 2) + (e & 3) < there ? sc[x][e] * p.qs : kNegBig);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -666,8 +670,12 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         const int sees = lim - kManyTile * t;
         if (sees > 0 && (entries & (sees >= 64 ? ~0ull : (1ull << sees) - 1)) != 0) l = no_number();
       }
-      const f32x4_t scales = s_value[stage];
-      const float largest = fmaxf(fmaxf(sums[0] * fabsf(scales[0]), sums[1] * fabsf(scales[1])), fmaxf(sums[2] * fabsf(scales[2]), sums[3] * fabsf(scales[3])));
+      float scales[2 * NX], largest = 0.f;
+#pragma unroll
+      for (int b = 0; b < 2 * NX; ++b) {
+        scales[b] = s_value[stage][2 * x0 + b];
+        largest = fmaxf(largest, sums[b] * fabsf(scales[b]));
+      }
       if (__builtin_expect(__any(largest * level > kLevelMost), 0)) {
         const float both = fmaxf(largest, __shfl_xor(largest, 32, 64)), to = both * level > kLevelMost ? level_for(both) : level, was = to / level;
 #pragma unroll
@@ -675,7 +683,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         level = to;
       }
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < 2 * NX; ++b) {
         u32x4_t hi, lo;
         if (b == 0) __builtin_amdgcn_s_setprio(1);
         const float f = scales[b] * level;
@@ -685,7 +693,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
           split_halves(pe[b >> 1][8 * (b & 1) + 2 * y], pe[b >> 1][8 * (b & 1) + 2 * y + 1], f, h, r);
           hi[y] = h; lo[y] = r;
         }
-        if (b < 3) values(b + 1);
+        if (b + 1 < 2 * NX) values(b + 1);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) O[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[b & 1][j], __builtin_bit_cast(f16x8_v, hi), O[j], 0, 0, 0);
 #pragma unroll
@@ -695,8 +703,27 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
     __builtin_amdgcn_s_setprio(0);
     __syncthreads();
   }
-  if (mine + col >= columns) return;
   l += __shfl_xor(l, 32, 64);
+  if constexpr (HALVES) {                                        // (all have left the last tile behind)
+    float* other = reinterpret_cast<float*>(lds) + (wave & 1) * (NJ * 16 + 2) * 64 + lane;
+    if (wave >= 2) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) other[(16 * j + e) * 64] = O[j][e] * (1.f / level);
+      other[NJ * 16 * 64] = m; other[(NJ * 16 + 1) * 64] = l;
+    }
+    __syncthreads();
+    if (wave >= 2) return;
+    const float its = other[NJ * 16 * 64], top = fmaxf(m, its), f0 = fast_exp2(m - top), f1 = fast_exp2(its - top);
+    l = l * f0 + other[(NJ * 16 + 1) * 64] * f1;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) O[j][e] = O[j][e] * (1.f / level) * f0 + other[(16 * j + e) * 64] * f1;
+    m = top; level = 1.f;
+  }
+  if (mine + col >= columns) return;
   const int64_t at = (span.row + i) * p.Hq + kvh * p.g + (c - i * p.g);
   const bool whole = cut.parts == 1;
   float* to = whole ? p.out + at * D : p.part + (part * (p.t.rows * p.Hq) + at) * D;
@@ -822,7 +849,9 @@ void launch_attend(const AttendParams& p, const AttendLaunch& a, hipStream_t s) 
     return;
   }
   const int64_t pairs = (int64_t)p.t.B * p.Hkv;
-  paged_many_kernel<D><<<(unsigned)(pairs * a.blocks * a.parts), 64 * kManyWaves, 0, s>>>(p);
+  const unsigned groups = (unsigned)(pairs * a.blocks * a.parts);
+  if ((int64_t)p.t.max_new * p.g <= kManyColumns / 2) paged_many_kernel<D, true><<<groups, 64 * kManyWaves, 0, s>>>(p);
+  else paged_many_kernel<D, false><<<groups, 64 * kManyWaves, 0, s>>>(p);
   if (a.parts > 1) {
     const int64_t columns = (int64_t)p.t.max_new * p.g, per = 1024 / D;
     paged_fold_kernel<D><<<(unsigned)(pairs * ((columns + per - 1) / per)), 256, 0, s>>>(p);

@@ -343,7 +343,7 @@ def test_some_rows(dev, Hq, Hkv, d):
         both.check_attend(q, n, active=[1, 0, 1, 1, 0, 1], device_offsets=True)
 
 
-@pytest.mark.parametrize("n", [31, 32, 33, 63, 64, 65, 96, 127, 128, 129, 300])
+@pytest.mark.parametrize("n", [9, 15, 16, 17, 31, 32, 33, 63, 64, 65, 96, 127, 128, 129, 300])
 @pytest.mark.parametrize("L", [0, 32, 45])
 def test_ends_of_tiles(dev, n, L):
     for Hq, Hkv, d in ((4, 1, 128), (4, 4, 64)):
@@ -370,6 +370,9 @@ def test_parts_of_more_workgroups_than_run_at_once(dev):
     both = Both(dev, 69, 14, 2, 64, 64, 28000)
     n = np.random.default_rng(8).integers(5, 16, 69)
     both.append(np.where(np.arange(69) % 3 == 0, 9000, np.where(np.arange(69) % 3 == 1, 1, 500)))
+    _, q = both.append(n)
+    both.check_attend(q, n, every=7)
+    n = np.random.default_rng(9).integers(0, 10, 69)             # (two waves a column)
     _, q = both.append(n)
     both.check_attend(q, n, every=7)
     both = Both(dev, 9, 16, 8, 128, 32, 5000)
@@ -411,7 +414,7 @@ def test_the_sum_where_the_scale_is_zero_and_where_scores_are_large(dev):
     both.check_attend(q, [1, 1], tol=0.05)
 
 
-@pytest.mark.parametrize("n", [[1, 3], [40, 66]])
+@pytest.mark.parametrize("n", [[1, 3], [9, 14], [40, 66]])
 @pytest.mark.parametrize("d", [64, 128])
 def test_scales_of_any_kind(dev, n, d):
     # a cache filled by the caller: scales that are no powers of two, negative ones and zeros among them
@@ -430,7 +433,7 @@ def test_scales_of_any_kind(dev, n, d):
     both.check_attend(q, n)
 
 
-@pytest.mark.parametrize("n", [[1, 2], [6, 8], [40, 66]])
+@pytest.mark.parametrize("n", [[1, 2], [6, 8], [20, 31], [40, 66]])
 @pytest.mark.parametrize("d", [64, 128])
 def test_values_of_very_different_sizes(dev, n, d):
     # blocks of values from 1e-25 to 1e25, empty ones among them, under scores that let now these, now those weigh something.  A product of a weight and a value is in two
@@ -467,7 +470,7 @@ def test_values_of_very_different_sizes(dev, n, d):
                 assert np.abs(got[off[s] + i, h] - products.sum(axis=0)).max() <= 1e-5 * np.abs(products).max() + 1e-37, (s, i, h)
 
 
-@pytest.mark.parametrize("n", [[1, 2], [6, 8], [40, 66]])
+@pytest.mark.parametrize("n", [[1, 2], [6, 8], [20, 31], [40, 66]])
 @pytest.mark.parametrize("size", [1e-33, 1e-30, 1e30])
 def test_values_at_the_ends_of_the_range(dev, n, size):
     # scores that rise with the entries, so that the reference moves all along, over values whose level is as high, or as low, as it goes
@@ -498,7 +501,7 @@ def test_values_at_the_ends_of_the_range(dev, n, size):
             assert np.abs(got[off[s] + i] - ref).max() <= TOL * size, (s, i)
 
 
-@pytest.mark.parametrize("n", [[2, 5], [9, 16], [40, 66], [140, 200]])
+@pytest.mark.parametrize("n", [[2, 5], [9, 16], [18, 31], [40, 66], [140, 200]])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("before", [[0, 3], [75, 41], [900, 1500]])
 def test_what_a_row_does_not_see_does_not_reach_it(dev, n, d, before):

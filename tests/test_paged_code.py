@@ -20,7 +20,7 @@ def attend(tmp_path_factory):
 
 def test_attend_spills_nothing(attend):
     few, many = list(_kernels(attend, "paged_few_kernel")), list(_kernels(attend, "paged_many_kernel"))
-    assert len(few) == 16 and len(many) == 2
+    assert len(few) == 16 and len(many) == 4
     for name, body, waves in few + many:
         assert not any(l.startswith("scratch_") for l in body), name
         # (one tile of columns and four waves a workgroup: four workgroups a compute unit; the others two waves a SIMD)
