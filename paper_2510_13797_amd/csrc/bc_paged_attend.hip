@@ -12,9 +12,9 @@
 //
 // Two kernels:
 //   up to 32 columns: bound by memory, and by latency at both ends.  A row over 16,000, 32/8 heads, d = 128 (33 MB): 12.5 us; 64 rows over 4352 to 8704, 12/2 heads (216 MB): 38.7 (6.3 TB/s while it
-//   streams, as 1.07 GB in 171 us; a large read reaches 6.5); 1 to 8 rows of 16 sequences over 900 to 6000, 32/8 heads (121 MB): 28.6;
-//   more: bound by the matrix cores, large ones by the power limit.  4 x 2048 rows over 30,000, 32/8 heads: 4.95 ms, 0.79 PFLOP/s of the definition's products and 1.18 of those issued (a library
-//   product of 16384^3 reaches 1.37), matrix pipe busy 59 % of the cycles at 1.9 GHz; 512 rows over 7680: 105 us.
+//   streams, as 1.07 GB in 171 us; a large read reaches 6.5); 1 to 8 rows of 16 sequences over 900 to 6000, 32/8 heads (121 MB): 28.2 to 29.3;
+//   more: bound by the matrix cores, large ones by the power limit.  4 x 2048 rows over 30,000, 32/8 heads: 4.84 to 5.23 ms from card to card, 0.80 to 0.74 PFLOP/s of the definition's products and
+//   1.2 to 1.1 of those issued (a library product of 16384^3 reaches 1.39 to 1.32), matrix pipe busy 59 % of the cycles at 1.9 to 1.8 GHz; 512 rows over 7680: 103 to 108 us.
 #include "bc_paged.h"
 
 namespace bc {
