@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(2 * D, Elem<T>::size == 2 ? 5 : 4) paged_appen
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int item = min(it + u, it_end - 1), value = item >= p.Hkv, h = item - value * p.Hkv;
-      if (stays) {                         // what it holds, for the case that the scale grows
+      if (stays) {                         // what it holds, for the case that the scale grows (half of it: 256 * 2^120 is no number of 32 bits)
         const uint8_t* old = (value ? p.v : p.k) + ((((int64_t)page * p.Hkv + h) << p.t.page_shift) * D);
         if (value) {
 #pragma unroll
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(2 * D, Elem<T>::size == 2 ? 5 : 4) paged_appen
           unpack_e4m3(*reinterpret_cast<const uint32_t*>(old + key_at<D>(r, ln.o2)), x[u][1]);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { x[u][0][e] *= was[u]; x[u][1][e] *= was[u]; }
+        for (int e = 0; e < 4; ++e) { x[u][0][e] *= 0.5f * was[u]; x[u][1][e] *= 0.5f * was[u]; }
       } else if (!value) {
         if (norm) norm_head<T, D, NORM>(x[u], w, p.eps);
         ln.template turn<false>(x[u][0], x[u][1]);
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(2 * D, Elem<T>::size == 2 ? 5 : 4) paged_appen
       float most = 0.f;
 #pragma unroll
       for (int i = 0; i < kPagedBlock; ++i) most = fmaxf(most, s_most[u][i]);
-      const float scale = fmaxf(power_of_two(scale_exponent(most)), was[u]), inv = inverse_of(scale);
+      const float scale = fmaxf(power_of_two(scale_exponent(most)), was[u]), inv = inverse_of(scale) * (stays ? 2.f : 1.f);
       const int64_t head = (int64_t)page * p.Hkv + h;
       if (threadIdx.x == 0) (value ? p.vs : p.ks)[head * per_page + block] = scale;
       uint8_t* to = (value ? p.v : p.k) + (head << p.t.page_shift) * D;

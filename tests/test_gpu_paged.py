@@ -244,6 +244,25 @@ def test_what_is_not_finite(dev):
     both.check_pool(before)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_entries_stay(dev, dtype, d):
+    # the largest magnitudes there are become 256 * 2^120, which is no number of 32 bits by itself: chunks and rows that join their block leave them what they are
+    import torch
+    both = Both(dev, 3, 4, 2, d, 16, 80, dtype)
+    x = both.packed(30)
+    top = torch.finfo(both.dtype).max
+    h = x.view(30, 8, d)
+    h[::3, 4:, 1], h[1::4, 4:, d - 2] = top, -top
+    before = both.pool()
+    both.append([9, 13, 3], packed=x)
+    both.check_pool(before)
+    for n in ([2, 5, 30], [1, 1, 1], [3, 0, 2]):
+        both.append(n)
+        both.check_pool(before)
+    assert both.c.err.item() == 0
+
+
 def test_sequences_that_cannot_take_part_are_left_alone(dev):
     import torch
     from paper_2510_13797_amd import bc
