@@ -760,6 +760,7 @@ class PagedCache:
         self.k_scale, self.v_scale = (torch.full((self.pages, self.Hkv, self.page_rows // 16), float("nan"), device=device) for _ in range(2))
         self.device = self.k_pages.device
         self._width = (self.Hq + 2 * self.Hkv) * self.d
+        self._given_table = table                  # (it may come from any stream)
         if table is None:
             table = torch.zeros(self.B, self.table_pages, dtype=torch.int32, device=device)
         else:
@@ -771,6 +772,12 @@ class PagedCache:
         self._c = bc_pages(*(t.data_ptr() for t in self._own()), self.pages, self.page_rows, self.table_pages, 0)
         self._refs = C.byref(self.shape), C.byref(self._c)
         self._home = _stream_ptr() if self.device.type == "cuda" else None
+
+    def _noted(self, stream, *tensors):
+        """Notes on the call's stream what may be freed behind it: the caller's tensors, a table among them, and off the cache's own stream all that it owns."""
+        _used_here(self._given_table, *tensors)
+        if stream != self._home:
+            _used_here(*self._own())
 
     def _own(self):
         return self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.table, self.lengths, self.err, self._arrivals
@@ -842,9 +849,7 @@ class PagedCache:
                                                   2 * half, _ptr(q_weight), _ptr(k_weight), eps, _ptr(keep), _ptr(active), q.data_ptr(), stream)
         if st != BC_OK:
             _check(st)
-        _used_here(qkv, positions, inv_freq, q_weight, k_weight, keep, active, given, offsets if offsets is row_offsets else None)
-        if stream != self._home:
-            _used_here(*self._own())
+        self._noted(stream, qkv, positions, inv_freq, q_weight, k_weight, keep, active, given, offsets if offsets is row_offsets else None)
         return q
 
     def attend(self, q, row_offsets=None, max_new=None, max_len=None, active=None, out=None):
@@ -877,9 +882,7 @@ class PagedCache:
             st = lib.bc_paged_attend(shape, pages, rows, _ptr(offsets), most, q.data_ptr(), out.data_ptr(), _ptr(active), ws.data_ptr(), nbytes, stream)
         if st != BC_OK:
             _check(st)
-        _used_here(q, active, given, offsets if offsets is row_offsets else None)
-        if stream != self._home:
-            _used_here(*self._own())
+        self._noted(stream, q, active, given, offsets if offsets is row_offsets else None)
         return out
 
     def entries(self, s):

@@ -604,6 +604,34 @@ def test_layers_that_share_a_table_and_run_at_once(dev):
         assert all(torch.equal(a, b) for a, b in zip(got[i], alone[i]))
 
 
+def test_a_given_table_stays_while_a_call_is_in_work(dev):
+    # table and cache are dropped with calls still waiting on a stream of their own: the table's memory is not given out again before them
+    import torch
+    from paper_2510_13797_amd import bc
+    B, Hq, Hkv, d = 2, 4, 1, 64
+    x, pos, none = torch.randn(B, (Hq + 2 * Hkv) * d, device=dev).bfloat16(), torch.zeros(B, dtype=torch.int32, device=dev), torch.zeros(0, device=dev)
+    q, stream = torch.randn(B, Hq, d, device=dev).bfloat16(), torch.cuda.Stream()
+
+    def call(cache, kind):
+        return cache.append(x, pos, none) if kind == "append" else cache.attend(q)
+
+    for kind in ("append", "attend"):
+        table = torch.zeros(B, 1 << 16, dtype=torch.int32, device=dev)
+        table[:, 0] = torch.arange(B, device=dev)
+        at, size = table.data_ptr(), table.shape
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            cache = bc.PagedCache(B, Hq, Hkv, d, B, 16, 1 << 16, dev, table=table)
+            cache.append(x, pos, none)
+            stream.synchronize()
+            torch.cuda._sleep(20_000_000)
+            call(cache, kind)
+        del cache, table
+        other = torch.empty(size, dtype=torch.int32, device=dev)
+        assert not stream.query() and other.data_ptr() != at, kind
+        stream.synchronize()
+
+
 def test_an_empty_cache_of_zeros(dev):
     both = Both(dev, 2, 8, 2, 128, 16, 400)
     both.append([300, 5], packed=both.packed(305) * 0)

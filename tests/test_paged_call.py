@@ -75,3 +75,28 @@ def test_cache_hands_the_library_its_tensors(monkeypatch, native):
     assert got[:8] == [C.addressof(cache.shape), C.addressof(cache._c), 2, 0, 1, q.data_ptr(), out.data_ptr(), active.data_ptr()] and got[9] == 48
     assert cache._c.max_len == 70
     assert [getattr(cache._c, n) for n in ("k", "v", "k_scale", "v_scale", "table", "len", "err")] == [t.data_ptr() for t in cache._own()[:7]]
+
+
+@pytest.mark.parametrize("at_home", [True, False])
+def test_a_given_table_is_noted_at_every_call(monkeypatch, at_home):
+    # (it may come from another stream than the cache's, whose own tensors are noted where a call is on another one)
+    bc.load()
+    noted = []
+    table = torch.zeros(2, 4, dtype=torch.int32)
+    caches = [bc.PagedCache(2, 4, 1, 64, 9, 32, 4, "cpu", table=t) for t in (table, None)]
+    monkeypatch.setattr(bc, "_current_device", lambda: None)
+    monkeypatch.setattr(bc, "_stream_ptr", lambda: 7)
+    monkeypatch.setattr(bc, "_used_here", lambda *t: noted.extend(x for x in t if x is not None))
+    monkeypatch.setattr(bc, "_paged_calls", None)
+
+    class Library:
+        bc_paged_workspace_bytes = staticmethod(lambda *a: 48)
+        bc_paged_attend = staticmethod(lambda *a: bc.BC_OK)
+
+    monkeypatch.setattr(bc, "_lib", Library())
+    for cache, given in zip(caches, (True, False)):
+        cache._home = 7 if at_home else 8
+        del noted[:]
+        cache.attend(torch.zeros(2, 4, 64, dtype=torch.bfloat16))
+        assert any(x is cache.table for x in noted) == (given or not at_home)
+        assert any(x is cache.lengths for x in noted) == (not at_home)
