@@ -408,8 +408,8 @@ def to_device(x, dtype: str, device):
 _torch_c = _torch_stream = None       # torch._C and torch.Stream, once a call has used the device
 
 
-def _stream_ptr():
-    """torch's current stream of the current device, as a number (0.2 us; by way of
+def _stream_ptr(device=None):
+    """torch's current stream of the current device (or the one given, its index), as a number (0.2 us; by way of
     torch.cuda.current_stream() 3 us, a third of a small decode step's call)."""
     global _torch_c, _torch_stream
     if _torch_c is None:
@@ -417,7 +417,7 @@ def _stream_ptr():
         torch.cuda.current_stream()                # (initialises the device if nothing has)
         _torch_stream = torch.Stream
         _torch_c = torch._C
-    return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice())
+    return _torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice() if device is None else device)
 
 
 def _current_device():
@@ -771,7 +771,12 @@ class PagedCache:
         self._arrivals = torch.zeros(self.B * self.Hkv, dtype=torch.int32, device=device)
         self._c = bc_pages(*(t.data_ptr() for t in self._own()), self.pages, self.page_rows, self.table_pages, 0)
         self._refs = C.byref(self.shape), C.byref(self._c)
-        self._home = _stream_ptr() if self.device.type == "cuda" else None
+        self._home = self._home_stream(self.device)
+
+    @staticmethod
+    def _home_stream(device):
+        """The stream that what is allocated on the device now belongs to: that device's, whichever is the current one."""
+        return _stream_ptr(device.index) if device.type == "cuda" else None
 
     def _noted(self, stream, *tensors):
         """Notes on the call's stream what may be freed behind it: the caller's tensors, a table among them, and off the cache's own stream all that it owns."""

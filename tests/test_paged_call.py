@@ -100,3 +100,21 @@ def test_a_given_table_is_noted_at_every_call(monkeypatch, at_home):
         cache.attend(torch.zeros(2, 4, 64, dtype=torch.bfloat16))
         assert any(x is cache.table for x in noted) == (given or not at_home)
         assert any(x is cache.lengths for x in noted) == (not at_home)
+
+
+def test_the_home_of_a_cache_is_its_devices_stream(monkeypatch):
+    # built while another device is the current one: that device's current stream is a stranger's (torch's side stands in)
+    class Torch:
+        _cuda_getDevice = staticmethod(lambda: 0)
+        _cuda_getCurrentRawStream = staticmethod(lambda device: 100 + device)
+
+    monkeypatch.setattr(bc, "_torch_c", Torch())
+    monkeypatch.setattr(bc, "load", lambda: None)
+    monkeypatch.setattr(bc, "_is", lambda *a: None)
+
+    class Pool(torch.Tensor):                              # (host memory that says it is on the second device)
+        device = torch.device("cuda", 1)
+
+    full = torch.full
+    monkeypatch.setattr(torch, "full", lambda *a, **kw: full(*a, **kw).as_subclass(Pool))
+    assert bc.PagedCache(2, 4, 1, 64, 9, 32, 4, "cpu", table=torch.zeros(2, 4, dtype=torch.int32))._home == 101
