@@ -798,7 +798,11 @@ struct AttendLaunch {
 // read again.  512 rows over 7680, 32/8 heads, in three, four, five parts 135, 115, 153 us.  One round of workgroups at most, and so:
 //   69 x 15 rows over 1400-27,900, 14/2 heads, d = 64   237, 184     8 x 50-500 over 300-20,000, 12/2   555, 438     9 x 256 over 4000, 32/8   298, 273
 //   the same, all over 27,900                           270, 258     3 x 400 over 6000, 32/8            208, 190     20 x 64 over 3000, 32/8   119, 119 (ends of three tiles: 132)
+// Where a call fills the chip several times over, another part saves little of its time and takes as much memory as its outputs
+// (17 x 8200 rows, 32/8 heads, over a table of 2^20 entries: 7 GB in three parts for 0.8 % of the count above): no more parts
+// than 256 MB hold, seven for 2048 rows of 32 heads, two for three rounds of workgroups.
 constexpr int kMostParts = 16, kManyGroups = 512;
+constexpr int64_t kPartBytes = 256 << 20;
 constexpr double kEndTiles = 5, kFoldTiles = 0.012;
 constexpr int64_t kStreamBytes = 96 << 20;
 AttendLaunch plan_attend(const bc_shape* sh, int64_t rows, int64_t max_new, int64_t max_len) {
@@ -820,7 +824,8 @@ AttendLaunch plan_attend(const bc_shape* sh, int64_t rows, int64_t max_new, int6
   a.blocks = (int)((columns + kManyColumns - 1) / kManyColumns);
   const int64_t groups = pairs * a.blocks;
   double least = 0;
-  for (int64_t parts = 1; parts <= kMostParts && (parts == 1 || parts <= tiles / 8); ++parts) {
+  const int64_t part_bytes = rows * sh->Hq * (sh->d + 2) * 4;
+  for (int64_t parts = 1; parts <= kMostParts && (parts == 1 || (parts <= tiles / 8 && parts * part_bytes <= kPartBytes)); ++parts) {
     const double rounds = (double)((groups * parts + kManyGroups - 1) / kManyGroups), fold = parts > 1 ? kFoldTiles * (double)(groups * parts) : 0;
     const double cost = rounds * ((double)tiles / 2 / (double)parts + kEndTiles) + fold;
     if (parts == 1 || cost < least) { least = cost; a.parts = (int)parts; }

@@ -92,6 +92,18 @@ def test_workspace_goes_by_the_rows_there_are():
             assert 16 <= got <= max(alone, 16) * (n + B - 1) / n + 64, (B, n, d, got, alone)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_workspace_has_an_end(d):
+    # parts are worth their memory where a call does not fill the chip; chunks of thousands of rows, also over a table that could hold far more than they need
+    for B, n, longest in ((5, 8200, 131072), (2, 4097, 1 << 20), (17, 8200, 1 << 20), (81, 6028, 1 << 20), (1, 1 << 20, 1 << 20), (512, 4096, 1 << 26), (4, 2048, 30000),
+                          (1, 512, 7680), (69, 15, 27900), (1 << 20, 1, 1 << 20), (300, 9, 1 << 20)):
+        for Hq, Hkv in ((32, 8), (12, 2), (4, 1), (7, 7)):
+            got = bc.bc_paged_workspace_bytes(shape(Hq, Hkv, d, B=B), B * n, n, longest)
+            assert 16 <= got <= (256 << 20) + 16, (B, n, longest, Hq, Hkv, got)
+    # (512 rows over 7680 in four parts, as measured)
+    assert bc.bc_paged_workspace_bytes(shape(32, 8, 128, B=1), 512, 512, 7680) == 4 * 512 * 32 * 130 * 4 + 16
+
+
 def test_struct_layout_matches_the_header(tmp_path):
     import os
     import shutil
