@@ -472,8 +472,9 @@ typedef struct {
  * What is not finite is stored as a NaN and does not count for the scale.  Bytes behind the last entry stay as they were.
  * A sequence that is not active or has no rows is left alone, and its rows of q with it; so is one with an invalid span, length, keep (0 .. len) or page, which sets
  * the state bit, and one that its row of the table cannot hold, which sets the capacity bit.  A page that is written to belongs to one sequence, and stands once in its
- * row of the table (shared pages are whole ones in front of it).  positions may be len itself where row_offsets is NULL; otherwise nothing that the call reads overlaps what it writes.  Calls that share arrivals must not overlap in time.  No limits beyond bc_qk_norm_rope's but B * Hkv <= 2^23, fewer than 2^31 rows, blocks of 16 in a pool (of a head) and
- * entries in a table's row. */
+ * row of the table (shared pages are whole ones in front of it).  positions may be len itself where row_offsets is NULL; otherwise nothing that the call reads overlaps what it writes.  Calls that share arrivals must not overlap in time.  No limits beyond bc_qk_norm_rope's but B * Hkv <= 2^23, fewer than 2^31 rows, blocks of 16 in a pool (of a head),
+ * entries in a table's row, and workgroups, B * (min(rows, max_new) / 16 + 2) of them at most (beyond: BC_ERR_SHAPE).  Those without rows cost time too: max_new is worth
+ * being the longest span. */
 int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t rows, const int64_t *row_offsets,
                         int32_t max_new, const void *qkv, int64_t qkv_row_stride, const int32_t *positions,
                         const float *inv_freq, int32_t rot, const void *q_weight, const void *k_weight, float eps,
@@ -487,6 +488,7 @@ int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t ro
  * state bit and is left alone; one with an invalid page for its entries sets the state bit, nothing is read out of range, and its rows of out are unspecified.
  * What is not finite shows in the rows that see it and nowhere else: a row of a head is NaN throughout for a key or its own query, for a value at its element at least and throughout at
  * most.  Scores, in log2, are smaller than 1e29.  What lies behind the last entry may be anything.  No atomics on results: they are reproducible.
+ * Fewer than 2^31 workgroups: with more than 32 columns (rows times query heads of a KV head) B * Hkv for every 128 that max_new makes (beyond: BC_ERR_SHAPE), so it is worth being the longest span here too.
  * workspace: bc_paged_workspace_bytes() of the call's rows and max_new and of pages' max_len (table_pages * page_rows where that is 0 or more); 16-byte aligned, no initialisation.  Calls that share workspace or arrivals must not overlap in time. */
 size_t bc_paged_workspace_bytes(const bc_shape *shape, int64_t rows, int32_t max_new, int32_t max_len);
 int32_t bc_paged_attend(const bc_shape *shape, const bc_pages *pages, int64_t rows, const int64_t *row_offsets,

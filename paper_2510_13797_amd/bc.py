@@ -815,7 +815,8 @@ class PagedCache:
     def append(self, qkv, positions, inv_freq, row_offsets=None, max_new=None, q_weight=None, k_weight=None, eps=1e-6, keep=None,
                active=None, q=None):
         """bc_paged_append: qkv [rows, (Hq + 2 Hkv) d] (rows may lie apart), positions [rows] int32, inv_freq [rot / 2] fp32, weights [d] or None, keep [B]
-        int32 or None, active [B] uint8 or None.  row_offsets [B + 1]: None (a row a sequence), host integers, or an int64 device tensor with max_new, the longest span.
+        int32 or None, active [B] uint8 or None.  row_offsets [B + 1]: None (a row a sequence), host integers, or an int64 device tensor with max_new, the longest span
+        (None: rows, and every sequence is dealt workgroups for as many: slow where there are many of both).
         Returns q [rows, Hq, d] bf16 (rows of sequences that take no part: as they were, in a new tensor unspecified)."""
         torch, dev = self.torch, self.device
         if dev.index != _current_device():                     # the stream is that device's

@@ -5,6 +5,7 @@
 // and a word of values holds the four keys that a lane has weights of: neither goes through LDS, and nothing is transposed.
 #pragma once
 #include "bc_common.h"
+#include "bc_paged_grid.h"
 
 namespace bc {
 

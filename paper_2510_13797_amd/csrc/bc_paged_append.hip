@@ -34,7 +34,8 @@ struct AppendParams {
   float* vs;
   int32_t Hq, Hkv, half;
   int32_t* arrivals;           // [B * Hkv] zero between launches
-  uint32_t blocks, turns;      // block kernel: blocks of a sequence, workgroups of a block,
+  uint32_t base;               // block kernel: the launch's first workgroup,
+  uint32_t blocks, turns;      // blocks of a sequence, workgroups of a block,
   int32_t kv_turns, kv_share;  // those that share its keys and values, and heads of either that each has;
   int32_t q_from, q_share;     // the first one that has queries, and heads that each has
   float eps;
@@ -109,8 +110,8 @@ __global__ void __launch_bounds__(2 * D, Elem<T>::size == 2 ? 5 : 4) paged_appen
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES, U = 4;
   __shared__ float s_most[U][kPagedBlock];
   const int lane = threadIdx.x % LPH, mine = threadIdx.x / LPH;      // a row of the block
-  const uint32_t of_sequence = p.blocks * p.turns;
-  const int s = blockIdx.x / of_sequence, at_block = blockIdx.x - s * of_sequence, j = at_block / p.turns, turn = at_block - j * p.turns;
+  const uint32_t of_sequence = p.blocks * p.turns, id = p.base + blockIdx.x;
+  const int s = id / of_sequence, at_block = id - s * of_sequence, j = at_block / p.turns, turn = at_block - j * p.turns;
   const AppendPlan plan = append_plan(p, s, threadIdx.x & 63, at_block == 0 && threadIdx.x < 64);
   if (plan.n == 0) return;
   const int start = plan.start, end = start + plan.n;
@@ -358,9 +359,12 @@ void launch_append(AppendParams& p, int64_t rows, hipStream_t s) {
     paged_append_one_kernel<T, D, NORM><<<p.t.B, 64 * (tasks < 16 ? tasks : 16), 0, s>>>(p);
     return;
   }
-  const unsigned grid = (unsigned)((int64_t)p.t.B * p.blocks * p.turns);
-  if (rows * (p.Hq + 2 * (int64_t)p.Hkv) * D * Elem<T>::size > (256LL << 20)) paged_append_kernel<T, D, NORM, true><<<grid, 2 * D, 0, s>>>(p);
-  else paged_append_kernel<T, D, NORM, false><<<grid, 2 * D, 0, s>>>(p);
+  const bool past = rows * (p.Hq + 2 * (int64_t)p.Hkv) * D * Elem<T>::size > (256LL << 20);
+  in_launches((int64_t)p.t.B * p.blocks * p.turns, 2 * D, [&](uint32_t base, unsigned groups) {
+    p.base = base;
+    if (past) paged_append_kernel<T, D, NORM, true><<<groups, 2 * D, 0, s>>>(p);
+    else paged_append_kernel<T, D, NORM, false><<<groups, 2 * D, 0, s>>>(p);
+  });
 }
 template <typename T>
 void launch_append(AppendParams& p, int64_t rows, int d, hipStream_t s) {

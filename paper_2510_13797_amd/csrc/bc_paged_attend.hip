@@ -36,7 +36,8 @@ struct AttendParams {
   float2* part_ml;             // [parts][rows * Hq] their maximum (log2) and sum
   int32_t Hq, Hkv, g, max_len;
   uint32_t max_chunks, chunk_tiles;     // few columns
-  int32_t blocks, parts;       // many: workgroups along a pair's columns, parts of its entries
+  int32_t blocks, parts;       // many: workgroups along a pair's columns, parts of its entries,
+  uint32_t base;               // the launch's first workgroup
   float qs;                    // scale * log2 e
 };
 
@@ -482,7 +483,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   __shared__ __attribute__((aligned(8))) uint16_t s_no_number[2][kManyWaves];      // entries with a value that is no number
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const uint32_t pairs = (uint32_t)p.t.B * p.Hkv;
-  uint32_t id = blockIdx.x;
+  uint32_t id = p.base + blockIdx.x;
   const int pair = id % pairs; id /= pairs;
   const int part = id % p.parts, block = p.blocks - 1 - id / p.parts;          // (the longest ones first)
   const int s = pair / p.Hkv, kvh = pair - s * p.Hkv;
@@ -743,8 +744,9 @@ template <int D>
 __global__ void __launch_bounds__(256) paged_fold_kernel(AttendParams p) {
   constexpr int UNITS = D / 4, PER = 256 / UNITS;
   const int64_t pairs = (int64_t)p.t.B * p.Hkv;
-  const int pair = blockIdx.x % pairs, s = pair / p.Hkv, kvh = pair - s * p.Hkv;
-  const int c = (int)(blockIdx.x / pairs) * PER + threadIdx.x / UNITS, unit = threadIdx.x % UNITS;
+  const uint32_t id = p.base + blockIdx.x;
+  const int pair = id % pairs, s = pair / p.Hkv, kvh = pair - s * p.Hkv;
+  const int c = (int)(id / pairs) * PER + threadIdx.x / UNITS, unit = threadIdx.x % UNITS;
   const AttendSpan span = attend_span(p, s);
   const int columns = span.n * p.g;
   if (c >= columns) return;
@@ -847,20 +849,23 @@ void launch_few(const AttendParams& p, const AttendLaunch& a, hipStream_t s) {
   else paged_few_kernel<D, CT, NW, false><<<groups, 64 * NW, 0, s>>>(p);
 }
 template <int D>
-void launch_attend(const AttendParams& p, const AttendLaunch& a, hipStream_t s) {
+void launch_attend(AttendParams& p, const AttendLaunch& a, hipStream_t s) {
   if (a.ct) {
     if (a.ct == 1) { if (a.waves == 8) launch_few<D, 1, 8>(p, a, s); else launch_few<D, 1, 4>(p, a, s); }
     else { if (a.waves == 8) launch_few<D, 2, 8>(p, a, s); else launch_few<D, 2, 4>(p, a, s); }
     return;
   }
-  const int64_t pairs = (int64_t)p.t.B * p.Hkv;
-  const unsigned groups = (unsigned)(pairs * a.blocks * a.parts);
-  if ((int64_t)p.t.max_new * p.g <= kManyColumns / 2) paged_many_kernel<D, true><<<groups, 64 * kManyWaves, 0, s>>>(p);
-  else paged_many_kernel<D, false><<<groups, 64 * kManyWaves, 0, s>>>(p);
-  if (a.parts > 1) {
-    const int64_t columns = (int64_t)p.t.max_new * p.g, per = 1024 / D;
-    paged_fold_kernel<D><<<(unsigned)(pairs * ((columns + per - 1) / per)), 256, 0, s>>>(p);
-  }
+  const int64_t pairs = (int64_t)p.t.B * p.Hkv, columns = (int64_t)p.t.max_new * p.g, per = 1024 / D;
+  in_launches(pairs * a.blocks * a.parts, 64 * kManyWaves, [&](uint32_t base, unsigned groups) {
+    p.base = base;
+    if (columns <= kManyColumns / 2) paged_many_kernel<D, true><<<groups, 64 * kManyWaves, 0, s>>>(p);
+    else paged_many_kernel<D, false><<<groups, 64 * kManyWaves, 0, s>>>(p);
+  });
+  if (a.parts == 1) return;
+  in_launches(pairs * ((columns + per - 1) / per), 256, [&](uint32_t base, unsigned groups) {
+    p.base = base;
+    paged_fold_kernel<D><<<groups, 256, 0, s>>>(p);
+  });
 }
 
 int64_t longest(const bc_pages* pg) {

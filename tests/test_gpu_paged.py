@@ -746,6 +746,51 @@ def test_the_last_places_of_the_longest_table(dev):
     assert c.err.item() == bc.BC_ERRBIT_CAPACITY and c.lengths.item() == start + n
 
 
+def test_appended_by_more_workgroups_than_a_launch_takes(dev):
+    # chunks whose longest is not given: each of 512 sequences may have all 524,288 rows as far as the host knows.  One sequence's workgroups are in both launches
+    import torch
+    from paper_2510_13797_amd import bc
+    B, n, d = 512, 1024, 128
+    gen = torch.Generator(device=dev).manual_seed(1)
+    x = torch.randn(B * n, 3 * d, generator=gen, device=dev).bfloat16()
+    pos, none, off = torch.zeros(B * n, dtype=torch.int32, device=dev), torch.zeros(0, device=dev), torch.arange(0, B * n + 1, n, device=dev)
+    caches, qs = [], []
+    for how in (dict(row_offsets=off), dict(row_offsets=off, max_new=n)):
+        c = bc.PagedCache(B, 1, 1, d, B, 1024, 1, dev)
+        c.table.copy_(torch.randperm(B, generator=torch.Generator().manual_seed(2)).view(B, 1))
+        qs.append(c.append(x, pos, none, **how))
+        assert (c.lengths == n).all() and c.err.item() == 0 and (c._arrivals == 0).all()
+        caches.append(c)
+    assert torch.equal(qs[0], x.view(B * n, 3, d)[:, :1]) and torch.equal(qs[0], qs[1])
+    for a, b in zip(caches[0]._own()[:4], caches[1]._own()[:4]):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    for s in (0, 255, 256, 511):
+        K, V = caches[0].entries(s)
+        for got, lo in ((K, 1), (V, 2)):
+            exact = OP.Sequence(1, d)
+            exact.append(_np(x[s * n:s * n + n]).reshape(n, 3, d)[:, lo:lo + 1])
+            assert np.array_equal(got, exact.numbers())
+
+
+def test_attended_by_more_workgroups_than_a_launch_takes(dev):
+    # 4096 sequences, each of which may have all 65,536 rows and a table of 65,536 entries: 2^24 workgroups
+    import torch
+    from paper_2510_13797_amd import bc
+    B, n, Hq, d = 4096, 16, 8, 64
+    c = bc.PagedCache(B, Hq, 1, d, B, 16, 4096, dev)
+    c.table[:, 0] = torch.randperm(B, device=dev)
+    gen = torch.Generator(device=dev).manual_seed(1)
+    x = torch.randn(B * n, (Hq + 2) * d, generator=gen, device=dev).bfloat16()
+    off = torch.arange(0, B * n + 1, n, device=dev)
+    q = c.append(x, torch.zeros(B * n, dtype=torch.int32, device=dev), torch.zeros(0, device=dev), row_offsets=off, max_new=n)
+    out = c.attend(q, row_offsets=off)
+    assert c.err.item() == 0 and torch.equal(out, c.attend(q, row_offsets=off, max_new=n, max_len=64))
+    for s in (0, 1, 2047, 2048, 4095):
+        K, V = c.entries(s)
+        for i in (0, 7, 15):
+            assert np.abs(_np(out[s * n + i]) - OA.decode_attention(_np(q[s * n + i]), K[:i + 1], V[:i + 1], d ** -0.5)).max() <= TOL
+
+
 def test_a_generation_with_beacons(dev):
     # Alg. 1 over pages: prompts, tokens, and a beacon in the place of every full window (its own attention over the window first), ratios 4 and 7
     both = Both(dev, 3, 12, 2, 128, 16, 80)
