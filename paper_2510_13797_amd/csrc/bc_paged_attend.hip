@@ -101,6 +101,13 @@ constexpr float kLevelMost = 16384.f, kLevelStart = 0x1p127f;
 __device__ __forceinline__ float level_for(float largest) {      // 2^8 over it, as a power of two (up to 2^127)
   return __uint_as_float(min(254u, 254u + 8u - (__float_as_uint(largest) >> 23)) << 23);
 }
+// What a reference that moves up by `by` (log2, a whole number, or anything beyond 2^23) does to them: the level goes up with it, as far as it goes; from there on the sums come down by the factor that is
+// returned, to nothing where there are none yet.  (By exponents: as a product level and move may pass what 32 bits hold where neither does.)
+__device__ __forceinline__ float raise_level(float& level, float by) {
+  const float up = (float)((int)(__float_as_uint(level) >> 23) - 127) + by, most = fminf(up, 127.f);
+  level = __uint_as_float((uint32_t)(127 + (int)most) << 23);
+  return fast_exp2(most - up);
+}
 __device__ __forceinline__ f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -257,15 +264,13 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
           top = rows_allreduce_max(top);
           const float to = top > m[ct] + (CT == 1 ? 0.f : kLazy) ? ceilf(top) : m[ct];
           if (!__any(to > m[ct])) return;
-          const float up = level[ct] * fast_exp2(to - m[ct]);
+          const float down = raise_level(level[ct], to - m[ct]);
           l[ct] *= fast_exp2(m[ct] - to);
           m[ct] = to;
-          if (!(up <= kLevelStart)) {        // (as high as it goes: the sums come down instead, to nothing where there are none yet)
-            const float down = kLevelStart / up;
+          if (down != 1.f) {
 #pragma unroll
             for (int j = 0; j < 4 * H; ++j) o[ct][j] *= down;
           }
-          level[ct] = fminf(up, kLevelStart);
         };
         // With two tiles of columns vector work counts: the maximum is formed only where weights get large (38.7 -> 35.3 us for 16 x 1-8 rows over 900 to 6000,
         // 32/8 heads).  With one, a wave's two or three tiles would pay for forming the first one's weights twice.
@@ -655,14 +660,12 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 #pragma unroll
           for (int e = 0; e < 16; ++e) top = fmaxf(top, 32 * x + 8 * (e >> 2) + (e & 3) < there ? sc[x][e] * p.qs : kNegBig);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float to = top > m + kLazy ? ceilf(top) : m, was = fast_exp2(m - to), up = level * fast_exp2(to - m);
+        const float to = top > m + kLazy ? ceilf(top) : m, was = fast_exp2(m - to), down = raise_level(level, to - m);
         m = to; l *= was;
-        if (!(up <= kLevelStart)) {            // (as high as it goes: the sums come down instead, to nothing where there are none yet)
-          const float down = kLevelStart / up;
+        if (down != 1.f) {
 #pragma unroll
           for (int j = 0; j < NJ; ++j) O[j] *= down;
         }
-        level = fminf(up, kLevelStart);
         weights();
       }
       l += psum;

@@ -716,6 +716,72 @@ def test_places_beyond_32_bits(dev):
     assert c.err.item() == 0
 
 
+# ------------------------------------------------------------------ ends of the range
+def _weighed(dev, n, d, before, z, values, new_z, new_values, page=16, Hq=4, Hkv=2, scale=np.log(2.0)):
+    """A cache whose entries have the scores z (log2, exact in e4m3; under a query of ones at element 0) and the values `values` [entries, d], and n new rows a
+    sequence with new_z and new_values [row]; -> (what attend gives, as float64, the weights' products [sequence][row] -> [entry, Hkv, d] in 64 bits, and the largest product of a
+    weight and its block's value scale [sequence][row] -> [Hkv])."""
+    import torch
+    both = Both(dev, len(n), Hq, Hkv, d, page, max(b + m for b, m in zip(before, n)))
+    both.c.shape.scale = scale
+
+    def rows(count, score, value):
+        x = torch.zeros(count, Hq + 2 * Hkv, d, device=dev, dtype=torch.float64)
+        x[:, Hq:Hq + Hkv, 0] = torch.as_tensor(np.asarray(score), device=dev)[:, None]
+        x[:, Hq + Hkv:] = torch.as_tensor(np.asarray(value), device=dev)[:, None]
+        return x.view(count, -1).to(both.dtype)
+
+    both.append(before, packed=torch.cat([rows(b, z(np.arange(b)), values(np.arange(b))) for b in before]))
+    both.append(n, packed=torch.cat([rows(m, new_z(np.arange(m)), new_values(np.arange(m))) for m in n]))
+    q = torch.zeros(sum(n), Hq, d, device=dev, dtype=torch.bfloat16)
+    q[:, :, 0] = 1.0
+    off = np.concatenate([[0], np.cumsum(n)])
+    got = _np(both.c.attend(q, row_offsets=off))
+    qs, products = float(np.float32(np.float32(scale) * np.float32(1.4426950408889634))), []
+    heaviest = []
+    for s in range(len(n)):
+        K, V = both.k[s].numbers(), both.v[s].numbers()
+        products.append([]), heaviest.append([])
+        for i in range(n[s]):
+            e = before[s] + i + 1
+            t = qs * K[:e, :, 0]
+            w = np.exp2(t - t.max(axis=0))
+            w /= w.sum(axis=0)
+            products[-1].append(w[:, :, None] * V[:e])
+            heaviest[-1].append((w * np.repeat(both.v[s].scales, 16, axis=1)[:, :e].T).max(axis=0))
+    assert both.c.err.item() == 0
+    return got, off, products, heaviest
+
+
+def _close(got, off, products, heaviest, least=2e-38):
+    """Outputs within 1e-4 of the sum of their products' magnitudes: scores of up to 128 that are off by 2^-24 make weights that are off by 1e-5, halves in two parts 2^-22; and
+    `least`, what 32 bits hold at their end; and what halves hold at theirs: a weight's product with its block's scale is in steps of 2^-24 where the largest sum of up to eight weights
+    times their block's scale came to 2^8 or more, so it is off by half of a step, 2^-25 / 2^5 of the largest product of one weight and a scale, and its entry by 448 times that."""
+    for s, rows in enumerate(products):
+        for i, p in enumerate(rows):
+            for h in range(got.shape[1]):
+                kvh = h // (got.shape[1] // p.shape[1])
+                x = p[:, kvh]
+                steps = np.count_nonzero(x, axis=0) * 448 * 2.0 ** -30 * heaviest[s][i][kvh]
+                assert (np.abs(got[off[s] + i, h] - x.sum(axis=0)) <= 1e-4 * np.abs(x).sum(axis=0) + steps + least).all(), (s, i, h)
+
+
+MANY_ROWS = [[1, 2], [6, 8], [20, 31], [40, 66]]
+
+
+@pytest.mark.parametrize("n", MANY_ROWS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gap,size", [(104, 2.0 ** -14), (120, 1.0), (28, 1e-28)])
+@pytest.mark.parametrize("last", [0.0, 1.0])
+def test_sums_stay_where_the_reference_moves_far(dev, n, d, gap, size, last):
+    # scores 28 to 120 higher over values of zero: what was summed before is the result, small as its weights are by then.  (New rows with values make their block's scale theirs, and
+    # heavy weights of that block hide what is as small.)
+    r = np.random.default_rng(2)
+    v = size * r.standard_normal((700, d))
+    given = _weighed(dev, n, d, [600, 333], lambda j: np.where(j < 256, 0.0, float(gap)), lambda j: np.where(j[:, None] < 256, v[j], 0.0), lambda j: 0.0 * j, lambda j: last * v[j])
+    _close(*given)
+
+
 # ------------------------------------------------------------------ together
 def test_the_last_places_of_the_longest_table(dev):
     # a row of the table that holds 2^31 - 1024 entries, nearly all of them in one page; new rows at its end, in a call for more of them
