@@ -97,16 +97,25 @@ __device__ __forceinline__ float no_number() {
 // The level of a column's values.  Weights times their block's value scale enter products in half precision, so what they are brought to has to go with the product: sums
 // are kept as `f` times what they are, f a power of two, so that no factor passes 2^14 and the largest came to 2^8 when f was last set.  What was small beside that is as small
 // in the result.  f starts where nothing is too large and sums are zero.
-constexpr float kLevelMost = 16384.f, kLevelStart = 0x1p127f;
-__device__ __forceinline__ float level_for(float largest) {      // 2^8 over it, as a power of two (up to 2^127)
-  return __uint_as_float(min(254u, 254u + 8u - (__float_as_uint(largest) >> 23)) << 23);
+constexpr int kLevelTop = 119;                 // log2
+constexpr float kLevelMost = 16384.f, kLevelStart = 0x1p119f;
+__device__ __forceinline__ float level_for(float largest) {      // 2^8 over it, as a power of two (up to 2^kLevelTop)
+  return __uint_as_float(min(127u + kLevelTop, 254u + 8u - (__float_as_uint(largest) >> 23)) << 23);
 }
 // What a reference that moves up by `by` (log2, a whole number, or anything beyond 2^23) does to them: the level goes up with it, as far as it goes; from there on the sums come down by the factor that is
 // returned, to nothing where there are none yet.  (By exponents: as a product level and move may pass what 32 bits hold where neither does.)
 __device__ __forceinline__ float raise_level(float& level, float by) {
-  const float up = (float)((int)(__float_as_uint(level) >> 23) - 127) + by, most = fminf(up, 127.f);
+  const float up = (float)((int)(__float_as_uint(level) >> 23) - 127) + by, most = fminf(up, (float)kLevelTop);
   level = __uint_as_float((uint32_t)(127 + (int)most) << 23);
   return fast_exp2(most - up);
+}
+// A scale times the level passes what 32 bits hold where the scale is 2^9 or more, the level high and the weights next to nothing (or none that the column sees): such a scale leaves its exponent beyond 2^8 to
+// the weights, which are 2^8 at most.
+constexpr uint32_t kFarScale = (127 + 9) << 23;                  // (bits)
+__device__ __forceinline__ float far_scale(float& scale) {
+  const uint32_t u = __float_as_uint(scale), e = max((u >> 23 & 255u), 127u + 8u) - (127u + 8u);
+  scale = __uint_as_float(u - (e << 23));
+  return __uint_as_float((127u + e) << 23);
 }
 __device__ __forceinline__ f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -242,7 +251,9 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
           if (key0 + 16 * (r >> 2) + 4 * g4 + (r & 3) >= key_lim[0]) sc[0][r >> 2][r & 3] = 2.f * kNegBig;
       }
       f16x8_v part[CT][2];
-      const float v0 = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i)), v1 = __uint_as_float(lane_value(__float_as_uint(v_scale), 2 * i + 1));
+      const uint32_t u0 = lane_value(__float_as_uint(v_scale), 2 * i), u1 = lane_value(__float_as_uint(v_scale), 2 * i + 1);
+      const float v0 = __uint_as_float(u0), v1 = __uint_as_float(u1);
+      const bool far = max(u0 & 0x7fffffffu, u1 & 0x7fffffffu) >= kFarScale;        // (by the scalar unit)
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         float w[8], sums[2], sum;
@@ -292,11 +303,17 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
           for (int j = 0; j < 4 * H; ++j) o[ct][j] *= was;
           level[ct] = to;
         }
+        float s0 = v0, s1 = v1;
+        if (__builtin_expect(far, 0)) {
+          const float f0 = far_scale(s0), f1 = far_scale(s1);
+#pragma unroll
+          for (int r = 0; r < 8; ++r) w[r] *= r < 4 ? f0 : f1;
+        }
         u32x4_t hi, lo;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           uint32_t h, x;
-          split_halves(w[2 * r], w[2 * r + 1], (r < 2 ? v0 : v1) * level[ct], h, x);
+          split_halves(w[2 * r], w[2 * r + 1], (r < 2 ? s0 : s1) * level[ct], h, x);
           hi[r] = h; lo[r] = x;
         }
         part[ct][0] = __builtin_bit_cast(f16x8_v, hi);
@@ -483,7 +500,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   constexpr int NX = HALVES ? 1 : 2, KS = D / 16, NJ = D / 32, K_BYTES = kManyTile * D * 2, STAGE = 2 * K_BYTES, BLOCK_BYTES = kPagedBlock * D;
   __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
   __shared__ float s_rest[2][kManyWaves];                        // what the conversion left of a block's key scale,
-  __shared__ int s_uneven;                                       // whether that has been anything but ones,
+  __shared__ int s_odd;                                          // 1: that has been something but ones; 2: a value scale has been beyond kFarScale
   __shared__ __attribute__((aligned(16))) float s_value[2][kManyWaves];                                 // value scales,
   __shared__ __attribute__((aligned(8))) uint16_t s_no_number[2][kManyWaves];      // entries with a value that is no number
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
@@ -548,7 +565,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
     if (lane == 0) {
       s_rest[stage][wave] = ke ? 1.f : k_scale;
       s_value[stage][wave] = v_scale;
-      if (!ke) s_uneven = 1;
+      const bool far = (__float_as_uint(v_scale) & 0x7fffffffu) >= kFarScale;
+      if (__builtin_expect(!ke || far, 0)) atomicOr(&s_odd, (ke ? 0 : 1) | (far ? 2 : 0));
     }
 #pragma unroll
     for (int x = 0; x < D / 64; ++x) {                           // rows of the block: 4 * group + (lane / 4) % 4
@@ -597,7 +615,7 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
   };
 
   fetch(cut.t0);
-  if (tid == 0) s_uneven = 0;
+  if (tid == 0) s_odd = 0;
   __syncthreads();
   put(cut.t0, 0);
   if (cut.t0 + 1 < cut.t1) fetch(cut.t0 + 1);
@@ -626,9 +644,9 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
         for (int j = 0; j < NJ; ++j) a[b & 1][j] = *reinterpret_cast<const f16x8_v*>(tile + K_BYTES + (2 * x0 + b) * (NJ * 1024) + j * 1024 + half * 512 + col * 16);
       };
       values(0);
-      const bool uneven = __builtin_amdgcn_readfirstlane(s_uneven) != 0;
+      const int odd = __builtin_amdgcn_readfirstlane(s_odd);
       // result e of sc[x]: entry 32 (x0 + x) + 8 (e / 4) + 4 half + e % 4 of the tile, of its block 2 (x0 + x) + e / 8
-      if (__builtin_expect(uneven, 0)) {
+      if (__builtin_expect(odd & 1, 0)) {
 #pragma unroll
         for (int x = 0; x < NX; ++x)
 #pragma unroll
@@ -685,6 +703,14 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
 #pragma unroll
         for (int j = 0; j < NJ; ++j) O[j] *= was;
         level = to;
+      }
+      if (__builtin_expect(odd & 2, 0)) {
+#pragma unroll
+        for (int b = 0; b < 2 * NX; ++b) {
+          const float f = far_scale(scales[b]);
+#pragma unroll
+          for (int y = 0; y < 8; ++y) pe[b >> 1][8 * (b & 1) + y] *= f;
+        }
       }
 #pragma unroll
       for (int b = 0; b < 2 * NX; ++b) {

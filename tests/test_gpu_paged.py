@@ -782,6 +782,30 @@ def test_sums_stay_where_the_reference_moves_far(dev, n, d, gap, size, last):
     _close(*given)
 
 
+@pytest.mark.parametrize("n", MANY_ROWS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gap,stretch", [(56, 1.0), (112, 1.0), (120, 1.0), (120, 1.03), (240, 1.0)])
+def test_large_values_of_little_weight_behind_zeros(dev, n, d, gap, stretch):
+    # values of thousands whose weights are 2^-56 and less, behind values of zero, whose level is as high as it goes
+    r = np.random.default_rng(3)
+    v = 3000.0 * r.standard_normal((700, d))
+    given = _weighed(dev, n, d, [600, 333], lambda j: np.where(j < 256, 0.0, -float(gap)), lambda j: np.where(j[:, None] < 256, 0.0, v[j]),
+                                  lambda j: 0.0 * j - gap, lambda j: v[j], scale=stretch * np.log(2.0))
+    _close(*given)
+
+
+@pytest.mark.parametrize("n", [[2, 3], [8, 5], [20, 31], [40, 66], [200, 130]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_large_values_that_a_row_does_not_see(dev, n, d):
+    # the first new row ends a block of zeros, those behind it have values of thousands: zeros for the one, numbers for the others
+    r = np.random.default_rng(4)
+    v = 3000.0 * r.standard_normal((700, d))
+    given = _weighed(dev, n, d, [15, 47], lambda j: 0.0 * j, lambda j: np.zeros((len(j), d)), lambda j: 0.0 * j, lambda j: np.where(j[:, None] < 1, 0.0, v[j]))
+    _close(*given)
+    got, off = given[:2]
+    assert (got[0] == 0).all() and (got[off[1]] == 0).all()
+
+
 # ------------------------------------------------------------------ together
 def test_the_last_places_of_the_longest_table(dev):
     # a row of the table that holds 2^31 - 1024 entries, nearly all of them in one page; new rows at its end, in a call for more of them
