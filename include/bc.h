@@ -484,7 +484,8 @@ int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t ro
  *   out[i,h,:] = sum_j softmax_j(scale * q[i,h,:] . K_j[kvh,:]) V_j[kvh,:],  j over entries 0 .. L - n + i.
  * One row a sequence is a decode step, a few are drafted tokens that are checked, many a chunk of a prompt.  q: [rows, Hq, d] BF16 (kv_dtype is not read);
  * out: [rows, Hq, d] fp32.  scale finite and >= 0.  Scales of blocks may be any finite numbers.  A softmax weight enters its product with
- * V in two half-precision parts: 22 bits, and at least 2^-29 of the row's largest product of a weight and its block's largest value; weights below 2^-126 of their row's largest are zero.  Sequences that are not active or have no rows are left alone, their rows of out with them; one with an invalid span, fewer entries than rows or more than max_len sets the
+ * V in two half-precision parts: 22 bits, and at least 2^-29 of the row's largest product of a weight and its block's largest value; weights below 2^-126 of their row's largest (2^-86
+ * where the row sees values beyond 2^46) may count as zero.  Sequences that are not active or have no rows are left alone, their rows of out with them; one with an invalid span, fewer entries than rows or more than max_len sets the
  * state bit and is left alone; one with an invalid page for its entries sets the state bit, nothing is read out of range, and its rows of out are unspecified.
  * What is not finite shows in the rows that see it and nowhere else: a row of a head is NaN throughout for a key or its own query, for a value at its element at least and throughout at
  * most.  Scores, in log2, are smaller than 1e29.  What lies behind the last entry may be anything.  No atomics on results: they are reproducible.

@@ -117,6 +117,18 @@ __device__ __forceinline__ float far_scale(float& scale) {
   scale = __uint_as_float(u - (e << 23));
   return __uint_as_float((127u + e) << 23);
 }
+// What waves, halves of a workgroup, parts and teams hand over: sums of weights times values, their reference and their sum of weights.  Sums of up to 2^39 may pass what 32 bits hold where their mean, the result,
+// does not: those at a level below 2^-40 (of values above 2^48 or so) are in a unit of 2^-40, for which their sum of weights is negative.  Where only some are, the others come to that unit.
+constexpr float kUnit = 0x1p-40f;
+__device__ __forceinline__ float inverse_power(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }      // 1 / x of a power of two
+__device__ __forceinline__ float unit_at(float level) { return level < kUnit ? kUnit : 1.f; }
+__device__ __forceinline__ float in_unit(float weights, float unit) { return unit < 1.f ? -weights : weights; }
+// The unit for sums of one and another (of which the least sum of weights is enough), and what brings those of `weights` to it.
+__device__ __forceinline__ float unit_for(float unit, float least_weights) { return least_weights < 0.f ? kUnit : unit; }
+__device__ __forceinline__ float to_unit(float weights, float unit) { return weights < 0.f ? 1.f : unit; }
+// The result: a sum over its weights, out of its unit.  (The hardware's reciprocal is off by 2^-23 at most, as sums of some weights are.)
+template <typename V>
+__device__ __forceinline__ V mean_of(const V& sum, float weights, float unit) { return sum * __builtin_amdgcn_rcpf(weights) * inverse_power(unit); }
 __device__ __forceinline__ f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -377,8 +389,8 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const float sum = rows_allreduce_sum(l[ct]);
-    const float f = 1.f / level[ct];
-    if (g4 == 0) { s_ml[wave][16 * ct + c16][0] = m[ct]; s_ml[wave][16 * ct + c16][1] = sum; }
+    const float unit = unit_at(level[ct]), f = unit * inverse_power(level[ct]);
+    if (g4 == 0) { s_ml[wave][16 * ct + c16][0] = m[ct]; s_ml[wave][16 * ct + c16][1] = in_unit(sum, unit); }
 #pragma unroll
     for (int h = 0; h < H; ++h)
 #pragma unroll
@@ -395,21 +407,21 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
   };
   for (int at = tid; at < own * (D / 4); at += 64 * NW) {
     const int c = at / (D / 4), x = 4 * (at % (D / 4));
-    float top = kNegBig;
+    float top = kNegBig, least = 0.f, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, s_ml[w][c][0]);
-    float sum = 0.f;
+    for (int w = 0; w < NW; ++w) { top = fmaxf(top, s_ml[w][c][0]); least = fminf(least, s_ml[w][c][1]); }
+    const float unit = unit_for(1.f, least);
     f32x4_t r{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float f = fast_exp2(s_ml[w][c][0] - top);
-      sum += f * s_ml[w][c][1];
-      r += f * *reinterpret_cast<const f32x4_t*>(&s_o[w][c][x]);
+      const float f = fast_exp2(s_ml[w][c][0] - top), l = s_ml[w][c][1];
+      sum += f * fabsf(l);
+      r += f * to_unit(l, unit) * *reinterpret_cast<const f32x4_t*>(&s_o[w][c][x]);
     }
-    if (whole) *result(c, x) = r * (1.f / sum);
+    if (whole) *result(c, x) = mean_of(r, sum, unit);
     else {
       store16_past(parts, mine + 4 * (c * D + x), r);
-      if (x == 0) store8_past(parts, mine + 4 * (COLS * D + 2 * c), top, sum);
+      if (x == 0) store8_past(parts, mine + 4 * (COLS * D + 2 * c), top, in_unit(sum, unit));
     }
   }
   if (whole) return;
@@ -429,7 +441,7 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
     constexpr int N = decltype(together)::value;             // parts that a thread asks for at once
     for (int at = tid - team * pieces; at < pieces && team < teams; at += 64 * NW) {
       const int c = at / (D / 4), x = 4 * (at % (D / 4));
-      float top = kNegBig, sum = 0.f;
+      float top = kNegBig, sum = 0.f, unit = 1.f;
       f32x4_t r{0.f, 0.f, 0.f, 0.f};
       for (uint32_t k0 = team; k0 < chunks; k0 += N * teams) {
         u32x2_v ml[N];
@@ -440,22 +452,23 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
           ml[k] = load8_past(parts, place + 4 * (COLS * D + 2 * c));
           part[k] = load16_past(parts, place + 4 * (c * D + x));
         }
-        float high = top;
+        float high = top, least = 0.f;
 #pragma unroll
-        for (int k = 0; k < N; ++k) high = fmaxf(high, __uint_as_float(ml[k][0]));
-        const float was = fast_exp2(top - high);
-        top = high; sum *= was; r *= was;
+        for (int k = 0; k < N; ++k) { high = fmaxf(high, __uint_as_float(ml[k][0])); least = fminf(least, __uint_as_float(ml[k][1])); }
+        const float was = fast_exp2(top - high), to = unit_for(unit, least);
+        top = high; sum *= was; r *= to < unit ? was * kUnit : was;
+        unit = to;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-          const float f = k0 + k * teams < chunks ? fast_exp2(__uint_as_float(ml[k][0]) - top) : 0.f;
-          sum += f * __uint_as_float(ml[k][1]);
-          r += f * part[k];
+          const float f = k0 + k * teams < chunks ? fast_exp2(__uint_as_float(ml[k][0]) - top) : 0.f, l = __uint_as_float(ml[k][1]);
+          sum += f * fabsf(l);
+          r += f * to_unit(l, unit) * part[k];
         }
       }
-      if (teams == 1) *result(c, x) = r * (1.f / sum);
+      if (teams == 1) *result(c, x) = mean_of(r, sum, unit);
       else {
         *reinterpret_cast<f32x4_t*>(&s_o[0][0][0] + (team * pieces + at) * 4) = r;
-        if (x == 0) { s_team[team * own + c][0] = top; s_team[team * own + c][1] = sum; }
+        if (x == 0) { s_team[team * own + c][0] = top; s_team[team * own + c][1] = in_unit(sum, unit); }
       }
     }
   };
@@ -466,15 +479,16 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
     __syncthreads();
     if (tid < pieces) {
       const int c = tid / (D / 4), x = 4 * (tid % (D / 4));
-      float top = kNegBig, sum = 0.f;
-      for (int k = 0; k < teams; ++k) top = fmaxf(top, s_team[k * own + c][0]);
+      float top = kNegBig, least = 0.f, sum = 0.f;
+      for (int k = 0; k < teams; ++k) { top = fmaxf(top, s_team[k * own + c][0]); least = fminf(least, s_team[k * own + c][1]); }
+      const float unit = unit_for(1.f, least);
       f32x4_t r{0.f, 0.f, 0.f, 0.f};
       for (int k = 0; k < teams; ++k) {
-        const float f = fast_exp2(s_team[k * own + c][0] - top);
-        sum += f * s_team[k * own + c][1];
-        r += f * *reinterpret_cast<const f32x4_t*>(&s_o[0][0][0] + (k * pieces + tid) * 4);
+        const float f = fast_exp2(s_team[k * own + c][0] - top), l = s_team[k * own + c][1];
+        sum += f * fabsf(l);
+        r += f * to_unit(l, unit) * *reinterpret_cast<const f32x4_t*>(&s_o[0][0][0] + (k * pieces + tid) * 4);
       }
-      *result(c, x) = r * (1.f / sum);
+      *result(c, x) = mean_of(r, sum, unit);
     }
   }
 }
@@ -734,37 +748,39 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
     __syncthreads();
   }
   l += __shfl_xor(l, 32, 64);
+  float unit = unit_at(level), f = unit * inverse_power(level);
   if constexpr (HALVES) {                                        // (all have left the last tile behind)
     float* other = reinterpret_cast<float*>(lds) + (wave & 1) * (NJ * 16 + 2) * 64 + lane;
     if (wave >= 2) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) other[(16 * j + e) * 64] = O[j][e] * (1.f / level);
-      other[NJ * 16 * 64] = m; other[(NJ * 16 + 1) * 64] = l;
+        for (int e = 0; e < 16; ++e) other[(16 * j + e) * 64] = O[j][e] * f;
+      other[NJ * 16 * 64] = m; other[(NJ * 16 + 1) * 64] = in_unit(l, unit);
     }
     __syncthreads();
     if (wave >= 2) return;
-    const float its = other[NJ * 16 * 64], top = fmaxf(m, its), f0 = fast_exp2(m - top), f1 = fast_exp2(its - top);
-    l = l * f0 + other[(NJ * 16 + 1) * 64] * f1;
+    const float its = other[NJ * 16 * 64], weights = other[(NJ * 16 + 1) * 64], top = fmaxf(m, its), f0 = fast_exp2(m - top), f1 = fast_exp2(its - top);
+    const float both = unit_for(unit, weights), u0 = both < unit ? f0 * kUnit : f0, u1 = f1 * to_unit(weights, both);
+    l = l * f0 + fabsf(weights) * f1;
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) O[j][e] = O[j][e] * (1.f / level) * f0 + other[(16 * j + e) * 64] * f1;
-    m = top; level = 1.f;
+      for (int e = 0; e < 16; ++e) O[j][e] = O[j][e] * f * u0 + other[(16 * j + e) * 64] * u1;
+    m = top; unit = both; f = 1.f;
   }
   if (mine + col >= columns) return;
   const int64_t at = (span.row + i) * p.Hq + kvh * p.g + (c - i * p.g);
   const bool whole = cut.parts == 1;
   float* to = whole ? p.out + at * D : p.part + (part * (p.t.rows * p.Hq) + at) * D;
-  const float f = 1.f / level, inv = whole ? 1.f / l : 1.f;      // (one after the other: their product may be too small)
-  if (!whole && half == 0) p.part_ml[part * (p.t.rows * p.Hq) + at] = make_float2(m, l);
+  const float mean = whole ? __builtin_amdgcn_rcpf(l) : 1.f, out = whole ? f * inverse_power(unit) : f;      // (one after the other: either may leave the range that both together keep)
+  if (!whole && half == 0) p.part_ml[part * (p.t.rows * p.Hq) + at] = make_float2(m, in_unit(l, unit));
   // result e of block j: its row 8 (e / 4) + 4 half + e % 4
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     const int row = 8 * (e >> 2) + 4 * half + (e & 3);
-    if constexpr (D == 128) *reinterpret_cast<f32x4_t*>(to + 4 * row) = f32x4_t{O[0][e] * f * inv, O[1][e] * f * inv, O[NJ - 2][e] * f * inv, O[NJ - 1][e] * f * inv};
-    else *reinterpret_cast<f32x2_v*>(to + 2 * row) = f32x2_v{O[0][e] * f * inv, O[1][e] * f * inv};
+    if constexpr (D == 128) *reinterpret_cast<f32x4_t*>(to + 4 * row) = f32x4_t{O[0][e] * mean * out, O[1][e] * mean * out, O[NJ - 2][e] * mean * out, O[NJ - 1][e] * mean * out};
+    else *reinterpret_cast<f32x2_v*>(to + 2 * row) = f32x2_v{O[0][e] * mean * out, O[1][e] * mean * out};
   }
 }
 
@@ -783,7 +799,7 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(AttendParams p) {
   const ManyCut cut = many_cut(p.parts, span.L - span.n + 1 + last_row, 0);
   if (cut.parts == 1) return;
   const int64_t at = (span.row + i) * p.Hq + kvh * p.g + (c - i * p.g), step = p.t.rows * p.Hq;
-  float top = kNegBig, sum = 0.f;
+  float top = kNegBig, sum = 0.f, in = 1.f;
   f32x4_t r{0.f, 0.f, 0.f, 0.f};
   for (int k0 = 0; k0 < cut.parts; k0 += 8) {
     float2 ml[8];
@@ -794,18 +810,19 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(AttendParams p) {
       ml[k] = p.part_ml[from];
       x[k] = *reinterpret_cast<const f32x4_t*>(p.part + from * D + 4 * unit);
     }
-    float high = top;
+    float high = top, least = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) high = fmaxf(high, ml[k].x);
-    const float was = fast_exp2(top - high);
-    top = high; sum *= was; r *= was;
+    for (int k = 0; k < 8; ++k) { high = fmaxf(high, ml[k].x); least = fminf(least, ml[k].y); }
+    const float was = fast_exp2(top - high), to = unit_for(in, least);
+    top = high; sum *= was; r *= to < in ? was * kUnit : was;
+    in = to;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const float f = k0 + k < cut.parts ? fast_exp2(ml[k].x - top) : 0.f;
-      sum += f * ml[k].y; r += f * x[k];
+      sum += f * fabsf(ml[k].y); r += f * to_unit(ml[k].y, in) * x[k];
     }
   }
-  *reinterpret_cast<f32x4_t*>(p.out + at * D + 4 * unit) = r * (1.f / sum);
+  *reinterpret_cast<f32x4_t*>(p.out + at * D + 4 * unit) = mean_of(r, sum, in);
 }
 
 struct AttendLaunch {

@@ -728,7 +728,7 @@ def _weighed(dev, n, d, before, z, values, new_z, new_values, page=16, Hq=4, Hkv
     def rows(count, score, value):
         x = torch.zeros(count, Hq + 2 * Hkv, d, device=dev, dtype=torch.float64)
         x[:, Hq:Hq + Hkv, 0] = torch.as_tensor(np.asarray(score), device=dev)[:, None]
-        x[:, Hq + Hkv:] = torch.as_tensor(np.asarray(value), device=dev)[:, None]
+        x[:, Hq + Hkv:] = torch.as_tensor(np.array(value), device=dev)[:, None]
         return x.view(count, -1).to(both.dtype)
 
     both.append(before, packed=torch.cat([rows(b, z(np.arange(b)), values(np.arange(b))) for b in before]))
@@ -804,6 +804,52 @@ def test_large_values_that_a_row_does_not_see(dev, n, d):
     _close(*given)
     got, off = given[:2]
     assert (got[0] == 0).all() and (got[off[1]] == 0).all()
+
+
+@pytest.mark.parametrize("n", MANY_ROWS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("before", [[600, 333], [9000, 17]])
+@pytest.mark.parametrize("size", [1e36, 3e37])
+def test_sums_beyond_the_range_of_results_within(dev, n, d, before, size):
+    # hundreds and thousands of equal entries: the sum of the products is no number of 32 bits, their mean is one
+    v = np.where(np.arange(d) % 3 == 1, -size, size)
+    given = _weighed(dev, n, d, before, lambda j: (j % 8) / 4.0, lambda j: np.broadcast_to(v, (len(j), d)), lambda j: 0.0 * j,
+                     lambda j: np.broadcast_to(v, (len(j), d)), page=64)
+    _close(*given)
+
+
+@pytest.mark.parametrize("n", MANY_ROWS)
+def test_the_largest_values(dev, n):
+    # one entry in hundreds is as large as bf16 gets (in e4m3 240 * 2^120)
+    v = np.where(np.arange(700) % 97 == 5, 240 * 2.0 ** 120, 0.0)
+    given = _weighed(dev, n, 64, [600, 333], lambda j: 0.0 * j, lambda j: np.repeat(v[j][:, None], 64, axis=1), lambda j: 0.0 * j, lambda j: np.zeros((len(j), 64)))
+    _close(*given)
+
+
+@pytest.mark.parametrize("n", MANY_ROWS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("gap,size", [(28, 1e-28), (104, 2.0 ** -14), (120, 1.0), (120, 1e30)])
+@pytest.mark.parametrize("first", [True, False])
+def test_parts_whose_references_lie_far_apart(dev, n, d, gap, size, first):
+    # parts of long sequences that hold the values, in front of or behind parts of zeros whose scores are up to 120 higher
+    r = np.random.default_rng(6)
+    v = size * r.standard_normal((9200, d))
+    low = (lambda j: j < 4096) if first else (lambda j: j >= 4096)
+    given = _weighed(dev, n, d, [9000, 5000], lambda j: np.where(low(j), 0.0, float(gap)), lambda j: np.where(low(j)[:, None], v[j], 0.0), lambda j: 0.0 * j,
+                     lambda j: 0.0 * v[j] if first else v[j], page=64)
+    _close(*given)
+
+
+@pytest.mark.parametrize("n", MANY_ROWS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [1e-33, 1.0, 3e37])
+@pytest.mark.parametrize("at", [100, 4000, 8990])
+def test_one_heavy_entry_among_thousands(dev, n, d, size, at):
+    # the largest weight is alone in its wave and part, thousands of entries 2^-20 of it each lie in others: neither side's share of the other's sums leaves the range
+    r = np.random.default_rng(10)
+    v = size * r.uniform(0.5, 1.5, (9200, d)) * np.where(np.arange(d) % 2, 1.0, -1.0)
+    given = _weighed(dev, n, d, [9000, 5000], lambda j: np.where(j == at, 20.0, 0.0), lambda j: v[j], lambda j: 0.0 * j, lambda j: v[j], page=64)
+    _close(*given)
 
 
 # ------------------------------------------------------------------ together
