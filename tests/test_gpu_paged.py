@@ -452,6 +452,40 @@ def test_scales_of_any_kind(dev, n, d):
     both.check_attend(q, n)
 
 
+def _two_bf16_parts(w):
+    """What two bf16 parts hold of w (rounded to nearest): 17 bits."""
+    def bf16(x):
+        u = np.float32(x).view(np.uint32).astype(np.uint64)
+        return ((u + 0x7fff + (u >> 16 & 1)) >> 16 << 16).astype(np.uint32).view(np.float32).astype(np.float64)
+    hi = bf16(w)
+    return hi + bf16(w - hi)
+
+
+@pytest.mark.parametrize("n", [[1], [7], [20], [66], [300]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_have_22_bits(dev, n, d):
+    # entries that are all alike, with values of one: the result is what a weight's parts hold of it, sum over sum.  Two half-precision parts are off by 2^-23, the reciprocal by 2^-23, the sum of
+    # weights by 2^-24 at each of 11 steps (eight of a lane 3, lanes 2, blocks and tiles 6), the matrix product's by 2^-24 of what is summed so far at each of up to 44 entries, 22 * 2^-24.  Two
+    # bf16 parts would be off by up to 2^-18.
+    import torch
+    tol = 37 * 2.0 ** -24
+    Hq, Hkv = 4, 2
+    both = Both(dev, 1, Hq, Hkv, d, 16, 8 + n[0])
+    both.c.shape.scale = np.log(2.0)
+    x = torch.zeros(8 + n[0], Hq + 2 * Hkv, d, device=dev, dtype=torch.bfloat16)
+    x[:, Hq:Hq + Hkv, 0] = 1.0
+    x[:, Hq + Hkv:] = 1.0
+    both.append([8], packed=x[:8].reshape(8, -1))
+    both.append(n, packed=x[8:].reshape(n[0], -1))
+    q = torch.zeros(n[0], Hq, d, device=dev, dtype=torch.bfloat16)
+    q[:, :, 0] = 3.0 * torch.rand(n[0], Hq, generator=both.gen, device=dev)
+    w = np.exp2(_np(q[:36, :, 0]))
+    off = (np.abs(_two_bf16_parts(w) - w) / w).max()
+    assert n[0] < 20 or off > 1.5 * tol
+    got = _np(both.c.attend(q, row_offsets=[0, n[0]])[:36])
+    assert np.abs(got - 1.0).max() <= tol, np.abs(got - 1.0).max()
+
+
 @pytest.mark.parametrize("n", [[1, 2], [6, 8], [20, 31], [40, 66]])
 @pytest.mark.parametrize("d", [64, 128])
 def test_values_of_very_different_sizes(dev, n, d):
