@@ -443,12 +443,18 @@ int32_t bc_sample_tokens(int32_t B, int32_t V, const void *logits, int32_t logit
                          const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
                          const float *u, const uint8_t *active, int32_t *tokens, float *logprob, void *stream);
 
-/* A cache in pages of 8-bit entries, for batches that outgrow the slabs above: half of their bytes, and pages that sequences can share (the samples of one prompt,
- * Sec. 4, have its pages in common).  A page holds page_rows entries of every KV head; entry j of sequence s is row j % page_rows of page
- * table[s * table_pages + j / page_rows].  Which pages a sequence has is the caller's business: the library reads the table and never writes it.
- *  k, v: device, pages * Hkv * page_rows * d bytes each, [pages][Hkv][page_rows / 4] groups of four entries, of the keys [d / 64][4][64] bytes and of the values [d][4],
- *  in e4m3 (OCP: no infinities, largest 448).  k_scale, v_scale: device fp32 [pages][Hkv][page_rows / 16]: a value is its byte's times the scale of its block of 16 entries.
- * Beacons, windows and prompts are the caller's too: a beacon takes the place of its window by bc_paged_append with keep. */
+/* A cache in pages of 8-bit entries, for batches that outgrow the slabs above: half of their bytes, and
+ * pages that sequences can share (the samples of one prompt, Sec. 4, have its pages in common).
+ * A page holds page_rows entries of every KV head; entry j of sequence s is row j % page_rows of page
+ * table[s * table_pages + j / page_rows].  Which pages a sequence has is the caller's business: the
+ * library reads the table and never writes it.
+ *   k, v: device, pages * Hkv * page_rows * d bytes each, in e4m3 (OCP: no infinities, largest 448):
+ *   [pages][Hkv][page_rows / 4] groups of four entries, of the keys [d / 64][4][64] bytes and of the
+ *   values [d][4].
+ *   k_scale, v_scale: device fp32 [pages][Hkv][page_rows / 16]: a value is its byte's times the scale of
+ *   its block of 16 entries.
+ * Beacons, windows and prompts are the caller's too: a beacon takes the place of its window by
+ * bc_paged_append with keep. */
 typedef struct {
   void *k, *v;             /* 16-byte aligned                                       */
   float *k_scale, *v_scale;
@@ -462,35 +468,60 @@ typedef struct {
   int32_t max_len;         /* no sequence that attends is longer (sizes grid and workspace); 0: table_pages * page_rows */
 } bc_pages;
 
-/* Rows of a layer's packed projections as new entries, in one pass: the norms and the rotation of bc_qk_norm_rope (same qkv, positions, inv_freq, rot, weights and eps;
- * shape's kv_dtype is their type), the queries to q [rows, Hq, d] in BF16 whatever the type (NULL: not wanted), keys and values into the pages.
- * Sequence s's new rows are [row_offsets[s], row_offsets[s+1]) (row_offsets: DEVICE [B + 1], spans within [0, rows) and of at most max_new rows, a HOST value; NULL: row s,
- * with rows == B and max_new 1).  They become entries start, start + 1, ... and len[s] = start + their number, where start = len[s], or keep[s] where keep (device [B], NULL: none)
- * is given: entries from keep[s] on are dropped (a beacon's window, drafted tokens that were not accepted).
- * The scale of a block is the least power of two s >= 2^-120 with |x| <= 448 s for every x written to it since its first entry: it grows with its entries (those that stay
- * are rounded again: exact but for magnitudes below 2^-6 of their new scale) and starts anew with a first one.  The scale of a block that holds entries has to be such a power of two.
- * What is not finite is stored as a NaN and does not count for the scale.  Bytes behind the last entry stay as they were.
- * A sequence that is not active or has no rows is left alone, and its rows of q with it; so is one with an invalid span, length, keep (0 .. len) or page, which sets
- * the state bit, and one that its row of the table cannot hold, which sets the capacity bit.  A page that is written to belongs to one sequence, and stands once in its
- * row of the table (shared pages are whole ones in front of it).  positions may be len itself where row_offsets is NULL; otherwise nothing that the call reads overlaps what it writes.  Calls that share arrivals must not overlap in time.  No limits beyond bc_qk_norm_rope's but B * Hkv <= 2^23, fewer than 2^31 rows, blocks of 16 in a pool (of a head),
- * entries in a table's row, and workgroups, B * (min(rows, max_new) / 16 + 2) of them at most (beyond: BC_ERR_SHAPE).  Those without rows cost time too: max_new is worth
- * being the longest span. */
+/* Rows of a layer's packed projections as new entries, in one pass: the norms and the rotation of
+ * bc_qk_norm_rope (same qkv, positions, inv_freq, rot, weights and eps; shape's kv_dtype is their type),
+ * the queries to q [rows, Hq, d] in BF16 whatever the type (NULL: not wanted), keys and values into the
+ * pages.
+ * Sequence s's new rows are [row_offsets[s], row_offsets[s+1]) (row_offsets: DEVICE [B + 1], spans within
+ * [0, rows) and of at most max_new rows, a HOST value; NULL: row s, with rows == B and max_new 1).  They
+ * become entries start, start + 1, ... and len[s] = start + their number, where start = len[s], or keep[s]
+ * where keep (device [B], NULL: none) is given: entries from keep[s] on are dropped (a beacon's window,
+ * drafted tokens that were not accepted).
+ * The scale of a block is the least power of two s >= 2^-120 with |x| <= 448 s for every x written to it
+ * since its first entry: it grows with its entries (those that stay are rounded again: exact but for
+ * magnitudes below 2^-6 of their new scale) and starts anew with a first one.  The scale of a block that
+ * holds entries has to be such a power of two.  What is not finite is stored as a NaN and does not count
+ * for the scale.  Bytes behind the last entry stay as they were.
+ * A sequence that is not active or has no rows is left alone, and its rows of q with it; so is one with an
+ * invalid span, length, keep (0 .. len) or page, which sets the state bit, and one that its row of the
+ * table cannot hold, which sets the capacity bit.
+ * A page that is written to belongs to one sequence, and stands once in its row of the table (shared pages
+ * are whole ones in front of it).  positions may be len itself where row_offsets is NULL; otherwise
+ * nothing that the call reads overlaps what it writes.  Calls that share arrivals must not overlap in
+ * time.
+ * No limits beyond bc_qk_norm_rope's but (else BC_ERR_SHAPE) B * Hkv <= 2^23 and fewer than 2^31 rows,
+ * blocks of 16 in a pool (of a head), entries in a table's row, and workgroups: B * (min(rows, max_new) /
+ * 16 + 2) of them at most.  Those without rows cost time too, so max_new is worth being the longest span. */
 int32_t bc_paged_append(const bc_shape *shape, const bc_pages *pages, int64_t rows, const int64_t *row_offsets,
                         int32_t max_new, const void *qkv, int64_t qkv_row_stride, const int32_t *positions,
                         const float *inv_freq, int32_t rot, const void *q_weight, const void *k_weight, float eps,
                         const int32_t *keep, const uint8_t *active, void *q, void *stream);
 
-/* Attention of the newest rows, whose keys and values are in the pages already: with L = len[s] entries and n rows of sequence s (spans as for bc_paged_append),
- *   out[i,h,:] = sum_j softmax_j(scale * q[i,h,:] . K_j[kvh,:]) V_j[kvh,:],  j over entries 0 .. L - n + i.
- * One row a sequence is a decode step, a few are drafted tokens that are checked, many a chunk of a prompt.  q: [rows, Hq, d] BF16 (kv_dtype is not read);
- * out: [rows, Hq, d] fp32.  scale finite and >= 0.  Scales of blocks may be any finite numbers.  A softmax weight enters its product with
- * V in two half-precision parts: 22 bits, and at least 2^-29 of the row's largest product of a weight and its block's largest value; weights below 2^-126 of their row's largest (2^-86
- * where the row sees values beyond 2^46) may count as zero.  Sequences that are not active or have no rows are left alone, their rows of out with them; one with an invalid span, fewer entries than rows or more than max_len sets the
- * state bit and is left alone; one with an invalid page for its entries sets the state bit, nothing is read out of range, and its rows of out are unspecified.
- * What is not finite shows in the rows that see it and nowhere else: a row of a head is NaN throughout for a key or its own query, for a value at its element at least and throughout at
- * most.  Scores, in log2, are smaller than 1e29.  What lies behind the last entry may be anything.  No atomics on results: they are reproducible.
- * Fewer than 2^31 workgroups: with more than 32 columns (rows times query heads of a KV head) B * Hkv for every 128 that max_new makes (beyond: BC_ERR_SHAPE), so it is worth being the longest span here too.
- * workspace: bc_paged_workspace_bytes() of the call's rows and max_new and of pages' max_len (table_pages * page_rows where that is 0 or more); 16-byte aligned, no initialisation.  Calls that share workspace or arrivals must not overlap in time. */
+/* Attention of the newest rows, whose keys and values are in the pages already: with L = len[s] entries
+ * and n rows of sequence s (spans as for bc_paged_append),
+ *   out[i,h,:] = sum_j softmax_j(scale * q[i,h,:] . K_j[kvh,:]) V_j[kvh,:],  j over entries 0 .. L - n +
+ *   i.
+ * One row a sequence is a decode step, a few are drafted tokens that are checked, many a chunk of a
+ * prompt.
+ *   q: [rows, Hq, d] BF16 (kv_dtype is not read); out: [rows, Hq, d] fp32.
+ *   scale: finite and >= 0.  Scales of blocks may be any finite numbers; a key scale times scale is below
+ *   2^127.  Scores, in log2, are smaller than 1e29.
+ *   A softmax weight enters its product with V in two half-precision parts: 22 bits, and at least 2^-29 of
+ *   the row's largest product of a weight and its block's largest value.  Weights below 2^-126 of their
+ *   row's largest (2^-86 where the row sees values beyond 2^46) may count as zero.
+ * Sequences that are not active or have no rows are left alone, their rows of out with them; one with an
+ * invalid span, fewer entries than rows or more than max_len sets the state bit and is left alone; one
+ * with an invalid page for its entries sets the state bit, nothing is read out of range, and its rows of
+ * out are unspecified.
+ * What is not finite shows in the rows that see it and nowhere else: a row of a head is NaN throughout for
+ * a key or its own query, for a value at its element at least and throughout at most.  What lies behind
+ * the last entry may be anything.  No atomics on results: they are reproducible.
+ * Fewer than 2^31 workgroups (else BC_ERR_SHAPE): with more than 32 columns (rows times query heads of a
+ * KV head) B * Hkv for every 128 that max_new makes, times parts of the entries, so max_new is worth being
+ * the longest span here too.
+ * workspace: bc_paged_workspace_bytes() of the call's rows and max_new and of pages' max_len (table_pages
+ * * page_rows where that is 0 or more), 256 MB at most; 16-byte aligned, no initialisation.  Calls that
+ * share workspace or arrivals must not overlap in time. */
 size_t bc_paged_workspace_bytes(const bc_shape *shape, int64_t rows, int32_t max_new, int32_t max_len);
 int32_t bc_paged_attend(const bc_shape *shape, const bc_pages *pages, int64_t rows, const int64_t *row_offsets,
                         int32_t max_new, const void *q, float *out, const uint8_t *active, void *workspace,

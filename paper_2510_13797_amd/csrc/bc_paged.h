@@ -1,8 +1,9 @@
 // The cache in pages of 8-bit entries, as its two calls see it (bc_paged_append.hip writes, bc_paged_attend.hip reads).
 //
-// An entry is a key and a value in e4m3, d bytes each, and a block of 16 entries of a head has one scale, a power of two.  Entries lie in groups of four:
-// keys [d / 64][4][64], values [d][4].  So sixteen keys of a head are the first operand of a matrix product as they come from memory, 16 bytes a lane and 256 in a row,
-// and a word of values holds the four keys that a lane has weights of: neither goes through LDS, and nothing is transposed.
+// An entry is a key and a value in e4m3, d bytes each, and a block of 16 entries of a head has one scale, a power of two.  Entries lie in
+// groups of four: keys [d / 64][4][64], values [d][4].  So sixteen keys of a head are the first operand of a matrix product as they come
+// from memory, 16 bytes a lane and 256 in a row, and a word of values holds the four keys that a lane has weights of: neither goes through
+// LDS, and nothing is transposed.
 #pragma once
 #include "bc_common.h"
 #include "bc_paged_grid.h"

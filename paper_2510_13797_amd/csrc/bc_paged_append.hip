@@ -1,17 +1,20 @@
 // bc_paged_append: rows of packed projections -> queries in bf16, and keys and values as entries of a cache in 8-bit pages (Alg. 1's "KV is updated
-// internally", "encode b" and "encode the prompt", over pages): RMS norm of the query and key heads, rotation by position, and e4m3 with a scale for each block of 16
-// entries and head.
+// internally", "encode b" and "encode the prompt", over pages): RMS norm of the query and key heads, rotation by position, and e4m3 with a
+// scale for each block of 16 entries and head.
 //
-//   y, o: as in bc_rope.hip.  Block scale s = 2^e, the least one (e >= -120) with |x| <= 448 s for every finite x written to the block since its first entry;
-//   an entry's byte is e4m3(x / s).  A block's scale only grows while it holds entries; those that stay then become e4m3(old * old s / s).
+//   y, o: as in bc_rope.hip.  Block scale s = 2^e, the least one (e >= -120) with |x| <= 448 s for every finite x written to the block
+//   since its first entry; an entry's byte is e4m3(x / s).  A block's scale only grows while it holds entries; those that stay then become
+//   e4m3(old * old s / s).
 //
-// A power of two: dividing by it is exact, so an e4m3 value keeps its bits when a block's scale grows (but for the few below 2^-6), and an entry's error is the one
-// rounding, 2^-4 of its value, that any scale would leave.
+// A power of two: dividing by it is exact, so an e4m3 value keeps its bits when a block's scale grows (but for the few below 2^-6), and an
+// entry's error is the one rounding, 2^-4 of its value, that any scale would leave.
 //
-// Bound by memory where rows are many (139,008 rows of 12/2 heads, d = 128, bf16: 1.07 GB in 186 us, 5.7 TB/s; torch's copy of 2 GiB reaches 5.1), by the latency of tables and
-// loads where they are few (24 chunks of up to 130 rows, 14/2 heads, d = 64, fp32: 8.8 us; a row of 32/8 heads: 4.2, beside 9 of the call).  Two kernels:
+// Bound by memory where rows are many (139,008 rows of 12/2 heads, d = 128, bf16: 1.07 GB in 186 us, 5.7 TB/s; torch's copy of 2 GiB
+// reaches 5.1), by the latency of tables and loads where they are few (24 chunks of up to 130 rows, 14/2 heads, d = 64, fp32: 8.8 us; a row
+// of 32/8 heads: 4.2, beside 9 of the call).  Two kernels:
 //   a block of 16 entries a workgroup (few rows: several, which share the heads), d / 8 lanes a row: the block's largest magnitude goes through LDS;
-//   one new row a sequence at most (a decode step): a workgroup a sequence, a wave for the key or the value of a head; the rest of the block is touched only where its scale grows.
+//   one new row a sequence at most (a decode step): a workgroup a sequence, a wave for the key or the value of a head; the rest of the
+//   block is touched only where its scale grows.
 #include "bc_paged.h"
 #include "bc_rope_lane.h"
 
@@ -103,8 +106,9 @@ __device__ __forceinline__ void norm_head(float (&x)[2][4], const float (&w)[2][
   for (int e = 0; e < 4; ++e) { x[0][e] *= r * w[0][e]; x[1][e] *= r * w[1][e]; }
 }
 
-// 16 rows' lanes: 256 threads, 128 for d = 64.  A block has p.turns workgroups: the first kv_turns share the heads of keys and of values, the others those of queries; one alone has all.
-// (Five waves a SIMD: 256 x 2-4 rows 29.6 us with four, 28.0.  In fp32 with norms that is two registers short.)
+// 16 rows' lanes: 256 threads, 128 for d = 64.  A block has p.turns workgroups: the first kv_turns share the heads of keys and of values,
+// the others those of queries; one alone has all.  (Five waves a SIMD: 256 x 2-4 rows 29.6 us with four, 28.0.  In fp32 with norms that is
+// two registers short.)
 template <typename T, int D, bool NORM, bool STREAM>
 __global__ void __launch_bounds__(2 * D, Elem<T>::size == 2 ? 5 : 4) paged_append_kernel(AppendParams p) {
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES, U = 4;
@@ -115,8 +119,8 @@ __global__ void __launch_bounds__(2 * D, Elem<T>::size == 2 ? 5 : 4) paged_appen
   const AppendPlan plan = append_plan(p, s, threadIdx.x & 63, at_block == 0 && threadIdx.x < 64);
   if (plan.n == 0) return;
   const int start = plan.start, end = start + plan.n;
-  // The length moves when all of the sequence's workgroups have read it, those without rows among them: counted behind the work (in front of it the loads behind the count, which
-  // come back in order, waited for its answer: 2 us).
+  // The length moves when all of the sequence's workgroups have read it, those without rows among them: counted behind the work (in front
+  // of it the loads behind the count, which come back in order, waited for its answer: 2 us).
   auto leave = [&] {
     __syncthreads();
     if (threadIdx.x != 0 || __hip_atomic_fetch_add(p.arrivals + s * p.Hkv, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (int)of_sequence - 1) return;
@@ -245,7 +249,8 @@ __global__ void __launch_bounds__(2 * D, Elem<T>::size == 2 ? 5 : 4) paged_appen
   leave();
 }
 
-// One new row at most: a workgroup a sequence, whose waves take the keys' and values' heads and then the queries' by turns, and at the end the length.
+// One new row at most: a workgroup a sequence, whose waves take the keys' and values' heads and then the queries' by turns, and at the end
+// the length.
 template <typename T, int D, bool NORM>
 __global__ void __launch_bounds__(1024) paged_append_one_kernel(AppendParams p) {
   constexpr int LPH = D / 8, ES = Elem<T>::size, HEAD = D * ES, PER = 64 / LPH;
@@ -299,7 +304,8 @@ __global__ void __launch_bounds__(1024) paged_append_one_kernel(AppendParams p) 
     const float scale = fmaxf(power_of_two(scale_exponent(most)), was), inv = inverse_of(scale);
     if (lane == 0) *scales = scale;
     if (kept && __builtin_amdgcn_readfirstlane(__float_as_uint(scale)) != __builtin_amdgcn_readfirstlane(__float_as_uint(was))) {
-      // the entries that stay: words of four bytes, of the keys one row's, of the values four rows'; stored byte by byte, those of the new row not at all
+      // the entries that stay: words of four bytes, of the keys one row's, of the values four rows'; stored byte by byte, those of the new
+      // row not at all
       const float ratio = was * inv;
       for (int i = lane; i < ((kept + 3) >> 2) * D; i += 64) {
         uint8_t* word = to + first * D + 4 * i;
@@ -332,9 +338,12 @@ __global__ void __launch_bounds__(1024) paged_append_one_kernel(AppendParams p) 
   if (threadIdx.x == 0) p.t.len[s] = start + 1;
 }
 
-// Workgroups of a block: more where there are few rows, of keys and values as of queries.  (us, 32/8 heads, bf16: keys and values all in one workgroup, and shared out)
+// Workgroups of a block: more where there are few rows, of keys and values as of queries.  (us, 32/8 heads, bf16: keys and values all in
+// one workgroup, and shared out)
 //   5 x 1-15 rows 18.0, 8.9     64 x 2-8 19.9, 13.1     1 x 2000 28.7, 19.0     256 x 2-4 27.6, 28.0
 // 1024, 1536, 2048, 4096 workgroups: 1 x 2000 rows 23.3, 28.0, 28.0, 28.0; 400 x 2-4 43.5, 39.5, 72, 80.
+// (Into empty sequences.  Behind 300 to 1500 entries, where most blocks hold some that are read and looked at again: 256 x 2-4 rows 36, 400 x
+// 2-4 65.)
 constexpr int64_t kAppendGroups = 1024;
 void deal_blocks(AppendParams& p, int64_t rows) {
   const int64_t blocks = (rows + kPagedBlock - 1) / kPagedBlock + p.t.B, of_q = p.q ? (p.Hq + 3) / 4 : 0, of_kv = (2 * (int64_t)p.Hkv + 3) / 4;      // (four heads at a time)

@@ -1,20 +1,23 @@
-// bc_paged_attend: attention of every sequence's newest rows over its entries in 8-bit pages (Sec. 2's attention; rows of a decode step, drafted tokens that are
-// checked, chunks of a prompt).
+// bc_paged_attend: attention of every sequence's newest rows over its entries in 8-bit pages (Sec. 2's attention; rows of a decode step,
+// drafted tokens that are checked, chunks of a prompt).
 //
 //   out[i, h] = sum_j softmax_j(scale q[i, h] . K_j) V_j,  j over entries 0 .. L - n + i of the L there are, n of them the rows' own
 //   K_j = key bytes * their block's scale, V_j likewise
 //
-// The query heads of a KV head see the same entries, so (row, head) pairs are the columns of the products: column i * g + h.  A tile is two blocks of 16 entries, which
-// come from memory as operands (bc_paged.h) and become bf16 or half precision by the hardware's conversions, exactly: S^T = K.Q^T by 16x16x32 MFMA, whose result has four entries of a
-// column in a lane; a word of values is those four entries of one element, so O^T += V^T.P^T takes both as they are.  A key scale that is a power of
-// two goes along with the conversion, exactly; others are factors of their block's scores.  Values become half precision without their scale, which is a factor of the
-// weights; those enter their product in two half-precision parts (22 bits) at a level that goes with the products (kLevelMost).  Softmax online, sums in fp32.
+// The query heads of a KV head see the same entries, so (row, head) pairs are the columns of the products: column i * g + h.  A tile is two
+// blocks of 16 entries, which come from memory as operands (bc_paged.h) and become bf16 or half precision by the hardware's conversions,
+// exactly: S^T = K.Q^T by 16x16x32 MFMA, whose result has four entries of a column in a lane; a word of values is those four entries of one
+// element, so O^T += V^T.P^T takes both as they are.  A key scale that is a power of two goes along with the conversion, exactly; others
+// are factors of their block's scores.  Values become half precision without their scale, which is a factor of the weights; those enter
+// their product in two half-precision parts (22 bits) at a level that goes with the products (kLevelMost).  Softmax online, sums in fp32.
 //
 // Two kernels:
-//   up to 32 columns: bound by memory, and by latency at both ends.  A row over 16,000, 32/8 heads, d = 128 (33 MB): 12.5 us; 64 rows over 4352 to 8704, 12/2 heads (216 MB): 38.7 (6.3 TB/s while it
-//   streams, as 1.07 GB in 171 us; a large read reaches 6.5); 1 to 8 rows of 16 sequences over 900 to 6000, 32/8 heads (121 MB): 28.2 to 29.3;
-//   more: bound by the matrix cores, large ones by the power limit.  4 x 2048 rows over 30,000, 32/8 heads: 4.84 to 5.23 ms from card to card, 0.80 to 0.74 PFLOP/s of the definition's products and
-//   1.2 to 1.1 of those issued (a library product of 16384^3 reaches 1.39 to 1.32), matrix pipe busy 59 % of the cycles at 1.9 to 1.8 GHz; 512 rows over 7680: 103 to 108 us.
+//   up to 32 columns: bound by memory, and by latency at both ends.  A row over 16,000, 32/8 heads, d = 128 (33 MB): 12.6 us; 64 rows over
+//   4352 to 8704, 12/2 heads (216 MB): 38.7 (6.3 TB/s while it streams, as 1.07 GB in 171 us; a large read reaches 6.5); 1 to 8 rows of 16
+//   sequences over 900 to 6000, 32/8 heads (121 MB): 28.2 to 29.3;
+//   more: bound by the matrix cores, large ones by the power limit.  4 x 2048 rows over 30,000, 32/8 heads: 4.9 to 5.2 ms from card to
+//   card, 0.79 to 0.74 PFLOP/s of the definition's products and 1.2 to 1.1 of those issued (a library product of 16384^3 reaches 1.39 to
+//   1.32), matrix pipe busy 59 % of the cycles at 1.9 to 1.8 GHz; 512 rows over 7680: 103 to 108 us.
 #include "bc_paged.h"
 
 namespace bc {
@@ -94,31 +97,34 @@ __device__ __forceinline__ float no_number() {
   asm volatile("v_mov_b32 %0, 0x7fc00000" : "=v"(x));
   return x;
 }
-// The level of a column's values.  Weights times their block's value scale enter products in half precision, so what they are brought to has to go with the product: sums
-// are kept as `f` times what they are, f a power of two, so that no factor passes 2^14 and the largest came to 2^8 when f was last set.  What was small beside that is as small
-// in the result.  f starts where nothing is too large and sums are zero.
+// The level of a column's values.  Weights times their block's value scale enter products in half precision, so what they are brought to
+// has to go with the product: sums are kept as `f` times what they are, f a power of two, so that no factor passes 2^14 and the largest
+// came to 2^8 when f was last set.  What was small beside that is as small in the result.  f starts where nothing is too large and sums are
+// zero.
 constexpr int kLevelTop = 119;                 // log2
 constexpr float kLevelMost = 16384.f, kLevelStart = 0x1p119f;
 __device__ __forceinline__ float level_for(float largest) {      // 2^8 over it, as a power of two (up to 2^kLevelTop)
   return __uint_as_float(min(127u + kLevelTop, 254u + 8u - (__float_as_uint(largest) >> 23)) << 23);
 }
-// What a reference that moves up by `by` (log2, a whole number, or anything beyond 2^23) does to them: the level goes up with it, as far as it goes; from there on the sums come down by the factor that is
-// returned, to nothing where there are none yet.  (By exponents: as a product level and move may pass what 32 bits hold where neither does.)
+// What a reference that moves up by `by` (log2, a whole number, or anything beyond 2^23) does to them: the level goes up with it, as far as
+// it goes; from there on the sums come down by the factor that is returned, to nothing where there are none yet.  (By exponents: as a
+// product level and move may pass what 32 bits hold where neither does.)
 __device__ __forceinline__ float raise_level(float& level, float by) {
   const float up = (float)((int)(__float_as_uint(level) >> 23) - 127) + by, most = fminf(up, (float)kLevelTop);
   level = __uint_as_float((uint32_t)(127 + (int)most) << 23);
   return fast_exp2(most - up);
 }
-// A scale times the level passes what 32 bits hold where the scale is 2^9 or more, the level high and the weights next to nothing (or none that the column sees): such a scale leaves its exponent beyond 2^8 to
-// the weights, which are 2^8 at most.
+// A scale times the level passes what 32 bits hold where the scale is 2^9 or more, the level high and the weights next to nothing (or none
+// that the column sees): such a scale leaves its exponent beyond 2^8 to the weights, which are 2^8 at most.
 constexpr uint32_t kFarScale = (127 + 9) << 23;                  // (bits)
 __device__ __forceinline__ float far_scale(float& scale) {
   const uint32_t u = __float_as_uint(scale), e = max((u >> 23 & 255u), 127u + 8u) - (127u + 8u);
   scale = __uint_as_float(u - (e << 23));
   return __uint_as_float((127u + e) << 23);
 }
-// What waves, halves of a workgroup, parts and teams hand over: sums of weights times values, their reference and their sum of weights.  Sums of up to 2^39 may pass what 32 bits hold where their mean, the result,
-// does not: those at a level below 2^-40 (of values above 2^48 or so) are in a unit of 2^-40, for which their sum of weights is negative.  Where only some are, the others come to that unit.
+// What waves, halves of a workgroup, parts and teams hand over: sums of weights times values, their reference and their sum of weights.
+// Sums of up to 2^39 may pass what 32 bits hold where their mean, the result, does not: those at a level below 2^-40 (of values above 2^48
+// or so) are in a unit of 2^-40, for which their sum of weights is negative.  Where only some are, the others come to that unit.
 constexpr float kUnit = 0x1p-40f;
 __device__ __forceinline__ float inverse_power(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }      // 1 / x of a power of two
 __device__ __forceinline__ float unit_at(float level) { return level < kUnit ? kUnit : 1.f; }
@@ -146,8 +152,8 @@ __device__ __forceinline__ AttendSpan attend_span(const AttendParams& p, int s) 
   return {span.row, bad ? 0 : span.n, L, bad};
 }
 
-// Up to 16 * CT columns a KV head.  The waves of a workgroup have the tiles of its chunk of a (sequence, KV head) pair by turns.  Where a pair has several chunks, each leaves its
-// sums in the workspace, and the workgroup that is the last to arrive adds them up in their order.
+// Up to 16 * CT columns a KV head.  The waves of a workgroup have the tiles of its chunk of a (sequence, KV head) pair by turns.  Where a
+// pair has several chunks, each leaves its sums in the workspace, and the workgroup that is the last to arrive adds them up in their order.
 template <int D, int CT, int NW, bool STREAM>
 __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(AttendParams p) {
   constexpr int H = D / 64, COLS = 16 * CT, PITCH = D + 4, BLOCK_BYTES = kPagedBlock * D, SUMS = COLS * (D + 2);
@@ -161,8 +167,8 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
 
   const uint32_t pairs = (uint32_t)p.t.B * p.Hkv, chunk = blockIdx.x / pairs;
   const int pair = blockIdx.x - chunk * pairs, s = pair / p.Hkv, kvh = pair - s * p.Hkv;
-  // 32 tiles of the wave at a time: lane 2 i + b has block b of the i-th.  (Which ones they are follows from the chunk's number alone: the table is asked for together with the
-  // length.)
+  // 32 tiles of the wave at a time: lane 2 i + b has block b of the i-th.  (Which ones they are follows from the chunk's number alone: the
+  // table is asked for together with the length.)
   const uint32_t t0 = chunk * p.chunk_tiles;
   const int most = (p.t.table_pages << per_page) - 1;
   auto page_of = [&](uint32_t tb) { return p.t.table[(int64_t)s * p.t.table_pages + (min(2 * (int)(tb + NW * (lane >> 1)) + (lane & 1), most) >> per_page)]; };
@@ -209,14 +215,15 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
     }
     const uint32_t unit = (((uint32_t)page * p.Hkv + kvh) << per_page) + (at_block & ((1 << per_page) - 1));
     const float qs = CT == 1 ? 1.f : p.qs, k_scale = CT == 1 ? p.ks[unit] * p.qs : p.ks[unit], v_scale = p.vs[unit];
-    // (With one tile of columns key scales are always factors of the scores: two ways through the code cost a short step half a microsecond, 9.7 -> 10.3 us.)
+    // (With one tile of columns key scales are always factors of the scores: two ways through the code cost a short step half a
+    // microsecond, 9.7 -> 10.3 us.)
     const bool uneven = CT == 1 || __any(at_block <= last && (lane >> 1) < count && !power_of_two_scale(k_scale));
 
-    // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are formed, its values
-    // behind the weights' product.
+    // A tile's keys and values have their registers to themselves: the next tile's keys are asked for as soon as this one's scores are
+    // formed, its values behind the weights' product.
     u32x4_t key[2][H], value[2][H];
-    // (Behind the last tile one 16-byte piece of it in every lane's place: with a branch about the loads the compiler did not know how many were on their way, and
-    // waited for all of them in front of the scores: 14.1 us for a row over 16,000, 13.3 so.)
+    // (Behind the last tile one 16-byte piece of it in every lane's place: with a branch about the loads the compiler did not know how many
+    // were on their way, and waited for all of them in front of the scores: 14.1 us for a row over 16,000, 13.3 so.)
     auto load = [&](u32x4_t (&x)[2][H], const uint8_t* pool, uint32_t at_lane, int i) {
       const uint32_t lane_at = i < count ? at_lane : 0;
       i = min(i, count - 1);
@@ -295,8 +302,8 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
             for (int j = 0; j < 4 * H; ++j) o[ct][j] *= down;
           }
         };
-        // With two tiles of columns vector work counts: the maximum is formed only where weights get large (38.7 -> 35.3 us for 16 x 1-8 rows over 900 to 6000,
-        // 32/8 heads).  With one, a wave's two or three tiles would pay for forming the first one's weights twice.
+        // With two tiles of columns vector work counts: the maximum is formed only where weights get large (38.7 -> 35.3 us for 16 x 1-8
+        // rows over 900 to 6000, 32/8 heads).  With one, a wave's two or three tiles would pay for forming the first one's weights twice.
         if constexpr (CT == 1) {
           move();
           weights();
@@ -342,8 +349,8 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
             for (int j = 0; j < 4; ++j) value[b][h][j] &= mask;
         }
       }
-      // A value that is no number would reach the columns that do not see it, by a weight of zero: its bytes become zeros, and the columns that do see it get a sum
-      // of weights that is no number.
+      // A value that is no number would reach the columns that do not see it, by a weight of zero: its bytes become zeros, and the columns
+      // that do see it get a sum of weights that is no number.
       if (__builtin_expect(n > 1 && ends, 0)) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -494,10 +501,11 @@ __global__ void __launch_bounds__(64 * NW, few_waves(CT, NW)) paged_few_kernel(A
 }
 
 // ---------------------------------------------------------------------------
-// Many columns: 32 a wave, the workgroup's four share tiles of 64 entries.  A wave brings the bytes of one of a tile's four blocks, converts them (keys
-// to bf16, values to half precision) and leaves them in LDS as the operands of 32x32x16 products, 16 bytes a lane: keys [32 entries][d / 16][half][entry],
-// element 16 i + 8 half + e of a key (its place among the 32 turned by i, so that the writes meet no bank twice); values [16 entries][j][half][row], element (d / 32) row + j: a word's four
-// keys are half of an operand, the lane's other word the other half, and results have d / 32 elements in a row.
+// Many columns: 32 a wave, the workgroup's four share tiles of 64 entries.  A wave brings the bytes of one of a tile's four blocks,
+// converts them (keys to bf16, values to half precision) and leaves them in LDS as the operands of 32x32x16 products, 16 bytes a lane: keys
+// [32 entries][d / 16][half][entry], element 16 i + 8 half + e of a key (its place among the 32 turned by i, so that the writes meet no
+// bank twice); values [16 entries][j][half][row], element (d / 32) row + j: a word's four keys are half of an operand, the lane's other
+// word the other half, and results have d / 32 elements in a row.
 // ---------------------------------------------------------------------------
 constexpr int kManyWaves = 4, kManyColumns = 32 * kManyWaves, kManyTile = 16 * kManyWaves;
 // Tiles of a block of columns, and those of one of its parts.
@@ -507,8 +515,9 @@ __device__ __forceinline__ ManyCut many_cut(int parts, int lim, int part) {
   return {tiles, (int)((int64_t)tiles * part / n), (int)((int64_t)tiles * (part + 1) / n), n};
 }
 
-// Up to 64 columns (HALVES): two waves have a column, and of every tile half of the entries each; their sums meet in LDS at the end.  (With two of the four waves idle, the same
-// SIMDs had all the work of both workgroups: 18 x 2-5 rows over 10,000-30,000, 16/2 heads, 93 -> 71.5 us; 100 x 16 over 500-2000, 32/8, 135 -> 104.)
+// Up to 64 columns (HALVES): two waves have a column, and of every tile half of the entries each; their sums meet in LDS at the end.  (With
+// two of the four waves idle, the same SIMDs had all the work of both workgroups: 18 x 2-5 rows over 10,000-30,000, 16/2 heads, 93 -> 71.5
+// us; 100 x 16 over 500-2000, 32/8, 135 -> 104.)
 template <int D, bool HALVES>
 __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendParams p) {
   constexpr int NX = HALVES ? 1 : 2, KS = D / 16, NJ = D / 32, K_BYTES = kManyTile * D * 2, STAGE = 2 * K_BYTES, BLOCK_BYTES = kPagedBlock * D;
@@ -639,7 +648,8 @@ __global__ void __launch_bounds__(64 * kManyWaves, 2) paged_many_kernel(AttendPa
     if (t + 2 < cut.t1) fetch(t + 2);
     if (t < seen) {
       const char* tile = lds + stage * STAGE;
-      // (The wave that has products to issue goes first: the other of its SIMD forms weights meanwhile.  5.15 -> 4.81 ms; with the weights first 5.16.)
+      // (The wave that has products to issue goes first: the other of its SIMD forms weights meanwhile.  5.15 -> 4.81 ms; with the weights
+      // first 5.16.)
       __builtin_amdgcn_s_setprio(1);
       f32x16_t sc[NX];
 #pragma unroll
@@ -838,12 +848,17 @@ struct AttendLaunch {
 //   4 x 2000, 32/8                       11.0, 10.2     1 x 500, 32/8                                 6.4,  7.4
 //   128 x 300-3000, 12/2                 26.0, 24.0     64 x 400, 12/2                                8.4,  8.9
 //   32 x 4000, 32/8                      48.9, 46.9     64 x 1000, 32/8 (more pairs than 256)        26.0, 27.6
-// and two to eight rows: 1 x 8000, 32/8 28.1, 19.1; 64 x 1000, 12/2 16.9, 15.5; 1 x 500, 32/8 9.6, 10.7; 128 x 300, 32/8 26.8, 38.4.  More and smaller workgroups (four waves, 768): 19.8 for
-// the first.  Two tiles of columns leave twice the sums to add up: chunks of at least sixteen tiles (1 x 8000: 19.1 -> 15.9, others as they were).
+// and two to eight rows: 1 x 8000, 32/8 28.1, 19.1; 64 x 1000, 12/2 16.9, 15.5; 1 x 500, 32/8 9.6, 10.7; 128 x 300, 32/8 26.8, 38.4.  More
+// and smaller workgroups (four waves, 768): 19.8 for the first.  Two tiles of columns leave twice the sums to add up: chunks of at least
+// sixteen tiles (1 x 8000: 19.1 -> 15.9, others as they were).
 // Caches beyond some 100 MB go past the caches: 64 x 1000 rows, 32/8 heads (131 MB) 30.2 -> 26.7; 128 x 300 (79 MB) 17.5 -> 18.3.
-// (Chunks of equal size for all sequences of a batch, worked out by every workgroup from the lengths: 2.3 us more for one tile of columns, nothing gained with two.)
-// Many columns: as many parts as cost least, in tiles of 64: rounds of the workgroups that run at once (two a compute unit), a workgroup's tiles and its two ends, and parts written and
-// read again.  512 rows over 7680, 32/8 heads, in three, four, five parts 135, 115, 153 us.  One round of workgroups at most, and so:
+// (Chunks of equal size for all sequences of a batch, worked out by every workgroup from the lengths: 2.3 us more for one tile of columns,
+// nothing gained with two.)
+// Workgroups that run at once are those of d = 128, by registers and LDS.  With d = 64 there is room for more, 768 of many columns, 512 of
+// eight waves and one tile; cuts for it have not been measured.
+// Many columns: as many parts as cost least, in tiles of 64: rounds of the workgroups that run at once (two a compute unit), a workgroup's
+// tiles and its two ends, and parts written and read again.  512 rows over 7680, 32/8 heads, in three, four, five parts 135, 115, 153 us.
+// One round of workgroups at most, and so:
 //   69 x 15 rows over 1400-27,900, 14/2 heads, d = 64   237, 184     8 x 50-500 over 300-20,000, 12/2   555, 438     9 x 256 over 4000, 32/8   298, 273
 //   the same, all over 27,900                           270, 258     3 x 400 over 6000, 32/8            208, 190     20 x 64 over 3000, 32/8   119, 119 (ends of three tiles: 132)
 // Where a call fills the chip several times over, another part saves little of its time and takes as much memory as its outputs

@@ -1,6 +1,6 @@
-// Grids of more threads than one launch takes.  HIP launches fewer than 2^32 threads at once, 2^24 workgroups of 256; the paged cache's calls may have up to 2^31 - 1 workgroups
-// (each sequence may have all of a call's rows, as far as the host knows).  Those go out in several launches, each of which is told its first workgroup.  No HIP here: a host
-// test plays it through.
+// Grids of more threads than one launch takes.  HIP launches fewer than 2^32 threads at once, 2^24 workgroups of 256; the paged cache's
+// calls may have up to 2^31 - 1 workgroups (each sequence may have all of a call's rows, as far as the host knows).  Those go out in
+// several launches, each of which is told its first workgroup.  No HIP here: a host test plays it through.
 #pragma once
 #include <cstdint>
 

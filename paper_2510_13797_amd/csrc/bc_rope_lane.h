@@ -1,5 +1,6 @@
-// A lane's share of a head under norm and rotation: d / 8 lanes have a head, eight elements a lane, in two pieces of four that are each other's partners in
-// the rotation.  Shared by the kernels that turn packed projections into q, k and v (bc_rope.hip) and into entries of a cache (bc_paged.hip).
+// A lane's share of a head under norm and rotation: d / 8 lanes have a head, eight elements a lane, in two pieces of four that are each
+// other's partners in the rotation.  Shared by the kernels that turn packed projections into q, k and v (bc_rope.hip) and into entries of a
+// cache (bc_paged_append.hip).
 #pragma once
 #include "bc_common.h"
 
