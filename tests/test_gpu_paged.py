@@ -658,7 +658,7 @@ def test_a_given_table_stays_while_a_call_is_in_work(dev):
             cache = bc.PagedCache(B, Hq, Hkv, d, B, 16, 1 << 16, dev, table=table)
             cache.append(x, pos, none)
             stream.synchronize()
-            torch.cuda._sleep(20_000_000)
+            torch.cuda._sleep(500_000_000)         # 0.2 s
             call(cache, kind)
         del cache, table
         other = torch.empty(size, dtype=torch.int32, device=dev)
